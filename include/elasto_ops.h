@@ -88,6 +88,134 @@ elasto_status elasto_op_conv2d_tile(int B, int H, int W, int C, int N, int k, in
 elasto_status elasto_op_attention(void* stream, const void* qkv, void* out, int batch, int n, int heads,
                                   int* status_device);
 
+/* ------------------------------------------------------------------------
+ * An attention sublayer over long token sequences with 8-bit weights: rows to
+ * e4m3, products of e4m3 rows, norms and positions of queries and keys, and
+ * attention in a sliding window. Forward only, like the rest of the library.
+ * Strides are in elements. A call allocates nothing and keeps nothing; it may
+ * be captured into a graph. */
+
+/* Operand type of these calls besides ELASTO_F32 and ELASTO_BF16: IEEE f16. */
+enum { ELASTO_F16 = 2 };
+
+/* q e4m3 [rows, cols] and scale fp32 [ceil(cols / 128), rows]: each row of x
+ * (x_type ELASTO_F32, _BF16 or _F16) in blocks of 128 columns, the last block
+ * what is left. Of a block, in fp32 arithmetic:
+ *   a = max(largest |x|, 2^-100),  scale[b, r] = a / 448,
+ *   q = x * (448 / a) rounded to the nearest e4m3 (ties to even),
+ * so x is about q * scale. A NaN in a block makes its scale and all its values
+ * NaN; an infinity makes its scale infinite, its own value NaN and the others 0.
+ * ldx, ldq >= cols: row strides; lds >= rows: stride of scale's rows. Columns
+ * past cols are neither read nor written. x, q and scale need their types'
+ * alignment; 16-byte rows of x and 8-byte rows of q are read and written wide. */
+elasto_status elasto_op_quantize_fp8(void* stream, const void* x, int x_type, long long ldx, void* q, long long ldq,
+                                     float* scale, long long lds, int rows, int cols);
+
+/* out[M, N] = epilogue(acc), acc[m, n] = sum over blocks b of 128 columns of
+ *   a_scale[b, m] * w_scale[n / 128, b] * (sum over the block of A[m, k] W[n, k])
+ * in fp32. A e4m3 [M, K] (row stride lda) with a_scale fp32 [ceil(K / 128), M]
+ * (row stride lds >= M), as elasto_op_quantize_fp8 makes them; W e4m3 [N, K] (row
+ * stride ldw) with w_scale fp32 [ceil(N / 128), ceil(K / 128)], dense; bias fp32 [N] or
+ * NULL. epilogue: ELASTO_EPI_BIAS_BF16, _BIAS_GELU_BF16, _BIAS_F32, or
+ * _BIAS_RESID_F32 (out += acc + bias); out has row stride ldo >= N.
+ * M, N, K >= 1, of any size; A and W 16-byte aligned with lda and ldw multiples of
+ * 16 (>= K); columns past K are not read. The result does not depend on lda, ldw,
+ * ldo, and is the same in every call. */
+elasto_status elasto_op_gemm_fp8(void* stream, const void* A, long long lda, const float* a_scale, long long lds,
+                                 const void* W, long long ldw, const float* w_scale, const float* bias, void* out,
+                                 long long ldo, int M, int N, int K, int epilogue, int* status_device);
+
+/* Queries and keys of `rows` tokens: each head of each row divided by the root
+ * of its mean square (plus eps), multiplied by the gain of its channel, and its
+ * first rot_dim channels rotated by the row's position; all in fp32, rounded
+ * once. Keys, and values unchanged, optionally go to the rows of a cache.
+ *   y = x * rsqrt(mean(x^2) + eps) * gain
+ *   pair j of rot_dim / 2: channels (j, j + rot_dim / 2), or (2 j, 2 j + 1) if
+ *   interleaved != 0, (a, b) -> (a c - b s, b c + a s), with c and s from row
+ *   positions[r] of cos_sin: rot_dim / 2 cosines, then rot_dim / 2 sines.
+ * Head h of row r of q is at q + r * q_row + h * q_head, and so on: the columns of
+ * a QKV product's output are taken as they are. An output may be its own input
+ * (the same strides, and for k and v no slots); else it must not overlap the inputs.
+ * k and v of row r go to row slots[r] of k_out and v_out (slots NULL: row r). A
+ * negative slot stores neither. Slots that are stored must differ from one another.
+ * A row with a position outside [0, n_positions), or a slot >= n_slots, is left
+ * out, and *status_device is set to ELASTO_ERR_INVALID_ARG.
+ * Refused: head_dim not a multiple of 8 up to 256; rot_dim not a multiple of 16
+ * up to head_dim (0: no rotation); strides that are no multiples of 8; data not
+ * 16-byte aligned. */
+typedef struct {
+  int dtype; /* of q, k, v and the outputs: ELASTO_BF16 or ELASTO_F16 */
+  int rows, heads_q, heads_k, head_dim, rot_dim, interleaved;
+  float eps; /* >= 0 */
+  const void* q; /* heads_q heads (0: no queries, q and q_out are not used) */
+  long long q_row, q_head;
+  const void* k; /* heads_k heads (0: no keys and values) */
+  long long k_row, k_head;
+  const void* v; /* heads_k heads, copied to v_out; or NULL */
+  long long v_row, v_head;
+  void* q_out;
+  long long q_out_row, q_out_head;
+  void* k_out;
+  long long k_out_row, k_out_head;
+  void* v_out;
+  long long v_out_row, v_out_head;
+  const float* q_gain; /* [head_dim], or NULL: ones */
+  const float* k_gain;
+  const float* cos_sin; /* [n_positions, rot_dim], 16-byte aligned (rot_dim 0: not used, nor are positions) */
+  const int32_t* positions; /* [rows] */
+  int n_positions;
+  const int32_t* slots; /* [rows], or NULL */
+  int n_slots;
+} elasto_qk_norm_rope_args;
+elasto_status elasto_op_qk_norm_rope(void* stream, const elasto_qk_norm_rope_args* args, int* status_device);
+
+/* Attention of `batch` sequences in a sliding window, the first tokens staying
+ * visible. A sequence with nq queries and nk keys has its queries at the last
+ * positions: query i at p = nk - nq + i. It sees key j, 0 <= j < nk, if
+ *   causal != 0:  j <= p and (j >= p - window or j < sinks);
+ *   causal == 0:  |j - p| <= window or j < sinks or p < sinks (class tokens and
+ *                 the like: seen by all, and seeing all);
+ * window < 0: no limit. A query before the first key (p < 0) sees nothing.
+ *   out = softmax over the visible keys of (scale q . k), times v;
+ * a query that sees nothing gets zeros. Keys and values that no query sees, and
+ * NaN or infinite ones at places hidden from a query, do not change its result.
+ * heads is a multiple of heads_kv: head h reads key head h / (heads / heads_kv).
+ * head_dim: a multiple of 8 up to 128. Softmax statistics and sums in fp32; the
+ * probabilities are rounded to the operand type for the product with v.
+ * Queries: sequence b has the rows q_start[b] to q_start[b + 1] of q and out, at
+ *   most max_queries; q_start NULL: max_queries rows each. q and out have q_rows rows.
+ * Keys: packed, the rows kv_start[b] to kv_start[b + 1] of k and v, which have
+ *   kv_rows rows; or (kv_start NULL) in a cache of kv_rows rows per sequence, k_batch
+ *   and v_batch apart, the first kv_len[b] of them (kv_len NULL: max_keys). At most
+ *   max_keys each; max_keys <= kv_rows.
+ * Lengths on the device past these limits are cut to them; nothing is read or
+ * written outside them. Rows of out that belong to no sequence are left as they were.
+ * max_queries == 1 runs the single-token form.
+ * Strides of q, k, v and out are multiples of 8, the data is 16-byte aligned.
+ * out may not overlap the inputs. */
+typedef struct {
+  int dtype; /* of q, k, v and out: ELASTO_BF16 or ELASTO_F16 */
+  int batch, heads, heads_kv, head_dim;
+  int causal, window, sinks;
+  float scale; /* > 0 */
+  int max_queries;
+  long long q_rows;
+  const int32_t* q_start; /* [batch + 1] or NULL */
+  const void* q;
+  long long q_row, q_head;
+  void* out;
+  long long out_row, out_head;
+  int max_keys;
+  long long kv_rows;
+  const int32_t* kv_start; /* [batch + 1] or NULL */
+  const int32_t* kv_len;   /* [batch] or NULL; only without kv_start */
+  const void* k;
+  long long k_batch, k_row, k_head;
+  const void* v;
+  long long v_batch, v_row, v_head;
+} elasto_window_attention_args;
+elasto_status elasto_op_window_attention(void* stream, const elasto_window_attention_args* args, int* status_device);
+
 /* Self-test of the bounded device-side wait that every kernel above (and the
  * forward's kernels) uses instead of an unbounded spin: one thread waits on an
  * mbarrier of one arrival. armed != 0: the arrival is made first and the wait

@@ -20,6 +20,7 @@ LIB_PATH = os.path.join(_HERE, "libelasto.so")
 
 ARCH_VIT, ARCH_RESNET50 = 1, 2
 F32, BF16 = 0, 1
+F16 = 2  # operand type of the calls for long sequences (models are stored as F32 or BF16)
 OK, ERR_INVALID_ARG, ERR_BAD_TABLE, ERR_BAD_MODE, ERR_OOM, ERR_CUDA, ERR_UNSUPPORTED, ERR_TIMEOUT, ERR_GUARD = (
     0, -1, -2, -3, -4, -5, -6, -7, -8)
 Q_N_MODES, Q_PACKED_BYTES, Q_SHARED_BYTES, Q_WORKSPACE_BYTES, Q_ARENA_BYTES, Q_MODE_MACS, Q_LAUNCHES = range(7)
@@ -28,6 +29,7 @@ EPI_BIAS_BF16, EPI_BIAS_GELU_BF16, EPI_BIAS_RESID_F32, EPI_BIAS_F32, EPI_BIAS_RE
 EPI_BIAS_RELU_F16, EPI_BIAS_F16, EPI_BIAS_RESID_RELU_F16 = range(6, 9)  # A, W, resid, out in IEEE f16
 
 c_int, c_void_p, c_size_t, c_int64 = ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int64
+c_longlong = ctypes.c_longlong
 P_i32 = ctypes.POINTER(ctypes.c_int32)
 
 
@@ -60,6 +62,29 @@ class DnProfile(ctypes.Structure):
 class LaunchRecord(ctypes.Structure):
     _fields_ = [("kind", c_int), ("layer", c_int), ("m", c_int), ("n", c_int), ("k", c_int),
                 ("ms", ctypes.c_float), ("macs", ctypes.c_double), ("bytes", ctypes.c_double)]
+
+
+def _strided(*names):
+    """(data, row stride, head stride) fields of each tensor."""
+    return [f for n in names for f in ((n, c_void_p), (n + "_row", c_longlong), (n + "_head", c_longlong))]
+
+
+class QkNormRope(ctypes.Structure):
+    """elasto_qk_norm_rope_args."""
+    _fields_ = ([(f, c_int) for f in ("dtype", "rows", "heads_q", "heads_k", "head_dim", "rot_dim", "interleaved")] +
+                [("eps", ctypes.c_float)] + _strided("q", "k", "v", "q_out", "k_out", "v_out") +
+                [("q_gain", c_void_p), ("k_gain", c_void_p), ("cos_sin", c_void_p), ("positions", c_void_p),
+                 ("n_positions", c_int), ("slots", c_void_p), ("n_slots", c_int)])
+
+
+class WindowAttention(ctypes.Structure):
+    """elasto_window_attention_args."""
+    _fields_ = ([(f, c_int) for f in ("dtype", "batch", "heads", "heads_kv", "head_dim", "causal", "window", "sinks")] +
+                [("scale", ctypes.c_float), ("max_queries", c_int), ("q_rows", c_longlong), ("q_start", c_void_p)] +
+                _strided("q", "out") +
+                [("max_keys", c_int), ("kv_rows", c_longlong), ("kv_start", c_void_p), ("kv_len", c_void_p)] +
+                [(n + f, t) for n in "kv" for f, t in (("", c_void_p), ("_batch", c_longlong), ("_row", c_longlong),
+                                                       ("_head", c_longlong))])
 
 
 class ElastoError(RuntimeError):
@@ -113,6 +138,12 @@ def lib() -> ctypes.CDLL:
         "elasto_op_layernorm": [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int],
         "elasto_op_softmax": [c_void_p, c_void_p, c_void_p, c_int, c_int],
         "elasto_op_attention": [c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_void_p],
+        "elasto_op_quantize_fp8": [c_void_p, c_void_p, c_int, c_longlong, c_void_p, c_longlong, c_void_p, c_longlong,
+                                   c_int, c_int],
+        "elasto_op_gemm_fp8": [c_void_p, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p,
+                               c_void_p, c_void_p, c_longlong, c_int, c_int, c_int, c_int, c_void_p],
+        "elasto_op_qk_norm_rope": [c_void_p, ctypes.POINTER(QkNormRope), c_void_p],
+        "elasto_op_window_attention": [c_void_p, ctypes.POINTER(WindowAttention), c_void_p],
         "elasto_op_bounded_wait": [c_void_p, c_int, c_void_p, c_void_p],
         "elasto_op_grid_barrier": [c_void_p, c_int, c_void_p, c_void_p, c_void_p],
     }
@@ -412,6 +443,26 @@ def elasto_op_softmax(stream, x, y, rows, cols) -> None:
 
 def elasto_op_attention(stream, qkv, out, batch, n, heads, status=0) -> None:
     _check(lib().elasto_op_attention(stream, qkv, out, batch, n, heads, status), "elasto_op_attention")
+
+
+def elasto_op_quantize_fp8(stream, x, x_type, ldx, q, ldq, scale, lds, rows, cols) -> None:
+    """Rows to e4m3 with an fp32 scale for each block of 128 columns (scale is [blocks, rows])."""
+    _check(lib().elasto_op_quantize_fp8(stream, x, x_type, ldx, q, ldq, scale, lds, rows, cols),
+           "elasto_op_quantize_fp8")
+
+
+def elasto_op_gemm_fp8(stream, A, lda, a_scale, lds, W, ldw, w_scale, bias, out, ldo, M, N, K, epilogue,
+                       status=0) -> None:
+    _check(lib().elasto_op_gemm_fp8(stream, A, lda, a_scale, lds, W, ldw, w_scale, bias, out, ldo, M, N, K, epilogue,
+                                    status), "elasto_op_gemm_fp8")
+
+
+def elasto_op_qk_norm_rope(stream, args: QkNormRope, status=0) -> None:
+    _check(lib().elasto_op_qk_norm_rope(stream, args, status), "elasto_op_qk_norm_rope")
+
+
+def elasto_op_window_attention(stream, args: WindowAttention, status=0) -> None:
+    _check(lib().elasto_op_window_attention(stream, args, status), "elasto_op_window_attention")
 
 
 def elasto_op_bounded_wait(stream, armed: bool, status, elapsed_ns) -> None:

@@ -323,4 +323,26 @@ cudaError_t convert_to_bf16(const void* src, int src_dtype, size_t n, bf16* dst,
 cudaError_t convert_to_bf16_lo(const void* src, int src_dtype, size_t n, bf16* dst, cudaStream_t s);
 cudaError_t convert_to_f32(const void* src, int src_dtype, size_t n, float* dst, cudaStream_t s);
 
+// ---------------------------------------------------------------- long sequences, 8-bit weights
+// (arguments checked by the entry points in ops_api.cu)
+cudaError_t quantize_fp8_launch(const void* x, int x_type, long long ldx, uint8_t* q, long long ldq, float* scale,
+                                long long lds, int rows, int cols, cudaStream_t s);
+struct Fp8Gemm {
+  const uint8_t* A;
+  long long lda;
+  const float* a_scale;
+  long long lds;
+  const uint8_t* W;
+  long long ldw;
+  const float* w_scale;
+  const float* bias;
+  void* out;
+  long long ldo;
+  int M, N, K, epi;
+  int* status;
+};
+elasto_status gemm_fp8_launch(const Fp8Gemm& g, cudaStream_t s);
+cudaError_t qk_norm_rope_launch(const elasto_qk_norm_rope_args& a, int* status, cudaStream_t s);
+elasto_status window_attention_launch(const elasto_window_attention_args& a, int* status, cudaStream_t s);
+
 }  // namespace elasto

@@ -10,6 +10,15 @@ using namespace elasto;
 
 namespace {
 
+bool aligned(const void* p, unsigned bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+bool strides8(long long a, long long b) { return a % 8 == 0 && b % 8 == 0 && a >= 0 && b >= 0; }
+// a strided [rows, heads, head_dim] tensor of 16-bit values
+bool tensor16(const void* p, long long row, long long head) { return p && aligned(p, 16) && strides8(row, head); }
+elasto_status refuse(const char* what, elasto_status st = ELASTO_ERR_INVALID_ARG) {
+  set_error(what);
+  return st;
+}
+
 // The bounded wait every kernel uses (mbar_wait: a time limit, then false),
 // on an mbarrier of one arrival. armed != 0: that arrival is made first, so
 // the wait returns at once; armed == 0: nothing ever arrives, the wait gives
@@ -146,6 +155,107 @@ elasto_status elasto_op_layernorm(void* stream, const float* x, const float* gam
   ELASTO_CUDA_TRY(
       layernorm_launch(x, gamma, beta, static_cast<bf16*>(y), rows, d, d, static_cast<cudaStream_t>(stream)));
   return ELASTO_OK;
+}
+
+elasto_status elasto_op_quantize_fp8(void* stream, const void* x, int x_type, long long ldx, void* q, long long ldq,
+                                     float* scale, long long lds, int rows, int cols) {
+  clear_error();
+  if (!x || !q || !scale || rows <= 0 || cols <= 0 || ldx < cols || ldq < cols || lds < rows)
+    return refuse("elasto_op_quantize_fp8: null pointer, size or stride");
+  if (x_type != ELASTO_F32 && x_type != ELASTO_BF16 && x_type != ELASTO_F16)
+    return refuse("elasto_op_quantize_fp8: x_type must be ELASTO_F32, ELASTO_BF16 or ELASTO_F16");
+  if (!aligned(x, x_type == ELASTO_F32 ? 4 : 2) || !aligned(scale, 4))
+    return refuse("elasto_op_quantize_fp8: x or scale misaligned for its type");
+  if (static_cast<long long>(rows) * ((cols + 127LL) / 128) > 0x7fffffffLL)
+    return refuse("elasto_op_quantize_fp8: more than 2^31 blocks", ELASTO_ERR_UNSUPPORTED);
+  elasto_status st = check_device();
+  if (st != ELASTO_OK) return st;
+  ELASTO_CUDA_TRY(quantize_fp8_launch(x, x_type, ldx, static_cast<uint8_t*>(q), ldq, scale, lds, rows, cols,
+                                      static_cast<cudaStream_t>(stream)));
+  return ELASTO_OK;
+}
+
+elasto_status elasto_op_gemm_fp8(void* stream, const void* A, long long lda, const float* a_scale, long long lds,
+                                 const void* W, long long ldw, const float* w_scale, const float* bias, void* out,
+                                 long long ldo, int M, int N, int K, int epilogue, int* status_device) {
+  clear_error();
+  if (!A || !a_scale || !W || !w_scale || !out || M <= 0 || N <= 0 || K <= 0 || lda < K || ldw < K || lds < M || ldo < N)
+    return refuse("elasto_op_gemm_fp8: null pointer, size or stride");
+  if (!aligned(A, 16) || !aligned(W, 16) || lda % 16 != 0 || ldw % 16 != 0)
+    return refuse("elasto_op_gemm_fp8: A and W need 16-byte aligned rows");
+  if (epilogue != ELASTO_EPI_BIAS_BF16 && epilogue != ELASTO_EPI_BIAS_GELU_BF16 && epilogue != ELASTO_EPI_BIAS_RESID_F32 &&
+      epilogue != ELASTO_EPI_BIAS_F32)
+    return refuse("elasto_op_gemm_fp8: epilogue");
+  const bool f32 = epilogue == ELASTO_EPI_BIAS_RESID_F32 || epilogue == ELASTO_EPI_BIAS_F32;
+  if (!aligned(out, f32 ? 4 : 2) || !aligned(a_scale, 4) || !aligned(w_scale, 4) || !aligned(bias, 4))
+    return refuse("elasto_op_gemm_fp8: out, a scale or the bias misaligned for its type");
+  elasto_status st = check_device();
+  if (st != ELASTO_OK) return st;
+  return gemm_fp8_launch({static_cast<const uint8_t*>(A), lda, a_scale, lds, static_cast<const uint8_t*>(W), ldw, w_scale,
+                          bias, out, ldo, M, N, K, epilogue, status_device},
+                         static_cast<cudaStream_t>(stream));
+}
+
+elasto_status elasto_op_qk_norm_rope(void* stream, const elasto_qk_norm_rope_args* args, int* status_device) {
+  clear_error();
+  if (!args) return refuse("elasto_op_qk_norm_rope: null arguments");
+  const elasto_qk_norm_rope_args& a = *args;
+  if (a.dtype != ELASTO_BF16 && a.dtype != ELASTO_F16) return refuse("elasto_op_qk_norm_rope: dtype");
+  if (a.rows <= 0 || a.heads_q < 0 || a.heads_k < 0 || a.heads_q + static_cast<long long>(a.heads_k) <= 0 ||
+      a.heads_q + 2LL * a.heads_k > 65536)
+    return refuse("elasto_op_qk_norm_rope: rows or heads");
+  if (a.head_dim <= 0 || a.head_dim % 8 != 0 || a.head_dim > 256)
+    return refuse("elasto_op_qk_norm_rope: head_dim must be a multiple of 8 up to 256", ELASTO_ERR_UNSUPPORTED);
+  if (a.rot_dim < 0 || a.rot_dim % 16 != 0 || a.rot_dim > a.head_dim)
+    return refuse("elasto_op_qk_norm_rope: rot_dim must be a multiple of 16 up to head_dim", ELASTO_ERR_UNSUPPORTED);
+  if (!(a.eps >= 0.0f) || a.eps > 3.0e38f) return refuse("elasto_op_qk_norm_rope: eps");
+  if (a.heads_q > 0 && (!tensor16(a.q, a.q_row, a.q_head) || !tensor16(a.q_out, a.q_out_row, a.q_out_head)))
+    return refuse("elasto_op_qk_norm_rope: q or q_out (null, alignment or strides)");
+  if (a.heads_k > 0 && (!tensor16(a.k, a.k_row, a.k_head) || !tensor16(a.k_out, a.k_out_row, a.k_out_head)))
+    return refuse("elasto_op_qk_norm_rope: k or k_out (null, alignment or strides)");
+  if (a.heads_k > 0 && (a.v || a.v_out) &&
+      (!tensor16(a.v, a.v_row, a.v_head) || !tensor16(a.v_out, a.v_out_row, a.v_out_head)))
+    return refuse("elasto_op_qk_norm_rope: v or v_out (null, alignment or strides)");
+  if (a.heads_k > 0 && a.slots && (a.k == a.k_out || (a.v && a.v == a.v_out)))
+    return refuse("elasto_op_qk_norm_rope: slots with an output that is its own input");
+  if ((a.q == a.q_out && a.heads_q > 0 && (a.q_row != a.q_out_row || a.q_head != a.q_out_head)) ||
+      (a.k == a.k_out && a.heads_k > 0 && (a.k_row != a.k_out_row || a.k_head != a.k_out_head)) ||
+      (a.v && a.v == a.v_out && a.heads_k > 0 && (a.v_row != a.v_out_row || a.v_head != a.v_out_head)))
+    return refuse("elasto_op_qk_norm_rope: an output that is its own input has other strides");
+  if (!aligned(a.q_gain, 16) || !aligned(a.k_gain, 16)) return refuse("elasto_op_qk_norm_rope: gains misaligned");
+  if (a.rot_dim > 0 && (!a.cos_sin || !aligned(a.cos_sin, 16) || !a.positions || !aligned(a.positions, 4) || a.n_positions <= 0))
+    return refuse("elasto_op_qk_norm_rope: cos_sin, positions or n_positions");
+  if (a.slots && (a.n_slots <= 0 || !aligned(a.slots, 4))) return refuse("elasto_op_qk_norm_rope: slots or n_slots");
+  elasto_status st = check_device();
+  if (st != ELASTO_OK) return st;
+  ELASTO_CUDA_TRY(qk_norm_rope_launch(a, status_device, static_cast<cudaStream_t>(stream)));
+  return ELASTO_OK;
+}
+
+elasto_status elasto_op_window_attention(void* stream, const elasto_window_attention_args* args, int* status_device) {
+  clear_error();
+  if (!args) return refuse("elasto_op_window_attention: null arguments");
+  const elasto_window_attention_args& a = *args;
+  if (a.dtype != ELASTO_BF16 && a.dtype != ELASTO_F16) return refuse("elasto_op_window_attention: dtype");
+  if (a.batch <= 0 || a.heads <= 0 || a.heads_kv <= 0 || a.heads % a.heads_kv != 0 || a.max_queries <= 0 || a.max_keys <= 0)
+    return refuse("elasto_op_window_attention: batch, heads, max_queries or max_keys");
+  if (a.head_dim <= 0 || a.head_dim % 8 != 0 || a.head_dim > 128)
+    return refuse("elasto_op_window_attention: head_dim must be a multiple of 8 up to 128", ELASTO_ERR_UNSUPPORTED);
+  if (a.sinks < 0 || !(a.scale > 0.0f) || a.scale > 3.0e38f) return refuse("elasto_op_window_attention: sinks or scale");
+  if (!tensor16(a.q, a.q_row, a.q_head) || !tensor16(a.out, a.out_row, a.out_head))
+    return refuse("elasto_op_window_attention: q or out (null, alignment or strides)");
+  if (!tensor16(a.k, a.k_row, a.k_head) || !tensor16(a.v, a.v_row, a.v_head) || !strides8(a.k_batch, a.v_batch))
+    return refuse("elasto_op_window_attention: k or v (null, alignment or strides)");
+  if (a.q_rows <= 0 || a.kv_rows <= 0 || a.q_rows > 0x7fffffffLL || a.kv_rows > 0x7fffffffLL || a.max_keys > a.kv_rows)
+    return refuse("elasto_op_window_attention: q_rows or kv_rows");
+  if (!a.q_start && static_cast<long long>(a.batch) * a.max_queries > a.q_rows)
+    return refuse("elasto_op_window_attention: q_rows is less than batch * max_queries");
+  if (a.kv_start && a.kv_len) return refuse("elasto_op_window_attention: kv_start and kv_len exclude one another");
+  if (!aligned(a.q_start, 4) || !aligned(a.kv_start, 4) || !aligned(a.kv_len, 4))
+    return refuse("elasto_op_window_attention: starts or lengths misaligned");
+  elasto_status st = check_device();
+  if (st != ELASTO_OK) return st;
+  return window_attention_launch(a, status_device, static_cast<cudaStream_t>(stream));
 }
 
 elasto_status elasto_op_softmax(void* stream, const float* x, float* y, int rows, int cols) {
