@@ -84,6 +84,13 @@ bool encode_tmap_plain(CUtensorMap* tm, const void* base, int rank, const uint64
 // 3-D bf16 tensor [d2][d1][d0] with byte strides s1 (between d1 rows) and s2.
 bool encode_tmap_3d(CUtensorMap* tm, const void* base, uint64_t d0, uint64_t d1, uint64_t d2, uint64_t s1,
                     uint64_t s2, uint32_t b0, uint32_t b1, uint32_t b2);
+// 16-bit tensor of rank 2-5 (dims innermost first, byte strides of dims 1..rank-1), 128-byte
+// swizzle, boxes of 64 values along the innermost axis; outside reads as zero.
+bool encode_tmap_16(CUtensorMap* tm, const void* base, bool bf, int rank, const uint64_t* dims,
+                    const uint64_t* strides_bytes, const uint32_t* box);
+// Rows of 8-bit values, 128-byte swizzle, box of 128 values x box_outer rows.
+bool encode_tmap_8(CUtensorMap* tm, const void* base, uint64_t inner, uint64_t outer, uint64_t row_stride_bytes,
+                   uint32_t box_outer);
 
 // ---------------------------------------------------------------- GEMM
 enum GemmEpi : int {
@@ -344,5 +351,6 @@ struct Fp8Gemm {
 elasto_status gemm_fp8_launch(const Fp8Gemm& g, cudaStream_t s);
 cudaError_t qk_norm_rope_launch(const elasto_qk_norm_rope_args& a, int* status, cudaStream_t s);
 elasto_status window_attention_launch(const elasto_window_attention_args& a, int* status, cudaStream_t s);
+cudaError_t window_attention_init_attributes();
 
 }  // namespace elasto

@@ -1,6 +1,29 @@
-// Attention in a sliding window, the first tokens staying visible (the
-// definition is at elasto_op_window_attention): a warp for each query and head,
-// one visible key at a time with the running maximum and sum of the softmax.
+// Attention in a sliding window, the first tokens staying visible (the definition
+// is at elasto_op_window_attention), for chunks and whole sequences of queries.
+//
+//   out = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale (q . k_j) - m)
+//
+// in one pass over the visible keys with the running maximum m and sum.
+//
+// A tile is 128 rows of Q: the `hg` query heads that share a key head, times
+// 128 / hg consecutive queries, so grouped heads read K and V once and a tile
+// spans few positions (fewer keys that only some of its rows see). A work item is
+// two tiles of one sequence and key head; they share the K/V stream. Roles:
+//   warp 0     TMA: Q of both tiles, then K and V tiles of 128 keys through a ring;
+//   warp 1     tcgen05.mma: S = Q K^T into TMEM, O += P V with P read from TMEM;
+//   warps 4-11 two groups of four, one for each tile, a row a thread: scores from
+//              TMEM to registers, mask, maximum, exp2, P back to TMEM (over S).
+// While one group works on its scores the tensor cores run the other's products.
+// O stays in TMEM; it is rescaled by its group only when a row's maximum has
+// grown by more than 2^8 (else P simply is up to 2^8: exact in the sums, and the
+// division at the end cancels it). S(t) is issued after PV(t - 1), so its arrival
+// also says that O is at rest.
+//
+// Key tiles: sinks below the window join its first tile (up to 64 of them), else
+// they have tiles of their own; a tile that no row of a group sees is skipped for it.
+// Tiles that all rows see wholly take no mask. In the others values that are not
+// finite are set to zero before the product, since 0 * NaN would reach rows that
+// do not see them; the rows that do see them get them added at the end.
 #include "common.h"
 #include "ptx.cuh"
 
@@ -8,75 +31,649 @@ namespace elasto {
 
 namespace {
 
-template <bool BF>
-__device__ __forceinline__ float value(const void* p, long long i) {
-  const uint16_t b = static_cast<const uint16_t*>(p)[i];
-  return BF ? __uint_as_float(static_cast<uint32_t>(b) << 16) : __half2float(__ushort_as_half(b));
+constexpr int THREADS = 384;
+// Registers of a thread: at launch, of the four producer and MMA warps, of the eight softmax warps.
+constexpr int REGS = 168, REGS_FEW = 56, REGS_MANY = 224;
+static_assert(128 * REGS_FEW + 256 * REGS_MANY <= THREADS * REGS, "register split");
+constexpr int QT = 128, KT = 128;  // rows and keys of a tile
+constexpr int HALF = 128 * 128;    // bytes of 128 rows of 64 16-bit values
+constexpr int SMEM_LIMIT = 232448;
+constexpr int TMEM_COLS = 512, O_COL = 256;
+constexpr float kLazy = 8.0f;  // log2 of how far a row's maximum may grow before O is rescaled
+
+template <int DP>
+struct Shape {
+  static constexpr int halves = DP / 64, tile = halves * HALF;
+  static constexpr int slots = DP == 128 ? 5 : 8;
+  static constexpr int smem = 1024 + (2 + slots) * tile + 512;
+};
+static_assert(Shape<128>::smem <= SMEM_LIMIT && Shape<64>::smem <= SMEM_LIMIT, "shared memory");
+
+struct Args {
+  int batch, heads, heads_kv, group, head_dim;
+  int causal, window, sinks;  // window and sinks cut to max_keys
+  float scale_log2;
+  int max_queries, q_rows;
+  const int* q_start;
+  void* out;
+  long long out_row, out_head;
+  int out32;  // rows of out start on 32 bytes
+  int max_keys, kv_rows;
+  const int* kv_start;
+  const int* kv_len;
+  const uint16_t* v;
+  long long v_batch, v_row, v_head;
+  int hg, nsub, qpt;  // heads and queries of a tile, tiles across a head group
+  int tiles;          // tiles (groups at work) of an item: 1 or 2
+  int qtiles;         // items along the longest sequence's queries
+  int items;
+  int* status;
+};
+
+// Rows of q and keys of sequence b, cut to what the host allows.
+__device__ __forceinline__ void sequence(const Args& a, int b, int& q0, int& nq, int& k0, int& nk) {
+  q0 = b * a.max_queries, nq = a.max_queries;
+  if (a.q_start) {
+    q0 = min(max(a.q_start[b], 0), a.q_rows);
+    nq = min(max(min(a.q_start[b + 1], a.q_rows) - q0, 0), a.max_queries);
+  }
+  k0 = 0, nk = a.max_keys;
+  if (a.kv_start) {
+    k0 = min(max(a.kv_start[b], 0), a.kv_rows);
+    nk = min(max(min(a.kv_start[b + 1], a.kv_rows) - k0, 0), a.max_keys);
+  } else if (a.kv_len) {
+    nk = min(max(a.kv_len[b], 0), a.max_keys);
+  }
+}
+
+// x[g] without an address, so that the arrays stay in registers.
+template <typename T>
+__device__ __forceinline__ T of(const T (&x)[2], int g) {
+  return g ? x[1] : x[0];
+}
+
+// What every role derives alike for a work item.
+struct Item {
+  int b, kvh, head0, nheads;    // first query head and how many of the tile's
+  int q0, nq, k0, nk;
+  int first[2], last[2];        // queries of each group's rows: [first, last] (empty: last < first)
+  int lo[2], hi[2];             // its band of keys (empty: hi < lo)
+  int sinks;                    // keys [0, sinks) that belong to the item whatever the band
+  int split, sink_tiles, base0; // see key_of
+  int tiles;                    // key tiles
+
+  // Column c of key tile t holds key base(t) + c, or key c where c < split and t == 0.
+  __device__ __forceinline__ int base(int t) const { return t < sink_tiles ? t * KT : base0 + (t - sink_tiles) * KT; }
+  __device__ __forceinline__ bool has_sinks(int t) const {
+    return sinks > 0 && (t < sink_tiles || (t == 0 && split > 0) || (split == 0 && sink_tiles == 0 && base(t) < sinks));
+  }
+  __device__ __forceinline__ bool needs(int g, int t) const {
+    const int low = of(lo, g), high = of(hi, g);
+    if (high < low) return false;
+    if (has_sinks(t)) return true;
+    const int b0 = base(t);
+    return t >= sink_tiles && b0 + KT - 1 >= low && b0 <= high;
+  }
+};
+
+__device__ __forceinline__ Item make_item(const Args& a, int id) {
+  Item it;
+  const int per = a.batch * a.heads_kv * a.nsub;
+  int q = id / per, r = id - q * per;
+  if (a.causal) q = a.qtiles - 1 - q;  // the longest rows of keys first
+  const int sub = r % a.nsub;
+  r /= a.nsub;
+  it.kvh = r % a.heads_kv;
+  it.b = r / a.heads_kv;
+  it.head0 = it.kvh * a.group + sub * a.hg;
+  it.nheads = min(a.hg, a.group - sub * a.hg);
+  sequence(a, it.b, it.q0, it.nq, it.k0, it.nk);
+  int lo = 0x7fffffff, hi = -1;
+  it.sinks = 0;
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    it.first[g] = (q * a.tiles + g) * a.qpt;
+    it.last[g] = g < a.tiles ? min(it.first[g] + a.qpt, it.nq) - 1 : it.first[g] - 1;
+    const int shift = it.nk - it.nq, pmax = shift + it.last[g], pmin = max(shift + it.first[g], 0);
+    it.lo[g] = 0, it.hi[g] = -1;
+    if (it.last[g] < it.first[g] || pmax < 0 || it.nk == 0) continue;
+    if (a.causal) {
+      it.lo[g] = max(0, pmin - a.window), it.hi[g] = pmax;
+      it.sinks = max(it.sinks, min(a.sinks, pmax + 1));
+    } else {
+      it.sinks = min(a.sinks, it.nk);
+      it.lo[g] = pmin < a.sinks ? 0 : max(0, pmin - a.window);
+      it.hi[g] = pmin < a.sinks ? it.nk - 1 : max(min(it.nk - 1, pmax + a.window), it.sinks - 1);
+    }
+    lo = min(lo, it.lo[g]), hi = max(hi, it.hi[g]);
+  }
+  it.split = it.sink_tiles = 0;
+  if (it.sinks > 0) {
+    const int pad = (it.sinks + 15) & ~15;
+    if (lo <= pad)
+      lo = 0;
+    else if (pad <= 64)
+      it.split = pad;
+    else
+      it.sink_tiles = (it.sinks + KT - 1) / KT;
+  }
+  it.base0 = lo - it.split;
+  it.tiles = hi < 0 ? 0 : it.sink_tiles + (hi - it.base0) / KT + 1;
+  return it;
+}
+
+// Bits [a, b] of a 32-bit word.
+__device__ __forceinline__ uint32_t bits(int a, int b) {
+  const uint32_t up = b < 0 ? 0u : b >= 31 ? 0xffffffffu : (2u << b) - 1u;
+  return a <= 0 ? up : a > 31 ? 0u : up & (0xffffffffu << a);
+}
+
+// The columns of key tile t that the row at position p sees.
+struct Seen {
+  int a0, a1, b1;  // columns [a0, a1] and [0, b1]
+  __device__ __forceinline__ uint32_t word(int w) const { return bits(a0 - 32 * w, a1 - 32 * w) | bits(0, b1 - 32 * w); }
+};
+__device__ __forceinline__ Seen seen_columns(const Args& a, const Item& it, int t, int p) {
+  Seen s;
+  const int base = it.base(t);
+  const bool split = t == 0 && it.split > 0, sink_tile = t < it.sink_tiles;
+  int lo = max(p - a.window, 0), hi = a.causal ? p : min(p + a.window, it.nk - 1);
+  int sinks = min(a.sinks, a.causal ? p + 1 : it.nk);
+  if (!a.causal && p < a.sinks) lo = 0, hi = it.nk - 1;
+  if (p < 0) hi = -1, sinks = 0;
+  s.a0 = max(lo - base, split ? it.split : 0);
+  s.a1 = sink_tile || hi < 0 ? -1 : hi - base;
+  s.b1 = sinks - 1 - (split ? 0 : base);
+  return s;
+}
+
+__device__ __forceinline__ void store32(void* p, const uint32_t (&r)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+               "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
 }
 
 template <bool BF>
-__global__ void __launch_bounds__(256) window_attention_kernel(const __grid_constant__ elasto_window_attention_args a) {
+__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
+  return BF ? pack_bf16x2(lo, hi) : pack_f16x2(lo, hi);
+}
+template <bool BF>
+__device__ __forceinline__ float2 unpack16(uint32_t w) {
+  return BF ? make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u))
+            : __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+// Non-zero bits where one of the two values is infinite or NaN.
+template <bool BF>
+__device__ __forceinline__ uint32_t bad16(uint32_t w) {
+  constexpr uint32_t e = BF ? 0x7f807f80u : 0x7c007c00u;
+  const uint32_t x = (w & e) ^ e;  // a half of zeros: all exponent bits set
+  return ((x & 0xffffu) == 0 ? 0xffffu : 0u) | ((x >> 16) == 0 ? 0xffff0000u : 0u);
+}
+
+// Sets the values of a V tile that are not finite to zero (128 threads of a group,
+// number r); true if there were any. A quick look first: 0 * x is NaN for them alone.
+template <bool BF, int DP>
+__device__ __forceinline__ bool clear_bad_values(uint8_t* v, int r, int seq, volatile int* flag) {
+  uint4* c = reinterpret_cast<uint4*>(v);
+  uint32_t bad = 0;
+#pragma unroll 4
+  for (int i = 0; i < DP / 8; ++i) {
+    const uint4 w = c[r + 128 * i];
+    bad |= bad16<BF>(w.x) | bad16<BF>(w.y) | bad16<BF>(w.z) | bad16<BF>(w.w);
+  }
+  if (!__any_sync(0xffffffffu, bad != 0)) return false;
+  *flag = seq;
+  __threadfence_block();
+  for (int i = 0; i < DP / 8; ++i) {
+    uint4 w = c[r + 128 * i];
+    w.x &= ~bad16<BF>(w.x), w.y &= ~bad16<BF>(w.y), w.z &= ~bad16<BF>(w.z), w.w &= ~bad16<BF>(w.w);
+    c[r + 128 * i] = w;
+  }
+  fence_async_smem();
+  return true;
+}
+
+template <bool BF, int DP>
+__global__ void __launch_bounds__(THREADS, 1)
+    window_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                            const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmK16,
+                            const __grid_constant__ CUtensorMap tmV16, const __grid_constant__ Args a) {
+  using S = Shape<DP>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* qbuf = smem;                 // [group] 128 rows, in halves of 64 channels
+  uint8_t* ring = smem + 2 * S::tile;   // [slot] a K or V tile, in halves of 64 channels
+  uint64_t* bars = reinterpret_cast<uint64_t*>(ring + S::slots * S::tile);
+  uint64_t* full = bars;                // [slot]
+  uint64_t* empty = full + S::slots;    // [slot]
+  uint64_t* q_full = empty + S::slots;  // [group]
+  uint64_t* q_empty = q_full + 2;
+  uint64_t* s_full = q_empty + 2;
+  uint64_t* p_full = s_full + 2;        // 128 arrivals
+  uint64_t* o_full = p_full + 2;
+  uint64_t* drain = o_full + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  volatile int* bad_seq = reinterpret_cast<int*>(tmem_slot + 1);  // [2] item (by its number in this CTA) with bad values
+
+  const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < S::slots; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 1);
+    }
+    for (int g = 0; g < 2; ++g) {
+      mbar_init(&q_full[g], 1);
+      mbar_init(&q_empty[g], 1);
+      mbar_init(&s_full[g], 1);
+      mbar_init(&p_full[g], 128);
+      mbar_init(&o_full[g], 1);
+      bad_seq[g] = -1;
+    }
+    mbar_init(drain, 1);
+    fence_barrier_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(tmem_slot, TMEM_COLS);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = warp_uniform(static_cast<int>(*tmem_slot));
   pdl_wait();
   pdl_trigger();
-  const int lane = threadIdx.x & 31;
-  const long long unit = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-  const int head = static_cast<int>(unit % a.heads), i = static_cast<int>(unit / a.heads % a.max_queries);
-  const int b = static_cast<int>(unit / a.heads / a.max_queries);
-  if (b >= a.batch) return;
-  long long q0 = static_cast<long long>(b) * a.max_queries, nq = a.max_queries;
-  if (a.q_start) {
-    q0 = min(max(static_cast<long long>(a.q_start[b]), 0LL), a.q_rows);
-    nq = min(min(static_cast<long long>(a.q_start[b + 1]), a.q_rows) - q0, nq);
+
+  if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FEW));
+  if (warp == 0) {
+    // ------------------------------------------------------------ producer
+    if (elect_one()) {
+      tma_prefetch_desc(&tmQ);
+      tma_prefetch_desc(&tmK);
+      tma_prefetch_desc(&tmV);
+      uint32_t seq = 0, nq[2] = {0, 0};  // K/V tiles and Q tiles issued
+      bool ok = true;
+      for (int id = blockIdx.x; id < a.items && ok; id += gridDim.x) {
+        const Item it = make_item(a, id);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          if (!ok || it.hi[g] < it.lo[g]) continue;
+          ok = mbar_wait(&q_empty[g], (nq[g] & 1) ^ 1);
+          if (!ok) continue;
+          mbar_expect_tx(&q_full[g], S::halves * a.hg * a.qpt * 128);
+          for (int h = 0; h < S::halves; ++h)
+            tma_load_3d(qbuf + g * S::tile + h * HALF, &tmQ, &q_full[g], 64 * h, it.head0, it.q0 + it.first[g]);
+          ++nq[g];
+        }
+        const int batch = a.kv_start ? 0 : it.b;
+        for (int t = 0; t < it.tiles && ok; ++t)
+          for (int kv = 0; kv < 2 && ok; ++kv, ++seq) {
+            const uint32_t slot = seq % S::slots;
+            ok = mbar_wait(&empty[slot], ((seq / S::slots) & 1) ^ 1);
+            if (!ok) break;
+            uint8_t* dst = ring + slot * S::tile;
+            mbar_expect_tx(&full[slot], S::tile);
+            const int row = it.k0 + it.base(t);
+            for (int h = 0; h < S::halves; ++h) {
+              if (t > 0 || it.split == 0) {
+                tma_load_4d(dst + h * HALF, kv ? &tmV : &tmK, &full[slot], 64 * h, it.kvh, row, batch);
+              } else {  // sinks, then the window's first keys, 16 at a time
+                for (int c = 0; c < KT; c += 16)
+                  tma_load_4d(dst + h * HALF + c * 128, kv ? &tmV16 : &tmK16, &full[slot], 64 * h, it.kvh,
+                              c < it.split ? it.k0 + c : row + c, batch);
+              }
+            }
+          }
+      }
+      if (!ok) record_status(a.status, ELASTO_ERR_TIMEOUT);
+      // all copies have landed before the CTA exits
+      for (uint32_t s = seq > S::slots ? seq - S::slots : 0; s < seq; ++s) mbar_wait(&full[s % S::slots], (s / S::slots) & 1);
+      for (int g = 0; g < 2; ++g)
+        if (nq[g] > 0) mbar_wait(&q_full[g], (nq[g] - 1) & 1);
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ MMA issuer
+    const int dn = (a.head_dim + 15) & ~15;  // channels that the products take
+    const uint32_t idesc_s = idesc_16_f32(QT, KT, !BF);
+    const uint32_t idesc_o = idesc_16_f32(QT, dn, !BF, false, true);
+    uint32_t seq = 0, nq[2] = {0, 0}, np[2] = {0, 0};
+    bool ok = true, issued = false;
+    for (int id = blockIdx.x; id < a.items && ok; id += gridDim.x) {
+      const Item it = make_item(a, id);
+      bool started_s[2] = {false, false}, started_o[2] = {false, false};
+      int last_s[2] = {-1, -1};
+      for (int t = 0; t < it.tiles; ++t)
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+          if (it.needs(g, t)) last_s[g] = t;
+      auto issue_s = [&](int g, int t) -> bool {  // (K(t) has landed)
+        if (!started_s[g]) {
+          if (!mbar_wait_warp(&q_full[g], nq[g] & 1)) return false;
+          ++nq[g];
+          started_s[g] = true;
+          tc_fence_after();
+        }
+        const uint32_t slot = (seq + 2 * t) % S::slots;
+        const uint64_t dq = sdesc_sw128(smem_addr(qbuf + g * S::tile), 16, 1024);
+        const uint64_t dk = sdesc_sw128(smem_addr(ring + slot * S::tile), 16, 1024);
+        for (int k = 0; k < dn / 16; ++k) {
+          const uint64_t off = (k >> 2) * (HALF >> 4) + 2 * (k & 3);
+          tc_mma_warp(tmem + g * KT, dq + off, dk + off, idesc_s, k != 0);
+        }
+        tc_commit_warp(&s_full[g]);
+        if (t == last_s[g]) tc_commit_warp(&q_empty[g]);
+        issued = true;
+        return true;
+      };
+      auto landed = [&](uint32_t s) -> bool {
+        const bool r = mbar_wait_warp(&full[s % S::slots], (s / S::slots) & 1);
+        tc_fence_after();
+        return r;
+      };
+      if (it.tiles > 0) {
+        ok = landed(seq);
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+          if (ok && it.needs(g, 0)) ok = issue_s(g, 0);
+        if (ok) tc_commit_warp(&empty[seq % S::slots]);
+      }
+      for (int t = 0; t < it.tiles && ok; ++t) {
+        const uint32_t vs = seq + 2 * t + 1;
+        ok = landed(vs);
+        const bool more = t + 1 < it.tiles;
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          if (ok && it.needs(g, t)) ok = mbar_wait_warp(&p_full[g], np[g] & 1);
+          if (!ok) continue;
+          if (it.needs(g, t)) {
+            ++np[g];
+            tc_fence_after();
+            const uint64_t dv = sdesc_sw128(smem_addr(ring + (vs % S::slots) * S::tile), HALF, 1024);
+            for (int k = 0; k < KT / 16; ++k)
+              tc_mma_tmem_a_warp(tmem + O_COL + g * DP, tmem + g * KT + 8 * k, dv + 128 * k, idesc_o, started_o[g] || k != 0);
+            started_o[g] = true;
+            issued = true;
+            if (t == last_s[g]) tc_commit_warp(&o_full[g]);
+          }
+          if (g == 1) tc_commit_warp(&empty[vs % S::slots]);
+          if (more) {
+            if (g == 0) ok = landed(vs + 1);
+            if (ok && it.needs(g, t + 1)) ok = issue_s(g, t + 1);
+            if (ok && g == 1) tc_commit_warp(&empty[(vs + 1) % S::slots]);
+          }
+        }
+      }
+      seq += 2 * it.tiles;
+    }
+    if (!ok && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
+    if (issued) {
+      tc_commit_warp(drain);
+      mbar_wait_warp(drain, 0);
+    }
+  } else if (warp >= 4) {
+    // ------------------------------------------------------------ softmax, a row a thread
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_MANY));
+    const int g = (warp - 4) >> 2, r = (warp & 3) * 32 + lane;  // row of the tile = TMEM lane
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t s_tm = tmem + lanes + g * KT, o_tm = tmem + lanes + O_COL + g * DP;
+    const float sc = a.scale_log2;
+    uint32_t seq = 0, ns = 0, no = 0;
+    int nth = 0;
+    bool ok = true;
+    for (int id = blockIdx.x; id < a.items && ok; id += gridDim.x, ++nth) {
+      const Item it = make_item(a, id);
+      const int first = of(it.first, g), last = of(it.last, g);
+      if (last < first) {
+        seq += 2 * it.tiles;
+        continue;
+      }
+      const int qi = first + r / a.hg, head = r % a.hg;
+      const bool mine = r < a.qpt * a.hg && qi <= last && head < it.nheads;
+      const int shift = it.nk - it.nq, p = shift + qi;
+      const int pmin = shift + first, pmax = shift + last;
+      float m = -INFINITY, sum = 0.0f;
+      bool any = false;
+      for (int t = 0; t < it.tiles && ok; ++t) {
+        if (!it.needs(g, t)) continue;
+        const int base = it.base(t);
+        // every row sees every column
+        const bool whole = t >= it.sink_tiles && !(t == 0 && it.split > 0) && pmin >= 0 && base >= pmax - a.window &&
+                           base + KT - 1 <= (a.causal ? pmin : min(it.nk - 1, pmin + a.window));
+        ok = __all_sync(0xffffffffu, mbar_wait(&s_full[g], ns & 1));
+        if (!ok) break;
+        ++ns;
+        tc_fence_after();
+        uint32_t v[4][32];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tmem_ld_32x32b_x32(s_tm + 32 * i, v[i]);
+        if (!whole) {
+          const uint32_t vs = seq + 2 * t + 1;
+          ok = __all_sync(0xffffffffu, mbar_wait(&full[vs % S::slots], (vs / S::slots) & 1));
+          if (!ok) break;
+          clear_bad_values<BF, DP>(ring + (vs % S::slots) * S::tile, r, nth, &bad_seq[nth & 1]);
+        }
+        tmem_ld_wait();
+        if (!whole) {
+          const Seen s = seen_columns(a, it, t, p);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t w = s.word(i);
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (!(w >> j & 1)) v[i][j] = 0xff800000u;
+          }
+        }
+        float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 32; j += 2)
+            t4[(j >> 1) & 3] = max3(t4[(j >> 1) & 3], __uint_as_float(v[i][j]), __uint_as_float(v[i][j + 1]));
+        const float top = fmaxf(m, fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])));
+        if (__any_sync(0xffffffffu, (top - m) * sc > kLazy)) {
+          // (top - m is NaN while both are -inf: nothing seen yet, nothing to rescale)
+          const float keep = m == -INFINITY ? 0.0f : ex2_approx((m - top) * sc);
+          if (any) {
+            uint32_t o[32];
+            for (int c = 0; c < DP; c += 32) {
+              tmem_ld_32x32b_x32(o_tm + c, o);
+              tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 32; j += 2) {
+                const float2 x = mul2(make_float2(__uint_as_float(o[j]), __uint_as_float(o[j + 1])), make_float2(keep, keep));
+                o[j] = __float_as_uint(x.x), o[j + 1] = __float_as_uint(x.y);
+              }
+              uint32_t lo[16], hi[16];
+#pragma unroll
+              for (int j = 0; j < 16; ++j) lo[j] = o[j], hi[j] = o[16 + j];
+              tmem_st_16(o_tm + c, lo);
+              tmem_st_16(o_tm + c + 16, hi);
+            }
+            tmem_st_wait();
+          }
+          sum *= keep;
+          m = top;
+        }
+        any = true;
+        const float neg = m == -INFINITY ? 0.0f : -m * sc;
+        const float2 sc2 = make_float2(sc, sc), neg2 = make_float2(neg, neg);
+        float2 add[2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int j = 0; j < 32; j += 2) {
+            const float2 x = fma2(make_float2(__uint_as_float(v[i][j]), __uint_as_float(v[i][j + 1])), sc2, neg2);
+            const float2 e = make_float2(ex2_approx(x.x), ex2_approx(x.y));
+            pk[j >> 1] = pack16<BF>(e.x, e.y);
+            add[(j >> 1) & 1] = add2(add[(j >> 1) & 1], e);
+          }
+          tmem_st_16(s_tm + 16 * i, pk);
+        }
+        sum += (add[0].x + add[0].y) + (add[1].x + add[1].y);
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive(&p_full[g]);
+      }
+      seq += 2 * it.tiles;
+      if (!ok) break;
+      // ------------------------------------------------------------ result rows
+      uint16_t* out = static_cast<uint16_t*>(a.out) + static_cast<long long>(it.q0 + qi) * a.out_row +
+                      static_cast<long long>(it.head0 + head) * a.out_head;
+      if (any) {
+        ok = __all_sync(0xffffffffu, mbar_wait(&o_full[g], no & 1));
+        if (!ok) break;
+        ++no;
+        tc_fence_after();
+      }
+      const bool sees = mine && p >= 0 && it.nk > 0;
+      const float inv = 1.0f / sum;
+      const bool bad = any && bad_seq[nth & 1] == nth;
+#pragma unroll
+      for (int c = 0; c < DP; c += 32) {
+        uint32_t o[32];
+        if (any) {
+          tmem_ld_32x32b_x32(o_tm + c, o);
+          tmem_ld_wait();
+        }
+        if (bad && sees) {
+          // values that are not finite were left out of the product: add those that this row sees
+          for (int t = 0; t < it.tiles; ++t) {
+            const Seen s = seen_columns(a, it, t, p);
+            for (int col = 0; col < KT; ++col) {
+              if (!(s.word(col >> 5) >> (col & 31) & 1)) continue;
+              const long long key = it.k0 + (t == 0 && col < it.split ? col : it.base(t) + col);
+              const uint16_t* vp = a.v + (a.kv_start ? 0 : it.b * a.v_batch) + key * a.v_row + it.kvh * a.v_head + c;
+#pragma unroll
+              for (int j = 0; j < 32; j += 2) {
+                if (c + j >= a.head_dim) continue;
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(vp + j);
+                const uint32_t b2 = bad16<BF>(w);
+                const float2 x = unpack16<BF>(w);
+                if (b2 & 0xffffu) o[j] = __float_as_uint(__uint_as_float(o[j]) + x.x);
+                if (b2 >> 16) o[j + 1] = __float_as_uint(__uint_as_float(o[j + 1]) + x.y);
+              }
+            }
+          }
+        }
+        if (!mine) continue;
+        uint32_t pk[16];
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) {
+          const float2 x = mul2(make_float2(__uint_as_float(o[j]), __uint_as_float(o[j + 1])), make_float2(inv, inv));
+          pk[j >> 1] = sees ? pack16<BF>(x.x, x.y) : 0u;
+        }
+#pragma unroll
+        for (int j = 0; j < 16; j += 8) {
+          const int ch = c + 2 * j;
+          if (a.out32 && ch + 16 <= a.head_dim) {
+            const uint32_t w[8] = {pk[j], pk[j + 1], pk[j + 2], pk[j + 3], pk[j + 4], pk[j + 5], pk[j + 6], pk[j + 7]};
+            store32(out + ch, w);
+          } else {
+            if (ch < a.head_dim) *reinterpret_cast<uint4*>(out + ch) = make_uint4(pk[j], pk[j + 1], pk[j + 2], pk[j + 3]);
+            if (ch + 8 < a.head_dim)
+              *reinterpret_cast<uint4*>(out + ch + 8) = make_uint4(pk[j + 4], pk[j + 5], pk[j + 6], pk[j + 7]);
+          }
+        }
+      }
+      tc_fence_before();
+    }
+    if (!ok && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
   }
-  long long k0 = 0, nk = a.max_keys;
-  if (a.kv_start) {
-    k0 = min(max(static_cast<long long>(a.kv_start[b]), 0LL), a.kv_rows);
-    nk = min(min(static_cast<long long>(a.kv_start[b + 1]), a.kv_rows) - k0, nk);
-  } else if (a.kv_len) {
-    nk = min(static_cast<long long>(a.kv_len[b]), nk);
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem, TMEM_COLS);
   }
-  if (i >= nq) return;
-  nk = max(nk, 0LL);
-  const long long p = nk - nq + i, w = a.window < 0 ? a.max_keys : a.window;
-  const int d = a.head_dim, kvh = head / (a.heads / a.heads_kv);
-  float q[4], o[4] = {}, m = -INFINITY, sum = 0.0f;
-  for (int t = 0; t < 4; ++t)
-    q[t] = lane + 32 * t < d ? value<BF>(a.q, (q0 + i) * a.q_row + head * a.q_head + lane + 32 * t) * a.scale : 0.0f;
-  for (long long j = 0; p >= 0 && j < nk; ++j) {
-    const bool near = j >= p - w && j <= p + w;
-    const bool seen = a.causal ? j <= p && (near || j < a.sinks) : near || j < a.sinks || p < a.sinks;
-    if (!seen) continue;
-    const long long kr = b * (a.kv_start ? 0LL : a.k_batch) + (k0 + j) * a.k_row + kvh * a.k_head;
-    const long long vr = b * (a.kv_start ? 0LL : a.v_batch) + (k0 + j) * a.v_row + kvh * a.v_head;
-    float x = 0.0f;
-    for (int t = 0; t < 4; ++t)
-      if (lane + 32 * t < d) x = fmaf(q[t], value<BF>(a.k, kr + lane + 32 * t), x);
-    for (int s = 16; s > 0; s >>= 1) x += __shfl_xor_sync(0xffffffffu, x, s);
-    const float top = fmaxf(m, x), keep = expf(m - top), e = expf(x - top);
-    m = top;
-    sum = fmaf(sum, keep, e);
-    for (int t = 0; t < 4; ++t)
-      if (lane + 32 * t < d) o[t] = fmaf(o[t], keep, e * value<BF>(a.v, vr + lane + 32 * t));
-  }
-  const bool any = p >= 0 && nk > 0;
-  for (int t = 0; t < 4; ++t) {
-    const float y = any ? o[t] / sum : 0.0f;
-    const long long at = (q0 + i) * a.out_row + head * a.out_head + lane + 32 * t;
-    if (lane + 32 * t < d) static_cast<uint16_t*>(a.out)[at] = BF ? __bfloat16_as_ushort(__float2bfloat16_rn(y)) : __half_as_ushort(__float2half_rn(y));
-  }
+}
+
+// [batch][rows][heads][channels] of 16-bit values in boxes of 64 channels x `box_heads` x `box_rows`.
+bool map_of(CUtensorMap* tm, const void* p, bool bf, const elasto_window_attention_args& a, uint64_t heads, uint64_t rows,
+            uint64_t batch, long long head_s, long long row_s, long long batch_s, uint32_t box_heads, uint32_t box_rows) {
+  // (the stride of an axis of one element is never used; the encoder wants a multiple of 16 all the same)
+  const uint64_t dims[4] = {static_cast<uint64_t>(a.head_dim), heads, rows, batch};
+  const uint64_t strides[3] = {static_cast<uint64_t>(head_s) * 2, static_cast<uint64_t>(row_s) * 2,
+                               static_cast<uint64_t>(batch_s) * 2};
+  const uint32_t box[4] = {64, box_heads, box_rows, 1};
+  return encode_tmap_16(tm, p, bf, batch_s >= 0 ? 4 : 3, dims, strides, box);
+}
+
+template <bool BF, int DP>
+cudaError_t launch(const CUtensorMap (&tm)[5], const Args& a, cudaStream_t s) {
+  const int grid = a.items < num_sms() ? a.items : num_sms();
+  return launch_pdl(window_attention_kernel<BF, DP>, dim3(grid), dim3(THREADS), Shape<DP>::smem, s, tm[0], tm[1], tm[2],
+                    tm[3], tm[4], a);
 }
 
 }  // namespace
 
-elasto_status window_attention_launch(const elasto_window_attention_args& a, int* status, cudaStream_t s) {
-  const long long units = static_cast<long long>(a.batch) * a.max_queries * a.heads;
-  if (units > 8LL * 0x7fffffffLL) {
+cudaError_t window_attention_init_attributes() {
+  cudaError_t e = cudaSuccess;
+  auto set = [&](auto* f, int bytes) {
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  };
+  set(window_attention_kernel<true, 64>, Shape<64>::smem);
+  set(window_attention_kernel<false, 64>, Shape<64>::smem);
+  set(window_attention_kernel<true, 128>, Shape<128>::smem);
+  set(window_attention_kernel<false, 128>, Shape<128>::smem);
+  // the register split adds up only if the kernels were built with the launch's count
+  auto check = [&](auto* f) {
+    cudaFuncAttributes at{};
+    if (e == cudaSuccess) e = cudaFuncGetAttributes(&at, f);
+    if (e == cudaSuccess && at.numRegs != REGS) e = cudaErrorInvalidConfiguration;
+  };
+  check(window_attention_kernel<true, 64>);
+  check(window_attention_kernel<false, 64>);
+  check(window_attention_kernel<true, 128>);
+  check(window_attention_kernel<false, 128>);
+  return e;
+}
+
+elasto_status window_attention_launch(const elasto_window_attention_args& u, int* status, cudaStream_t s) {
+  Args a{};
+  a.batch = u.batch, a.heads = u.heads, a.heads_kv = u.heads_kv, a.group = u.heads / u.heads_kv, a.head_dim = u.head_dim;
+  a.causal = u.causal != 0;
+  a.window = u.window < 0 || u.window > u.max_keys ? u.max_keys : u.window;
+  a.sinks = u.sinks > u.max_keys ? u.max_keys : u.sinks;
+  a.scale_log2 = u.scale * 1.4426950408889634f;
+  a.max_queries = u.max_queries, a.q_rows = static_cast<int>(u.q_rows), a.q_start = u.q_start;
+  a.out = u.out, a.out_row = u.out_row, a.out_head = u.out_head;
+  a.out32 = reinterpret_cast<uintptr_t>(u.out) % 32 == 0 && u.out_row % 16 == 0 && u.out_head % 16 == 0;
+  a.max_keys = u.max_keys, a.kv_rows = static_cast<int>(u.kv_rows), a.kv_start = u.kv_start, a.kv_len = u.kv_len;
+  a.v = static_cast<const uint16_t*>(u.v), a.v_batch = u.v_batch, a.v_row = u.v_row, a.v_head = u.v_head;
+  a.status = status;
+  // heads of a tile: the whole group, or for more than 32 equal parts of it
+  a.nsub = (a.group + 31) / 32;
+  a.hg = (a.group + a.nsub - 1) / a.nsub;
+  a.qpt = QT / a.hg;
+  const long long per = static_cast<long long>(a.batch) * a.heads_kv * a.nsub;
+  const long long rows = (a.max_queries + a.qpt - 1LL) / a.qpt;
+  a.tiles = rows * per > num_sms() ? 2 : 1;  // one tile an item where the chip would be half empty
+  const long long qtiles = (rows + a.tiles - 1) / a.tiles;
+  if (qtiles * per > 0x3fffffffLL) {
     set_error("elasto_op_window_attention: too many queries");
     return ELASTO_ERR_UNSUPPORTED;
   }
-  const dim3 grid(static_cast<unsigned>((units + 7) / 8));
-  ELASTO_CUDA_TRY(a.dtype == ELASTO_BF16 ? launch_pdl(window_attention_kernel<true>, grid, dim3(256), 0, s, a)
-                                         : launch_pdl(window_attention_kernel<false>, grid, dim3(256), 0, s, a));
+  a.qtiles = static_cast<int>(qtiles);
+  a.items = static_cast<int>(qtiles * per);
+  const bool bf = u.dtype == ELASTO_BF16;
+  const uint64_t kvb = u.kv_start ? 1 : u.batch;
+  const long long kb = u.kv_start ? 0 : u.k_batch, vb = u.kv_start ? 0 : u.v_batch;
+  CUtensorMap tm[5];
+  if (!map_of(&tm[0], u.q, bf, u, u.heads, u.q_rows, 1, u.q_head, u.q_row, -1, a.hg, a.qpt) ||
+      !map_of(&tm[1], u.k, bf, u, u.heads_kv, u.kv_rows, kvb, u.k_head, u.k_row, kb, 1, KT) ||
+      !map_of(&tm[2], u.v, bf, u, u.heads_kv, u.kv_rows, kvb, u.v_head, u.v_row, vb, 1, KT) ||
+      !map_of(&tm[3], u.k, bf, u, u.heads_kv, u.kv_rows, kvb, u.k_head, u.k_row, kb, 1, 16) ||
+      !map_of(&tm[4], u.v, bf, u, u.heads_kv, u.kv_rows, kvb, u.v_head, u.v_row, vb, 1, 16)) {
+    set_error("elasto_op_window_attention: cuTensorMapEncodeTiled failed (alignment, strides or size)");
+    return ELASTO_ERR_UNSUPPORTED;
+  }
+  cudaError_t e;
+  if (u.head_dim <= 64)
+    e = bf ? launch<true, 64>(tm, a, s) : launch<false, 64>(tm, a, s);
+  else
+    e = bf ? launch<true, 128>(tm, a, s) : launch<false, 128>(tm, a, s);
+  ELASTO_CUDA_TRY(e);
   return ELASTO_OK;
 }
 
