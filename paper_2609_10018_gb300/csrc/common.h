@@ -349,6 +349,7 @@ struct Fp8Gemm {
   int* status;
 };
 elasto_status gemm_fp8_launch(const Fp8Gemm& g, cudaStream_t s);
+cudaError_t gemm_fp8_init_attributes();
 cudaError_t qk_norm_rope_launch(const elasto_qk_norm_rope_args& a, int* status, cudaStream_t s);
 elasto_status window_attention_launch(const elasto_window_attention_args& a, int* status, cudaStream_t s);
 cudaError_t window_attention_init_attributes();

@@ -1,8 +1,18 @@
 // Product of e4m3 rows with e4m3 weights, both with fp32 scales for blocks of 128:
 //   out[m, n] = epi( sum_b as[b, m] ws[n / 128, b] sum_{k in block b} A[m, k] W[n, k] + bias[n] ).
 //
-// A 64 x 64 tile per CTA; each block of 128 columns is staged in shared memory as
-// fp32 and summed in fp32, then scaled into the tile's sums.
+// The scales are fp32 numbers, so the tensor core cannot apply them: the sum over
+// a block of 128 columns is one accumulator in TMEM, and the running sum lives in
+// registers, where block b is added as acc += part * (as ws). A k-block is one
+// 128-byte row of A and W in the 128-byte swizzle: four K = 32 steps.
+//   warp 0      TMA producer of a ring of A and W tiles;
+//   warp 1      tcgen05.mma (kind::f8f6f4), block after block into two accumulators
+//               in turn;
+//   warps 4-11  read the finished accumulator while the other fills; two warps share
+//               32 rows, each half of the tile's columns (a row a thread); after the
+//               last block they add the bias and store.
+#include <algorithm>
+
 #include "act.cuh"
 #include "common.h"
 #include "ptx.cuh"
@@ -11,76 +21,442 @@ namespace elasto {
 
 namespace {
 
-constexpr int T = 64, BK = 32, SCALE_BLOCK = 128;
+constexpr int THREADS = 384, EPI_WARPS = 8;
+constexpr int REGS = 168, REGS_FEW = 40, REGS_MANY = 232;  // at launch; of warps 0-3 and 4-11 after the split
+static_assert(128 * REGS_FEW + 256 * REGS_MANY <= THREADS * REGS, "register split");
+constexpr int BM = 128, BK = 128, A_STAGE = BM * BK;
+constexpr int TMEM_COLS = 512;
+constexpr int MAX_STAGES = 8;
+constexpr int PIECE = 32 * 128;  // output staging of an epilogue warp: 32 rows of 128 bytes, two of them
+constexpr int PIECES = 2 * EPI_WARPS * PIECE;
+constexpr int SMEM_LIMIT = 232448;
 
-__device__ __forceinline__ float e4m3_value(uint8_t v) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(v)));
-  return __low2float(*reinterpret_cast<__half2*>(&h));
+template <bool PAIR, int BN>
+struct Tile {
+  static constexpr int b_stage = (PAIR ? BN / 2 : BN) * BK, stage = A_STAGE + b_stage;
+  static constexpr int room = (SMEM_LIMIT - 1024 - 512 - PIECES) / stage;
+  static constexpr int stages = room < MAX_STAGES ? room : MAX_STAGES;
+  static constexpr int smem = 1024 + stages * stage + PIECES + 512;
+  static constexpr int tm = PAIR ? 2 * BM : BM;
+  static constexpr int cols = BN / 2;  // of an epilogue warp
+};
+
+struct Args {
+  int M, N, K, nkb;
+  const float* a_scale;
+  long long lds;
+  const float* w_scale;
+  const float* bias;
+  void* out;
+  long long ldo;
+  int tma;  // rows of out start on 16 bytes: tiles leave by TMA
+  int* status;
+};
+
+template <int EPI>
+constexpr bool f32_out = EPI == EPI_BIAS_RESID_F32 || EPI == EPI_BIAS_F32;
+
+template <int EPI>
+__device__ __forceinline__ void store_one(const Args& a, long long at, float x) {
+  if constexpr (EPI == EPI_BIAS_F32)
+    static_cast<float*>(a.out)[at] = x;
+  else if constexpr (EPI == EPI_BIAS_RESID_F32)
+    static_cast<float*>(a.out)[at] += x;
+  else
+    static_cast<bf16*>(a.out)[at] = __float2bfloat16_rn(x);
 }
 
-__global__ void __launch_bounds__(256) gemm_fp8_kernel(Fp8Gemm g) {
-  __shared__ float sa[T][BK + 1], sw[T][BK + 1];
-  pdl_wait();
-  pdl_trigger();
-  const int tiles_n = (g.N + T - 1) / T;
-  const int m0 = static_cast<int>(blockIdx.x / tiles_n) * T, n0 = static_cast<int>(blockIdx.x % tiles_n) * T;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int nkb = (g.K + SCALE_BLOCK - 1) / SCALE_BLOCK;
-  float acc[4][4] = {};
-  for (int b = 0; b < nkb; ++b) {
-    float part[4][4] = {};
-    for (int k0 = b * SCALE_BLOCK; k0 < min(g.K, (b + 1) * SCALE_BLOCK); k0 += BK) {
-      __syncthreads();
-      for (int i = threadIdx.x; i < T * BK; i += 256) {
-        const int r = i / BK, k = i % BK;
-        sa[r][k] = m0 + r < g.M && k0 + k < g.K ? e4m3_value(g.A[static_cast<size_t>(m0 + r) * g.lda + k0 + k]) : 0.0f;
-        sw[r][k] = n0 + r < g.N && k0 + k < g.K ? e4m3_value(g.W[static_cast<size_t>(n0 + r) * g.ldw + k0 + k]) : 0.0f;
-      }
-      __syncthreads();
-#pragma unroll 8
-      for (int k = 0; k < BK; ++k)
+// 32 finished columns of a warp's 32 rows, a row a lane: out[row0 + lane, col .. col + 32). part: which
+// 64 bytes of a 128-byte staging row (16-bit types take two chunks). NARROW: one chunk of a 16-bit
+// type is all the warp has; its rows are 64 bytes, not swizzled.
+template <int EPI, bool NARROW>
+__device__ __forceinline__ void store_chunk(const Args& a, const CUtensorMap* tmC, uint8_t* piece, int part, int lane, int row0,
+                                            int col, float2 (&x)[16]) {
+  if constexpr (EPI == EPI_BIAS_GELU_BF16) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+    for (int j = 0; j < 16; ++j) x[j] = gelu2(x[j]);
+  }
+  if (!a.tma) {
+    // transposed in shared memory, so that a row's values leave together
+    float* t = reinterpret_cast<float*>(piece);
+    __syncwarp();
 #pragma unroll
-          for (int j = 0; j < 4; ++j) part[i][j] = fmaf(sa[ty * 4 + i][k], sw[tx + 16 * j][k], part[i][j]);
+    for (int j = 0; j < 16; ++j) {
+      t[lane * 32 + ((2 * j) ^ lane)] = x[j].x;
+      t[lane * 32 + ((2 * j + 1) ^ lane)] = x[j].y;
     }
+    __syncwarp();
+    if (col + lane < a.N)
+      for (int i = 0; i < 32 && row0 + i < a.M; ++i)
+        store_one<EPI>(a, (row0 + i) * a.ldo + col + lane, t[i * 32 + (lane ^ i)]);
+    return;
+  }
+  // 16-byte pieces of the staging row, swizzled as the box is
+  uint8_t* const rowp = piece + lane * (NARROW ? 64 : 128);
+  if constexpr (f32_out<EPI>) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int m = m0 + ty * 4 + i;
-      const float as = m < g.M ? g.a_scale[static_cast<size_t>(b) * g.lds + m] : 0.0f;
+    for (int j = 0; j < 8; ++j)
+      *reinterpret_cast<float4*>(rowp + ((j ^ (lane & 7)) << 4)) = make_float4(x[2 * j].x, x[2 * j].y, x[2 * j + 1].x, x[2 * j + 1].y);
+  } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int n = n0 + tx + 16 * j;
-        if (m < g.M && n < g.N)
-          acc[i][j] = fmaf(part[i][j], as * g.w_scale[static_cast<size_t>(n / SCALE_BLOCK) * nkb + b], acc[i][j]);
-      }
+    for (int j = 0; j < 4; ++j)
+      *reinterpret_cast<uint4*>(rowp + (NARROW ? j << 4 : ((4 * part + j) ^ (lane & 7)) << 4)) =
+          make_uint4(pack_bf16x2(x[4 * j].x, x[4 * j].y), pack_bf16x2(x[4 * j + 1].x, x[4 * j + 1].y),
+                     pack_bf16x2(x[4 * j + 2].x, x[4 * j + 2].y), pack_bf16x2(x[4 * j + 3].x, x[4 * j + 3].y));
+    if (!NARROW) {
+      if (part == 0) return;
+      col -= 32;
     }
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int m = m0 + ty * 4 + i, n = n0 + tx + 16 * j;
-      if (m >= g.M || n >= g.N) continue;
-      const size_t at = static_cast<size_t>(m) * g.ldo + n;
-      const float y = acc[i][j] + (g.bias ? g.bias[n] : 0.0f);
-      if (g.epi == EPI_BIAS_BF16) static_cast<bf16*>(g.out)[at] = __float2bfloat16_rn(y);
-      if (g.epi == EPI_BIAS_GELU_BF16) static_cast<bf16*>(g.out)[at] = __float2bfloat16_rn(gelu(y));
-      if (g.epi == EPI_BIAS_F32) static_cast<float*>(g.out)[at] = y;
-      if (g.epi == EPI_BIAS_RESID_F32) static_cast<float*>(g.out)[at] += y;
+  fence_async_smem();
+  __syncwarp();
+  if (elect_one()) {
+    if (row0 < a.M) {
+      if constexpr (EPI == EPI_BIAS_RESID_F32)
+        tma_add_2d(tmC, piece, col, row0);
+      else
+        tma_store_2d(tmC, piece, col, row0);
     }
+    bulk_commit();
+  }
+}
+
+template <bool PAIR, int BN, int EPI>
+__global__ void __launch_bounds__(THREADS, 1)
+    gemm_fp8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                    const __grid_constant__ CUtensorMap tmC, const __grid_constant__ Args a) {
+  using T = Tile<PAIR, BN>;
+  constexpr int S = T::stages;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* sA = smem;
+  uint8_t* sB = smem + S * A_STAGE;
+  uint8_t* pieces = smem + S * T::stage;
+  uint64_t* full = reinterpret_cast<uint64_t*>(pieces + PIECES);
+  uint64_t* empty = full + MAX_STAGES;
+  uint64_t* tfull = empty + MAX_STAGES;  // [2]
+  uint64_t* tempty = tfull + 2;          // [2]
+  uint64_t* drain = tempty + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+
+  const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const int rank = PAIR ? warp_uniform(static_cast<int>(cluster_ctarank())) : 0;
+  const int t_start = PAIR ? warp_uniform(static_cast<int>(cluster_id_x())) : static_cast<int>(blockIdx.x);
+  const int t_stride = PAIR ? warp_uniform(static_cast<int>(cluster_count_x())) : static_cast<int>(gridDim.x);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < S; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&tfull[i], 1);
+      mbar_init(&tempty[i], (PAIR ? 2 : 1) * EPI_WARPS);
+    }
+    mbar_init(drain, 1);
+    fence_barrier_init();
+  }
+  if (warp == 0) {
+    if constexpr (PAIR) {
+      tmem_alloc_pair(tmem_slot, TMEM_COLS);
+      tmem_relinquish_pair();
+    } else {
+      tmem_alloc(tmem_slot, TMEM_COLS);
+      tmem_relinquish();
+    }
+  }
+  if (warp == 1 && elect_one()) {
+    tma_prefetch_desc(&tmA);
+    tma_prefetch_desc(&tmB);
+  }
+  tc_fence_before();
+  if constexpr (PAIR)
+    cluster_sync_all();
+  else
+    __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = warp_uniform(static_cast<int>(*tmem_slot));
+  pdl_wait();
+  pdl_trigger();
+
+  const int nt = (a.N + BN - 1) / BN, tiles = (a.M + T::tm - 1) / T::tm * nt, nkb = a.nkb;
+  if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FEW));
+  if (warp == 0) {
+    // ------------------------------------------------------------ producer
+    if (elect_one()) {
+      uint32_t seq = 0;
+      bool ok = true;
+      for (int t = t_start; t < tiles && ok; t += t_stride) {
+        const int m0 = t / nt * T::tm + rank * BM, n0 = t % nt * BN + rank * (BN / 2);
+        for (int kb = 0; kb < nkb; ++kb, ++seq) {
+          const uint32_t s = seq % S;
+          ok = mbar_wait(&empty[s], ((seq / S) & 1) ^ 1);
+          if (!ok) break;
+          if constexpr (PAIR) {
+            const uint32_t lead = cluster_map(smem_addr(&full[s]), 0);
+            if (rank == 0) mbar_expect_tx(&full[s], 2 * T::stage);
+            tma_load_2d_pair(sA + s * A_STAGE, &tmA, lead, kb * BK, m0);
+            tma_load_2d_pair(sB + s * T::b_stage, &tmB, lead, kb * BK, n0);
+          } else {
+            mbar_expect_tx(&full[s], T::stage);
+            tma_load_2d(sA + s * A_STAGE, &tmA, &full[s], kb * BK, m0);
+            tma_load_2d(sB + s * T::b_stage, &tmB, &full[s], kb * BK, n0);
+          }
+        }
+      }
+      if (!ok) record_status(a.status, ELASTO_ERR_TIMEOUT);
+      // all copies have landed before the CTA exits (a pair's are counted on the even CTA's barriers)
+      if (rank == 0)
+        for (uint32_t q = seq > S ? seq - S : 0; q < seq; ++q) mbar_wait(&full[q % S], (q / S) & 1);
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ MMA issuer
+    if (rank == 0) {
+      const uint32_t idesc = idesc_e4m3_f32(T::tm, BN);
+      uint32_t seq = 0;
+      bool ok = true;
+      for (int t = t_start; t < tiles && ok; t += t_stride)
+        for (int kb = 0; kb < nkb; ++kb, ++seq) {
+          const uint32_t s = seq % S, acc = seq & 1;
+          ok = mbar_wait_warp(&tempty[acc], ((seq >> 1) & 1) ^ 1) && mbar_wait_warp(&full[s], (seq / S) & 1);
+          if (!ok) break;
+          tc_fence_after();
+          const uint64_t da = sdesc_sw128(smem_addr(sA + s * A_STAGE), 16, 1024);
+          const uint64_t db = sdesc_sw128(smem_addr(sB + s * T::b_stage), 16, 1024);
+#pragma unroll
+          for (int k = 0; k < BK / 32; ++k) {
+            if constexpr (PAIR)
+              tc_mma_f8_pair_warp(tmem + acc * 256, da + 2 * k, db + 2 * k, idesc, k != 0);
+            else
+              tc_mma_f8_warp(tmem + acc * 256, da + 2 * k, db + 2 * k, idesc, k != 0);
+          }
+          if constexpr (PAIR) {
+            tc_commit_pair_multicast_warp(&empty[s], 0x3);
+            tc_commit_pair_multicast_warp(&tfull[acc], 0x3);
+          } else {
+            tc_commit_warp(&empty[s]);
+            tc_commit_warp(&tfull[acc]);
+          }
+        }
+      if (!ok && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
+      if (seq > 0) {
+        if constexpr (PAIR) {
+          if (elect_one()) tc_commit_pair(drain);
+        } else {
+          tc_commit_warp(drain);
+        }
+        mbar_wait_warp(drain, 0);
+      }
+    }
+  } else if (warp >= 4) {
+    // ------------------------------------------------------------ sums and epilogue
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_MANY));
+    constexpr int C = T::cols;
+    const int q = warp & 3, h = (warp - 4) >> 2;
+    const uint32_t tm = tmem + (static_cast<uint32_t>(q * 32) << 16) + h * C;
+    uint8_t* const piece = pieces + (warp - 4) * 2 * PIECE;
+    uint32_t seq = 0;
+    bool ok = true;
+    // scales of the first two blocks and the bias of a tile, requested before the tile ahead of it is stored
+    const float *as, *ws;
+    float sa0, sw0, sa1, sw1, bias[C / 32];
+    auto request = [&](int t) {
+      if (t >= tiles) return;
+      const int row = min(t / nt * T::tm + rank * BM + q * 32 + lane, a.M - 1), col = t % nt * BN + h * C;
+      as = a.a_scale + row;
+      ws = a.w_scale + static_cast<size_t>(min(col, a.N - 1) / 128) * nkb;
+      const int k1 = nkb > 1 ? 1 : 0;
+      sa0 = __ldg(as), sw0 = __ldg(ws), sa1 = __ldg(as + k1 * a.lds), sw1 = __ldg(ws + k1);
+#pragma unroll
+      for (int c = 0; c < C / 32; ++c)
+        bias[c] = a.bias && col + 32 * c + lane < a.N ? __ldg(a.bias + col + 32 * c + lane) : 0.0f;
+    };
+    request(t_start);
+    for (int t = t_start; t < tiles && ok; t += t_stride) {
+      const int row0 = t / nt * T::tm + rank * BM + q * 32, col0 = t % nt * BN + h * C;
+      float2 acc[C / 2];
+#pragma unroll
+      for (int j = 0; j < C / 2; ++j) acc[j] = make_float2(0.0f, 0.0f);
+      float s0 = sa0 * sw0, s1 = sa1 * sw1;  // of this block and the next; the one after is on its way
+      for (int kb = 0; kb < nkb; ++kb, ++seq) {
+        const int p = seq & 1;
+        const float sa = kb + 2 < nkb ? __ldg(as + (kb + 2) * a.lds) : 0.0f, sw = kb + 2 < nkb ? __ldg(ws + kb + 2) : 0.0f;
+        ok = __all_sync(0xffffffffu, mbar_wait(&tfull[p], (seq >> 1) & 1));
+        if (!ok) break;
+        tc_fence_after();
+        const float2 s2 = make_float2(s0, s0);
+        auto add = [&](const uint32_t (&v)[32], int c) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            acc[16 * c + j] = fma2(make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), s2, acc[16 * c + j]);
+        };
+        auto release = [&] {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            if constexpr (PAIR)
+              mbar_arrive_cluster(cluster_map(smem_addr(&tempty[p]), 0));
+            else
+              mbar_arrive(&tempty[p]);
+          }
+        };
+        uint32_t v[2][32];
+        tmem_ld_32x32b_x32(tm + p * 256, v[0]);
+        if constexpr (C >= 64) tmem_ld_32x32b_x32(tm + p * 256 + 32, v[1]);
+        tmem_ld_wait();
+        if constexpr (C < 128) release();
+        add(v[0], 0);
+        if constexpr (C == 128) tmem_ld_32x32b_x32(tm + p * 256 + 64, v[0]);
+        if constexpr (C >= 64) add(v[1], 1);
+        if constexpr (C == 128) {
+          tmem_ld_32x32b_x32(tm + p * 256 + 96, v[1]);
+          tmem_ld_wait();
+          release();
+          add(v[0], 2);
+          add(v[1], 3);
+        }
+        s0 = s1;
+        s1 = sa * sw;
+      }
+      if (!ok) break;
+      float b[C / 32];
+#pragma unroll
+      for (int c = 0; c < C / 32; ++c) b[c] = bias[c];
+      request(t + t_stride);
+      constexpr bool narrow = C == 32 && !f32_out<EPI>;
+      constexpr int per = f32_out<EPI> || narrow ? 1 : 2;  // chunks of a staging piece
+#pragma unroll
+      for (int c = 0; c < C / 32; ++c) {
+        const int col = col0 + 32 * c, part = c % per;
+        if (col - 32 * part >= a.N) continue;
+        if (a.bias)
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            acc[16 * c + j] = add2(acc[16 * c + j], make_float2(__shfl_sync(0xffffffffu, b[c], 2 * j),
+                                                                __shfl_sync(0xffffffffu, b[c], 2 * j + 1)));
+        float2 x[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x[j] = acc[16 * c + j];
+        if (part == 0) {  // the piece's last store has read it
+          if (elect_one()) bulk_wait_read<1>();
+          __syncwarp();
+        }
+        store_chunk<EPI, narrow>(a, &tmC, piece + (c / per & 1) * PIECE, part, lane, row0, col, x);
+      }
+    }
+    if (elect_one()) bulk_wait_all();
+    if (!ok && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if constexpr (PAIR) cluster_sync_all();
+  if (warp == 0) {
+    __syncwarp();
+    tc_fence_after();
+    if constexpr (PAIR)
+      tmem_dealloc_pair(tmem, TMEM_COLS);
+    else
+      tmem_dealloc(tmem, TMEM_COLS);
+  }
+}
+
+template <bool PAIR, int BN, int EPI>
+cudaError_t launch(const Fp8Gemm& g, const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& tc, const Args& a, cudaStream_t s) {
+  using T = Tile<PAIR, BN>;
+  const long long tiles = (g.M + T::tm - 1LL) / T::tm * ((g.N + BN - 1LL) / BN);
+  if constexpr (PAIR) {
+    int pairs = 0;
+    const cudaError_t e = max_cta_pairs(reinterpret_cast<const void*>(gemm_fp8_kernel<PAIR, BN, EPI>), THREADS, T::smem, &pairs);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // see launch_pdl
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3(static_cast<unsigned>(2 * std::min<long long>(tiles, pairs)));
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = T::smem;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, gemm_fp8_kernel<PAIR, BN, EPI>, ta, tb, tc, a);
+  } else {
+    return launch_pdl(gemm_fp8_kernel<PAIR, BN, EPI>, dim3(static_cast<unsigned>(std::min<long long>(tiles, num_sms()))),
+                      dim3(THREADS), T::smem, s, ta, tb, tc, a);
+  }
+}
+
+template <bool PAIR, int BN>
+cudaError_t launch_epi(const Fp8Gemm& g, const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& tc, const Args& a, cudaStream_t s) {
+  switch (g.epi) {
+    case EPI_BIAS_BF16: return launch<PAIR, BN, EPI_BIAS_BF16>(g, ta, tb, tc, a, s);
+    case EPI_BIAS_GELU_BF16: return launch<PAIR, BN, EPI_BIAS_GELU_BF16>(g, ta, tb, tc, a, s);
+    case EPI_BIAS_RESID_F32: return launch<PAIR, BN, EPI_BIAS_RESID_F32>(g, ta, tb, tc, a, s);
+    default: return launch<PAIR, BN, EPI_BIAS_F32>(g, ta, tb, tc, a, s);
+  }
+}
+
+template <bool PAIR, int BN, int EPI>
+void set_attributes(cudaError_t* e) {
+  auto* f = gemm_fp8_kernel<PAIR, BN, EPI>;
+  if (*e == cudaSuccess) *e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, Tile<PAIR, BN>::smem);
+  cudaFuncAttributes at{};
+  if (*e == cudaSuccess) *e = cudaFuncGetAttributes(&at, f);
+  // the register split adds up only if the kernel was built with the launch's count
+  if (*e == cudaSuccess && at.numRegs != REGS) *e = cudaErrorInvalidConfiguration;
+}
+template <bool PAIR, int BN>
+void set_attributes_of(cudaError_t* e) {
+  set_attributes<PAIR, BN, EPI_BIAS_BF16>(e);
+  set_attributes<PAIR, BN, EPI_BIAS_GELU_BF16>(e);
+  set_attributes<PAIR, BN, EPI_BIAS_RESID_F32>(e);
+  set_attributes<PAIR, BN, EPI_BIAS_F32>(e);
 }
 
 }  // namespace
 
+cudaError_t gemm_fp8_init_attributes() {
+  cudaError_t e = cudaSuccess;
+  set_attributes_of<true, 256>(&e);
+  set_attributes_of<false, 128>(&e);
+  set_attributes_of<false, 64>(&e);
+  return e;
+}
+
 elasto_status gemm_fp8_launch(const Fp8Gemm& g, cudaStream_t s) {
-  const long long tiles = ((g.M + T - 1LL) / T) * ((g.N + T - 1LL) / T);
-  if (tiles > 0x7fffffffLL) {
+  const long long rows = (g.M + BM - 1LL) / BM;
+  if (rows * ((g.N + 63LL) / 64) > 0x7fffffffLL) {
     set_error("elasto_op_gemm_fp8: output too large");
     return ELASTO_ERR_UNSUPPORTED;
   }
-  ELASTO_CUDA_TRY(launch_pdl(gemm_fp8_kernel, dim3(static_cast<unsigned>(tiles)), dim3(256), 0, s, g));
+  Args a{};
+  a.M = g.M, a.N = g.N, a.K = g.K, a.nkb = (g.K + BK - 1) / BK;
+  a.a_scale = g.a_scale, a.lds = g.lds, a.w_scale = g.w_scale, a.bias = g.bias;
+  a.out = g.out, a.ldo = g.ldo, a.status = g.status;
+  const int size = g.epi == EPI_BIAS_RESID_F32 || g.epi == EPI_BIAS_F32 ? 4 : 2;
+  const uintptr_t starts = reinterpret_cast<uintptr_t>(g.out) | static_cast<uintptr_t>(g.ldo * size);
+  a.tma = starts % 16 == 0;
+  const int sms = num_sms();
+  const long long pair_tiles = (g.M + 255LL) / 256 * ((g.N + 255LL) / 256);
+  const int bn = pair_tiles >= sms / 2 ? 256 : rows * ((g.N + 127LL) / 128) >= sms ? 128 : 64;
+  CUtensorMap ta, tb, tc{};
+  const uint64_t od[2] = {static_cast<uint64_t>(g.N), static_cast<uint64_t>(g.M)}, os[1] = {static_cast<uint64_t>(g.ldo) * size};
+  const bool narrow = bn == 64 && size == 2;
+  const uint32_t ob[2] = {narrow ? 32u : 128u / size, 32};
+  if ((a.tma && !encode_tmap_plain(&tc, g.out, 2, od, os, ob, size == 4, !narrow)) ||
+      !encode_tmap_8(&ta, g.A, g.K, g.M, g.lda, BM) || !encode_tmap_8(&tb, g.W, g.K, g.N, g.ldw, bn == 256 ? 128 : bn)) {
+    set_error("elasto_op_gemm_fp8: cuTensorMapEncodeTiled failed (alignment or size)");
+    return ELASTO_ERR_UNSUPPORTED;
+  }
+  if (bn == 256) {
+    ELASTO_CUDA_TRY((launch_epi<true, 256>(g, ta, tb, tc, a, s)));
+  } else if (bn == 128) {
+    ELASTO_CUDA_TRY((launch_epi<false, 128>(g, ta, tb, tc, a, s)));
+  } else {
+    ELASTO_CUDA_TRY((launch_epi<false, 64>(g, ta, tb, tc, a, s)));
+  }
   return ELASTO_OK;
 }
 

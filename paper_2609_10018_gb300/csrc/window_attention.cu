@@ -187,12 +187,6 @@ __device__ __forceinline__ Seen seen_columns(const Args& a, const Item& it, int 
   return s;
 }
 
-__device__ __forceinline__ void store32(void* p, const uint32_t (&r)[8]) {
-  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
-               "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-               : "memory");
-}
-
 template <bool BF>
 __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
   return BF ? pack_bf16x2(lo, hi) : pack_f16x2(lo, hi);
@@ -567,7 +561,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           const int ch = c + 2 * j;
           if (a.out32 && ch + 16 <= a.head_dim) {
             const uint32_t w[8] = {pk[j], pk[j + 1], pk[j + 2], pk[j + 3], pk[j + 4], pk[j + 5], pk[j + 6], pk[j + 7]};
-            store32(out + ch, w);
+            store_32b(out + ch, w);
           } else {
             if (ch < a.head_dim) *reinterpret_cast<uint4*>(out + ch) = make_uint4(pk[j], pk[j + 1], pk[j + 2], pk[j + 3]);
             if (ch + 8 < a.head_dim)

@@ -77,6 +77,13 @@ def test_sizes(M, N, K, epi):
     _check(M, N, K, epi)
 
 
+@pytest.mark.parametrize("M,N,K", [(2560, 2304, 256), (2500, 2101, 392), (5000, 1100, 136), (257, 20000, 130)])
+@pytest.mark.parametrize("epi", [BF16, GELU, RESID, F32])
+def test_large_outputs(M, N, K, epi):
+    """Enough tiles for CTA pairs; whole, ragged and odd."""
+    _check(M, N, K, epi)
+
+
 @pytest.mark.parametrize("M,N,K", [(1, 64, 128), (12, 257, 300), (129, 255, 384), (513, 1030, 777), (300, 512, 1152)])
 @pytest.mark.parametrize("epi", [GELU, RESID])
 def test_gelu_and_residual(M, N, K, epi):
