@@ -29,14 +29,15 @@ constexpr int TMEM_COLS = 512;
 constexpr int MAX_STAGES = 8;
 constexpr int PIECE = 32 * 128;  // output staging of an epilogue warp: 32 rows of 128 bytes, two of them
 constexpr int PIECES = 2 * EPI_WARPS * PIECE;
+constexpr int TAIL = EPI_WARPS * 128 + 512;  // 32 values of the bias for each epilogue warp, barriers
 constexpr int SMEM_LIMIT = 232448;
 
 template <bool PAIR, int BN>
 struct Tile {
   static constexpr int b_stage = (PAIR ? BN / 2 : BN) * BK, stage = A_STAGE + b_stage;
-  static constexpr int room = (SMEM_LIMIT - 1024 - 512 - PIECES) / stage;
+  static constexpr int room = (SMEM_LIMIT - 1024 - TAIL - PIECES) / stage;
   static constexpr int stages = room < MAX_STAGES ? room : MAX_STAGES;
-  static constexpr int smem = 1024 + stages * stage + PIECES + 512;
+  static constexpr int smem = 1024 + stages * stage + PIECES + TAIL;
   static constexpr int tm = PAIR ? 2 * BM : BM;
   static constexpr int cols = BN / 2;  // of an epilogue warp
 };
@@ -132,7 +133,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint8_t* sA = smem;
   uint8_t* sB = smem + S * A_STAGE;
   uint8_t* pieces = smem + S * T::stage;
-  uint64_t* full = reinterpret_cast<uint64_t*>(pieces + PIECES);
+  float* sbias = reinterpret_cast<float*>(pieces + PIECES);
+  uint64_t* full = reinterpret_cast<uint64_t*>(sbias + EPI_WARPS * 32);
   uint64_t* empty = full + MAX_STAGES;
   uint64_t* tfull = empty + MAX_STAGES;  // [2]
   uint64_t* tempty = tfull + 2;          // [2]
@@ -254,6 +256,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     const int q = warp & 3, h = (warp - 4) >> 2;
     const uint32_t tm = tmem + (static_cast<uint32_t>(q * 32) << 16) + h * C;
     uint8_t* const piece = pieces + (warp - 4) * 2 * PIECE;
+    float* const sb = sbias + (warp - 4) * 32;
     uint32_t seq = 0;
     bool ok = true;
     // scales of the first two blocks and the bias of a tile, requested before the tile ahead of it is stored
@@ -328,14 +331,20 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (int c = 0; c < C / 32; ++c) {
         const int col = col0 + 32 * c, part = c % per;
         if (col - 32 * part >= a.N) continue;
-        if (a.bias)
-#pragma unroll
-          for (int j = 0; j < 16; ++j)
-            acc[16 * c + j] = add2(acc[16 * c + j], make_float2(__shfl_sync(0xffffffffu, b[c], 2 * j),
-                                                                __shfl_sync(0xffffffffu, b[c], 2 * j + 1)));
         float2 x[16];
 #pragma unroll
         for (int j = 0; j < 16; ++j) x[j] = acc[16 * c + j];
+        if (a.bias) {  // broadcast from shared memory: shuffles took a quarter of the epilogue
+          __syncwarp();
+          sb[lane] = b[c];
+          __syncwarp();
+#pragma unroll
+          for (int j = 0; j < 16; j += 2) {
+            const float4 b4 = reinterpret_cast<const float4*>(sb)[j / 2];
+            x[j] = add2(x[j], make_float2(b4.x, b4.y));
+            x[j + 1] = add2(x[j + 1], make_float2(b4.z, b4.w));
+          }
+        }
         if (part == 0) {  // the piece's last store has read it
           if (elect_one()) bulk_wait_read<1>();
           __syncwarp();
