@@ -18,8 +18,18 @@ namespace elasto {
 
 namespace {
 
-constexpr int THREADS = 256, UNROLL = 4;
+constexpr int THREADS = 256, UNROLL = 2, MIN_CTAS = 8;
 constexpr int PER_CTA = THREADS / 16 * UNROLL;  // blocks of 128 columns
+
+// n / d for n < 2^31 (Granlund and Montgomery's multiplication by a reciprocal).
+struct Divisor {
+  unsigned d, mul, shift;
+  explicit Divisor(unsigned v) : d(v), shift(0) {
+    while ((1ull << shift) < d) ++shift;
+    mul = static_cast<unsigned>(((1ull << 32) * ((1ull << shift) - d)) / d + 1);
+  }
+  __device__ __forceinline__ unsigned quotient(unsigned n) const { return (__umulhi(mul, n) + n) >> shift; }
+};
 
 // Two values to e4m3 (round to nearest even, saturating), the first in the low byte.
 __device__ __forceinline__ uint32_t pack_e4m3x2(float lo, float hi) {
@@ -28,85 +38,118 @@ __device__ __forceinline__ uint32_t pack_e4m3x2(float lo, float hi) {
   return r;
 }
 
-template <int TYPE>
-__device__ __forceinline__ float value_at(const void* x, size_t i) {
-  if constexpr (TYPE == ELASTO_F32) return static_cast<const float*>(x)[i];
-  if constexpr (TYPE == ELASTO_BF16) return __bfloat162float(static_cast<const bf16*>(x)[i]);
-  return __half2float(static_cast<const __half*>(x)[i]);
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
 }
 
+// Bits of one 16-bit value (in the low half) as fp32.
 template <int TYPE>
-__device__ __forceinline__ float2 pair_at(uint32_t w) {
+__device__ __forceinline__ float value_of(uint32_t bits) {
+  if constexpr (TYPE == ELASTO_BF16) return __uint_as_float(bits << 16);
+  return __half2float(__ushort_as_half(static_cast<unsigned short>(bits)));
+}
+template <int TYPE>
+__device__ __forceinline__ float2 pair_of16(uint32_t w) {
   if constexpr (TYPE == ELASTO_BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
   return __half22float2(*reinterpret_cast<const __half2*>(&w));
 }
 
+// A lane's eight values as they lie in memory.
+template <int TYPE>
+struct Eight {
+  static constexpr bool f32 = TYPE == ELASTO_F32;
+  uint32_t w[f32 ? 8 : 4];
+
+  __device__ __forceinline__ void load_wide(const void* x, size_t at) {
+    const uint4* p = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(x) + at * (f32 ? 4 : 2));
+    const uint4 a = __ldcs(p);
+    w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+    if constexpr (f32) {
+      const uint4 b = __ldcs(p + 1);
+      w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+    }
+  }
+  // the first n of them, the others 0
+  __device__ __forceinline__ void load_some(const void* x, size_t at, int n) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if constexpr (f32) {
+        w[j] = j < n ? static_cast<const uint32_t*>(x)[at + j] : 0u;
+      } else {
+        const uint32_t v = j < n ? static_cast<const uint16_t*>(x)[at + j] : 0u;
+        w[j / 2] = j & 1 ? w[j / 2] | v << 16 : v;
+      }
+    }
+  }
+  // the largest |value|'s bits: of fp32, or of the 16-bit type
+  __device__ __forceinline__ uint32_t top() const {
+    if constexpr (f32) {
+      uint32_t t = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) t = max(t, w[j] & 0x7fffffffu);
+      return t;
+    } else {
+      const uint32_t t = max_u16x2(max_u16x2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), max_u16x2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
+      return max(t & 0xffffu, t >> 16);
+    }
+  }
+  __device__ __forceinline__ uint2 codes(float inv) const {
+    uint32_t c[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float2 v;
+      if constexpr (f32)
+        v = make_float2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]));
+      else
+        v = pair_of16<TYPE>(w[j]);
+      v = mul2(v, make_float2(inv, inv));
+      c[j] = pack_e4m3x2(v.x, v.y);
+    }
+    return make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
+  }
+};
+
 // WIDE: rows of x start on 16 bytes and those of q on 8.
 template <int TYPE, bool WIDE>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, MIN_CTAS)
     quantize_kernel(const void* __restrict__ x, long long ldx, uint8_t* __restrict__ q, long long ldq,
-                    float* __restrict__ scale, long long lds, unsigned total, unsigned nb, int cols) {
+                    float* __restrict__ scale, long long lds, unsigned total, Divisor nb, int cols) {
   pdl_wait();
   pdl_trigger();
   const int l = threadIdx.x & 15;
   const unsigned first = blockIdx.x * PER_CTA + (threadIdx.x >> 4);
-  float v[UNROLL][8];
-  unsigned row[UNROLL], blk[UNROLL];
+  Eight<TYPE> v[UNROLL];
 #pragma unroll
   for (int u = 0; u < UNROLL; ++u) {
-    const unsigned i = first + u * (THREADS / 16);
-    row[u] = i / nb;
-    blk[u] = i - row[u] * nb;
-    const int c = static_cast<int>(blk[u]) * 128 + l * 8;
-    const size_t at = static_cast<size_t>(row[u]) * ldx + c;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[u][j] = 0.0f;
-    if (i < total) {
-      if (WIDE && c + 8 <= cols) {
-        if constexpr (TYPE == ELASTO_F32) {
-          const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(x) + at);
-          const float4 a = __ldcs(p), b = __ldcs(p + 1);
-          v[u][0] = a.x, v[u][1] = a.y, v[u][2] = a.z, v[u][3] = a.w;
-          v[u][4] = b.x, v[u][5] = b.y, v[u][6] = b.z, v[u][7] = b.w;
-        } else {
-          const uint4 w = __ldcs(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(x) + at));
-          const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float2 f = pair_at<TYPE>(ws[j]);
-            v[u][2 * j] = f.x;
-            v[u][2 * j + 1] = f.y;
-          }
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (c + j < cols) v[u][j] = value_at<TYPE>(x, at + j);
-      }
-    }
+    const unsigned i = first + u * (THREADS / 16), row = nb.quotient(i);
+    const int c = static_cast<int>(i - row * nb.d) * 128 + l * 8, left = i < total ? cols - c : 0;
+    const size_t at = static_cast<size_t>(row) * ldx + c;
+    if (WIDE && left >= 8)
+      v[u].load_wide(x, at);
+    else
+      v[u].load_some(x, at, left);
   }
 #pragma unroll
   for (int u = 0; u < UNROLL; ++u) {
-    const unsigned i = first + u * (THREADS / 16);
-    uint32_t top = __float_as_uint(7.888609052210118e-31f);  // 2^-100
-#pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[u][j]) & 0x7fffffffu);
+    const unsigned i = first + u * (THREADS / 16), row = nb.quotient(i), blk = i - row * nb.d;
+    uint32_t top = v[u].top();
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
     if (i >= total) continue;
-    const float a = __uint_as_float(top), inv = __fdiv_rn(448.0f, a);
-    const int c = static_cast<int>(blk[u]) * 128 + l * 8;
-    if (l == 0) scale[static_cast<size_t>(blk[u]) * lds + row[u]] = __fdiv_rn(a, 448.0f);
-    uint32_t w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = pack_e4m3x2(__fmul_rn(v[u][2 * j], inv), __fmul_rn(v[u][2 * j + 1], inv));
-    uint8_t* const out = q + static_cast<size_t>(row[u]) * ldq + c;
+    if constexpr (TYPE != ELASTO_F32) top = __float_as_uint(value_of<TYPE>(top));
+    const float a = __uint_as_float(max(top, 0x0d800000u));  // 2^-100 at least
+    const uint2 c8 = v[u].codes(__fdiv_rn(448.0f, a));
+    const int c = static_cast<int>(blk) * 128 + l * 8;
+    if (l == 0) scale[static_cast<size_t>(blk) * lds + row] = __fdiv_rn(a, 448.0f);
+    uint8_t* const out = q + static_cast<size_t>(row) * ldq + c;
     if (WIDE && c + 8 <= cols) {
-      *reinterpret_cast<uint2*>(out) = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+      *reinterpret_cast<uint2*>(out) = c8;
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (c + j < cols) out[j] = static_cast<uint8_t>(w[j >> 1] >> (8 * (j & 1)));
+        if (c + j < cols) out[j] = static_cast<uint8_t>((j < 4 ? c8.x : c8.y) >> (8 * (j & 3)));
     }
   }
 }
@@ -114,7 +157,8 @@ __global__ void __launch_bounds__(THREADS)
 template <int TYPE>
 cudaError_t launch(const void* x, long long ldx, uint8_t* q, long long ldq, float* scale, long long lds, int rows,
                    int cols, cudaStream_t s) {
-  const unsigned nb = static_cast<unsigned>((cols + 127LL) / 128), total = static_cast<unsigned>(rows) * nb;
+  const Divisor nb(static_cast<unsigned>((cols + 127LL) / 128));
+  const unsigned total = static_cast<unsigned>(rows) * nb.d;
   const dim3 grid((total + PER_CTA - 1) / PER_CTA), block(THREADS);
   const long long size = TYPE == ELASTO_F32 ? 4 : 2;
   const bool wide = reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx * size % 16 == 0 &&
