@@ -6,8 +6,8 @@
 // registers, where block b is added as acc += part * (as ws). A k-block is one
 // 128-byte row of A and W in the 128-byte swizzle: four K = 32 steps.
 //   warp 0      TMA producer of a ring of A and W tiles;
-//   warp 1      tcgen05.mma (kind::f8f6f4), block after block into two accumulators
-//               in turn;
+//   warp 1      tcgen05.mma (kind::f8f6f4), block after block into two (256 columns) or
+//               four accumulators in turn;
 //   warps 4-11  read the finished accumulator while the other fills; two warps share
 //               32 rows, each half of the tile's columns (a row a thread); after the
 //               last block they add the bias and store.
@@ -15,6 +15,7 @@
 
 #include "act.cuh"
 #include "common.h"
+#include "fp8_common.h"
 #include "ptx.cuh"
 
 namespace elasto {
@@ -40,6 +41,7 @@ struct Tile {
   static constexpr int smem = 1024 + stages * stage + PIECES + TAIL;
   static constexpr int tm = PAIR ? 2 * BM : BM;
   static constexpr int cols = BN / 2;  // of an epilogue warp
+  static constexpr int accs = BN == 256 ? 2 : 4;  // accumulators
 };
 
 struct Args {
@@ -56,16 +58,6 @@ struct Args {
 
 template <int EPI>
 constexpr bool f32_out = EPI == EPI_BIAS_RESID_F32 || EPI == EPI_BIAS_F32;
-
-template <int EPI>
-__device__ __forceinline__ void store_one(const Args& a, long long at, float x) {
-  if constexpr (EPI == EPI_BIAS_F32)
-    static_cast<float*>(a.out)[at] = x;
-  else if constexpr (EPI == EPI_BIAS_RESID_F32)
-    static_cast<float*>(a.out)[at] += x;
-  else
-    static_cast<bf16*>(a.out)[at] = __float2bfloat16_rn(x);
-}
 
 // 32 finished columns of a warp's 32 rows, a row a lane: out[row0 + lane, col .. col + 32). part: which
 // 64 bytes of a 128-byte staging row (16-bit types take two chunks). NARROW: one chunk of a 16-bit
@@ -89,7 +81,7 @@ __device__ __forceinline__ void store_chunk(const Args& a, const CUtensorMap* tm
     __syncwarp();
     if (col + lane < a.N)
       for (int i = 0; i < 32 && row0 + i < a.M; ++i)
-        store_one<EPI>(a, (row0 + i) * a.ldo + col + lane, t[i * 32 + (lane ^ i)]);
+        fp8_store_one<EPI>(a.out, (row0 + i) * a.ldo + col + lane, t[i * 32 + (lane ^ i)]);
     return;
   }
   // 16-byte pieces of the staging row, swizzled as the box is
@@ -136,9 +128,9 @@ __global__ void __launch_bounds__(THREADS, 1)
   float* sbias = reinterpret_cast<float*>(pieces + PIECES);
   uint64_t* full = reinterpret_cast<uint64_t*>(sbias + EPI_WARPS * 32);
   uint64_t* empty = full + MAX_STAGES;
-  uint64_t* tfull = empty + MAX_STAGES;  // [2]
-  uint64_t* tempty = tfull + 2;          // [2]
-  uint64_t* drain = tempty + 2;
+  uint64_t* tfull = empty + MAX_STAGES;  // [accumulator]
+  uint64_t* tempty = tfull + T::accs;
+  uint64_t* drain = tempty + T::accs;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
 
   const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
@@ -150,7 +142,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_init(&full[i], 1);
       mbar_init(&empty[i], 1);
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < T::accs; ++i) {
       mbar_init(&tfull[i], 1);
       mbar_init(&tempty[i], (PAIR ? 2 : 1) * EPI_WARPS);
     }
@@ -218,8 +210,8 @@ __global__ void __launch_bounds__(THREADS, 1)
       bool ok = true;
       for (int t = t_start; t < tiles && ok; t += t_stride)
         for (int kb = 0; kb < nkb; ++kb, ++seq) {
-          const uint32_t s = seq % S, acc = seq & 1;
-          ok = mbar_wait_warp(&tempty[acc], ((seq >> 1) & 1) ^ 1) && mbar_wait_warp(&full[s], (seq / S) & 1);
+          const uint32_t s = seq % S, acc = seq % T::accs;
+          ok = mbar_wait_warp(&tempty[acc], ((seq / T::accs) & 1) ^ 1) && mbar_wait_warp(&full[s], (seq / S) & 1);
           if (!ok) break;
           tc_fence_after();
           const uint64_t da = sdesc_sw128(smem_addr(sA + s * A_STAGE), 16, 1024);
@@ -227,9 +219,9 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
           for (int k = 0; k < BK / 32; ++k) {
             if constexpr (PAIR)
-              tc_mma_f8_pair_warp(tmem + acc * 256, da + 2 * k, db + 2 * k, idesc, k != 0);
+              tc_mma_f8_pair_warp(tmem + acc * BN, da + 2 * k, db + 2 * k, idesc, k != 0);
             else
-              tc_mma_f8_warp(tmem + acc * 256, da + 2 * k, db + 2 * k, idesc, k != 0);
+              tc_mma_f8_warp(tmem + acc * BN, da + 2 * k, db + 2 * k, idesc, k != 0);
           }
           if constexpr (PAIR) {
             tc_commit_pair_multicast_warp(&empty[s], 0x3);
@@ -281,9 +273,9 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (int j = 0; j < C / 2; ++j) acc[j] = make_float2(0.0f, 0.0f);
       float s0 = sa0 * sw0, s1 = sa1 * sw1;  // of this block and the next; the one after is on its way
       for (int kb = 0; kb < nkb; ++kb, ++seq) {
-        const int p = seq & 1;
+        const uint32_t p = seq % T::accs;
         const float sa = kb + 2 < nkb ? __ldg(as + (kb + 2) * a.lds) : 0.0f, sw = kb + 2 < nkb ? __ldg(ws + kb + 2) : 0.0f;
-        ok = __all_sync(0xffffffffu, mbar_wait(&tfull[p], (seq >> 1) & 1));
+        ok = __all_sync(0xffffffffu, mbar_wait(&tfull[p], (seq / T::accs) & 1));
         if (!ok) break;
         tc_fence_after();
         const float2 s2 = make_float2(s0, s0);
@@ -303,15 +295,15 @@ __global__ void __launch_bounds__(THREADS, 1)
           }
         };
         uint32_t v[2][32];
-        tmem_ld_32x32b_x32(tm + p * 256, v[0]);
-        if constexpr (C >= 64) tmem_ld_32x32b_x32(tm + p * 256 + 32, v[1]);
+        tmem_ld_32x32b_x32(tm + p * BN, v[0]);
+        if constexpr (C >= 64) tmem_ld_32x32b_x32(tm + p * BN + 32, v[1]);
         tmem_ld_wait();
         if constexpr (C < 128) release();
         add(v[0], 0);
-        if constexpr (C == 128) tmem_ld_32x32b_x32(tm + p * 256 + 64, v[0]);
+        if constexpr (C == 128) tmem_ld_32x32b_x32(tm + p * BN + 64, v[0]);
         if constexpr (C >= 64) add(v[1], 1);
         if constexpr (C == 128) {
-          tmem_ld_32x32b_x32(tm + p * 256 + 96, v[1]);
+          tmem_ld_32x32b_x32(tm + p * BN + 96, v[1]);
           tmem_ld_wait();
           release();
           add(v[0], 2);
@@ -424,6 +416,16 @@ void set_attributes_of(cudaError_t* e) {
   set_attributes<PAIR, BN, EPI_BIAS_F32>(e);
 }
 
+// Estimated microseconds with 128 x 64, 128 x 128 or (CTA pairs) 256 x 256 tiles: waves of tiles, each
+// its k-blocks and an epilogue. Fitted to launches of 1 to 50432 rows: 256 x 8192 x 8192 57 us in two
+// waves of 64 columns, 23 in one of 128; 1000 x 1000 x 1160 6.2 us with 64 columns, 6.8 with 128.
+double tile_cost(const Fp8Gemm& g, int nkb, int bn) {
+  const int tm = bn == 256 ? 256 : 128, units = bn == 256 ? num_sms() / 2 : num_sms();
+  const long long tiles = (g.M + tm - 1LL) / tm * ((g.N + bn - 1LL) / bn), waves = (tiles + units - 1) / units;
+  const double block = bn == 256 ? 0.40 : bn == 128 ? 0.32 : 0.30, epilogue = bn == 256 ? 2.1 : bn == 128 ? 1.0 : 0.4;
+  return 2.2 + waves * (nkb * block + epilogue);
+}
+
 }  // namespace
 
 cudaError_t gemm_fp8_init_attributes() {
@@ -431,25 +433,26 @@ cudaError_t gemm_fp8_init_attributes() {
   set_attributes_of<true, 256>(&e);
   set_attributes_of<false, 128>(&e);
   set_attributes_of<false, 64>(&e);
-  return e;
+  return e == cudaSuccess ? gemm_fp8_tokens_init_attributes() : e;
 }
 
 elasto_status gemm_fp8_launch(const Fp8Gemm& g, cudaStream_t s) {
-  const long long rows = (g.M + BM - 1LL) / BM;
-  if (rows * ((g.N + 63LL) / 64) > 0x7fffffffLL) {
+  if ((g.M + BM - 1LL) / BM * ((g.N + 63LL) / 64) > 0x7fffffffLL) {
     set_error("elasto_op_gemm_fp8: output too large");
     return ELASTO_ERR_UNSUPPORTED;
   }
+  const int nkb = (g.K + BK - 1) / BK;
+  int bn = 64;
+  for (int n : {128, 256})
+    if (tile_cost(g, nkb, n) < tile_cost(g, nkb, bn)) bn = n;
+  if (gemm_fp8_tokens_cost(g, nkb) < tile_cost(g, nkb, bn)) return gemm_fp8_tokens_launch(g, s);
   Args a{};
-  a.M = g.M, a.N = g.N, a.K = g.K, a.nkb = (g.K + BK - 1) / BK;
+  a.M = g.M, a.N = g.N, a.K = g.K, a.nkb = nkb;
   a.a_scale = g.a_scale, a.lds = g.lds, a.w_scale = g.w_scale, a.bias = g.bias;
   a.out = g.out, a.ldo = g.ldo, a.status = g.status;
   const int size = g.epi == EPI_BIAS_RESID_F32 || g.epi == EPI_BIAS_F32 ? 4 : 2;
   const uintptr_t starts = reinterpret_cast<uintptr_t>(g.out) | static_cast<uintptr_t>(g.ldo * size);
   a.tma = starts % 16 == 0;
-  const int sms = num_sms();
-  const long long pair_tiles = (g.M + 255LL) / 256 * ((g.N + 255LL) / 256);
-  const int bn = pair_tiles >= sms / 2 ? 256 : rows * ((g.N + 127LL) / 128) >= sms ? 128 : 64;
   CUtensorMap ta, tb, tc{};
   const uint64_t od[2] = {static_cast<uint64_t>(g.N), static_cast<uint64_t>(g.M)}, os[1] = {static_cast<uint64_t>(g.ldo) * size};
   const bool narrow = bn == 64 && size == 2;
