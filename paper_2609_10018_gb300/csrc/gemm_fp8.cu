@@ -59,29 +59,88 @@ struct Args {
 template <int EPI>
 constexpr bool f32_out = EPI == EPI_BIAS_RESID_F32 || EPI == EPI_BIAS_F32;
 
+// A warp's 32 rows x CW columns of out from shared memory (32-bit words: fp32 values or pairs of 16-bit ones;
+// word w of row r at r * 32 + (w ^ r)), where rows start on any value. A row leaves in 4-byte words; one of
+// 16-bit values that starts inside a word has a single value at either end and pairs across two words between.
+template <int EPI, int CW>
+__device__ __forceinline__ void store_rows(const Args& a, const uint32_t* t, int lane, int row0, int col0) {
+  const int left = a.N - col0;
+  if (row0 + 32 > a.M || left < CW) {  // the last rows or columns: value by value
+#pragma unroll
+    for (int c = lane; c < CW; c += 32) {
+      const long long at = row0 * a.ldo + col0 + c;
+#pragma unroll 8
+      for (int i = 0; i < 32; ++i) {
+        if (row0 + i >= a.M || c >= left) continue;
+        if constexpr (f32_out<EPI>)
+          fp8_store_one<EPI>(a.out, at + i * a.ldo, __uint_as_float(t[i * 32 + (c ^ i)]));
+        else
+          static_cast<uint16_t*>(a.out)[at + i * a.ldo] = static_cast<uint16_t>(t[i * 32 + ((c >> 1) ^ i)] >> (16 * (c & 1)));
+      }
+    }
+    return;
+  }
+  if constexpr (f32_out<EPI>) {
+    float* p = static_cast<float*>(a.out) + row0 * a.ldo + col0 + lane;
+#pragma unroll 8
+    for (int i = 0; i < 32; ++i, p += a.ldo) {
+      const float y = __uint_as_float(t[i * 32 + (lane ^ i)]);
+      *p = EPI == EPI_BIAS_RESID_F32 ? *p + y : y;
+    }
+  } else {
+    constexpr int W = CW / 2, R = 32 / W;  // words of a row, rows at a time
+    const int l = lane % W, sub = lane / W;
+    // whether even and odd rows of this lane start inside a word
+    const uint32_t first = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(a.out) >> 1) +
+                           static_cast<uint32_t>(row0 + sub) * static_cast<uint32_t>(a.ldo) + col0;
+    const bool in0 = first & 1, in1 = (first + R * static_cast<uint32_t>(a.ldo)) & 1;
+    const uint32_t take0 = in0 ? 0x5432 : 0x3210, take1 = in1 ? 0x5432 : 0x3210;
+    const bool on0 = !in0 || l < W - 1, on1 = !in1 || l < W - 1;
+    uint16_t* p = static_cast<uint16_t*>(a.out) + (row0 + sub) * a.ldo + col0 + 2 * l;
+    const long long step = R * a.ldo;
+#pragma unroll 4
+    for (int i = sub; i < 32; i += 2 * R, p += 2 * step) {
+      const uint32_t w0 = __byte_perm(t[i * 32 + (l ^ i)], t[i * 32 + ((l + 1) ^ i)], take0);
+      const uint32_t w1 = __byte_perm(t[(i + R) * 32 + (l ^ (i + R))], t[(i + R) * 32 + ((l + 1) ^ (i + R))], take1);
+      if (on0) *reinterpret_cast<uint32_t*>(p + in0) = w0;
+      if (on1) *reinterpret_cast<uint32_t*>(p + step + in1) = w1;
+    }
+    // the two ends of such rows, a row a lane
+    const uint32_t own = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(a.out) >> 1) +
+                         static_cast<uint32_t>(row0 + lane) * static_cast<uint32_t>(a.ldo) + col0;
+    if (own & 1) {
+      uint16_t* const r = static_cast<uint16_t*>(a.out) + (row0 + lane) * a.ldo + col0;
+      r[0] = static_cast<uint16_t>(t[lane * 32 + lane]);
+      r[CW - 1] = static_cast<uint16_t>(t[lane * 32 + ((W - 1) ^ lane)] >> 16);
+    }
+  }
+}
+
 // 32 finished columns of a warp's 32 rows, a row a lane: out[row0 + lane, col .. col + 32). part: which
 // 64 bytes of a 128-byte staging row (16-bit types take two chunks). NARROW: one chunk of a 16-bit
 // type is all the warp has; its rows are 64 bytes, not swizzled.
 template <int EPI, bool NARROW>
-__device__ __forceinline__ void store_chunk(const Args& a, const CUtensorMap* tmC, uint8_t* piece, int part, int lane, int row0,
-                                            int col, float2 (&x)[16]) {
+__device__ __forceinline__ void store_chunk(const Args& a, const CUtensorMap* tmC, uint8_t* base, uint8_t* piece, int part, int lane,
+                                            int row0, int col, float2 (&x)[16]) {
   if constexpr (EPI == EPI_BIAS_GELU_BF16) {
 #pragma unroll
     for (int j = 0; j < 16; ++j) x[j] = gelu2(x[j]);
   }
   if (!a.tma) {
-    // transposed in shared memory, so that a row's values leave together
-    float* t = reinterpret_cast<float*>(piece);
-    __syncwarp();
+    uint32_t* const t = reinterpret_cast<uint32_t*>(base);
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
-      t[lane * 32 + ((2 * j) ^ lane)] = x[j].x;
-      t[lane * 32 + ((2 * j + 1) ^ lane)] = x[j].y;
+      if constexpr (f32_out<EPI>) {
+        t[lane * 32 + ((2 * j) ^ lane)] = __float_as_uint(x[j].x);
+        t[lane * 32 + ((2 * j + 1) ^ lane)] = __float_as_uint(x[j].y);
+      } else {
+        t[lane * 32 + ((16 * part + j) ^ lane)] = pack_bf16x2(x[j].x, x[j].y);
+      }
     }
+    if (!f32_out<EPI> && !NARROW && part == 0) return;
     __syncwarp();
-    if (col + lane < a.N)
-      for (int i = 0; i < 32 && row0 + i < a.M; ++i)
-        fp8_store_one<EPI>(a.out, (row0 + i) * a.ldo + col + lane, t[i * 32 + (lane ^ i)]);
+    store_rows<EPI, f32_out<EPI> || NARROW ? 32 : 64>(a, t, lane, row0, col - 32 * part);
+    __syncwarp();
     return;
   }
   // 16-byte pieces of the staging row, swizzled as the box is
@@ -341,7 +400,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           if (elect_one()) bulk_wait_read<1>();
           __syncwarp();
         }
-        store_chunk<EPI, narrow>(a, &tmC, piece + (c / per & 1) * PIECE, part, lane, row0, col, x);
+        store_chunk<EPI, narrow>(a, &tmC, piece, piece + (c / per & 1) * PIECE, part, lane, row0, col, x);
       }
     }
     if (elect_one()) bulk_wait_all();
