@@ -498,11 +498,27 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
   return pair_of(r);
 }
 
-// 32 bytes to global memory (32-byte aligned) in one instruction: a whole sector.
-__device__ __forceinline__ void store_32b(void* p, const uint32_t (&r)[8]) {
-  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
-               "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+// ------------------------------------------------------------------ work stealing
+// Asks for the next block of the grid that has not been started; the answer (16
+// bytes) arrives in shared memory, counted on the mbarrier. After an answer
+// without a block no other request is made.
+__device__ __forceinline__ void request_block(void* answer, uint64_t* bar) {
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
+                   smem_addr(answer)),
+               "r"(smem_addr(bar))
                : "memory");
+}
+// blockIdx.x of the block that this one may run in its place, or -1.
+__device__ __forceinline__ int requested_block(const void* answer) {
+  uint32_t got, x;
+  asm volatile(
+      "{\n .reg .pred p;\n .reg .b128 r;\n ld.shared.b128 r, [%2];\n"
+      " clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n selp.u32 %0, 1, 0, p;\n mov.u32 %1, 0;\n"
+      " @p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n}\n"
+      : "=r"(got), "=r"(x)
+      : "r"(smem_addr(answer))
+      : "memory");
+  return got ? static_cast<int>(x) : -1;
 }
 
 // Device status word: first error wins.

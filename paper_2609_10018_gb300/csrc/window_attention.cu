@@ -19,11 +19,17 @@
 // division at the end cancels it). S(t) is issued after PV(t - 1), so its arrival
 // also says that O is at rest.
 //
-// Key tiles: sinks below the window join its first tile (up to 64 of them), else
-// they have tiles of their own; a tile that no row of a group sees is skipped for it.
-// Tiles that all rows see wholly take no mask. In the others values that are not
-// finite are set to zero before the product, since 0 * NaN would reach rows that
-// do not see them; the rows that do see them get them added at the end.
+// Key tiles have 128 keys, the last one and the one of the sinks 32 or 64 where
+// that is enough; one that no row of a group sees is skipped for it. Tiles that all
+// rows see wholly take no mask. In the others values that are not finite are set to
+// zero before the product, since 0 * NaN would reach rows that do not see them; the
+// rows that do see them get them added at the end.
+//
+// Items differ in length (ragged sequences, causal rows, class tokens that see
+// everything), so the grid has a block for each and the blocks that run take over
+// those not yet started (cluster launch control), the longest first.
+#include <type_traits>
+
 #include "common.h"
 #include "ptx.cuh"
 
@@ -38,14 +44,15 @@ static_assert(128 * REGS_FEW + 256 * REGS_MANY <= THREADS * REGS, "register spli
 constexpr int QT = 128, KT = 128;  // rows and keys of a tile
 constexpr int HALF = 128 * 128;    // bytes of 128 rows of 64 16-bit values
 constexpr int SMEM_LIMIT = 232448;
+constexpr int STAGING = 8 * 32 * 128;  // 32 rows of 64 channels of out for each softmax warp
 constexpr int TMEM_COLS = 512, O_COL = 256;
 constexpr float kLazy = 8.0f;  // log2 of how far a row's maximum may grow before O is rescaled
 
 template <int DP>
 struct Shape {
   static constexpr int halves = DP / 64, tile = halves * HALF;
-  static constexpr int slots = DP == 128 ? 5 : 8;
-  static constexpr int smem = 1024 + (2 + slots) * tile + 512;
+  static constexpr int slots = DP == 128 ? 4 : 8;
+  static constexpr int smem = 1024 + (2 + slots) * tile + STAGING + 512;
 };
 static_assert(Shape<128>::smem <= SMEM_LIMIT && Shape<64>::smem <= SMEM_LIMIT, "shared memory");
 
@@ -57,13 +64,13 @@ struct Args {
   const int* q_start;
   void* out;
   long long out_row, out_head;
-  int out32;  // rows of out start on 32 bytes
   int max_keys, kv_rows;
   const int* kv_start;
   const int* kv_len;
   const uint16_t* v;
   long long v_batch, v_row, v_head;
   int hg, nsub, qpt;  // heads and queries of a tile, tiles across a head group
+  int by_hg;          // row / hg = row * by_hg >> 16 (rows < 128, hg <= 32)
   int tiles;          // tiles (groups at work) of an item: 1 or 2
   int qtiles;         // items along the longest sequence's queries
   int items;
@@ -99,20 +106,22 @@ struct Item {
   int first[2], last[2];        // queries of each group's rows: [first, last] (empty: last < first)
   int lo[2], hi[2];             // its band of keys (empty: hi < lo)
   int sinks;                    // keys [0, sinks) that belong to the item whatever the band
-  int split, sink_tiles, base0; // see key_of
+  int sink_tiles, base0, end;   // tiles of the sinks alone; the band's first key and the one behind its last
   int tiles;                    // key tiles
 
-  // Column c of key tile t holds key base(t) + c, or key c where c < split and t == 0.
+  // Key tile t holds keys base(t) .. base(t) + width(t).
   __device__ __forceinline__ int base(int t) const { return t < sink_tiles ? t * KT : base0 + (t - sink_tiles) * KT; }
-  __device__ __forceinline__ bool has_sinks(int t) const {
-    return sinks > 0 && (t < sink_tiles || (t == 0 && split > 0) || (split == 0 && sink_tiles == 0 && base(t) < sinks));
+  __device__ __forceinline__ int width(int t) const {
+    const int left = (t < sink_tiles ? sinks : end) - base(t);
+    return left <= 32 ? 32 : left <= 64 ? 64 : KT;
   }
+  __device__ __forceinline__ bool has_sinks(int t) const { return t < sink_tiles || (sink_tiles == 0 && base(t) < sinks); }
   __device__ __forceinline__ bool needs(int g, int t) const {
     const int low = of(lo, g), high = of(hi, g);
     if (high < low) return false;
     if (has_sinks(t)) return true;
     const int b0 = base(t);
-    return t >= sink_tiles && b0 + KT - 1 >= low && b0 <= high;
+    return b0 + KT - 1 >= low && b0 <= high;
   }
 };
 
@@ -147,18 +156,16 @@ __device__ __forceinline__ Item make_item(const Args& a, int id) {
     }
     lo = min(lo, it.lo[g]), hi = max(hi, it.hi[g]);
   }
-  it.split = it.sink_tiles = 0;
+  it.sink_tiles = 0;
   if (it.sinks > 0) {
-    const int pad = (it.sinks + 15) & ~15;
-    if (lo <= pad)
+    if (lo <= ((it.sinks + 31) & ~31))
       lo = 0;
-    else if (pad <= 64)
-      it.split = pad;
     else
       it.sink_tiles = (it.sinks + KT - 1) / KT;
   }
-  it.base0 = lo - it.split;
-  it.tiles = hi < 0 ? 0 : it.sink_tiles + (hi - it.base0) / KT + 1;
+  it.base0 = lo;
+  it.end = hi + 1;
+  it.tiles = hi < 0 ? 0 : it.sink_tiles + (hi - lo) / KT + 1;
   return it;
 }
 
@@ -176,14 +183,13 @@ struct Seen {
 __device__ __forceinline__ Seen seen_columns(const Args& a, const Item& it, int t, int p) {
   Seen s;
   const int base = it.base(t);
-  const bool split = t == 0 && it.split > 0, sink_tile = t < it.sink_tiles;
   int lo = max(p - a.window, 0), hi = a.causal ? p : min(p + a.window, it.nk - 1);
   int sinks = min(a.sinks, a.causal ? p + 1 : it.nk);
   if (!a.causal && p < a.sinks) lo = 0, hi = it.nk - 1;
   if (p < 0) hi = -1, sinks = 0;
-  s.a0 = max(lo - base, split ? it.split : 0);
-  s.a1 = sink_tile || hi < 0 ? -1 : hi - base;
-  s.b1 = sinks - 1 - (split ? 0 : base);
+  s.a0 = lo - base;
+  s.a1 = t < it.sink_tiles || hi < 0 ? -1 : hi - base;
+  s.b1 = sinks - 1 - base;
   return s;
 }
 
@@ -204,40 +210,57 @@ __device__ __forceinline__ uint32_t bad16(uint32_t w) {
   return ((x & 0xffffu) == 0 ? 0xffffu : 0u) | ((x >> 16) == 0 ? 0xffff0000u : 0u);
 }
 
-// Sets the values of a V tile that are not finite to zero (128 threads of a group,
-// number r); true if there were any. A quick look first: 0 * x is NaN for them alone.
+// acc + 0 * w: NaN from the first infinite or NaN value on.
+template <bool BF>
+__device__ __forceinline__ void look16(uint32_t w, uint32_t& acc) {
+  if constexpr (BF)
+    asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(acc) : "r"(w), "r"(0u));
+  else
+    asm("fma.rn.f16x2 %0, %1, %2, %0;" : "+r"(acc) : "r"(w), "r"(0u));
+}
+
+// Sets the values of the first `rows` rows of a V tile that are not finite to zero (128
+// threads of a group, number r); the item's number goes to *flag if there were any.
 template <bool BF, int DP>
-__device__ __forceinline__ bool clear_bad_values(uint8_t* v, int r, int seq, volatile int* flag) {
-  uint4* c = reinterpret_cast<uint4*>(v);
-  uint32_t bad = 0;
-#pragma unroll 4
-  for (int i = 0; i < DP / 8; ++i) {
-    const uint4 w = c[r + 128 * i];
-    bad |= bad16<BF>(w.x) | bad16<BF>(w.y) | bad16<BF>(w.z) | bad16<BF>(w.w);
-  }
-  if (!__any_sync(0xffffffffu, bad != 0)) return false;
+__device__ __forceinline__ void clear_bad_values(uint8_t* v, int rows, int r, int seq, volatile int* flag) {
+  const int n = rows * 8;  // 16-byte pieces of 64 channels
+  uint32_t acc[2] = {0u, 0u};
+#pragma unroll
+  for (int h = 0; h < DP / 64; ++h)
+#pragma unroll 2
+    for (int i = r; i < n; i += 256) {
+      const uint4 x = reinterpret_cast<const uint4*>(v + h * HALF)[i];
+      look16<BF>(x.x, acc[0]), look16<BF>(x.y, acc[0]), look16<BF>(x.z, acc[0]), look16<BF>(x.w, acc[0]);
+      if (i + 128 < n) {
+        const uint4 y = reinterpret_cast<const uint4*>(v + h * HALF)[i + 128];
+        look16<BF>(y.x, acc[1]), look16<BF>(y.y, acc[1]), look16<BF>(y.z, acc[1]), look16<BF>(y.w, acc[1]);
+      }
+    }
+  if (!__any_sync(0xffffffffu, (bad16<BF>(acc[0]) | bad16<BF>(acc[1])) != 0)) return;
   *flag = seq;
   __threadfence_block();
-  for (int i = 0; i < DP / 8; ++i) {
-    uint4 w = c[r + 128 * i];
-    w.x &= ~bad16<BF>(w.x), w.y &= ~bad16<BF>(w.y), w.z &= ~bad16<BF>(w.z), w.w &= ~bad16<BF>(w.w);
-    c[r + 128 * i] = w;
-  }
+  for (int h = 0; h < DP / 64; ++h)
+    for (int i = r; i < n; i += 128) {
+      uint4* p = reinterpret_cast<uint4*>(v + h * HALF) + i;
+      uint4 w = *p;
+      w.x &= ~bad16<BF>(w.x), w.y &= ~bad16<BF>(w.y), w.z &= ~bad16<BF>(w.z), w.w &= ~bad16<BF>(w.w);
+      *p = w;
+    }
   fence_async_smem();
-  return true;
 }
 
 template <bool BF, int DP>
 __global__ void __launch_bounds__(THREADS, 1)
     window_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                            const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmK16,
-                            const __grid_constant__ CUtensorMap tmV16, const __grid_constant__ Args a) {
+                            const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmK32,
+                            const __grid_constant__ CUtensorMap tmV32, const __grid_constant__ Args a) {
   using S = Shape<DP>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* qbuf = smem;                 // [group] 128 rows, in halves of 64 channels
   uint8_t* ring = smem + 2 * S::tile;   // [slot] a K or V tile, in halves of 64 channels
-  uint64_t* bars = reinterpret_cast<uint64_t*>(ring + S::slots * S::tile);
+  uint8_t* staging = ring + S::slots * S::tile;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(staging + STAGING);
   uint64_t* full = bars;                // [slot]
   uint64_t* empty = full + S::slots;    // [slot]
   uint64_t* q_full = empty + S::slots;  // [group]
@@ -246,7 +269,11 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint64_t* p_full = s_full + 2;        // 128 arrivals
   uint64_t* o_full = p_full + 2;
   uint64_t* drain = o_full + 2;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  uint64_t* next_full = drain + 1;       // [2] the answer for item n in next[n & 1]
+  uint64_t* next_empty = next_full + 2;  // [2] read by the MMA warp and the softmax warps
+  uint4* next = reinterpret_cast<uint4*>(bars + 40);  // [2]
+  static_assert(2 * S::slots + 15 <= 40, "barriers");
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(next + 2);
   volatile int* bad_seq = reinterpret_cast<int*>(tmem_slot + 1);  // [2] item (by its number in this CTA) with bad values
 
   const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
@@ -261,6 +288,8 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_init(&s_full[g], 1);
       mbar_init(&p_full[g], 128);
       mbar_init(&o_full[g], 1);
+      mbar_init(&next_full[g], 1);
+      mbar_init(&next_empty[g], 9);
       bad_seq[g] = -1;
     }
     mbar_init(drain, 1);
@@ -277,6 +306,16 @@ __global__ void __launch_bounds__(THREADS, 1)
   pdl_wait();
   pdl_trigger();
 
+  // item n + 1 for a warp that is done with item n (all its lanes call); -1: none, -2: the wait gave up
+  auto following = [&](int n) -> int {
+    ++n;
+    if (!__all_sync(0xffffffffu, mbar_wait(&next_full[n & 1], ((n - 1) >> 1) & 1))) return -2;
+    const int id = requested_block(next + (n & 1));
+    fence_async_smem();  // read before the next answer is written there
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&next_empty[n & 1]);
+    return id;
+  };
   if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FEW));
   if (warp == 0) {
     // ------------------------------------------------------------ producer
@@ -286,7 +325,8 @@ __global__ void __launch_bounds__(THREADS, 1)
       tma_prefetch_desc(&tmV);
       uint32_t seq = 0, nq[2] = {0, 0};  // K/V tiles and Q tiles issued
       bool ok = true;
-      for (int id = blockIdx.x; id < a.items && ok; id += gridDim.x) {
+      int id = blockIdx.x;
+      for (int n = 0; ok && id >= 0; ++n) {
         const Item it = make_item(a, id);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
@@ -299,24 +339,33 @@ __global__ void __launch_bounds__(THREADS, 1)
           ++nq[g];
         }
         const int batch = a.kv_start ? 0 : it.b;
-        for (int t = 0; t < it.tiles && ok; ++t)
+        for (int t = 0; t < it.tiles && ok; ++t) {
+          const int width = it.width(t), row = it.k0 + it.base(t);
           for (int kv = 0; kv < 2 && ok; ++kv, ++seq) {
             const uint32_t slot = seq % S::slots;
             ok = mbar_wait(&empty[slot], ((seq / S::slots) & 1) ^ 1);
             if (!ok) break;
             uint8_t* dst = ring + slot * S::tile;
-            mbar_expect_tx(&full[slot], S::tile);
-            const int row = it.k0 + it.base(t);
+            mbar_expect_tx(&full[slot], S::halves * width * 128);
             for (int h = 0; h < S::halves; ++h) {
-              if (t > 0 || it.split == 0) {
+              if (width == KT) {
                 tma_load_4d(dst + h * HALF, kv ? &tmV : &tmK, &full[slot], 64 * h, it.kvh, row, batch);
-              } else {  // sinks, then the window's first keys, 16 at a time
-                for (int c = 0; c < KT; c += 16)
-                  tma_load_4d(dst + h * HALF + c * 128, kv ? &tmV16 : &tmK16, &full[slot], 64 * h, it.kvh,
-                              c < it.split ? it.k0 + c : row + c, batch);
+              } else {
+                for (int c = 0; c < width; c += 32)
+                  tma_load_4d(dst + h * HALF + c * 128, kv ? &tmV32 : &tmK32, &full[slot], 64 * h, it.kvh, row + c, batch);
               }
             }
           }
+        }
+        if (!ok) break;
+        // the next item, asked for once this one's loads are under way
+        const int m = n + 1;
+        ok = mbar_wait(&next_empty[m & 1], ((n >> 1) & 1) ^ 1);
+        if (!ok) break;
+        mbar_expect_tx(&next_full[m & 1], 16);
+        request_block(next + (m & 1), &next_full[m & 1]);
+        ok = mbar_wait(&next_full[m & 1], (n >> 1) & 1);
+        id = requested_block(next + (m & 1));
       }
       if (!ok) record_status(a.status, ELASTO_ERR_TIMEOUT);
       // all copies have landed before the CTA exits
@@ -327,11 +376,11 @@ __global__ void __launch_bounds__(THREADS, 1)
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer
     const int dn = (a.head_dim + 15) & ~15;  // channels that the products take
-    const uint32_t idesc_s = idesc_16_f32(QT, KT, !BF);
     const uint32_t idesc_o = idesc_16_f32(QT, dn, !BF, false, true);
     uint32_t seq = 0, nq[2] = {0, 0}, np[2] = {0, 0};
     bool ok = true, issued = false;
-    for (int id = blockIdx.x; id < a.items && ok; id += gridDim.x) {
+    int id = blockIdx.x;
+    for (int n = 0; id >= 0; ++n) {
       const Item it = make_item(a, id);
       bool started_s[2] = {false, false}, started_o[2] = {false, false};
       int last_s[2] = {-1, -1};
@@ -349,6 +398,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         const uint32_t slot = (seq + 2 * t) % S::slots;
         const uint64_t dq = sdesc_sw128(smem_addr(qbuf + g * S::tile), 16, 1024);
         const uint64_t dk = sdesc_sw128(smem_addr(ring + slot * S::tile), 16, 1024);
+        const uint32_t idesc_s = idesc_16_f32(QT, it.width(t), !BF);
         for (int k = 0; k < dn / 16; ++k) {
           const uint64_t off = (k >> 2) * (HALF >> 4) + 2 * (k & 3);
           tc_mma_warp(tmem + g * KT, dq + off, dk + off, idesc_s, k != 0);
@@ -382,7 +432,8 @@ __global__ void __launch_bounds__(THREADS, 1)
             ++np[g];
             tc_fence_after();
             const uint64_t dv = sdesc_sw128(smem_addr(ring + (vs % S::slots) * S::tile), HALF, 1024);
-            for (int k = 0; k < KT / 16; ++k)
+            const int steps = it.width(t) / 16;
+            for (int k = 0; k < steps; ++k)
               tc_mma_tmem_a_warp(tmem + O_COL + g * DP, tmem + g * KT + 8 * k, dv + 128 * k, idesc_o, started_o[g] || k != 0);
             started_o[g] = true;
             issued = true;
@@ -397,8 +448,9 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
       }
       seq += 2 * it.tiles;
+      id = ok ? following(n) : -2;
     }
-    if (!ok && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
+    if (id == -2 && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
     if (issued) {
       tc_commit_warp(drain);
       mbar_wait_warp(drain, 0);
@@ -410,47 +462,50 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t s_tm = tmem + lanes + g * KT, o_tm = tmem + lanes + O_COL + g * DP;
     const float sc = a.scale_log2;
+    uint8_t* const stage = staging + (warp - 4) * (STAGING / 8);
     uint32_t seq = 0, ns = 0, no = 0;
-    int nth = 0;
     bool ok = true;
-    for (int id = blockIdx.x; id < a.items && ok; id += gridDim.x, ++nth) {
+    int id = blockIdx.x;
+    for (int nth = 0; id >= 0; ++nth) {
       const Item it = make_item(a, id);
       const int first = of(it.first, g), last = of(it.last, g);
       if (last < first) {
         seq += 2 * it.tiles;
+        id = following(nth);
         continue;
       }
-      const int qi = first + r / a.hg, head = r % a.hg;
-      const bool mine = r < a.qpt * a.hg && qi <= last && head < it.nheads;
+      const int own = r * a.by_hg >> 16;  // query of this row in the tile
+      const int qi = first + own, head = r - own * a.hg;
+      const bool mine = own < a.qpt && qi <= last && head < it.nheads;
       const int shift = it.nk - it.nq, p = shift + qi;
       const int pmin = shift + first, pmax = shift + last;
       float m = -INFINITY, sum = 0.0f;
       bool any = false;
-      for (int t = 0; t < it.tiles && ok; ++t) {
-        if (!it.needs(g, t)) continue;
+      // one key tile of 32 * NC columns
+      auto tile = [&](auto chunks, int t) -> bool {
+        constexpr int NC = decltype(chunks)::value;
         const int base = it.base(t);
         // every row sees every column
-        const bool whole = t >= it.sink_tiles && !(t == 0 && it.split > 0) && pmin >= 0 && base >= pmax - a.window &&
-                           base + KT - 1 <= (a.causal ? pmin : min(it.nk - 1, pmin + a.window));
-        ok = __all_sync(0xffffffffu, mbar_wait(&s_full[g], ns & 1));
-        if (!ok) break;
+        const bool whole = t >= it.sink_tiles && pmin >= 0 && base >= pmax - a.window &&
+                           base + 32 * NC - 1 <= (a.causal ? pmin : min(it.nk - 1, pmin + a.window));
+        if (!__all_sync(0xffffffffu, mbar_wait(&s_full[g], ns & 1))) return false;
         ++ns;
         tc_fence_after();
-        uint32_t v[4][32];
+        uint32_t v[NC][32];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) tmem_ld_32x32b_x32(s_tm + 32 * i, v[i]);
+        for (int i = 0; i < NC; ++i) tmem_ld_32x32b_x32(s_tm + 32 * i, v[i]);
         if (!whole) {
           const uint32_t vs = seq + 2 * t + 1;
-          ok = __all_sync(0xffffffffu, mbar_wait(&full[vs % S::slots], (vs / S::slots) & 1));
-          if (!ok) break;
-          clear_bad_values<BF, DP>(ring + (vs % S::slots) * S::tile, r, nth, &bad_seq[nth & 1]);
+          if (!__all_sync(0xffffffffu, mbar_wait(&full[vs % S::slots], (vs / S::slots) & 1))) return false;
+          clear_bad_values<BF, DP>(ring + (vs % S::slots) * S::tile, 32 * NC, r, nth, &bad_seq[nth & 1]);
         }
         tmem_ld_wait();
         if (!whole) {
           const Seen s = seen_columns(a, it, t, p);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < NC; ++i) {
             const uint32_t w = s.word(i);
+            if (__all_sync(0xffffffffu, w == 0xffffffffu)) continue;
 #pragma unroll
             for (int j = 0; j < 32; ++j)
               if (!(w >> j & 1)) v[i][j] = 0xff800000u;
@@ -458,7 +513,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < NC; ++i)
 #pragma unroll
           for (int j = 0; j < 32; j += 2)
             t4[(j >> 1) & 3] = max3(t4[(j >> 1) & 3], __uint_as_float(v[i][j]), __uint_as_float(v[i][j + 1]));
@@ -492,7 +547,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         const float2 sc2 = make_float2(sc, sc), neg2 = make_float2(neg, neg);
         float2 add[2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < NC; ++i) {
           uint32_t pk[16];
 #pragma unroll
           for (int j = 0; j < 32; j += 2) {
@@ -507,71 +562,87 @@ __global__ void __launch_bounds__(THREADS, 1)
         tmem_st_wait();
         tc_fence_before();
         mbar_arrive(&p_full[g]);
+        return true;
+      };
+      for (int t = 0; t < it.tiles && ok; ++t) {
+        if (!it.needs(g, t)) continue;
+        const int width = it.width(t);
+        ok = width == KT ? tile(std::integral_constant<int, 4>(), t)
+                         : width == 64 ? tile(std::integral_constant<int, 2>(), t) : tile(std::integral_constant<int, 1>(), t);
       }
       seq += 2 * it.tiles;
-      if (!ok) break;
       // ------------------------------------------------------------ result rows
-      uint16_t* out = static_cast<uint16_t*>(a.out) + static_cast<long long>(it.q0 + qi) * a.out_row +
-                      static_cast<long long>(it.head0 + head) * a.out_head;
-      if (any) {
+      if (ok && any) {
         ok = __all_sync(0xffffffffu, mbar_wait(&o_full[g], no & 1));
-        if (!ok) break;
         ++no;
         tc_fence_after();
+      }
+      if (!ok) {
+        id = -2;
+        break;
       }
       const bool sees = mine && p >= 0 && it.nk > 0;
       const float inv = 1.0f / sum;
       const bool bad = any && bad_seq[nth & 1] == nth;
 #pragma unroll
-      for (int c = 0; c < DP; c += 32) {
-        uint32_t o[32];
-        if (any) {
-          tmem_ld_32x32b_x32(o_tm + c, o);
-          tmem_ld_wait();
-        }
-        if (bad && sees) {
-          // values that are not finite were left out of the product: add those that this row sees
-          for (int t = 0; t < it.tiles; ++t) {
-            const Seen s = seen_columns(a, it, t, p);
-            for (int col = 0; col < KT; ++col) {
-              if (!(s.word(col >> 5) >> (col & 31) & 1)) continue;
-              const long long key = it.k0 + (t == 0 && col < it.split ? col : it.base(t) + col);
-              const uint16_t* vp = a.v + (a.kv_start ? 0 : it.b * a.v_batch) + key * a.v_row + it.kvh * a.v_head + c;
+      for (int c0 = 0; c0 < DP; c0 += 64) {
 #pragma unroll
-              for (int j = 0; j < 32; j += 2) {
-                if (c + j >= a.head_dim) continue;
-                const uint32_t w = *reinterpret_cast<const uint32_t*>(vp + j);
-                const uint32_t b2 = bad16<BF>(w);
-                const float2 x = unpack16<BF>(w);
-                if (b2 & 0xffffu) o[j] = __float_as_uint(__uint_as_float(o[j]) + x.x);
-                if (b2 >> 16) o[j + 1] = __float_as_uint(__uint_as_float(o[j + 1]) + x.y);
+        for (int c = c0; c < c0 + 64; c += 32) {
+          uint32_t o[32];
+          if (any) {
+            tmem_ld_32x32b_x32(o_tm + c, o);
+            tmem_ld_wait();
+          }
+          if (bad && sees) {
+            // values that are not finite were left out of the product: add those that this row sees
+            for (int t = 0; t < it.tiles; ++t) {
+              const Seen s = seen_columns(a, it, t, p);
+              for (int col = 0; col < it.width(t); ++col) {
+                if (!(s.word(col >> 5) >> (col & 31) & 1)) continue;
+                const long long key = it.k0 + it.base(t) + col;
+                const uint16_t* vp = a.v + (a.kv_start ? 0 : it.b * a.v_batch) + key * a.v_row + it.kvh * a.v_head + c;
+#pragma unroll
+                for (int j = 0; j < 32; j += 2) {
+                  if (c + j >= a.head_dim) continue;
+                  const uint32_t w = *reinterpret_cast<const uint32_t*>(vp + j);
+                  const uint32_t b2 = bad16<BF>(w);
+                  const float2 x = unpack16<BF>(w);
+                  if (b2 & 0xffffu) o[j] = __float_as_uint(__uint_as_float(o[j]) + x.x);
+                  if (b2 >> 16) o[j + 1] = __float_as_uint(__uint_as_float(o[j + 1]) + x.y);
+                }
               }
             }
           }
-        }
-        if (!mine) continue;
-        uint32_t pk[16];
+          // 16-byte pieces of a 128-byte row, so placed that writing a column and reading a row are without conflicts
 #pragma unroll
-        for (int j = 0; j < 32; j += 2) {
-          const float2 x = mul2(make_float2(__uint_as_float(o[j]), __uint_as_float(o[j + 1])), make_float2(inv, inv));
-          pk[j >> 1] = sees ? pack16<BF>(x.x, x.y) : 0u;
-        }
+          for (int j = 0; j < 4; ++j) {
+            uint32_t pk[4];
 #pragma unroll
-        for (int j = 0; j < 16; j += 8) {
-          const int ch = c + 2 * j;
-          if (a.out32 && ch + 16 <= a.head_dim) {
-            const uint32_t w[8] = {pk[j], pk[j + 1], pk[j + 2], pk[j + 3], pk[j + 4], pk[j + 5], pk[j + 6], pk[j + 7]};
-            store_32b(out + ch, w);
-          } else {
-            if (ch < a.head_dim) *reinterpret_cast<uint4*>(out + ch) = make_uint4(pk[j], pk[j + 1], pk[j + 2], pk[j + 3]);
-            if (ch + 8 < a.head_dim)
-              *reinterpret_cast<uint4*>(out + ch + 8) = make_uint4(pk[j + 4], pk[j + 5], pk[j + 6], pk[j + 7]);
+            for (int i = 0; i < 4; ++i) {
+              const float2 x = mul2(make_float2(__uint_as_float(o[8 * j + 2 * i]), __uint_as_float(o[8 * j + 2 * i + 1])), make_float2(inv, inv));
+              pk[i] = sees ? pack16<BF>(x.x, x.y) : 0u;
+            }
+            *reinterpret_cast<uint4*>(stage + lane * 128 + (((((c - c0) >> 3) + j) ^ (lane & 7)) << 4)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
           }
         }
+        __syncwarp();
+        // eight lanes a row: whole sectors leave together (a row a lane: ~100 clocks an instruction)
+        const int piece = lane & 7, ch = c0 + 8 * piece;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int k = 4 * i + (lane >> 3), row = (warp & 3) * 32 + k;
+          const int q = row * a.by_hg >> 16, h = row - q * a.hg;
+          if (ch < a.head_dim && q < a.qpt && first + q <= last && h < it.nheads)
+            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + static_cast<long long>(it.q0 + first + q) * a.out_row +
+                                      static_cast<long long>(it.head0 + h) * a.out_head + ch) =
+                *reinterpret_cast<const uint4*>(stage + k * 128 + ((piece ^ (k & 7)) << 4));
+        }
+        __syncwarp();
       }
       tc_fence_before();
+      id = following(nth);
     }
-    if (!ok && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
+    if (id == -2 && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
   }
   __syncthreads();
   if (warp == 1) {
@@ -594,8 +665,7 @@ bool map_of(CUtensorMap* tm, const void* p, bool bf, const elasto_window_attenti
 
 template <bool BF, int DP>
 cudaError_t launch(const CUtensorMap (&tm)[5], const Args& a, cudaStream_t s) {
-  const int grid = a.items < num_sms() ? a.items : num_sms();
-  return launch_pdl(window_attention_kernel<BF, DP>, dim3(grid), dim3(THREADS), Shape<DP>::smem, s, tm[0], tm[1], tm[2],
+  return launch_pdl(window_attention_kernel<BF, DP>, dim3(a.items), dim3(THREADS), Shape<DP>::smem, s, tm[0], tm[1], tm[2],
                     tm[3], tm[4], a);
 }
 
@@ -632,7 +702,6 @@ elasto_status window_attention_launch(const elasto_window_attention_args& u, int
   a.scale_log2 = u.scale * 1.4426950408889634f;
   a.max_queries = u.max_queries, a.q_rows = static_cast<int>(u.q_rows), a.q_start = u.q_start;
   a.out = u.out, a.out_row = u.out_row, a.out_head = u.out_head;
-  a.out32 = reinterpret_cast<uintptr_t>(u.out) % 32 == 0 && u.out_row % 16 == 0 && u.out_head % 16 == 0;
   a.max_keys = u.max_keys, a.kv_rows = static_cast<int>(u.kv_rows), a.kv_start = u.kv_start, a.kv_len = u.kv_len;
   a.v = static_cast<const uint16_t*>(u.v), a.v_batch = u.v_batch, a.v_row = u.v_row, a.v_head = u.v_head;
   a.status = status;
@@ -640,6 +709,7 @@ elasto_status window_attention_launch(const elasto_window_attention_args& u, int
   a.nsub = (a.group + 31) / 32;
   a.hg = (a.group + a.nsub - 1) / a.nsub;
   a.qpt = QT / a.hg;
+  a.by_hg = (65536 + a.hg - 1) / a.hg;
   const long long per = static_cast<long long>(a.batch) * a.heads_kv * a.nsub;
   const long long rows = (a.max_queries + a.qpt - 1LL) / a.qpt;
   a.tiles = rows * per > num_sms() ? 2 : 1;  // one tile an item where the chip would be half empty
@@ -657,8 +727,8 @@ elasto_status window_attention_launch(const elasto_window_attention_args& u, int
   if (!map_of(&tm[0], u.q, bf, u, u.heads, u.q_rows, 1, u.q_head, u.q_row, -1, a.hg, a.qpt) ||
       !map_of(&tm[1], u.k, bf, u, u.heads_kv, u.kv_rows, kvb, u.k_head, u.k_row, kb, 1, KT) ||
       !map_of(&tm[2], u.v, bf, u, u.heads_kv, u.kv_rows, kvb, u.v_head, u.v_row, vb, 1, KT) ||
-      !map_of(&tm[3], u.k, bf, u, u.heads_kv, u.kv_rows, kvb, u.k_head, u.k_row, kb, 1, 16) ||
-      !map_of(&tm[4], u.v, bf, u, u.heads_kv, u.kv_rows, kvb, u.v_head, u.v_row, vb, 1, 16)) {
+      !map_of(&tm[3], u.k, bf, u, u.heads_kv, u.kv_rows, kvb, u.k_head, u.k_row, kb, 1, 32) ||
+      !map_of(&tm[4], u.v, bf, u, u.heads_kv, u.kv_rows, kvb, u.v_head, u.v_row, vb, 1, 32)) {
     set_error("elasto_op_window_attention: cuTensorMapEncodeTiled failed (alignment, strides or size)");
     return ELASTO_ERR_UNSUPPORTED;
   }
