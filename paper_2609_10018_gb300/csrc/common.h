@@ -330,6 +330,17 @@ cudaError_t convert_to_bf16(const void* src, int src_dtype, size_t n, bf16* dst,
 cudaError_t convert_to_bf16_lo(const void* src, int src_dtype, size_t n, bf16* dst, cudaStream_t s);
 cudaError_t convert_to_f32(const void* src, int src_dtype, size_t n, float* dst, cudaStream_t s);
 
+// n / d for n < 2^31 (Granlund and Montgomery's multiplication by a reciprocal).
+struct Divisor {
+  unsigned d = 1, mul = 1, shift = 0;
+  Divisor() = default;
+  explicit Divisor(unsigned v) : d(v), shift(0) {
+    while ((1ull << shift) < d) ++shift;
+    mul = static_cast<unsigned>(((1ull << 32) * ((1ull << shift) - d)) / d + 1);
+  }
+  __device__ __forceinline__ unsigned quotient(unsigned n) const { return (__umulhi(mul, n) + n) >> shift; }
+};
+
 // ---------------------------------------------------------------- long sequences, 8-bit weights
 // (arguments checked by the entry points in ops_api.cu)
 cudaError_t quantize_fp8_launch(const void* x, int x_type, long long ldx, uint8_t* q, long long ldq, float* scale,

@@ -21,16 +21,6 @@ namespace {
 constexpr int THREADS = 256, UNROLL = 2, MIN_CTAS = 8;
 constexpr int PER_CTA = THREADS / 16 * UNROLL;  // blocks of 128 columns
 
-// n / d for n < 2^31 (Granlund and Montgomery's multiplication by a reciprocal).
-struct Divisor {
-  unsigned d, mul, shift;
-  explicit Divisor(unsigned v) : d(v), shift(0) {
-    while ((1ull << shift) < d) ++shift;
-    mul = static_cast<unsigned>(((1ull << 32) * ((1ull << shift) - d)) / d + 1);
-  }
-  __device__ __forceinline__ unsigned quotient(unsigned n) const { return (__umulhi(mul, n) + n) >> shift; }
-};
-
 // Two values to e4m3 (round to nearest even, saturating), the first in the low byte.
 __device__ __forceinline__ uint32_t pack_e4m3x2(float lo, float hi) {
   uint16_t r;

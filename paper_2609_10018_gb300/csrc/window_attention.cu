@@ -74,6 +74,7 @@ struct Args {
   int tiles;          // tiles (groups at work) of an item: 1 or 2
   int qtiles;         // items along the longest sequence's queries
   int items;
+  Divisor per_q, by_nsub, by_heads_kv;  // items of a step along the queries; the axes of one
   int* status;
 };
 
@@ -127,13 +128,11 @@ struct Item {
 
 __device__ __forceinline__ Item make_item(const Args& a, int id) {
   Item it;
-  const int per = a.batch * a.heads_kv * a.nsub;
-  int q = id / per, r = id - q * per;
+  int q = static_cast<int>(a.per_q.quotient(id)), r = id - q * static_cast<int>(a.per_q.d);
   if (a.causal) q = a.qtiles - 1 - q;  // the longest rows of keys first
-  const int sub = r % a.nsub;
-  r /= a.nsub;
-  it.kvh = r % a.heads_kv;
-  it.b = r / a.heads_kv;
+  const int r1 = static_cast<int>(a.by_nsub.quotient(r)), sub = r - r1 * a.nsub;
+  it.b = static_cast<int>(a.by_heads_kv.quotient(r1));
+  it.kvh = r1 - it.b * a.heads_kv;
   it.head0 = it.kvh * a.group + sub * a.hg;
   it.nheads = min(a.hg, a.group - sub * a.hg);
   sequence(a, it.b, it.q0, it.nq, it.k0, it.nk);
@@ -572,6 +571,16 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
       seq += 2 * it.tiles;
       // ------------------------------------------------------------ result rows
+      // eight lanes write a row, 16 bytes each, so that whole sectors leave together (a row a lane took ~100
+      // clocks an instruction): this lane's part of eight of the warp's rows
+      int to[8];  // query << 8 | head of the tile, -1: a row of no use
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int row = (warp & 3) * 32 + 4 * i + (lane >> 3), q = row * a.by_hg >> 16, h = row - q * a.hg;
+        to[i] = q < a.qpt && first + q <= last && h < it.nheads ? q << 8 | h : -1;
+      }
+      uint16_t* const out = static_cast<uint16_t*>(a.out) + static_cast<long long>(it.q0 + first) * a.out_row +
+                            static_cast<long long>(it.head0) * a.out_head + 8 * (lane & 7);
       if (ok && any) {
         ok = __all_sync(0xffffffffu, mbar_wait(&o_full[g], no & 1));
         ++no;
@@ -626,16 +635,14 @@ __global__ void __launch_bounds__(THREADS, 1)
           }
         }
         __syncwarp();
-        // eight lanes a row: whole sectors leave together (a row a lane: ~100 clocks an instruction)
-        const int piece = lane & 7, ch = c0 + 8 * piece;
+        if (c0 + 8 * (lane & 7) < a.head_dim) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int k = 4 * i + (lane >> 3), row = (warp & 3) * 32 + k;
-          const int q = row * a.by_hg >> 16, h = row - q * a.hg;
-          if (ch < a.head_dim && q < a.qpt && first + q <= last && h < it.nheads)
-            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + static_cast<long long>(it.q0 + first + q) * a.out_row +
-                                      static_cast<long long>(it.head0 + h) * a.out_head + ch) =
-                *reinterpret_cast<const uint4*>(stage + k * 128 + ((piece ^ (k & 7)) << 4));
+          for (int i = 0; i < 8; ++i) {
+            const int k = 4 * i + (lane >> 3);
+            if (to[i] >= 0)
+              *reinterpret_cast<uint4*>(out + (to[i] >> 8) * a.out_row + (to[i] & 255) * a.out_head + c0) =
+                  *reinterpret_cast<const uint4*>(stage + k * 128 + (((lane & 7) ^ (k & 7)) << 4));
+          }
         }
         __syncwarp();
       }
@@ -720,6 +727,7 @@ elasto_status window_attention_launch(const elasto_window_attention_args& u, int
   }
   a.qtiles = static_cast<int>(qtiles);
   a.items = static_cast<int>(qtiles * per);
+  a.per_q = Divisor(static_cast<unsigned>(per)), a.by_nsub = Divisor(a.nsub), a.by_heads_kv = Divisor(a.heads_kv);
   const bool bf = u.dtype == ELASTO_BF16;
   const uint64_t kvb = u.kv_start ? 1 : u.batch;
   const long long kb = u.kv_start ? 0 : u.k_batch, vb = u.kv_start ? 0 : u.v_batch;
