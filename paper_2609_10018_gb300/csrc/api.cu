@@ -60,6 +60,7 @@ cudaError_t ensure_kernel_attributes() {
     if (r == cudaSuccess) r = pk_init_attributes();
     if (r == cudaSuccess) r = gemm_fp8_init_attributes();
     if (r == cudaSuccess) r = window_attention_init_attributes();
+    if (r == cudaSuccess) r = window_decode_init_attributes();
     g_attr_err[dev] = r;
   });
   return g_attr_err[dev];

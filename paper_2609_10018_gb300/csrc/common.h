@@ -364,5 +364,8 @@ cudaError_t gemm_fp8_init_attributes();
 cudaError_t qk_norm_rope_launch(const elasto_qk_norm_rope_args& a, int* status, cudaStream_t s);
 elasto_status window_attention_launch(const elasto_window_attention_args& a, int* status, cudaStream_t s);
 cudaError_t window_attention_init_attributes();
+// The single-token form (max_queries == 1).
+elasto_status window_decode_launch(const elasto_window_attention_args& a, int* status, cudaStream_t s);
+cudaError_t window_decode_init_attributes();
 
 }  // namespace elasto

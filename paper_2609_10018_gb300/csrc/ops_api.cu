@@ -255,6 +255,7 @@ elasto_status elasto_op_window_attention(void* stream, const elasto_window_atten
     return refuse("elasto_op_window_attention: starts or lengths misaligned");
   elasto_status st = check_device();
   if (st != ELASTO_OK) return st;
+  if (a.max_queries == 1) return window_decode_launch(a, status_device, static_cast<cudaStream_t>(stream));
   return window_attention_launch(a, status_device, static_cast<cudaStream_t>(stream));
 }
 
