@@ -45,13 +45,16 @@ constexpr int QT = 128, KT = 128;  // rows and keys of a tile
 constexpr int HALF = 128 * 128;    // bytes of 128 rows of 64 16-bit values
 constexpr int SMEM_LIMIT = 232448;
 constexpr int STAGING = 8 * 32 * 128;  // 32 rows of 64 channels of out for each softmax warp
-constexpr int TMEM_COLS = 512, O_COL = 256;
+constexpr int TMEM_COLS = 512;
 constexpr float kLazy = 8.0f;  // log2 of how far a row's maximum may grow before O is rescaled
 
 template <int DP>
 struct Shape {
   static constexpr int halves = DP / 64, tile = halves * HALF;
   static constexpr int slots = DP == 128 ? 4 : 8;
+  static constexpr int scores = DP == 128 ? 2 : 3;  // S tiles in TMEM
+  static constexpr int o_col = scores * KT;
+  static_assert(o_col + 2 * DP <= TMEM_COLS, "tensor memory");
   static constexpr int smem = 1024 + (2 + slots) * tile + STAGING + 512;
 };
 static_assert(Shape<128>::smem <= SMEM_LIMIT && Shape<64>::smem <= SMEM_LIMIT, "shared memory");
@@ -264,14 +267,14 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint64_t* empty = full + S::slots;    // [slot]
   uint64_t* q_full = empty + S::slots;  // [group]
   uint64_t* q_empty = q_full + 2;
-  uint64_t* s_full = q_empty + 2;
-  uint64_t* p_full = s_full + 2;        // 128 arrivals
-  uint64_t* o_full = p_full + 2;
-  uint64_t* drain = o_full + 2;
+  uint64_t* s_full = q_empty + 2;        // [group][n & 1] its score tile n is in TMEM
+  uint64_t* p_full = s_full + 4;         // [place in TMEM] 128 arrivals
+  uint64_t* o_done = p_full + 3;         // [group][n & 1] its product n has been added to O
+  uint64_t* drain = o_done + 4;
   uint64_t* next_full = drain + 1;       // [2] the answer for item n in next[n & 1]
   uint64_t* next_empty = next_full + 2;  // [2] read by the MMA warp and the softmax warps
   uint4* next = reinterpret_cast<uint4*>(bars + 40);  // [2]
-  static_assert(2 * S::slots + 15 <= 40, "barriers");
+  static_assert(2 * S::slots + 4 + 4 + 3 + 4 + 1 + 4 <= 40, "barriers");
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(next + 2);
   volatile int* bad_seq = reinterpret_cast<int*>(tmem_slot + 1);  // [2] item (by its number in this CTA) with bad values
 
@@ -284,13 +287,15 @@ __global__ void __launch_bounds__(THREADS, 1)
     for (int g = 0; g < 2; ++g) {
       mbar_init(&q_full[g], 1);
       mbar_init(&q_empty[g], 1);
-      mbar_init(&s_full[g], 1);
-      mbar_init(&p_full[g], 128);
-      mbar_init(&o_full[g], 1);
+      mbar_init(&s_full[2 * g], 1);
+      mbar_init(&s_full[2 * g + 1], 1);
+      mbar_init(&o_done[2 * g], 1);
+      mbar_init(&o_done[2 * g + 1], 1);
       mbar_init(&next_full[g], 1);
       mbar_init(&next_empty[g], 9);
       bad_seq[g] = -1;
     }
+    for (int i = 0; i < S::scores; ++i) mbar_init(&p_full[i], 128);
     mbar_init(drain, 1);
     fence_barrier_init();
   }
@@ -376,75 +381,73 @@ __global__ void __launch_bounds__(THREADS, 1)
     // ------------------------------------------------------------ MMA issuer
     const int dn = (a.head_dim + 15) & ~15;  // channels that the products take
     const uint32_t idesc_o = idesc_16_f32(QT, dn, !BF, false, true);
-    uint32_t seq = 0, nq[2] = {0, 0}, np[2] = {0, 0};
+    uint32_t seq = 0, nq[2] = {0, 0}, ns[2] = {0, 0}, no[2] = {0, 0};  // K/V tiles; of a group: Q tiles, score tiles, products
+    uint32_t ks = 0, kp = 0;                                             // score tiles and products of both
     bool ok = true, issued = false;
     int id = blockIdx.x;
     for (int n = 0; id >= 0; ++n) {
       const Item it = make_item(a, id);
       bool started_s[2] = {false, false}, started_o[2] = {false, false};
-      int last_s[2] = {-1, -1};
-      for (int t = 0; t < it.tiles; ++t)
-#pragma unroll
-        for (int g = 0; g < 2; ++g)
-          if (it.needs(g, t)) last_s[g] = t;
-      auto issue_s = [&](int g, int t) -> bool {  // (K(t) has landed)
-        if (!started_s[g]) {
-          if (!mbar_wait_warp(&q_full[g], nq[g] & 1)) return false;
-          ++nq[g];
-          started_s[g] = true;
-          tc_fence_after();
-        }
-        const uint32_t slot = (seq + 2 * t) % S::slots;
-        const uint64_t dq = sdesc_sw128(smem_addr(qbuf + g * S::tile), 16, 1024);
-        const uint64_t dk = sdesc_sw128(smem_addr(ring + slot * S::tile), 16, 1024);
-        const uint32_t idesc_s = idesc_16_f32(QT, it.width(t), !BF);
-        for (int k = 0; k < dn / 16; ++k) {
-          const uint64_t off = (k >> 2) * (HALF >> 4) + 2 * (k & 3);
-          tc_mma_warp(tmem + g * KT, dq + off, dk + off, idesc_s, k != 0);
-        }
-        tc_commit_warp(&s_full[g]);
-        if (t == last_s[g]) tc_commit_warp(&q_empty[g]);
-        issued = true;
-        return true;
-      };
-      auto landed = [&](uint32_t s) -> bool {
-        const bool r = mbar_wait_warp(&full[s % S::slots], (s / S::slots) & 1);
+      auto landed = [&](uint32_t s) {
+        ok = ok && mbar_wait_warp(&full[s % S::slots], (s / S::slots) & 1);
         tc_fence_after();
-        return r;
       };
-      if (it.tiles > 0) {
-        ok = landed(seq);
-#pragma unroll
-        for (int g = 0; g < 2; ++g)
-          if (ok && it.needs(g, 0)) ok = issue_s(g, 0);
-        if (ok) tc_commit_warp(&empty[seq % S::slots]);
-      }
-      for (int t = 0; t < it.tiles && ok; ++t) {
-        const uint32_t vs = seq + 2 * t + 1;
-        ok = landed(vs);
-        const bool more = t + 1 < it.tiles;
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          if (ok && it.needs(g, t)) ok = mbar_wait_warp(&p_full[g], np[g] & 1);
-          if (!ok) continue;
-          if (it.needs(g, t)) {
-            ++np[g];
+      // The score tiles of both groups in the order (key tile, group), S::scores of them ahead of their products
+      // with V, which follow in the same order. Score tile k lies in TMEM at k % S::scores, its P over it; the
+      // next S there is issued after that product, and MMAs run in the order of their issue.
+      auto scores = [&](int t, int g) {
+        if (!ok || t >= it.tiles) return;
+        const uint32_t s = seq + 2 * t;
+        if (g == 0) landed(s);
+        if (ok && it.needs(g, t)) {
+          if (!started_s[g]) {
+            ok = mbar_wait_warp(&q_full[g], nq[g] & 1);
+            if (!ok) return;
+            ++nq[g];
+            started_s[g] = true;
             tc_fence_after();
-            const uint64_t dv = sdesc_sw128(smem_addr(ring + (vs % S::slots) * S::tile), HALF, 1024);
-            const int steps = it.width(t) / 16;
-            for (int k = 0; k < steps; ++k)
-              tc_mma_tmem_a_warp(tmem + O_COL + g * DP, tmem + g * KT + 8 * k, dv + 128 * k, idesc_o, started_o[g] || k != 0);
-            started_o[g] = true;
-            issued = true;
-            if (t == last_s[g]) tc_commit_warp(&o_full[g]);
           }
-          if (g == 1) tc_commit_warp(&empty[vs % S::slots]);
-          if (more) {
-            if (g == 0) ok = landed(vs + 1);
-            if (ok && it.needs(g, t + 1)) ok = issue_s(g, t + 1);
-            if (ok && g == 1) tc_commit_warp(&empty[(vs + 1) % S::slots]);
+          const uint32_t buf = ks++ % S::scores;
+          const uint64_t dq = sdesc_sw128(smem_addr(qbuf + g * S::tile), 16, 1024);
+          const uint64_t dk = sdesc_sw128(smem_addr(ring + s % S::slots * S::tile), 16, 1024);
+          const uint32_t idesc_s = idesc_16_f32(QT, it.width(t), !BF);
+          for (int k = 0; k < dn / 16; ++k) {
+            const uint64_t off = (k >> 2) * (HALF >> 4) + 2 * (k & 3);
+            tc_mma_warp(tmem + buf * KT, dq + off, dk + off, idesc_s, k != 0);
           }
+          tc_commit_warp(&s_full[2 * g + (ns[g]++ & 1)]);
+          if (t == it.sink_tiles + (of(it.hi, g) - it.base0) / KT) tc_commit_warp(&q_empty[g]);  // the group's last
+          issued = true;
         }
+        if (ok && g == 1) tc_commit_warp(&empty[s % S::slots]);
+      };
+      auto product = [&](int t, int g) {
+        if (!ok) return;
+        const uint32_t s = seq + 2 * t + 1;
+        if (g == 0) landed(s);
+        if (ok && it.needs(g, t)) {
+          const uint32_t buf = kp % S::scores;
+          ok = mbar_wait_warp(&p_full[buf], (kp / S::scores) & 1);
+          if (!ok) return;
+          ++kp;
+          tc_fence_after();
+          const uint64_t dv = sdesc_sw128(smem_addr(ring + (s % S::slots) * S::tile), HALF, 1024);
+          const int steps = it.width(t) / 16;
+          for (int k = 0; k < steps; ++k)
+            tc_mma_tmem_a_warp(tmem + S::o_col + g * DP, tmem + buf * KT + 8 * k, dv + 128 * k, idesc_o, started_o[g] || k != 0);
+          started_o[g] = true;
+          tc_commit_warp(&o_done[2 * g + (no[g]++ & 1)]);
+        }
+        if (ok && g == 1) tc_commit_warp(&empty[s % S::slots]);
+      };
+      scores(0, 0);
+      scores(0, 1);
+      if constexpr (S::scores == 3) scores(1, 0);
+      for (int t = 0; t < it.tiles && ok; ++t) {
+        product(t, 0);
+        scores(t + 1, S::scores == 3 ? 1 : 0);
+        product(t, 1);
+        scores(t + S::scores - 1, S::scores == 3 ? 0 : 1);
       }
       seq += 2 * it.tiles;
       id = ok ? following(n) : -2;
@@ -459,16 +462,17 @@ __global__ void __launch_bounds__(THREADS, 1)
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_MANY));
     const int g = (warp - 4) >> 2, r = (warp & 3) * 32 + lane;  // row of the tile = TMEM lane
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t s_tm = tmem + lanes + g * KT, o_tm = tmem + lanes + O_COL + g * DP;
+    const uint32_t o_tm = tmem + lanes + S::o_col + g * DP;
     const float sc = a.scale_log2;
     uint8_t* const stage = staging + (warp - 4) * (STAGING / 8);
-    uint32_t seq = 0, ns = 0, no = 0;
+    uint32_t seq = 0, ns = 0, no = 0;  // K/V tiles; score tiles of both groups, products of this one before the next
     bool ok = true;
     int id = blockIdx.x;
     for (int nth = 0; id >= 0; ++nth) {
       const Item it = make_item(a, id);
       const int first = of(it.first, g), last = of(it.last, g);
       if (last < first) {
+        for (int t = 0; t < it.tiles; ++t) ns += it.needs(g ^ 1, t);
         seq += 2 * it.tiles;
         id = following(nth);
         continue;
@@ -480,6 +484,14 @@ __global__ void __launch_bounds__(THREADS, 1)
       const int pmin = shift + first, pmax = shift + last;
       float m = -INFINITY, sum = 0.0f;
       bool any = false;
+      // Product n of this group. Two barriers take turns (for score tiles too: at most two of a group's are
+      // ahead), and every tile waits for the product before the last one, so that a barrier is never more than
+      // one phase from the one waited for. Barriers by place in TMEM would be: a group may skip many tiles.
+      auto product_done = [&](uint32_t n) -> bool {
+        const bool r = __all_sync(0xffffffffu, mbar_wait(&o_done[2 * g + (n & 1)], (n >> 1) & 1));
+        tc_fence_after();
+        return r;
+      };
       // one key tile of 32 * NC columns
       auto tile = [&](auto chunks, int t) -> bool {
         constexpr int NC = decltype(chunks)::value;
@@ -487,8 +499,9 @@ __global__ void __launch_bounds__(THREADS, 1)
         // every row sees every column
         const bool whole = t >= it.sink_tiles && pmin >= 0 && base >= pmax - a.window &&
                            base + 32 * NC - 1 <= (a.causal ? pmin : min(it.nk - 1, pmin + a.window));
-        if (!__all_sync(0xffffffffu, mbar_wait(&s_full[g], ns & 1))) return false;
-        ++ns;
+        const uint32_t buf = ns % S::scores, s_tm = tmem + lanes + buf * KT;
+        if (!__all_sync(0xffffffffu, mbar_wait(&s_full[2 * g + (no & 1)], (no >> 1) & 1))) return false;
+        if (no >= 2 && !product_done(no - 2)) return false;
         tc_fence_after();
         uint32_t v[NC][32];
 #pragma unroll
@@ -521,6 +534,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           // (top - m is NaN while both are -inf: nothing seen yet, nothing to rescale)
           const float keep = m == -INFINITY ? 0.0f : ex2_approx((m - top) * sc);
           if (any) {
+            if (!product_done(no - 1)) return false;
             uint32_t o[32];
             for (int c = 0; c < DP; c += 32) {
               tmem_ld_32x32b_x32(o_tm + c, o);
@@ -560,14 +574,20 @@ __global__ void __launch_bounds__(THREADS, 1)
         sum += (add[0].x + add[0].y) + (add[1].x + add[1].y);
         tmem_st_wait();
         tc_fence_before();
-        mbar_arrive(&p_full[g]);
+        mbar_arrive(&p_full[buf]);
+        ++no;
         return true;
       };
       for (int t = 0; t < it.tiles && ok; ++t) {
-        if (!it.needs(g, t)) continue;
-        const int width = it.width(t);
-        ok = width == KT ? tile(std::integral_constant<int, 4>(), t)
-                         : width == 64 ? tile(std::integral_constant<int, 2>(), t) : tile(std::integral_constant<int, 1>(), t);
+        const bool other = it.needs(g ^ 1, t);
+        if (g == 1 && other) ++ns;
+        if (it.needs(g, t)) {
+          const int width = it.width(t);
+          ok = width == KT ? tile(std::integral_constant<int, 4>(), t)
+                           : width == 64 ? tile(std::integral_constant<int, 2>(), t) : tile(std::integral_constant<int, 1>(), t);
+          ++ns;
+        }
+        if (g == 0 && other) ++ns;
       }
       seq += 2 * it.tiles;
       // ------------------------------------------------------------ result rows
@@ -582,9 +602,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       uint16_t* const out = static_cast<uint16_t*>(a.out) + static_cast<long long>(it.q0 + first) * a.out_row +
                             static_cast<long long>(it.head0) * a.out_head + 8 * (lane & 7);
       if (ok && any) {
-        ok = __all_sync(0xffffffffu, mbar_wait(&o_full[g], no & 1));
-        ++no;
-        tc_fence_after();
+        ok = product_done(no - 1);
       }
       if (!ok) {
         id = -2;

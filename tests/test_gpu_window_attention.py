@@ -149,6 +149,15 @@ def test_many_short_sequences():
     Case(n, n, 2, 1, 32, window=6, sinks=1, dtype=torch.float16).check()
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n,causal,window,sinks", [(257, True, 100, 0), (257, False, 100, 0), (700, False, 20, 1), (129, True, -1, 3),
+                                                   (513, True, 30, 40)])
+def test_many_items_with_uneven_tiles(n, causal, window, sinks, d):
+    """More work items than SMs, one of whose two tiles has few rows, none, or far fewer keys than the other."""
+    lens = [n - (i % 3) for i in range(48)]
+    Case(lens, lens, 4, 4, d, causal=causal, window=window, sinks=sinks).check()
+
+
 def test_long_sequence():
     Case([2900], [2900], 2, 1, 128, window=300, sinks=4).check()
     Case([1500], [1500], 1, 1, 64, causal=False, window=100, sinks=1).check()
