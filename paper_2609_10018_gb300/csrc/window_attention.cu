@@ -10,7 +10,8 @@
 // spans few positions (fewer keys that only some of its rows see). A work item is
 // two tiles of one sequence and key head; they share the K/V stream. Roles:
 //   warp 0     TMA: Q of both tiles, then K and V tiles of 128 keys through a ring;
-//   warp 1     tcgen05.mma: S = Q K^T into TMEM, O += P V with P read from TMEM;
+//   warps 1-2  tcgen05.mma, one for each tile: S = Q K^T into TMEM, O += P V with P read from TMEM;
+//   warp 3     looks through the V tiles that need it (below);
 //   warps 4-11 two groups of four, one for each tile, a row a thread: scores from
 //              TMEM to registers, mask, maximum, exp2, P back to TMEM (over S).
 // While one group works on its scores the tensor cores run the other's products.
@@ -44,18 +45,16 @@ static_assert(128 * REGS_FEW + 256 * REGS_MANY <= THREADS * REGS, "register spli
 constexpr int QT = 128, KT = 128;  // rows and keys of a tile
 constexpr int HALF = 128 * 128;    // bytes of 128 rows of 64 16-bit values
 constexpr int SMEM_LIMIT = 232448;
+constexpr int TAIL = 768;             // barriers, items
 constexpr int STAGING = 8 * 32 * 128;  // 32 rows of 64 channels of out for each softmax warp
-constexpr int TMEM_COLS = 512;
+constexpr int TMEM_COLS = 512, O_COL = 2 * KT;  // S (and P over it) of both groups, then O
 constexpr float kLazy = 8.0f;  // log2 of how far a row's maximum may grow before O is rescaled
 
 template <int DP>
 struct Shape {
   static constexpr int halves = DP / 64, tile = halves * HALF;
   static constexpr int slots = DP == 128 ? 4 : 8;
-  static constexpr int scores = DP == 128 ? 2 : 3;  // S tiles in TMEM
-  static constexpr int o_col = scores * KT;
-  static_assert(o_col + 2 * DP <= TMEM_COLS, "tensor memory");
-  static constexpr int smem = 1024 + (2 + slots) * tile + STAGING + 512;
+  static constexpr int smem = 1024 + (2 + slots) * tile + STAGING + TAIL;
 };
 static_assert(Shape<128>::smem <= SMEM_LIMIT && Shape<64>::smem <= SMEM_LIMIT, "shared memory");
 
@@ -103,31 +102,31 @@ __device__ __forceinline__ T of(const T (&x)[2], int g) {
   return g ? x[1] : x[0];
 }
 
-// What every role derives alike for a work item.
+// What every role derives alike for a work item. Key tile t holds the keys from base(t) on, width(t) of them.
 struct Item {
   int b, kvh, head0, nheads;    // first query head and how many of the tile's
   int q0, nq, k0, nk;
   int first[2], last[2];        // queries of each group's rows: [first, last] (empty: last < first)
-  int lo[2], hi[2];             // its band of keys (empty: hi < lo)
-  int sinks;                    // keys [0, sinks) that belong to the item whatever the band
-  int sink_tiles, base0, end;   // tiles of the sinks alone; the band's first key and the one behind its last
   int tiles;                    // key tiles
+  int sink_tiles, base0;        // those of the sinks alone, the first key of the others
+  int sink_width, last_width;   // of the first of the sinks' and of the last tile (the others have KT keys)
+  int with_sinks;               // tiles [0, with_sinks) hold sinks
+  int from[2], to[2];           // and tiles [from, to] the keys that the group's rows see besides (none: to < from)
+  int whole_from[2], whole_to[2];  // every row of the group sees every key of tiles [whole_from, whole_to]
 
-  // Key tile t holds keys base(t) .. base(t) + width(t).
   __device__ __forceinline__ int base(int t) const { return t < sink_tiles ? t * KT : base0 + (t - sink_tiles) * KT; }
   __device__ __forceinline__ int width(int t) const {
-    const int left = (t < sink_tiles ? sinks : end) - base(t);
-    return left <= 32 ? 32 : left <= 64 ? 64 : KT;
+    return t == tiles - 1 ? last_width : t < sink_tiles ? sink_width : KT;
   }
-  __device__ __forceinline__ bool has_sinks(int t) const { return t < sink_tiles || (sink_tiles == 0 && base(t) < sinks); }
+  // Some row of the group sees a key of the tile.
   __device__ __forceinline__ bool needs(int g, int t) const {
-    const int low = of(lo, g), high = of(hi, g);
-    if (high < low) return false;
-    if (has_sinks(t)) return true;
-    const int b0 = base(t);
-    return b0 + KT - 1 >= low && b0 <= high;
+    const int f = of(from, g), l = of(to, g);
+    return l >= f && (t < with_sinks || (t >= f && t <= l));
   }
+  __device__ __forceinline__ bool whole(int g, int t) const { return t >= of(whole_from, g) && t <= of(whole_to, g); }
 };
+
+__device__ __forceinline__ int tile_width(int keys) { return keys <= 32 ? 32 : keys <= 64 ? 64 : KT; }
 
 __device__ __forceinline__ Item make_item(const Args& a, int id) {
   Item it;
@@ -139,35 +138,50 @@ __device__ __forceinline__ Item make_item(const Args& a, int id) {
   it.head0 = it.kvh * a.group + sub * a.hg;
   it.nheads = min(a.hg, a.group - sub * a.hg);
   sequence(a, it.b, it.q0, it.nq, it.k0, it.nk);
-  int lo = 0x7fffffff, hi = -1;
-  it.sinks = 0;
+  const int shift = it.nk - it.nq;
+  int lo[2], hi[2], low = 0x7fffffff, high = -1, sinks = 0;  // the groups' bands of keys, and the item's
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
     it.first[g] = (q * a.tiles + g) * a.qpt;
     it.last[g] = g < a.tiles ? min(it.first[g] + a.qpt, it.nq) - 1 : it.first[g] - 1;
-    const int shift = it.nk - it.nq, pmax = shift + it.last[g], pmin = max(shift + it.first[g], 0);
-    it.lo[g] = 0, it.hi[g] = -1;
+    const int pmax = shift + it.last[g], pmin = max(shift + it.first[g], 0);
+    lo[g] = 0, hi[g] = -1;
     if (it.last[g] < it.first[g] || pmax < 0 || it.nk == 0) continue;
     if (a.causal) {
-      it.lo[g] = max(0, pmin - a.window), it.hi[g] = pmax;
-      it.sinks = max(it.sinks, min(a.sinks, pmax + 1));
+      lo[g] = max(0, pmin - a.window), hi[g] = pmax;
+      sinks = max(sinks, min(a.sinks, pmax + 1));
     } else {
-      it.sinks = min(a.sinks, it.nk);
-      it.lo[g] = pmin < a.sinks ? 0 : max(0, pmin - a.window);
-      it.hi[g] = pmin < a.sinks ? it.nk - 1 : max(min(it.nk - 1, pmax + a.window), it.sinks - 1);
+      sinks = min(a.sinks, it.nk);
+      lo[g] = pmin < a.sinks ? 0 : max(0, pmin - a.window);
+      hi[g] = pmin < a.sinks ? it.nk - 1 : max(min(it.nk - 1, pmax + a.window), sinks - 1);
     }
-    lo = min(lo, it.lo[g]), hi = max(hi, it.hi[g]);
+    low = min(low, lo[g]), high = max(high, hi[g]);
   }
   it.sink_tiles = 0;
-  if (it.sinks > 0) {
-    if (lo <= ((it.sinks + 31) & ~31))
-      lo = 0;
+  if (sinks > 0) {
+    if (low <= ((sinks + 31) & ~31))
+      low = 0;
     else
-      it.sink_tiles = (it.sinks + KT - 1) / KT;
+      it.sink_tiles = (sinks + KT - 1) / KT;
   }
-  it.base0 = lo;
-  it.end = hi + 1;
-  it.tiles = hi < 0 ? 0 : it.sink_tiles + (hi - lo) / KT + 1;
+  it.base0 = low;
+  it.with_sinks = (sinks + KT - 1) / KT;
+  it.sink_width = it.sink_tiles == 1 ? tile_width(sinks) : KT;
+  it.tiles = high < 0 ? 0 : it.sink_tiles + (high - low) / KT + 1;
+  it.last_width = tile_width(high + 1 - it.base(it.tiles - 1));
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    it.from[g] = 0, it.to[g] = -1, it.whole_from[g] = 0, it.whole_to[g] = -1;
+    if (hi[g] < lo[g]) continue;
+    it.from[g] = it.sink_tiles + (lo[g] - low) / KT;
+    it.to[g] = it.sink_tiles + (hi[g] - low) / KT;
+    const int pmin = shift + it.first[g], pmax = shift + it.last[g];
+    if (pmin < 0) continue;
+    // keys [pmax - window, until] (floor divisions: the differences may be negative)
+    const int until = a.causal ? pmin : min(it.nk - 1, pmin + a.window);
+    it.whole_from[g] = it.sink_tiles + max(0, (pmax - a.window - low + KT - 1) >> 7);
+    it.whole_to[g] = it.sink_tiles + ((until + 1 - low) >> 7) - 1;
+  }
   return it;
 }
 
@@ -221,34 +235,62 @@ __device__ __forceinline__ void look16(uint32_t w, uint32_t& acc) {
     asm("fma.rn.f16x2 %0, %1, %2, %0;" : "+r"(acc) : "r"(w), "r"(0u));
 }
 
-// Sets the values of the first `rows` rows of a V tile that are not finite to zero (128
-// threads of a group, number r); the item's number goes to *flag if there were any.
+// Sets the values of the first `rows` rows of a V tile that are not finite to zero (a
+// warp); the item's number goes to *flag if there were any.
 template <bool BF, int DP>
 __device__ __forceinline__ void clear_bad_values(uint8_t* v, int rows, int r, int seq, volatile int* flag) {
   const int n = rows * 8;  // 16-byte pieces of 64 channels
-  uint32_t acc[2] = {0u, 0u};
+  uint32_t acc = 0u;
 #pragma unroll
   for (int h = 0; h < DP / 64; ++h)
-#pragma unroll 2
-    for (int i = r; i < n; i += 256) {
-      const uint4 x = reinterpret_cast<const uint4*>(v + h * HALF)[i];
-      look16<BF>(x.x, acc[0]), look16<BF>(x.y, acc[0]), look16<BF>(x.z, acc[0]), look16<BF>(x.w, acc[0]);
-      if (i + 128 < n) {
-        const uint4 y = reinterpret_cast<const uint4*>(v + h * HALF)[i + 128];
-        look16<BF>(y.x, acc[1]), look16<BF>(y.y, acc[1]), look16<BF>(y.z, acc[1]), look16<BF>(y.w, acc[1]);
-      }
+    for (int i = r; i < n; i += 256) {  // (rows is a multiple of 32)
+      uint4 x[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = reinterpret_cast<const uint4*>(v + h * HALF)[i + 32 * k];
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        look16<BF>(x[k].x, acc), look16<BF>(x[k].y, acc), look16<BF>(x[k].z, acc), look16<BF>(x[k].w, acc);
     }
-  if (!__any_sync(0xffffffffu, (bad16<BF>(acc[0]) | bad16<BF>(acc[1])) != 0)) return;
+  if (!__any_sync(0xffffffffu, bad16<BF>(acc) != 0)) return;
   *flag = seq;
   __threadfence_block();
   for (int h = 0; h < DP / 64; ++h)
-    for (int i = r; i < n; i += 128) {
+    for (int i = r; i < n; i += 32) {
       uint4* p = reinterpret_cast<uint4*>(v + h * HALF) + i;
       uint4 w = *p;
       w.x &= ~bad16<BF>(w.x), w.y &= ~bad16<BF>(w.y), w.z &= ~bad16<BF>(w.z), w.w &= ~bad16<BF>(w.w);
       *p = w;
     }
   fence_async_smem();
+}
+
+// Values that are not finite were left out of the products: adds those that a row sees to its result, for
+// the 32 rows from row0 on (rare, so by the warp row by row and key by key).
+template <bool BF>
+__device__ __noinline__ void add_bad_values(const Args& a, const Item& it, int g, int row0, int lane) {
+  __syncwarp();
+  for (int r = row0; r < row0 + 32; ++r) {
+    const int q = r * a.by_hg >> 16, h = r - q * a.hg, qi = of(it.first, g) + q, p = it.nk - it.nq + qi;
+    if (q >= a.qpt || qi > of(it.last, g) || h >= it.nheads || p < 0) continue;
+    uint16_t* const out = static_cast<uint16_t*>(a.out) + static_cast<long long>(it.q0 + qi) * a.out_row +
+                          static_cast<long long>(it.head0 + h) * a.out_head;
+    for (int t = 0; t < it.tiles; ++t) {
+      const Seen s = seen_columns(a, it, t, p);
+      for (int col = 0; col < it.width(t); ++col) {
+        if (!(s.word(col >> 5) >> (col & 31) & 1)) continue;
+        const long long key = it.k0 + it.base(t) + col;
+        const uint16_t* v = a.v + (a.kv_start ? 0 : it.b * a.v_batch) + key * a.v_row + it.kvh * a.v_head;
+        for (int c = 2 * lane; c < a.head_dim; c += 64) {
+          const uint32_t w = *reinterpret_cast<const uint32_t*>(v + c), bad = bad16<BF>(w);
+          if (!bad) continue;
+          uint32_t* const o = reinterpret_cast<uint32_t*>(out + c);
+          const float2 x = unpack16<BF>(w), y = unpack16<BF>(*o);
+          *o = pack16<BF>(bad & 0xffffu ? x.x + y.x : y.x, bad >> 16 ? x.y + y.y : y.y);
+        }
+      }
+    }
+  }
+  __syncwarp();
 }
 
 template <bool BF, int DP>
@@ -267,36 +309,40 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint64_t* empty = full + S::slots;    // [slot]
   uint64_t* q_full = empty + S::slots;  // [group]
   uint64_t* q_empty = q_full + 2;
-  uint64_t* s_full = q_empty + 2;        // [group][n & 1] its score tile n is in TMEM
-  uint64_t* p_full = s_full + 4;         // [place in TMEM] 128 arrivals
-  uint64_t* o_done = p_full + 3;         // [group][n & 1] its product n has been added to O
-  uint64_t* drain = o_done + 4;
-  uint64_t* next_full = drain + 1;       // [2] the answer for item n in next[n & 1]
-  uint64_t* next_empty = next_full + 2;  // [2] read by the MMA warp and the softmax warps
-  uint4* next = reinterpret_cast<uint4*>(bars + 40);  // [2]
-  static_assert(2 * S::slots + 4 + 4 + 3 + 4 + 1 + 4 <= 40, "barriers");
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(next + 2);
-  volatile int* bad_seq = reinterpret_cast<int*>(tmem_slot + 1);  // [2] item (by its number in this CTA) with bad values
+  uint64_t* s_full = q_empty + 2;        // [group]
+  uint64_t* p_full = s_full + 2;         // [group] 128 arrivals
+  uint64_t* o_full = p_full + 2;         // [group]
+  uint64_t* drain = o_full + 2;          // [2]
+  uint64_t* item_full = drain + 2;       // [2] item n is in items[n & 1]
+  uint64_t* item_empty = item_full + 2;  // [2] read by the other warps
+  uint64_t* answered = item_empty + 2;
+  uint64_t* v_ready = answered + 1;      // [slot] the V tile there has been looked through
+  static_assert(3 * S::slots + 4 + 6 + 2 + 5 <= 48, "barriers");
+  uint4* answer = reinterpret_cast<uint4*>(bars + 48);
+  Item* items = reinterpret_cast<Item*>(answer + 1);  // [2]
+  static_assert(48 * 8 + 16 + 2 * sizeof(Item) + 4 + 32 <= TAIL, "barriers and items");
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(items + 2);
+  volatile int* bad_seq = reinterpret_cast<int*>(tmem_slot + 1);  // [8] item (by its number in this CTA) with bad values
 
   const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::slots; ++i) {
       mbar_init(&full[i], 1);
-      mbar_init(&empty[i], 1);
+      mbar_init(&empty[i], i & 1 ? 3 : 2);  // the two MMA warps; V tiles, in the odd slots: the one that looks through them
+      mbar_init(&v_ready[i], 1);
     }
+    for (int i = 0; i < 8; ++i) bad_seq[i] = -1;
     for (int g = 0; g < 2; ++g) {
       mbar_init(&q_full[g], 1);
       mbar_init(&q_empty[g], 1);
-      mbar_init(&s_full[2 * g], 1);
-      mbar_init(&s_full[2 * g + 1], 1);
-      mbar_init(&o_done[2 * g], 1);
-      mbar_init(&o_done[2 * g + 1], 1);
-      mbar_init(&next_full[g], 1);
-      mbar_init(&next_empty[g], 9);
-      bad_seq[g] = -1;
+      mbar_init(&s_full[g], 1);
+      mbar_init(&p_full[g], 128);
+      mbar_init(&o_full[g], 1);
+      mbar_init(&item_full[g], 1);
+      mbar_init(&item_empty[g], 11);
+      mbar_init(&drain[g], 1);
     }
-    for (int i = 0; i < S::scores; ++i) mbar_init(&p_full[i], 128);
-    mbar_init(drain, 1);
+    mbar_init(answered, 1);
     fence_barrier_init();
   }
   if (warp == 1) {
@@ -310,15 +356,16 @@ __global__ void __launch_bounds__(THREADS, 1)
   pdl_wait();
   pdl_trigger();
 
-  // item n + 1 for a warp that is done with item n (all its lanes call); -1: none, -2: the wait gave up
-  auto following = [&](int n) -> int {
-    ++n;
-    if (!__all_sync(0xffffffffu, mbar_wait(&next_full[n & 1], ((n - 1) >> 1) & 1))) return -2;
-    const int id = requested_block(next + (n & 1));
-    fence_async_smem();  // read before the next answer is written there
+  // Item n for a warp (all its lanes call): false after the last one, or when the wait gave up.
+  auto take = [&](uint32_t n, Item& it) -> bool {
+    if (!__all_sync(0xffffffffu, mbar_wait(&item_full[n & 1], (n >> 1) & 1))) {
+      if (lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
+      return false;
+    }
+    it = items[n & 1];
     __syncwarp();
-    if (lane == 0) mbar_arrive(&next_empty[n & 1]);
-    return id;
+    if (lane == 0) mbar_arrive(&item_empty[n & 1]);
+    return it.tiles >= 0;
   };
   if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FEW));
   if (warp == 0) {
@@ -330,11 +377,18 @@ __global__ void __launch_bounds__(THREADS, 1)
       uint32_t seq = 0, nq[2] = {0, 0};  // K/V tiles and Q tiles issued
       bool ok = true;
       int id = blockIdx.x;
-      for (int n = 0; ok && id >= 0; ++n) {
-        const Item it = make_item(a, id);
+      for (uint32_t n = 0; ok; ++n) {
+        ok = mbar_wait(&item_empty[n & 1], ((n >> 1) & 1) ^ 1);
+        if (!ok) break;
+        Item it;
+        it.tiles = -1;
+        if (id >= 0) it = make_item(a, id);
+        items[n & 1] = it;
+        mbar_arrive(&item_full[n & 1]);
+        if (id < 0) break;
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-          if (!ok || it.hi[g] < it.lo[g]) continue;
+          if (!ok || it.to[g] < it.from[g]) continue;
           ok = mbar_wait(&q_empty[g], (nq[g] & 1) ^ 1);
           if (!ok) continue;
           mbar_expect_tx(&q_full[g], S::halves * a.hg * a.qpt * 128);
@@ -363,13 +417,11 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         if (!ok) break;
         // the next item, asked for once this one's loads are under way
-        const int m = n + 1;
-        ok = mbar_wait(&next_empty[m & 1], ((n >> 1) & 1) ^ 1);
-        if (!ok) break;
-        mbar_expect_tx(&next_full[m & 1], 16);
-        request_block(next + (m & 1), &next_full[m & 1]);
-        ok = mbar_wait(&next_full[m & 1], (n >> 1) & 1);
-        id = requested_block(next + (m & 1));
+        fence_async_smem();  // (the last answer has been read)
+        mbar_expect_tx(answered, 16);
+        request_block(answer, answered);
+        ok = mbar_wait(answered, n & 1);
+        id = requested_block(answer);
       }
       if (!ok) record_status(a.status, ELASTO_ERR_TIMEOUT);
       // all copies have landed before the CTA exits
@@ -377,147 +429,156 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (int g = 0; g < 2; ++g)
         if (nq[g] > 0) mbar_wait(&q_full[g], (nq[g] - 1) & 1);
     }
-  } else if (warp == 1) {
-    // ------------------------------------------------------------ MMA issuer
-    const int dn = (a.head_dim + 15) & ~15;  // channels that the products take
-    const uint32_t idesc_o = idesc_16_f32(QT, dn, !BF, false, true);
-    uint32_t seq = 0, nq[2] = {0, 0}, ns[2] = {0, 0}, no[2] = {0, 0};  // K/V tiles; of a group: Q tiles, score tiles, products
-    uint32_t ks = 0, kp = 0;                                             // score tiles and products of both
+  } else if (warp <= 2) {
+    // ------------------------------------------------------------ MMA issuer of a group
+    // (A warp for each: what one spent on waits, commits and addresses, 500 clocks a tile and group besides the
+    // MMAs' issue, was what paced the kernel. An MMA's operands, and the branches to it, have to be known to be
+    // the same in all lanes, see tc_mma_warp.)
+    const int g = warp - 1;
+    const int ksteps = (a.head_dim + 15) / 16;  // channels that the products take
+    const uint32_t idesc_o = idesc_16_f32(QT, 16 * ksteps, !BF, false, true);
+    const uint32_t s_tm = tmem + g * KT, o_tm = tmem + O_COL + g * DP;
+    const uint32_t q_lo = sdesc_lo(smem_addr(qbuf + g * S::tile), 16);
+    constexpr uint32_t hi = sdesc_sw128_hi(1024);
+    uint32_t seq = 0, nq = 0, np = 0;  // K/V tiles, items, P tiles
     bool ok = true, issued = false;
-    int id = blockIdx.x;
-    for (int n = 0; id >= 0; ++n) {
-      const Item it = make_item(a, id);
-      bool started_s[2] = {false, false}, started_o[2] = {false, false};
+    Item it;
+    for (uint32_t n = 0; ok && warp_uniform(take(n, it)); ++n) {
+      const int tiles = warp_uniform(it.tiles), from = warp_uniform(of(it.from, g)), to = warp_uniform(of(it.to, g));
+      const int with_sinks = warp_uniform(to < from ? 0 : it.with_sinks), sink_tiles = warp_uniform(it.sink_tiles);
+      const int whole_from = warp_uniform(of(it.whole_from, g)), whole_to = warp_uniform(of(it.whole_to, g));
+      const int sink_width = warp_uniform(it.sink_width), last_width = warp_uniform(it.last_width);
+      auto width = [&](int t) { return t == tiles - 1 ? last_width : t < sink_tiles ? sink_width : KT; };
+      auto needs = [&](int t) { return t < with_sinks || (t >= from && t <= to); };
       auto landed = [&](uint32_t s) {
-        ok = ok && mbar_wait_warp(&full[s % S::slots], (s / S::slots) & 1);
+        ok = mbar_wait_warp(&full[s % S::slots], (s / S::slots) & 1);
         tc_fence_after();
+        return ok;
       };
-      // The score tiles of both groups in the order (key tile, group), S::scores of them ahead of their products
-      // with V, which follow in the same order. Score tile k lies in TMEM at k % S::scores, its P over it; the
-      // next S there is issued after that product, and MMAs run in the order of their issue.
-      auto scores = [&](int t, int g) {
-        if (!ok || t >= it.tiles) return;
+      auto scores = [&](int t) {
         const uint32_t s = seq + 2 * t;
-        if (g == 0) landed(s);
-        if (ok && it.needs(g, t)) {
-          if (!started_s[g]) {
-            ok = mbar_wait_warp(&q_full[g], nq[g] & 1);
-            if (!ok) return;
-            ++nq[g];
-            started_s[g] = true;
-            tc_fence_after();
+        if (!landed(s)) return;
+        if (needs(t)) {
+          const uint32_t k_lo = sdesc_lo(smem_addr(ring + s % S::slots * S::tile), 16);
+          const uint32_t idesc_s = idesc_16_f32(QT, width(t), !BF);
+#pragma unroll
+          for (int k = 0; k < DP / 16; ++k) {
+            const uint32_t off = (k >> 2) * (HALF >> 4) + 2 * (k & 3);
+            if (k < ksteps) tc_mma_warp_lo(s_tm, q_lo + off, k_lo + off, hi, idesc_s, k != 0);
           }
-          const uint32_t buf = ks++ % S::scores;
-          const uint64_t dq = sdesc_sw128(smem_addr(qbuf + g * S::tile), 16, 1024);
-          const uint64_t dk = sdesc_sw128(smem_addr(ring + s % S::slots * S::tile), 16, 1024);
-          const uint32_t idesc_s = idesc_16_f32(QT, it.width(t), !BF);
-          for (int k = 0; k < dn / 16; ++k) {
-            const uint64_t off = (k >> 2) * (HALF >> 4) + 2 * (k & 3);
-            tc_mma_warp(tmem + buf * KT, dq + off, dk + off, idesc_s, k != 0);
-          }
-          tc_commit_warp(&s_full[2 * g + (ns[g]++ & 1)]);
-          if (t == it.sink_tiles + (of(it.hi, g) - it.base0) / KT) tc_commit_warp(&q_empty[g]);  // the group's last
+          tc_commit_warp(&s_full[g]);
           issued = true;
         }
-        if (ok && g == 1) tc_commit_warp(&empty[s % S::slots]);
+        tc_commit_warp(&empty[s % S::slots]);
       };
-      auto product = [&](int t, int g) {
-        if (!ok) return;
-        const uint32_t s = seq + 2 * t + 1;
-        if (g == 0) landed(s);
-        if (ok && it.needs(g, t)) {
-          const uint32_t buf = kp % S::scores;
-          ok = mbar_wait_warp(&p_full[buf], (kp / S::scores) & 1);
-          if (!ok) return;
-          ++kp;
-          tc_fence_after();
-          const uint64_t dv = sdesc_sw128(smem_addr(ring + (s % S::slots) * S::tile), HALF, 1024);
-          const int steps = it.width(t) / 16;
-          for (int k = 0; k < steps; ++k)
-            tc_mma_tmem_a_warp(tmem + S::o_col + g * DP, tmem + buf * KT + 8 * k, dv + 128 * k, idesc_o, started_o[g] || k != 0);
-          started_o[g] = true;
-          tc_commit_warp(&o_done[2 * g + (no[g]++ & 1)]);
+      bool begun = false;
+      if (tiles > 0) {
+        if (to >= from) {
+          ok = mbar_wait_warp(&q_full[g], nq & 1);
+          ++nq;
         }
-        if (ok && g == 1) tc_commit_warp(&empty[s % S::slots]);
-      };
-      scores(0, 0);
-      scores(0, 1);
-      if constexpr (S::scores == 3) scores(1, 0);
+        if (ok) scores(0);
+      }
+      const int last_s = max(to, with_sinks - 1);
+      if (ok && tiles > 0 && last_s == 0) tc_commit_warp(&q_empty[g]);
+      for (int t = 0; t < tiles && ok; ++t) {
+        const uint32_t s = seq + 2 * t + 1;
+        if (needs(t)) {
+          if (!mbar_wait_warp(&p_full[g], np & 1)) {
+            ok = false;
+            break;
+          }
+          ++np;
+        }
+        if (!landed(s)) break;
+        if (needs(t)) {
+          const uint32_t slot = s % S::slots;
+          const bool masked = t < whole_from || t > whole_to;
+          if (masked) ok = mbar_wait_warp(&v_ready[slot], (s / S::slots) & 1);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t v_lo = sdesc_lo(smem_addr(ring + slot * S::tile), HALF);
+          const int steps = width(t) / 16;
+#pragma unroll
+          for (int k = 0; k < KT / 16; ++k)
+            if (k < steps) tc_mma_tmem_a_warp_lo(o_tm, s_tm + 8 * k, v_lo + 128 * k, hi, idesc_o, begun || k != 0);
+          begun = true;
+          if (t == last_s) tc_commit_warp(&o_full[g]);
+        }
+        tc_commit_warp(&empty[s % S::slots]);
+        if (t + 1 < tiles) {
+          scores(t + 1);
+          if (ok && t + 1 == last_s) tc_commit_warp(&q_empty[g]);
+        }
+      }
+      seq += 2 * tiles;
+    }
+    if (!ok && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
+    if (issued) {
+      tc_commit_warp(&drain[g]);
+      mbar_wait_warp(&drain[g], 0);
+    }
+  } else if (warp < 4) {
+    // ------------------------------------------------------------ a look through the V tiles with masks
+    uint32_t seq = 0;
+    bool ok = true;
+    Item it;
+    for (uint32_t n = 0; ok && take(n, it); ++n) {
       for (int t = 0; t < it.tiles && ok; ++t) {
-        product(t, 0);
-        scores(t + 1, S::scores == 3 ? 1 : 0);
-        product(t, 1);
-        scores(t + S::scores - 1, S::scores == 3 ? 0 : 1);
+        // (every V tile is waited for and given back, so that no slot is ever two tiles ahead)
+        const uint32_t vs = seq + 2 * t + 1, slot = vs % S::slots;
+        ok = mbar_wait_warp(&full[slot], (vs / S::slots) & 1);
+        if (!ok) break;
+        const bool masked = (it.needs(0, t) && !it.whole(0, t)) || (it.needs(1, t) && !it.whole(1, t));
+        if (masked) clear_bad_values<BF, DP>(ring + slot * S::tile, it.width(t), lane, n, &bad_seq[n & 7]);
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&v_ready[slot]);
+          mbar_arrive(&empty[slot]);
+        }
       }
       seq += 2 * it.tiles;
-      id = ok ? following(n) : -2;
     }
-    if (id == -2 && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
-    if (issued) {
-      tc_commit_warp(drain);
-      mbar_wait_warp(drain, 0);
-    }
-  } else if (warp >= 4) {
+    if (!ok && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
+  } else {
     // ------------------------------------------------------------ softmax, a row a thread
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_MANY));
     const int g = (warp - 4) >> 2, r = (warp & 3) * 32 + lane;  // row of the tile = TMEM lane
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t o_tm = tmem + lanes + S::o_col + g * DP;
+    const uint32_t s_tm = tmem + lanes + g * KT, o_tm = tmem + lanes + O_COL + g * DP;
     const float sc = a.scale_log2;
     uint8_t* const stage = staging + (warp - 4) * (STAGING / 8);
-    uint32_t seq = 0, ns = 0, no = 0;  // K/V tiles; score tiles of both groups, products of this one before the next
+    uint32_t ns = 0, no = 0;  // score tiles and items of this group
     bool ok = true;
-    int id = blockIdx.x;
-    for (int nth = 0; id >= 0; ++nth) {
-      const Item it = make_item(a, id);
+    Item it;
+    for (uint32_t nth = 0; ok && take(nth, it); ++nth) {
       const int first = of(it.first, g), last = of(it.last, g);
-      if (last < first) {
-        for (int t = 0; t < it.tiles; ++t) ns += it.needs(g ^ 1, t);
-        seq += 2 * it.tiles;
-        id = following(nth);
-        continue;
-      }
+      if (last < first) continue;
       const int own = r * a.by_hg >> 16;  // query of this row in the tile
       const int qi = first + own, head = r - own * a.hg;
       const bool mine = own < a.qpt && qi <= last && head < it.nheads;
       const int shift = it.nk - it.nq, p = shift + qi;
-      const int pmin = shift + first, pmax = shift + last;
       float m = -INFINITY, sum = 0.0f;
       bool any = false;
-      // Product n of this group. Two barriers take turns (for score tiles too: at most two of a group's are
-      // ahead), and every tile waits for the product before the last one, so that a barrier is never more than
-      // one phase from the one waited for. Barriers by place in TMEM would be: a group may skip many tiles.
-      auto product_done = [&](uint32_t n) -> bool {
-        const bool r = __all_sync(0xffffffffu, mbar_wait(&o_done[2 * g + (n & 1)], (n >> 1) & 1));
-        tc_fence_after();
-        return r;
-      };
-      // one key tile of 32 * NC columns
-      auto tile = [&](auto chunks, int t) -> bool {
-        constexpr int NC = decltype(chunks)::value;
-        const int base = it.base(t);
-        // every row sees every column
-        const bool whole = t >= it.sink_tiles && pmin >= 0 && base >= pmax - a.window &&
-                           base + 32 * NC - 1 <= (a.causal ? pmin : min(it.nk - 1, pmin + a.window));
-        const uint32_t buf = ns % S::scores, s_tm = tmem + lanes + buf * KT;
-        if (!__all_sync(0xffffffffu, mbar_wait(&s_full[2 * g + (no & 1)], (no >> 1) & 1))) return false;
-        if (no >= 2 && !product_done(no - 2)) return false;
+      // one key tile; MASKED: some row does not see some of its keys, or it has less than KT
+      auto tile = [&](auto masked, int t) -> bool {
+        constexpr int NC = KT / 32;
+        constexpr bool MASKED = decltype(masked)::value;
+        if (!__all_sync(0xffffffffu, mbar_wait(&s_full[g], ns & 1))) return false;
+        ++ns;
         tc_fence_after();
         uint32_t v[NC][32];
 #pragma unroll
         for (int i = 0; i < NC; ++i) tmem_ld_32x32b_x32(s_tm + 32 * i, v[i]);
-        if (!whole) {
-          const uint32_t vs = seq + 2 * t + 1;
-          if (!__all_sync(0xffffffffu, mbar_wait(&full[vs % S::slots], (vs / S::slots) & 1))) return false;
-          clear_bad_values<BF, DP>(ring + (vs % S::slots) * S::tile, 32 * NC, r, nth, &bad_seq[nth & 1]);
-        }
         tmem_ld_wait();
-        if (!whole) {
+        uint32_t live = 15;  // words of 32 columns that some row of the warp sees
+        if constexpr (MASKED) {
           const Seen s = seen_columns(a, it, t, p);
 #pragma unroll
           for (int i = 0; i < NC; ++i) {
-            const uint32_t w = s.word(i);
-            if (__all_sync(0xffffffffu, w == 0xffffffffu)) continue;
+            const uint32_t w = s.word(i);  // (no row sees a column past the tile's width)
+            if (!__any_sync(0xffffffffu, w)) live &= ~(1u << i);
+            if (__all_sync(0xffffffffu, w == 0xffffffffu) || !(live >> i & 1)) continue;
 #pragma unroll
             for (int j = 0; j < 32; ++j)
               if (!(w >> j & 1)) v[i][j] = 0xff800000u;
@@ -525,17 +586,19 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int i = 0; i < NC; ++i)
+        for (int i = 0; i < NC; ++i) {
+          if (MASKED && !(live >> i & 1)) continue;
 #pragma unroll
           for (int j = 0; j < 32; j += 2)
             t4[(j >> 1) & 3] = max3(t4[(j >> 1) & 3], __uint_as_float(v[i][j]), __uint_as_float(v[i][j + 1]));
+        }
         const float top = fmaxf(m, fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])));
         if (__any_sync(0xffffffffu, (top - m) * sc > kLazy)) {
           // (top - m is NaN while both are -inf: nothing seen yet, nothing to rescale)
           const float keep = m == -INFINITY ? 0.0f : ex2_approx((m - top) * sc);
           if (any) {
-            if (!product_done(no - 1)) return false;
             uint32_t o[32];
+#pragma unroll 1
             for (int c = 0; c < DP; c += 32) {
               tmem_ld_32x32b_x32(o_tm + c, o);
               tmem_ld_wait();
@@ -562,6 +625,12 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
           uint32_t pk[16];
+          if (MASKED && !(live >> i & 1)) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) pk[j] = 0u;
+            tmem_st_16(s_tm + 16 * i, pk);
+            continue;
+          }
 #pragma unroll
           for (int j = 0; j < 32; j += 2) {
             const float2 x = fma2(make_float2(__uint_as_float(v[i][j]), __uint_as_float(v[i][j + 1])), sc2, neg2);
@@ -574,22 +643,12 @@ __global__ void __launch_bounds__(THREADS, 1)
         sum += (add[0].x + add[0].y) + (add[1].x + add[1].y);
         tmem_st_wait();
         tc_fence_before();
-        mbar_arrive(&p_full[buf]);
-        ++no;
+        mbar_arrive(&p_full[g]);
         return true;
       };
       for (int t = 0; t < it.tiles && ok; ++t) {
-        const bool other = it.needs(g ^ 1, t);
-        if (g == 1 && other) ++ns;
-        if (it.needs(g, t)) {
-          const int width = it.width(t);
-          ok = width == KT ? tile(std::integral_constant<int, 4>(), t)
-                           : width == 64 ? tile(std::integral_constant<int, 2>(), t) : tile(std::integral_constant<int, 1>(), t);
-          ++ns;
-        }
-        if (g == 0 && other) ++ns;
+        if (it.needs(g, t)) ok = it.whole(g, t) ? tile(std::false_type(), t) : tile(std::true_type(), t);
       }
-      seq += 2 * it.tiles;
       // ------------------------------------------------------------ result rows
       // eight lanes write a row, 16 bytes each, so that whole sectors leave together (a row a lane took ~100
       // clocks an instruction): this lane's part of eight of the warp's rows
@@ -602,43 +661,26 @@ __global__ void __launch_bounds__(THREADS, 1)
       uint16_t* const out = static_cast<uint16_t*>(a.out) + static_cast<long long>(it.q0 + first) * a.out_row +
                             static_cast<long long>(it.head0) * a.out_head + 8 * (lane & 7);
       if (ok && any) {
-        ok = product_done(no - 1);
+        ok = __all_sync(0xffffffffu, mbar_wait(&o_full[g], no & 1));
+        ++no;
+        tc_fence_after();
       }
-      if (!ok) {
-        id = -2;
-        break;
-      }
+      if (!ok) break;
       const bool sees = mine && p >= 0 && it.nk > 0;
-      const float inv = 1.0f / sum;
-      const bool bad = any && bad_seq[nth & 1] == nth;
-#pragma unroll
+      const float inv = sees ? 1.0f / sum : 0.0f;  // (O of a row that sees nothing is 0)
+      // (loops that are not unrolled: the kernel's code has to fit the instruction caches, where twice the code
+      // made every part of it slower)
+#pragma unroll 1
       for (int c0 = 0; c0 < DP; c0 += 64) {
-#pragma unroll
-        for (int c = c0; c < c0 + 64; c += 32) {
+#pragma unroll 1
+        for (int c = 0; c < 64; c += 32) {
           uint32_t o[32];
           if (any) {
-            tmem_ld_32x32b_x32(o_tm + c, o);
+            tmem_ld_32x32b_x32(o_tm + c0 + c, o);
             tmem_ld_wait();
-          }
-          if (bad && sees) {
-            // values that are not finite were left out of the product: add those that this row sees
-            for (int t = 0; t < it.tiles; ++t) {
-              const Seen s = seen_columns(a, it, t, p);
-              for (int col = 0; col < it.width(t); ++col) {
-                if (!(s.word(col >> 5) >> (col & 31) & 1)) continue;
-                const long long key = it.k0 + it.base(t) + col;
-                const uint16_t* vp = a.v + (a.kv_start ? 0 : it.b * a.v_batch) + key * a.v_row + it.kvh * a.v_head + c;
+          } else {
 #pragma unroll
-                for (int j = 0; j < 32; j += 2) {
-                  if (c + j >= a.head_dim) continue;
-                  const uint32_t w = *reinterpret_cast<const uint32_t*>(vp + j);
-                  const uint32_t b2 = bad16<BF>(w);
-                  const float2 x = unpack16<BF>(w);
-                  if (b2 & 0xffffu) o[j] = __float_as_uint(__uint_as_float(o[j]) + x.x);
-                  if (b2 >> 16) o[j + 1] = __float_as_uint(__uint_as_float(o[j + 1]) + x.y);
-                }
-              }
-            }
+            for (int j = 0; j < 32; ++j) o[j] = 0u;
           }
           // 16-byte pieces of a 128-byte row, so placed that writing a column and reading a row are without conflicts
 #pragma unroll
@@ -647,9 +689,9 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const float2 x = mul2(make_float2(__uint_as_float(o[8 * j + 2 * i]), __uint_as_float(o[8 * j + 2 * i + 1])), make_float2(inv, inv));
-              pk[i] = sees ? pack16<BF>(x.x, x.y) : 0u;
+              pk[i] = pack16<BF>(x.x, x.y);
             }
-            *reinterpret_cast<uint4*>(stage + lane * 128 + (((((c - c0) >> 3) + j) ^ (lane & 7)) << 4)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+            *reinterpret_cast<uint4*>(stage + lane * 128 + ((((c >> 3) + j) ^ (lane & 7)) << 4)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
           }
         }
         __syncwarp();
@@ -664,10 +706,13 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         __syncwarp();
       }
+      if (any && bad_seq[nth & 7] == static_cast<int>(nth)) {
+        const Item copy = it;  // (in memory, which `it` itself is not)
+        add_bad_values<BF>(a, copy, g, (warp & 3) * 32, lane);
+      }
       tc_fence_before();
-      id = following(nth);
     }
-    if (id == -2 && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
+    if (!ok && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
   }
   __syncthreads();
   if (warp == 1) {
