@@ -10,8 +10,8 @@
 // spans few positions (fewer keys that only some of its rows see). A work item is
 // two tiles of one sequence and key head; they share the K/V stream. Roles:
 //   warp 0     TMA: Q of both tiles, then K and V tiles of 128 keys through a ring;
-//   warps 1-2  tcgen05.mma, one for each tile: S = Q K^T into TMEM, O += P V with P read from TMEM;
-//   warp 3     looks through the V tiles that need it (below);
+//   warp 1     tcgen05.mma: S = Q K^T into TMEM, O += P V with P read from TMEM;
+//   warps 2-3  look through the V tiles that need it (below);
 //   warps 4-11 two groups of four, one for each tile, a row a thread: scores from
 //              TMEM to registers, mask, maximum, exp2, P back to TMEM (over S).
 // While one group works on its scores the tensor cores run the other's products.
@@ -235,8 +235,8 @@ __device__ __forceinline__ void look16(uint32_t w, uint32_t& acc) {
     asm("fma.rn.f16x2 %0, %1, %2, %0;" : "+r"(acc) : "r"(w), "r"(0u));
 }
 
-// Sets the values of the first `rows` rows of a V tile that are not finite to zero (a
-// warp); the item's number goes to *flag if there were any.
+// Sets the values of the first `rows` rows of a V tile that are not finite to zero (64
+// threads, number r); the item's number goes to *flag if there were any.
 template <bool BF, int DP>
 __device__ __forceinline__ void clear_bad_values(uint8_t* v, int rows, int r, int seq, volatile int* flag) {
   const int n = rows * 8;  // 16-byte pieces of 64 channels
@@ -244,18 +244,18 @@ __device__ __forceinline__ void clear_bad_values(uint8_t* v, int rows, int r, in
 #pragma unroll
   for (int h = 0; h < DP / 64; ++h)
     for (int i = r; i < n; i += 256) {  // (rows is a multiple of 32)
-      uint4 x[8];
+      uint4 x[4];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = reinterpret_cast<const uint4*>(v + h * HALF)[i + 32 * k];
+      for (int k = 0; k < 4; ++k) x[k] = reinterpret_cast<const uint4*>(v + h * HALF)[i + 64 * k];
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
+      for (int k = 0; k < 4; ++k)
         look16<BF>(x[k].x, acc), look16<BF>(x[k].y, acc), look16<BF>(x[k].z, acc), look16<BF>(x[k].w, acc);
     }
   if (!__any_sync(0xffffffffu, bad16<BF>(acc) != 0)) return;
   *flag = seq;
   __threadfence_block();
   for (int h = 0; h < DP / 64; ++h)
-    for (int i = r; i < n; i += 32) {
+    for (int i = r; i < n; i += 64) {
       uint4* p = reinterpret_cast<uint4*>(v + h * HALF) + i;
       uint4 w = *p;
       w.x &= ~bad16<BF>(w.x), w.y &= ~bad16<BF>(w.y), w.z &= ~bad16<BF>(w.z), w.w &= ~bad16<BF>(w.w);
@@ -312,8 +312,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint64_t* s_full = q_empty + 2;        // [group]
   uint64_t* p_full = s_full + 2;         // [group] 128 arrivals
   uint64_t* o_full = p_full + 2;         // [group]
-  uint64_t* drain = o_full + 2;          // [2]
-  uint64_t* item_full = drain + 2;       // [2] item n is in items[n & 1]
+  uint64_t* drain = o_full + 2;
+  uint64_t* item_full = drain + 1;       // [2] item n is in items[n & 1]
   uint64_t* item_empty = item_full + 2;  // [2] read by the other warps
   uint64_t* answered = item_empty + 2;
   uint64_t* v_ready = answered + 1;      // [slot] the V tile there has been looked through
@@ -328,8 +328,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::slots; ++i) {
       mbar_init(&full[i], 1);
-      mbar_init(&empty[i], i & 1 ? 3 : 2);  // the two MMA warps; V tiles, in the odd slots: the one that looks through them
-      mbar_init(&v_ready[i], 1);
+      mbar_init(&empty[i], i & 1 ? 3 : 1);  // (V tiles, in the odd slots: the warps that look through them too)
+      mbar_init(&v_ready[i], 2);
     }
     for (int i = 0; i < 8; ++i) bad_seq[i] = -1;
     for (int g = 0; g < 2; ++g) {
@@ -340,8 +340,8 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_init(&o_full[g], 1);
       mbar_init(&item_full[g], 1);
       mbar_init(&item_empty[g], 11);
-      mbar_init(&drain[g], 1);
     }
+    mbar_init(drain, 1);
     mbar_init(answered, 1);
     fence_barrier_init();
   }
@@ -429,94 +429,99 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (int g = 0; g < 2; ++g)
         if (nq[g] > 0) mbar_wait(&q_full[g], (nq[g] - 1) & 1);
     }
-  } else if (warp <= 2) {
-    // ------------------------------------------------------------ MMA issuer of a group
-    // (A warp for each: what one spent on waits, commits and addresses, 500 clocks a tile and group besides the
-    // MMAs' issue, was what paced the kernel. An MMA's operands, and the branches to it, have to be known to be
-    // the same in all lanes, see tc_mma_warp.)
-    const int g = warp - 1;
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ MMA issuer
+    // The groups alternate, a product and the scores that follow it each, so that the one's run while the other
+    // group is at its scores. (A warp for each group: they fell into step, 3430 clocks a tile of both in place of
+    // 2600 at 128 channels.) What the warp spends between MMAs paces the kernel too: fields of the item in
+    // registers, and an MMA's operands, and the branches to it, known to be the same in all lanes (tc_mma_warp).
     const int ksteps = (a.head_dim + 15) / 16;  // channels that the products take
     const uint32_t idesc_o = idesc_16_f32(QT, 16 * ksteps, !BF, false, true);
-    const uint32_t s_tm = tmem + g * KT, o_tm = tmem + O_COL + g * DP;
-    const uint32_t q_lo = sdesc_lo(smem_addr(qbuf + g * S::tile), 16);
     constexpr uint32_t hi = sdesc_sw128_hi(1024);
-    uint32_t seq = 0, nq = 0, np = 0;  // K/V tiles, items, P tiles
+    const uint32_t q_lo = sdesc_lo(smem_addr(qbuf), 16), kv_lo = sdesc_lo(smem_addr(ring), 0);
+    constexpr uint32_t K_LBO = (16 >> 4) << 16, V_LBO = (HALF >> 4) << 16;  // leading byte offsets of K and V tiles
+    uint32_t seq = 0, nq[2] = {0, 0}, np[2] = {0, 0};  // K/V tiles; of a group: items, P tiles
     bool ok = true, issued = false;
     Item it;
     for (uint32_t n = 0; ok && warp_uniform(take(n, it)); ++n) {
-      const int tiles = warp_uniform(it.tiles), from = warp_uniform(of(it.from, g)), to = warp_uniform(of(it.to, g));
-      const int with_sinks = warp_uniform(to < from ? 0 : it.with_sinks), sink_tiles = warp_uniform(it.sink_tiles);
-      const int whole_from = warp_uniform(of(it.whole_from, g)), whole_to = warp_uniform(of(it.whole_to, g));
+      const int tiles = warp_uniform(it.tiles), sink_tiles = warp_uniform(it.sink_tiles);
       const int sink_width = warp_uniform(it.sink_width), last_width = warp_uniform(it.last_width);
+      int from[2], to[2], with_sinks[2], whole_from[2], whole_to[2], last[2];
+      bool begun[2] = {false, false};
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        from[g] = warp_uniform(it.from[g]), to[g] = warp_uniform(it.to[g]);
+        with_sinks[g] = warp_uniform(to[g] < from[g] ? 0 : it.with_sinks);
+        whole_from[g] = warp_uniform(it.whole_from[g]), whole_to[g] = warp_uniform(it.whole_to[g]);
+        last[g] = max(to[g], with_sinks[g] - 1);
+      }
       auto width = [&](int t) { return t == tiles - 1 ? last_width : t < sink_tiles ? sink_width : KT; };
-      auto needs = [&](int t) { return t < with_sinks || (t >= from && t <= to); };
       auto landed = [&](uint32_t s) {
-        ok = mbar_wait_warp(&full[s % S::slots], (s / S::slots) & 1);
+        ok = ok && mbar_wait_warp(&full[s % S::slots], (s / S::slots) & 1);
         tc_fence_after();
-        return ok;
       };
-      auto scores = [&](int t) {
-        const uint32_t s = seq + 2 * t;
-        if (!landed(s)) return;
-        if (needs(t)) {
-          const uint32_t k_lo = sdesc_lo(smem_addr(ring + s % S::slots * S::tile), 16);
-          const uint32_t idesc_s = idesc_16_f32(QT, width(t), !BF);
+      auto scores = [&](auto group, int t) {
+        constexpr int g = decltype(group)::value;
+        if (t >= tiles || !ok) return;
+        const uint32_t slot = (seq + 2 * t) % S::slots;
+        if (g == 0) landed(seq + 2 * t);
+        if (ok && (t < with_sinks[g] || (t >= from[g] && t <= to[g]))) {
+          if (t == (with_sinks[g] > 0 ? 0 : from[g])) {  // the first of the item
+            ok = mbar_wait_warp(&q_full[g], nq[g] & 1);
+            if (!ok) return;
+            ++nq[g];
+            tc_fence_after();
+          }
+          const uint32_t k_lo = kv_lo + K_LBO + slot * (S::tile >> 4), idesc_s = idesc_16_f32(QT, width(t), !BF);
 #pragma unroll
           for (int k = 0; k < DP / 16; ++k) {
             const uint32_t off = (k >> 2) * (HALF >> 4) + 2 * (k & 3);
-            if (k < ksteps) tc_mma_warp_lo(s_tm, q_lo + off, k_lo + off, hi, idesc_s, k != 0);
+            if (k < ksteps) tc_mma_warp_lo(tmem + g * KT, q_lo + g * (S::tile >> 4) + off, k_lo + off, hi, idesc_s, k != 0);
           }
           tc_commit_warp(&s_full[g]);
+          if (t == last[g]) tc_commit_warp(&q_empty[g]);
           issued = true;
         }
-        tc_commit_warp(&empty[s % S::slots]);
+        if (g == 1) tc_commit_warp(&empty[slot]);
       };
-      bool begun = false;
-      if (tiles > 0) {
-        if (to >= from) {
-          ok = mbar_wait_warp(&q_full[g], nq & 1);
-          ++nq;
-        }
-        if (ok) scores(0);
-      }
-      const int last_s = max(to, with_sinks - 1);
-      if (ok && tiles > 0 && last_s == 0) tc_commit_warp(&q_empty[g]);
-      for (int t = 0; t < tiles && ok; ++t) {
-        const uint32_t s = seq + 2 * t + 1;
-        if (needs(t)) {
-          if (!mbar_wait_warp(&p_full[g], np & 1)) {
-            ok = false;
-            break;
-          }
-          ++np;
-        }
-        if (!landed(s)) break;
-        if (needs(t)) {
-          const uint32_t slot = s % S::slots;
-          const bool masked = t < whole_from || t > whole_to;
-          if (masked) ok = mbar_wait_warp(&v_ready[slot], (s / S::slots) & 1);
-          if (!ok) break;
+      auto product = [&](auto group, int t) {
+        constexpr int g = decltype(group)::value;
+        if (!ok) return;
+        const uint32_t s = seq + 2 * t + 1, slot = s % S::slots;
+        if (g == 0) landed(s);
+        if (ok && (t < with_sinks[g] || (t >= from[g] && t <= to[g]))) {
+          if (t < whole_from[g] || t > whole_to[g]) ok = mbar_wait_warp(&v_ready[slot], (s / S::slots) & 1);
+          ok = ok && mbar_wait_warp(&p_full[g], np[g] & 1);
+          if (!ok) return;
+          ++np[g];
           tc_fence_after();
-          const uint32_t v_lo = sdesc_lo(smem_addr(ring + slot * S::tile), HALF);
+          const uint32_t v_lo = kv_lo + V_LBO + slot * (S::tile >> 4);
           const int steps = width(t) / 16;
 #pragma unroll
           for (int k = 0; k < KT / 16; ++k)
-            if (k < steps) tc_mma_tmem_a_warp_lo(o_tm, s_tm + 8 * k, v_lo + 128 * k, hi, idesc_o, begun || k != 0);
-          begun = true;
-          if (t == last_s) tc_commit_warp(&o_full[g]);
+            if (k < steps)
+              tc_mma_tmem_a_warp_lo(tmem + O_COL + g * DP, tmem + g * KT + 8 * k, v_lo + 128 * k, hi, idesc_o, begun[g] || k != 0);
+          begun[g] = true;
+          if (t == last[g]) tc_commit_warp(&o_full[g]);
         }
-        tc_commit_warp(&empty[s % S::slots]);
-        if (t + 1 < tiles) {
-          scores(t + 1);
-          if (ok && t + 1 == last_s) tc_commit_warp(&q_empty[g]);
-        }
+        if (g == 1) tc_commit_warp(&empty[slot]);
+      };
+      const std::integral_constant<int, 0> g0;
+      const std::integral_constant<int, 1> g1;
+      scores(g0, 0);
+      scores(g1, 0);
+      for (int t = 0; t < tiles && ok; ++t) {
+        product(g0, t);
+        scores(g0, t + 1);
+        product(g1, t);
+        scores(g1, t + 1);
       }
       seq += 2 * tiles;
     }
     if (!ok && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
     if (issued) {
-      tc_commit_warp(&drain[g]);
-      mbar_wait_warp(&drain[g], 0);
+      tc_commit_warp(drain);
+      mbar_wait_warp(drain, 0);
     }
   } else if (warp < 4) {
     // ------------------------------------------------------------ a look through the V tiles with masks
@@ -530,7 +535,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         ok = mbar_wait_warp(&full[slot], (vs / S::slots) & 1);
         if (!ok) break;
         const bool masked = (it.needs(0, t) && !it.whole(0, t)) || (it.needs(1, t) && !it.whole(1, t));
-        if (masked) clear_bad_values<BF, DP>(ring + slot * S::tile, it.width(t), lane, n, &bad_seq[n & 7]);
+        if (masked) clear_bad_values<BF, DP>(ring + slot * S::tile, it.width(t), (warp - 2) * 32 + lane, n, &bad_seq[n & 7]);
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(&v_ready[slot]);
