@@ -72,6 +72,7 @@ struct Args {
   const uint16_t* v;
   long long v_batch, v_row, v_head;
   int hg, nsub, qpt;  // heads and queries of a tile, tiles across a head group
+  int box_q;          // queries of 32 rows, 0 where hg does not divide 32
   int by_hg;          // row / hg = row * by_hg >> 16 (rows < 128, hg <= 32)
   int tiles;          // tiles (groups at work) of an item: 1 or 2
   int qtiles;         // items along the longest sequence's queries
@@ -297,7 +298,8 @@ template <bool BF, int DP>
 __global__ void __launch_bounds__(THREADS, 1)
     window_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                             const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmK32,
-                            const __grid_constant__ CUtensorMap tmV32, const __grid_constant__ Args a) {
+                            const __grid_constant__ CUtensorMap tmV32, const __grid_constant__ CUtensorMap tmO,
+                            const __grid_constant__ Args a) {
   using S = Shape<DP>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -655,16 +657,6 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (it.needs(g, t)) ok = it.whole(g, t) ? tile(std::false_type(), t) : tile(std::true_type(), t);
       }
       // ------------------------------------------------------------ result rows
-      // eight lanes write a row, 16 bytes each, so that whole sectors leave together (a row a lane took ~100
-      // clocks an instruction): this lane's part of eight of the warp's rows
-      int to[8];  // query << 8 | head of the tile, -1: a row of no use
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int row = (warp & 3) * 32 + 4 * i + (lane >> 3), q = row * a.by_hg >> 16, h = row - q * a.hg;
-        to[i] = q < a.qpt && first + q <= last && h < it.nheads ? q << 8 | h : -1;
-      }
-      uint16_t* const out = static_cast<uint16_t*>(a.out) + static_cast<long long>(it.q0 + first) * a.out_row +
-                            static_cast<long long>(it.head0) * a.out_head + 8 * (lane & 7);
       if (ok && any) {
         ok = __all_sync(0xffffffffu, mbar_wait(&o_full[g], no & 1));
         ++no;
@@ -672,6 +664,8 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
       if (!ok) break;
       const bool sees = mine && p >= 0 && it.nk > 0;
+      // the warp's 32 rows are whole queries of all the tile's heads
+      const bool boxed = a.box_q > 0 && first + ((warp & 3) + 1) * a.box_q - 1 <= last && it.nheads == a.hg;
       const float inv = sees ? 1.0f / sum : 0.0f;  // (O of a row that sees nothing is 0)
       // (loops that are not unrolled: the kernel's code has to fit the instruction caches, where twice the code
       // made every part of it slower)
@@ -699,24 +693,41 @@ __global__ void __launch_bounds__(THREADS, 1)
             *reinterpret_cast<uint4*>(stage + lane * 128 + ((((c >> 3) + j) ^ (lane & 7)) << 4)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
           }
         }
-        __syncwarp();
-        if (c0 + 8 * (lane & 7) < a.head_dim) {
-#pragma unroll
+        // Whole groups of rows leave by TMA. Else eight lanes write a row, 16 bytes each, so that whole sectors
+        // leave together (a row a lane took ~100 clocks an instruction; this, with its addresses, 1300 a half).
+        if (boxed) {
+          fence_async_smem();
+          __syncwarp();
+          if (elect_one()) {
+            tma_store_3d(&tmO, stage, c0, it.head0, it.q0 + first + (warp & 3) * a.box_q);
+            bulk_commit();
+            bulk_wait_read<0>();
+          }
+        } else {
+          __syncwarp();
+          uint16_t* const out = static_cast<uint16_t*>(a.out) + static_cast<long long>(it.q0 + first) * a.out_row +
+                                static_cast<long long>(it.head0) * a.out_head + c0 + 8 * (lane & 7);
+#pragma unroll 2
           for (int i = 0; i < 8; ++i) {
-            const int k = 4 * i + (lane >> 3);
-            if (to[i] >= 0)
-              *reinterpret_cast<uint4*>(out + (to[i] >> 8) * a.out_row + (to[i] & 255) * a.out_head + c0) =
+            const int k = 4 * i + (lane >> 3), row = (warp & 3) * 32 + k, q = row * a.by_hg >> 16, h = row - q * a.hg;
+            if (c0 + 8 * (lane & 7) < a.head_dim && q < a.qpt && first + q <= last && h < it.nheads)
+              *reinterpret_cast<uint4*>(out + q * a.out_row + h * a.out_head) =
                   *reinterpret_cast<const uint4*>(stage + k * 128 + (((lane & 7) ^ (k & 7)) << 4));
           }
         }
         __syncwarp();
       }
       if (any && bad_seq[nth & 7] == static_cast<int>(nth)) {
+        if (boxed) {
+          if (elect_one()) bulk_wait_all();
+          __syncwarp();
+        }
         const Item copy = it;  // (in memory, which `it` itself is not)
         add_bad_values<BF>(a, copy, g, (warp & 3) * 32, lane);
       }
       tc_fence_before();
     }
+    if (elect_one()) bulk_wait_all();
     if (!ok && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
   }
   __syncthreads();
@@ -739,9 +750,9 @@ bool map_of(CUtensorMap* tm, const void* p, bool bf, const elasto_window_attenti
 }
 
 template <bool BF, int DP>
-cudaError_t launch(const CUtensorMap (&tm)[5], const Args& a, cudaStream_t s) {
+cudaError_t launch(const CUtensorMap (&tm)[6], const Args& a, cudaStream_t s) {
   return launch_pdl(window_attention_kernel<BF, DP>, dim3(a.items), dim3(THREADS), Shape<DP>::smem, s, tm[0], tm[1], tm[2],
-                    tm[3], tm[4], a);
+                    tm[3], tm[4], tm[5], a);
 }
 
 }  // namespace
@@ -784,6 +795,7 @@ elasto_status window_attention_launch(const elasto_window_attention_args& u, int
   a.nsub = (a.group + 31) / 32;
   a.hg = (a.group + a.nsub - 1) / a.nsub;
   a.qpt = QT / a.hg;
+  a.box_q = 32 % a.hg == 0 ? 32 / a.hg : 0;
   a.by_hg = (65536 + a.hg - 1) / a.hg;
   const long long per = static_cast<long long>(a.batch) * a.heads_kv * a.nsub;
   const long long rows = (a.max_queries + a.qpt - 1LL) / a.qpt;
@@ -799,12 +811,13 @@ elasto_status window_attention_launch(const elasto_window_attention_args& u, int
   const bool bf = u.dtype == ELASTO_BF16;
   const uint64_t kvb = u.kv_start ? 1 : u.batch;
   const long long kb = u.kv_start ? 0 : u.k_batch, vb = u.kv_start ? 0 : u.v_batch;
-  CUtensorMap tm[5];
+  CUtensorMap tm[6]{};
   if (!map_of(&tm[0], u.q, bf, u, u.heads, u.q_rows, 1, u.q_head, u.q_row, -1, a.hg, a.qpt) ||
       !map_of(&tm[1], u.k, bf, u, u.heads_kv, u.kv_rows, kvb, u.k_head, u.k_row, kb, 1, KT) ||
       !map_of(&tm[2], u.v, bf, u, u.heads_kv, u.kv_rows, kvb, u.v_head, u.v_row, vb, 1, KT) ||
       !map_of(&tm[3], u.k, bf, u, u.heads_kv, u.kv_rows, kvb, u.k_head, u.k_row, kb, 1, 32) ||
-      !map_of(&tm[4], u.v, bf, u, u.heads_kv, u.kv_rows, kvb, u.v_head, u.v_row, vb, 1, 32)) {
+      !map_of(&tm[4], u.v, bf, u, u.heads_kv, u.kv_rows, kvb, u.v_head, u.v_row, vb, 1, 32) ||
+      (a.box_q > 0 && !map_of(&tm[5], u.out, bf, u, u.heads, u.q_rows, 1, u.out_head, u.out_row, -1, a.hg, a.box_q))) {
     set_error("elasto_op_window_attention: cuTensorMapEncodeTiled failed (alignment, strides or size)");
     return ELASTO_ERR_UNSUPPORTED;
   }
