@@ -11,7 +11,7 @@
 // two tiles of one sequence and key head; they share the K/V stream. Roles:
 //   warp 0     TMA: Q of both tiles, then K and V tiles of 128 keys through a ring;
 //   warp 1     tcgen05.mma: S = Q K^T into TMEM, O += P V with P read from TMEM;
-//   warps 2-3  look through the V tiles that need it (below);
+//   warps 2-3  look through the V tiles that need it (below); at 64 channels warp 2 issues MMAs;
 //   warps 4-11 two groups of four, one for each tile, a row a thread: scores from
 //              TMEM to registers, mask, maximum, exp2, P back to TMEM (over S).
 // While one group works on its scores the tensor cores run the other's products.
@@ -54,6 +54,9 @@ template <int DP>
 struct Shape {
   static constexpr int halves = DP / 64, tile = halves * HALF;
   static constexpr int slots = DP == 128 ? 4 : 8;
+  // MMA warps: at 64 channels one for each group, which then needs no step of the other (1024 x 1024 images 85 -> 78
+  // us); at 128, where the tensor cores have twice the work, two fell into step (prefill 272 -> 316 us).
+  static constexpr int issuers = DP == 128 ? 1 : 2, lookers = 3 - issuers;
   static constexpr int smem = 1024 + (2 + slots) * tile + STAGING + TAIL;
 };
 static_assert(Shape<128>::smem <= SMEM_LIMIT && Shape<64>::smem <= SMEM_LIMIT, "shared memory");
@@ -236,18 +239,18 @@ __device__ __forceinline__ void look16(uint32_t w, uint32_t& acc) {
     asm("fma.rn.f16x2 %0, %1, %2, %0;" : "+r"(acc) : "r"(w), "r"(0u));
 }
 
-// Sets the values of the first `rows` rows of a V tile that are not finite to zero (64
+// Sets the values of the first `rows` rows of a V tile that are not finite to zero (N
 // threads, number r); the item's number goes to *flag if there were any.
-template <bool BF, int DP>
+template <bool BF, int DP, int N>
 __device__ __forceinline__ void clear_bad_values(uint8_t* v, int rows, int r, int seq, volatile int* flag) {
   const int n = rows * 8;  // 16-byte pieces of 64 channels
   uint32_t acc = 0u;
 #pragma unroll
   for (int h = 0; h < DP / 64; ++h)
-    for (int i = r; i < n; i += 256) {  // (rows is a multiple of 32)
+    for (int i = r; i < n; i += 4 * N) {  // (rows is a multiple of 32)
       uint4 x[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) x[k] = reinterpret_cast<const uint4*>(v + h * HALF)[i + 64 * k];
+      for (int k = 0; k < 4; ++k) x[k] = reinterpret_cast<const uint4*>(v + h * HALF)[i + N * k];
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         look16<BF>(x[k].x, acc), look16<BF>(x[k].y, acc), look16<BF>(x[k].z, acc), look16<BF>(x[k].w, acc);
@@ -256,7 +259,7 @@ __device__ __forceinline__ void clear_bad_values(uint8_t* v, int rows, int r, in
   *flag = seq;
   __threadfence_block();
   for (int h = 0; h < DP / 64; ++h)
-    for (int i = r; i < n; i += 64) {
+    for (int i = r; i < n; i += N) {
       uint4* p = reinterpret_cast<uint4*>(v + h * HALF) + i;
       uint4 w = *p;
       w.x &= ~bad16<BF>(w.x), w.y &= ~bad16<BF>(w.y), w.z &= ~bad16<BF>(w.z), w.w &= ~bad16<BF>(w.w);
@@ -314,8 +317,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint64_t* s_full = q_empty + 2;        // [group]
   uint64_t* p_full = s_full + 2;         // [group] 128 arrivals
   uint64_t* o_full = p_full + 2;         // [group]
-  uint64_t* drain = o_full + 2;
-  uint64_t* item_full = drain + 1;       // [2] item n is in items[n & 1]
+  uint64_t* drain = o_full + 2;          // [MMA warp]
+  uint64_t* item_full = drain + 2;       // [2] item n is in items[n & 1]
   uint64_t* item_empty = item_full + 2;  // [2] read by the other warps
   uint64_t* answered = item_empty + 2;
   uint64_t* v_ready = answered + 1;      // [slot] the V tile there has been looked through
@@ -330,8 +333,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::slots; ++i) {
       mbar_init(&full[i], 1);
-      mbar_init(&empty[i], i & 1 ? 3 : 1);  // (V tiles, in the odd slots: the warps that look through them too)
-      mbar_init(&v_ready[i], 2);
+      mbar_init(&empty[i], i & 1 ? 3 : S::issuers);  // (V tiles, in the odd slots: the warps that look through them too)
+      mbar_init(&v_ready[i], S::lookers);
     }
     for (int i = 0; i < 8; ++i) bad_seq[i] = -1;
     for (int g = 0; g < 2; ++g) {
@@ -343,7 +346,8 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_init(&item_full[g], 1);
       mbar_init(&item_empty[g], 11);
     }
-    mbar_init(drain, 1);
+    mbar_init(&drain[0], 1);
+    mbar_init(&drain[1], 1);
     mbar_init(answered, 1);
     fence_barrier_init();
   }
@@ -431,12 +435,12 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (int g = 0; g < 2; ++g)
         if (nq[g] > 0) mbar_wait(&q_full[g], (nq[g] - 1) & 1);
     }
-  } else if (warp == 1) {
+  } else if (warp <= S::issuers) {
     // ------------------------------------------------------------ MMA issuer
-    // The groups alternate, a product and the scores that follow it each, so that the one's run while the other
-    // group is at its scores. (A warp for each group: they fell into step, 3430 clocks a tile of both in place of
-    // 2600 at 128 channels.) What the warp spends between MMAs paces the kernel too: fields of the item in
-    // registers, and an MMA's operands, and the branches to it, known to be the same in all lanes (tc_mma_warp).
+    // One warp for both groups alternates between them, a product and the scores that follow it each, so that the
+    // one's run while the other group is at its scores. What the warp spends between MMAs paces the kernel too:
+    // fields of the item in registers, and an MMA's operands, and the branches to it, known to be the same in all
+    // lanes (tc_mma_warp).
     const int ksteps = (a.head_dim + 15) / 16;  // channels that the products take
     const uint32_t idesc_o = idesc_16_f32(QT, 16 * ksteps, !BF, false, true);
     constexpr uint32_t hi = sdesc_sw128_hi(1024);
@@ -466,7 +470,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         constexpr int g = decltype(group)::value;
         if (t >= tiles || !ok) return;
         const uint32_t slot = (seq + 2 * t) % S::slots;
-        if (g == 0) landed(seq + 2 * t);
+        if (S::issuers == 2 || g == 0) landed(seq + 2 * t);
         if (ok && (t < with_sinks[g] || (t >= from[g] && t <= to[g]))) {
           if (t == (with_sinks[g] > 0 ? 0 : from[g])) {  // the first of the item
             ok = mbar_wait_warp(&q_full[g], nq[g] & 1);
@@ -484,13 +488,13 @@ __global__ void __launch_bounds__(THREADS, 1)
           if (t == last[g]) tc_commit_warp(&q_empty[g]);
           issued = true;
         }
-        if (g == 1) tc_commit_warp(&empty[slot]);
+        if (S::issuers == 2 || g == 1) tc_commit_warp(&empty[slot]);
       };
       auto product = [&](auto group, int t) {
         constexpr int g = decltype(group)::value;
         if (!ok) return;
         const uint32_t s = seq + 2 * t + 1, slot = s % S::slots;
-        if (g == 0) landed(s);
+        if (S::issuers == 2 || g == 0) landed(s);
         if (ok && (t < with_sinks[g] || (t >= from[g] && t <= to[g]))) {
           if (t < whole_from[g] || t > whole_to[g]) ok = mbar_wait_warp(&v_ready[slot], (s / S::slots) & 1);
           ok = ok && mbar_wait_warp(&p_full[g], np[g] & 1);
@@ -506,24 +510,38 @@ __global__ void __launch_bounds__(THREADS, 1)
           begun[g] = true;
           if (t == last[g]) tc_commit_warp(&o_full[g]);
         }
-        if (g == 1) tc_commit_warp(&empty[slot]);
+        if (S::issuers == 2 || g == 1) tc_commit_warp(&empty[slot]);
       };
       const std::integral_constant<int, 0> g0;
       const std::integral_constant<int, 1> g1;
-      scores(g0, 0);
-      scores(g1, 0);
-      for (int t = 0; t < tiles && ok; ++t) {
-        product(g0, t);
-        scores(g0, t + 1);
-        product(g1, t);
-        scores(g1, t + 1);
+      if constexpr (S::issuers == 2) {
+        auto run = [&](auto g) {
+          scores(g, 0);
+          for (int t = 0; t < tiles && ok; ++t) {
+            product(g, t);
+            scores(g, t + 1);
+          }
+        };
+        if (warp == 1)
+          run(g0);
+        else
+          run(g1);
+      } else {
+        scores(g0, 0);
+        scores(g1, 0);
+        for (int t = 0; t < tiles && ok; ++t) {
+          product(g0, t);
+          scores(g0, t + 1);
+          product(g1, t);
+          scores(g1, t + 1);
+        }
       }
       seq += 2 * tiles;
     }
     if (!ok && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
     if (issued) {
-      tc_commit_warp(drain);
-      mbar_wait_warp(drain, 0);
+      tc_commit_warp(&drain[warp - 1]);
+      mbar_wait_warp(&drain[warp - 1], 0);
     }
   } else if (warp < 4) {
     // ------------------------------------------------------------ a look through the V tiles with masks
@@ -537,7 +555,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         ok = mbar_wait_warp(&full[slot], (vs / S::slots) & 1);
         if (!ok) break;
         const bool masked = (it.needs(0, t) && !it.whole(0, t)) || (it.needs(1, t) && !it.whole(1, t));
-        if (masked) clear_bad_values<BF, DP>(ring + slot * S::tile, it.width(t), (warp - 2) * 32 + lane, n, &bad_seq[n & 7]);
+        if (masked) clear_bad_values<BF, DP, 32 * S::lookers>(ring + slot * S::tile, it.width(t), (warp - 4 + S::lookers) * 32 + lane, n, &bad_seq[n & 7]);
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(&v_ready[slot]);
@@ -681,6 +699,10 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
             for (int j = 0; j < 32; ++j) o[j] = 0u;
           }
+          if (c == 0) {  // the staging's last store has read it
+            if (elect_one()) bulk_wait_read<0>();
+            __syncwarp();
+          }
           // 16-byte pieces of a 128-byte row, so placed that writing a column and reading a row are without conflicts
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
@@ -701,7 +723,6 @@ __global__ void __launch_bounds__(THREADS, 1)
           if (elect_one()) {
             tma_store_3d(&tmO, stage, c0, it.head0, it.q0 + first + (warp & 3) * a.box_q);
             bulk_commit();
-            bulk_wait_read<0>();
           }
         } else {
           __syncwarp();
