@@ -42,6 +42,9 @@ struct Tile {
   static constexpr int tm = PAIR ? 2 * BM : BM;
   static constexpr int cols = BN / 2;  // of an epilogue warp
   static constexpr int accs = BN == 256 ? 2 : 4;  // accumulators
+  // Column halves of an accumulator, each with its own MMAs and barriers (256 columns: a half is read out while
+  // the other's products run)
+  static constexpr int halves = BN == 256 ? 2 : 1, half = BN / halves;
 };
 
 struct Args {
@@ -188,8 +191,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint64_t* full = reinterpret_cast<uint64_t*>(sbias + EPI_WARPS * 32);
   uint64_t* empty = full + MAX_STAGES;
   uint64_t* tfull = empty + MAX_STAGES;  // [accumulator]
-  uint64_t* tempty = tfull + T::accs;
-  uint64_t* drain = tempty + T::accs;
+  uint64_t* tempty = tfull + T::accs * T::halves;
+  uint64_t* drain = tempty + T::accs * T::halves;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
 
   const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
@@ -201,9 +204,9 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_init(&full[i], 1);
       mbar_init(&empty[i], 1);
     }
-    for (int i = 0; i < T::accs; ++i) {
+    for (int i = 0; i < T::accs * T::halves; ++i) {
       mbar_init(&tfull[i], 1);
-      mbar_init(&tempty[i], (PAIR ? 2 : 1) * EPI_WARPS);
+      mbar_init(&tempty[i], (PAIR ? 2 : 1) * EPI_WARPS / T::halves);
     }
     mbar_init(drain, 1);
     fence_barrier_init();
@@ -239,7 +242,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       uint32_t seq = 0;
       bool ok = true;
       for (int t = t_start; t < tiles && ok; t += t_stride) {
-        const int m0 = t / nt * T::tm + rank * BM, n0 = t % nt * BN + rank * (BN / 2);
+        const int m0 = t / nt * T::tm + rank * BM, n0 = t % nt * BN + rank * (T::half / 2);
         for (int kb = 0; kb < nkb; ++kb, ++seq) {
           const uint32_t s = seq % S;
           ok = mbar_wait(&empty[s], ((seq / S) & 1) ^ 1);
@@ -248,7 +251,8 @@ __global__ void __launch_bounds__(THREADS, 1)
             const uint32_t lead = cluster_map(smem_addr(&full[s]), 0);
             if (rank == 0) mbar_expect_tx(&full[s], 2 * T::stage);
             tma_load_2d_pair(sA + s * A_STAGE, &tmA, lead, kb * BK, m0);
-            tma_load_2d_pair(sB + s * T::b_stage, &tmB, lead, kb * BK, n0);
+            for (int h = 0; h < T::halves; ++h)  // (each half's columns from both CTAs)
+              tma_load_2d_pair(sB + s * T::b_stage + h * (T::b_stage / T::halves), &tmB, lead, kb * BK, n0 + h * T::half);
           } else {
             mbar_expect_tx(&full[s], T::stage);
             tma_load_2d(sA + s * A_STAGE, &tmA, &full[s], kb * BK, m0);
@@ -264,31 +268,39 @@ __global__ void __launch_bounds__(THREADS, 1)
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer
     if (rank == 0) {
-      const uint32_t idesc = idesc_e4m3_f32(T::tm, BN);
+      const uint32_t idesc = idesc_e4m3_f32(T::tm, T::half);
       uint32_t seq = 0;
       bool ok = true;
       for (int t = t_start; t < tiles && ok; t += t_stride)
         for (int kb = 0; kb < nkb; ++kb, ++seq) {
           const uint32_t s = seq % S, acc = seq % T::accs;
-          ok = mbar_wait_warp(&tempty[acc], ((seq / T::accs) & 1) ^ 1) && mbar_wait_warp(&full[s], (seq / S) & 1);
+          ok = mbar_wait_warp(&full[s], (seq / S) & 1);
           if (!ok) break;
-          tc_fence_after();
-          const uint64_t da = sdesc_sw128(smem_addr(sA + s * A_STAGE), 16, 1024);
-          const uint64_t db = sdesc_sw128(smem_addr(sB + s * T::b_stage), 16, 1024);
+          const uint32_t a_lo = sdesc_lo(smem_addr(sA + s * A_STAGE), 16), b_lo = sdesc_lo(smem_addr(sB + s * T::b_stage), 16);
 #pragma unroll
-          for (int k = 0; k < BK / 32; ++k) {
+          for (int h = 0; h < T::halves; ++h) {
+            const uint32_t i = acc * T::halves + h;
+            ok = mbar_wait_warp(&tempty[i], ((seq / T::accs) & 1) ^ 1);
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll
+            for (int k = 0; k < BK / 32; ++k) {
+              const uint32_t b = b_lo + h * (T::b_stage / T::halves / 16) + 2 * k;
+              if constexpr (PAIR)
+                tc_mma_f8_pair_warp_lo(tmem + i * T::half, a_lo + 2 * k, b, sdesc_sw128_hi(1024), idesc, k != 0);
+              else
+                tc_mma_f8_warp_lo(tmem + i * T::half, a_lo + 2 * k, b, sdesc_sw128_hi(1024), idesc, k != 0);
+            }
             if constexpr (PAIR)
-              tc_mma_f8_pair_warp(tmem + acc * BN, da + 2 * k, db + 2 * k, idesc, k != 0);
+              tc_commit_pair_multicast_warp(&tfull[i], 0x3);
             else
-              tc_mma_f8_warp(tmem + acc * BN, da + 2 * k, db + 2 * k, idesc, k != 0);
+              tc_commit_warp(&tfull[i]);
           }
-          if constexpr (PAIR) {
+          if (!ok) break;
+          if constexpr (PAIR)
             tc_commit_pair_multicast_warp(&empty[s], 0x3);
-            tc_commit_pair_multicast_warp(&tfull[acc], 0x3);
-          } else {
+          else
             tc_commit_warp(&empty[s]);
-            tc_commit_warp(&tfull[acc]);
-          }
         }
       if (!ok && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
       if (seq > 0) {
@@ -332,9 +344,9 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (int j = 0; j < C / 2; ++j) acc[j] = make_float2(0.0f, 0.0f);
       float s0 = sa0 * sw0, s1 = sa1 * sw1;  // of this block and the next; the one after is on its way
       for (int kb = 0; kb < nkb; ++kb, ++seq) {
-        const uint32_t p = seq % T::accs;
+        const uint32_t p = seq % T::accs, pb = T::halves == 2 ? 2 * p + h : p;  // accumulator, and its barrier
         const float sa = kb + 2 < nkb ? __ldg(as + (kb + 2) * a.lds) : 0.0f, sw = kb + 2 < nkb ? __ldg(ws + kb + 2) : 0.0f;
-        ok = __all_sync(0xffffffffu, mbar_wait(&tfull[p], (seq / T::accs) & 1));
+        ok = __all_sync(0xffffffffu, mbar_wait(&tfull[pb], (seq / T::accs) & 1));
         if (!ok) break;
         tc_fence_after();
         const float2 s2 = make_float2(s0, s0);
@@ -348,9 +360,9 @@ __global__ void __launch_bounds__(THREADS, 1)
           __syncwarp();
           if (lane == 0) {
             if constexpr (PAIR)
-              mbar_arrive_cluster(cluster_map(smem_addr(&tempty[p]), 0));
+              mbar_arrive_cluster(cluster_map(smem_addr(&tempty[pb]), 0));
             else
-              mbar_arrive(&tempty[p]);
+              mbar_arrive(&tempty[pb]);
           }
         };
         uint32_t v[2][32];
@@ -517,7 +529,7 @@ elasto_status gemm_fp8_launch(const Fp8Gemm& g, cudaStream_t s) {
   const bool narrow = bn == 64 && size == 2;
   const uint32_t ob[2] = {narrow ? 32u : 128u / size, 32};
   if ((a.tma && !encode_tmap_plain(&tc, g.out, 2, od, os, ob, size == 4, !narrow)) ||
-      !encode_tmap_8(&ta, g.A, g.K, g.M, g.lda, BM) || !encode_tmap_8(&tb, g.W, g.K, g.N, g.ldw, bn == 256 ? 128 : bn)) {
+      !encode_tmap_8(&ta, g.A, g.K, g.M, g.lda, BM) || !encode_tmap_8(&tb, g.W, g.K, g.N, g.ldw, bn == 256 ? 64 : bn)) {
     set_error("elasto_op_gemm_fp8: cuTensorMapEncodeTiled failed (alignment or size)");
     return ELASTO_ERR_UNSUPPORTED;
   }

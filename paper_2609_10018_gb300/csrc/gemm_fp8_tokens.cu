@@ -119,10 +119,9 @@ __global__ void __launch_bounds__(Shape<NT>::threads)
       ok = mbar_wait_warp(&tempty[p], ((i / T::accs) & 1) ^ 1) && mbar_wait_warp(&full[s], (i / S) & 1);
       if (!ok) break;
       tc_fence_after();
-      const uint64_t dw = sdesc_sw128(smem_addr(smem + s * T::stage), 16, 1024);
-      const uint64_t da = sdesc_sw128(smem_addr(smem + s * T::stage + W_STAGE), 16, 1024);
+      const uint32_t w_lo = sdesc_lo(smem_addr(smem + s * T::stage), 16), a_lo = sdesc_lo(smem_addr(smem + s * T::stage + W_STAGE), 16);
 #pragma unroll
-      for (int k = 0; k < BK / 32; ++k) tc_mma_f8_warp(tmem + p * NT, dw + 2 * k, da + 2 * k, idesc, k != 0);
+      for (int k = 0; k < BK / 32; ++k) tc_mma_f8_warp_lo(tmem + p * NT, w_lo + 2 * k, a_lo + 2 * k, sdesc_sw128_hi(1024), idesc, k != 0);
       tc_commit_warp(&empty[s]);
       tc_commit_warp(&tfull[p]);
     }
