@@ -29,6 +29,7 @@
 // Items differ in length (ragged sequences, causal rows, class tokens that see
 // everything), so the grid has a block for each and the blocks that run take over
 // those not yet started (cluster launch control), the longest first.
+#include <algorithm>
 #include <type_traits>
 
 #include "common.h"
@@ -48,6 +49,7 @@ constexpr int SMEM_LIMIT = 232448;
 constexpr int TAIL = 768;             // barriers, items
 constexpr int STAGING = 8 * 32 * 128;  // 32 rows of 64 channels of out for each softmax warp
 constexpr int TMEM_COLS = 512, O_COL = 2 * KT;  // S (and P over it) of both groups, then O
+constexpr int MAX_SPLIT = 8;
 constexpr float kLazy = 8.0f;  // log2 of how far a row's maximum may grow before O is rescaled
 
 template <int DP>
@@ -80,6 +82,7 @@ struct Args {
   int tiles;          // tiles (groups at work) of an item: 1 or 2
   int qtiles;         // items along the longest sequence's queries
   int items;
+  int split;          // CTAs (a cluster) that share an item's key tiles, one tile of rows each
   Divisor per_q, by_nsub, by_heads_kv;  // items of a step along the queries; the axes of one
   int* status;
 };
@@ -117,10 +120,20 @@ struct Item {
   int with_sinks;               // tiles [0, with_sinks) hold sinks
   int from[2], to[2];           // and tiles [from, to] the keys that the group's rows see besides (none: to < from)
   int whole_from[2], whole_to[2];  // every row of the group sees every key of tiles [whole_from, whole_to]
+  int begin, end;               // the CTA's tiles: [begin, end), all of them where a CTA has an item to itself
 
   __device__ __forceinline__ int base(int t) const { return t < sink_tiles ? t * KT : base0 + (t - sink_tiles) * KT; }
   __device__ __forceinline__ int width(int t) const {
     return t == tiles - 1 ? last_width : t < sink_tiles ? sink_width : KT;
+  }
+  // The first and the last of the CTA's tiles that the group needs (none: last < first).
+  __device__ __forceinline__ int first_tile(int g) const {
+    const int f = of(from, g);
+    return of(to, g) < f ? end : begin < with_sinks ? begin : max(f, begin);
+  }
+  __device__ __forceinline__ int last_tile(int g) const {
+    const int f = of(from, g), band = min(of(to, g), end - 1), sinks = min(with_sinks, end) - 1;
+    return of(to, g) < f ? -1 : band >= max(f, begin) ? max(band, sinks) : sinks >= begin ? sinks : -1;
   }
   // Some row of the group sees a key of the tile.
   __device__ __forceinline__ bool needs(int g, int t) const {
@@ -132,7 +145,7 @@ struct Item {
 
 __device__ __forceinline__ int tile_width(int keys) { return keys <= 32 ? 32 : keys <= 64 ? 64 : KT; }
 
-__device__ __forceinline__ Item make_item(const Args& a, int id) {
+__device__ __forceinline__ Item make_item(const Args& a, int id, int rank) {
   Item it;
   int q = static_cast<int>(a.per_q.quotient(id)), r = id - q * static_cast<int>(a.per_q.d);
   if (a.causal) q = a.qtiles - 1 - q;  // the longest rows of keys first
@@ -186,6 +199,7 @@ __device__ __forceinline__ Item make_item(const Args& a, int id) {
     it.whole_from[g] = it.sink_tiles + max(0, (pmax - a.window - low + KT - 1) >> 7);
     it.whole_to[g] = it.sink_tiles + ((until + 1 - low) >> 7) - 1;
   }
+  it.begin = it.tiles * rank / a.split, it.end = it.tiles * (rank + 1) / a.split;
   return it;
 }
 
@@ -269,11 +283,11 @@ __device__ __forceinline__ void clear_bad_values(uint8_t* v, int rows, int r, in
 }
 
 // Values that are not finite were left out of the products: adds those that a row sees to its result, for
-// the 32 rows from row0 on (rare, so by the warp row by row and key by key).
+// rows [row0, row1) (rare, so by the warp row by row and key by key).
 template <bool BF>
-__device__ __noinline__ void add_bad_values(const Args& a, const Item& it, int g, int row0, int lane) {
+__device__ __noinline__ void add_bad_values(const Args& a, const Item& it, int g, int row0, int row1, int lane) {
   __syncwarp();
-  for (int r = row0; r < row0 + 32; ++r) {
+  for (int r = row0; r < row1; ++r) {
     const int q = r * a.by_hg >> 16, h = r - q * a.hg, qi = of(it.first, g) + q, p = it.nk - it.nq + qi;
     if (q >= a.qpt || qi > of(it.last, g) || h >= it.nheads || p < 0) continue;
     uint16_t* const out = static_cast<uint16_t*>(a.out) + static_cast<long long>(it.q0 + qi) * a.out_row +
@@ -297,7 +311,63 @@ __device__ __noinline__ void add_bad_values(const Args& a, const Item& it, int g
   __syncwarp();
 }
 
+__device__ __forceinline__ float4 cluster_load4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ float2 cluster_load2(uint32_t addr) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr));
+  return v;
+}
+
+// The rows of a split item from the cluster's parts, in rank order, an equal share of the rows by each CTA (256 threads).
 template <bool BF, int DP>
+__device__ __forceinline__ void join(const Args& a, const Item& it, int rank, int thread, const float* part, const float2* stat,
+                                     const int* bad_seq) {
+  const int share = (QT + a.split - 1) / a.split, row0 = rank * share, row1 = min(row0 + share, QT);
+  for (int e = thread; e < (row1 - row0) * (DP / 4); e += 256) {
+    const int r = row0 + e / (DP / 4), piece = e % (DP / 4);
+    const int q = r * a.by_hg >> 16, h = r - q * a.hg, qi = it.first[0] + q;
+    if (q >= a.qpt || qi > it.last[0] || h >= it.nheads || 4 * piece >= a.head_dim) continue;
+    const uint32_t ms = smem_addr(stat + r), os = smem_addr(part + r * DP + ((piece ^ (r & 7)) << 2));
+    float2 st[MAX_SPLIT];
+    float4 o[MAX_SPLIT];
+    float top = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < MAX_SPLIT; ++k)
+      if (k < a.split) st[k] = cluster_load2(cluster_map(ms, k)), o[k] = cluster_load4(cluster_map(os, k));
+#pragma unroll
+    for (int k = 0; k < MAX_SPLIT; ++k)
+      if (k < a.split) top = fmaxf(top, st[k].x);
+    float total = 0.0f, y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < MAX_SPLIT; ++k)
+      if (k < a.split) {
+        // (a part without a finite score has sums of zeros, or NaN that must stay)
+        const float f = st[k].x == -INFINITY ? 1.0f : ex2_approx((st[k].x - top) * a.scale_log2);
+        total += st[k].y * f;
+        y[0] += o[k].x * f, y[1] += o[k].y * f, y[2] += o[k].z * f, y[3] += o[k].w * f;
+      }
+    const float inv = it.nk - it.nq + qi >= 0 ? 1.0f / total : 0.0f;
+    uint32_t* const out = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + static_cast<long long>(it.q0 + qi) * a.out_row +
+                                                      static_cast<long long>(it.head0 + h) * a.out_head + 4 * piece);
+    *reinterpret_cast<uint2*>(out) = make_uint2(pack16<BF>(y[0] * inv, y[1] * inv), pack16<BF>(y[2] * inv, y[3] * inv));
+  }
+  bool bad = false;
+  for (int k = 0; k < a.split; ++k) {
+    int v;
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(cluster_map(smem_addr(bad_seq), k)));
+    bad |= v == 0;
+  }
+  if (!bad) return;
+  named_bar_sync(1, 256);
+  const Item copy = it;
+  for (int r = row0 + (thread >> 5); r < row1; r += 8) add_bad_values<BF>(a, copy, 0, r, r + 1, thread & 31);
+}
+
+template <bool BF, int DP, bool SPLIT>
 __global__ void __launch_bounds__(THREADS, 1)
     window_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                             const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmK32,
@@ -330,6 +400,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   volatile int* bad_seq = reinterpret_cast<int*>(tmem_slot + 1);  // [8] item (by its number in this CTA) with bad values
 
   const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const int rank = SPLIT ? static_cast<int>(blockIdx.x) % a.split : 0;
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::slots; ++i) {
       mbar_init(&full[i], 1);
@@ -382,19 +453,19 @@ __global__ void __launch_bounds__(THREADS, 1)
       tma_prefetch_desc(&tmV);
       uint32_t seq = 0, nq[2] = {0, 0};  // K/V tiles and Q tiles issued
       bool ok = true;
-      int id = blockIdx.x;
+      int id = SPLIT ? static_cast<int>(blockIdx.x) / a.split : static_cast<int>(blockIdx.x);
       for (uint32_t n = 0; ok; ++n) {
         ok = mbar_wait(&item_empty[n & 1], ((n >> 1) & 1) ^ 1);
         if (!ok) break;
         Item it;
         it.tiles = -1;
-        if (id >= 0) it = make_item(a, id);
+        if (id >= 0) it = make_item(a, id, rank);
         items[n & 1] = it;
         mbar_arrive(&item_full[n & 1]);
         if (id < 0) break;
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-          if (!ok || it.to[g] < it.from[g]) continue;
+          if (!ok || it.last_tile(g) < it.first_tile(g)) continue;
           ok = mbar_wait(&q_empty[g], (nq[g] & 1) ^ 1);
           if (!ok) continue;
           mbar_expect_tx(&q_full[g], S::halves * a.hg * a.qpt * 128);
@@ -403,7 +474,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           ++nq[g];
         }
         const int batch = a.kv_start ? 0 : it.b;
-        for (int t = 0; t < it.tiles && ok; ++t) {
+        for (int t = SPLIT ? it.begin : 0; t < (SPLIT ? it.end : it.tiles) && ok; ++t) {
           const int width = it.width(t), row = it.k0 + it.base(t);
           for (int kv = 0; kv < 2 && ok; ++kv, ++seq) {
             const uint32_t slot = seq % S::slots;
@@ -422,6 +493,10 @@ __global__ void __launch_bounds__(THREADS, 1)
           }
         }
         if (!ok) break;
+        if (SPLIT) {
+          id = -1;
+          continue;
+        }
         // the next item, asked for once this one's loads are under way
         fence_async_smem();  // (the last answer has been read)
         mbar_expect_tx(answered, 16);
@@ -452,14 +527,16 @@ __global__ void __launch_bounds__(THREADS, 1)
     for (uint32_t n = 0; ok && warp_uniform(take(n, it)); ++n) {
       const int tiles = warp_uniform(it.tiles), sink_tiles = warp_uniform(it.sink_tiles);
       const int sink_width = warp_uniform(it.sink_width), last_width = warp_uniform(it.last_width);
-      int from[2], to[2], with_sinks[2], whole_from[2], whole_to[2], last[2];
+      const int begin = SPLIT ? warp_uniform(it.begin) : 0, end = SPLIT ? warp_uniform(it.end) : tiles;
+      int from[2], to[2], with_sinks[2], whole_from[2], whole_to[2], first[2], last[2];
       bool begun[2] = {false, false};
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
         from[g] = warp_uniform(it.from[g]), to[g] = warp_uniform(it.to[g]);
         with_sinks[g] = warp_uniform(to[g] < from[g] ? 0 : it.with_sinks);
         whole_from[g] = warp_uniform(it.whole_from[g]), whole_to[g] = warp_uniform(it.whole_to[g]);
-        last[g] = max(to[g], with_sinks[g] - 1);
+        first[g] = SPLIT ? warp_uniform(it.first_tile(g)) : with_sinks[g] > 0 ? 0 : from[g];
+        last[g] = SPLIT ? warp_uniform(it.last_tile(g)) : max(to[g], with_sinks[g] - 1);
       }
       auto width = [&](int t) { return t == tiles - 1 ? last_width : t < sink_tiles ? sink_width : KT; };
       auto landed = [&](uint32_t s) {
@@ -468,11 +545,11 @@ __global__ void __launch_bounds__(THREADS, 1)
       };
       auto scores = [&](auto group, int t) {
         constexpr int g = decltype(group)::value;
-        if (t >= tiles || !ok) return;
-        const uint32_t slot = (seq + 2 * t) % S::slots;
-        if (S::issuers == 2 || g == 0) landed(seq + 2 * t);
+        if (t >= end || !ok) return;
+        const uint32_t slot = (seq + 2 * (t - begin)) % S::slots;
+        if (S::issuers == 2 || g == 0) landed(seq + 2 * (t - begin));
         if (ok && (t < with_sinks[g] || (t >= from[g] && t <= to[g]))) {
-          if (t == (with_sinks[g] > 0 ? 0 : from[g])) {  // the first of the item
+          if (t == first[g]) {
             ok = mbar_wait_warp(&q_full[g], nq[g] & 1);
             if (!ok) return;
             ++nq[g];
@@ -493,7 +570,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       auto product = [&](auto group, int t) {
         constexpr int g = decltype(group)::value;
         if (!ok) return;
-        const uint32_t s = seq + 2 * t + 1, slot = s % S::slots;
+        const uint32_t s = seq + 2 * (t - begin) + 1, slot = s % S::slots;
         if (S::issuers == 2 || g == 0) landed(s);
         if (ok && (t < with_sinks[g] || (t >= from[g] && t <= to[g]))) {
           if (t < whole_from[g] || t > whole_to[g]) ok = mbar_wait_warp(&v_ready[slot], (s / S::slots) & 1);
@@ -516,8 +593,8 @@ __global__ void __launch_bounds__(THREADS, 1)
       const std::integral_constant<int, 1> g1;
       if constexpr (S::issuers == 2) {
         auto run = [&](auto g) {
-          scores(g, 0);
-          for (int t = 0; t < tiles && ok; ++t) {
+          scores(g, begin);
+          for (int t = begin; t < end && ok; ++t) {
             product(g, t);
             scores(g, t + 1);
           }
@@ -527,16 +604,16 @@ __global__ void __launch_bounds__(THREADS, 1)
         else
           run(g1);
       } else {
-        scores(g0, 0);
-        scores(g1, 0);
-        for (int t = 0; t < tiles && ok; ++t) {
+        scores(g0, begin);
+        scores(g1, begin);
+        for (int t = begin; t < end && ok; ++t) {
           product(g0, t);
           scores(g0, t + 1);
           product(g1, t);
           scores(g1, t + 1);
         }
       }
-      seq += 2 * tiles;
+      seq += 2 * (end - begin);
     }
     if (!ok && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
     if (issued) {
@@ -549,9 +626,10 @@ __global__ void __launch_bounds__(THREADS, 1)
     bool ok = true;
     Item it;
     for (uint32_t n = 0; ok && take(n, it); ++n) {
-      for (int t = 0; t < it.tiles && ok; ++t) {
+      const int begin = SPLIT ? it.begin : 0, end = SPLIT ? it.end : it.tiles;
+      for (int t = begin; t < end && ok; ++t) {
         // (every V tile is waited for and given back, so that no slot is ever two tiles ahead)
-        const uint32_t vs = seq + 2 * t + 1, slot = vs % S::slots;
+        const uint32_t vs = seq + 2 * (t - begin) + 1, slot = vs % S::slots;
         ok = mbar_wait_warp(&full[slot], (vs / S::slots) & 1);
         if (!ok) break;
         const bool masked = (it.needs(0, t) && !it.whole(0, t)) || (it.needs(1, t) && !it.whole(1, t));
@@ -562,7 +640,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           mbar_arrive(&empty[slot]);
         }
       }
-      seq += 2 * it.tiles;
+      seq += 2 * (end - begin);
     }
     if (!ok && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
   } else {
@@ -671,7 +749,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         mbar_arrive(&p_full[g]);
         return true;
       };
-      for (int t = 0; t < it.tiles && ok; ++t) {
+      for (int t = SPLIT ? it.begin : 0; t < (SPLIT ? it.end : it.tiles) && ok; ++t) {
         if (it.needs(g, t)) ok = it.whole(g, t) ? tile(std::false_type(), t) : tile(std::true_type(), t);
       }
       // ------------------------------------------------------------ result rows
@@ -682,6 +760,26 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
       if (!ok) break;
       const bool sees = mine && p >= 0 && it.nk > 0;
+      if constexpr (SPLIT) {
+        // this CTA's maximum, sum and O of each row, for the cluster (the ring is done with: O is complete)
+        float* const part = reinterpret_cast<float*>(ring) + r * DP;
+        reinterpret_cast<float2*>(staging)[r] = make_float2(any ? m : -INFINITY, sum);
+#pragma unroll 1
+        for (int c = 0; c < DP; c += 32) {
+          uint32_t o[32];
+          if (any) {
+            tmem_ld_32x32b_x32(o_tm + c, o);
+            tmem_ld_wait();
+          } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = 0u;
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j)  // (16-byte pieces swizzled by the row: no bank conflicts)
+            *reinterpret_cast<uint4*>(part + ((((c >> 2) + j) ^ (r & 7)) << 2)) = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+        }
+        continue;
+      }
       // the warp's 32 rows are whole queries of all the tile's heads
       const bool boxed = a.box_q > 0 && first + ((warp & 3) + 1) * a.box_q - 1 <= last && it.nheads == a.hg;
       const float inv = sees ? 1.0f / sum : 0.0f;  // (O of a row that sees nothing is 0)
@@ -744,12 +842,23 @@ __global__ void __launch_bounds__(THREADS, 1)
           __syncwarp();
         }
         const Item copy = it;  // (in memory, which `it` itself is not)
-        add_bad_values<BF>(a, copy, g, (warp & 3) * 32, lane);
+        add_bad_values<BF>(a, copy, g, (warp & 3) * 32, (warp & 3) * 32 + 32, lane);
       }
       tc_fence_before();
     }
     if (elect_one()) bulk_wait_all();
     if (!ok && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
+    if constexpr (SPLIT) {
+      __syncwarp();
+      cluster_sync_all();
+      join<BF, DP>(a, items[0], rank, threadIdx.x - 128, reinterpret_cast<const float*>(ring),
+                   reinterpret_cast<const float2*>(staging), const_cast<const int*>(bad_seq));
+    }
+  }
+  if constexpr (SPLIT) {
+    __syncwarp();
+    if (warp < 4) cluster_sync_all();
+    cluster_sync_all();  // the peers have read this CTA's results
   }
   __syncthreads();
   if (warp == 1) {
@@ -772,8 +881,24 @@ bool map_of(CUtensorMap* tm, const void* p, bool bf, const elasto_window_attenti
 
 template <bool BF, int DP>
 cudaError_t launch(const CUtensorMap (&tm)[6], const Args& a, cudaStream_t s) {
-  return launch_pdl(window_attention_kernel<BF, DP>, dim3(a.items), dim3(THREADS), Shape<DP>::smem, s, tm[0], tm[1], tm[2],
-                    tm[3], tm[4], tm[5], a);
+  if (a.split == 1)
+    return launch_pdl(window_attention_kernel<BF, DP, false>, dim3(a.items), dim3(THREADS), Shape<DP>::smem, s, tm[0], tm[1], tm[2],
+                      tm[3], tm[4], tm[5], a);
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // see launch_pdl
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = a.split;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.gridDim = dim3(a.items * a.split);
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = Shape<DP>::smem;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, window_attention_kernel<BF, DP, true>, tm[0], tm[1], tm[2], tm[3], tm[4], tm[5], a);
 }
 
 }  // namespace
@@ -783,20 +908,22 @@ cudaError_t window_attention_init_attributes() {
   auto set = [&](auto* f, int bytes) {
     if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   };
-  set(window_attention_kernel<true, 64>, Shape<64>::smem);
-  set(window_attention_kernel<false, 64>, Shape<64>::smem);
-  set(window_attention_kernel<true, 128>, Shape<128>::smem);
-  set(window_attention_kernel<false, 128>, Shape<128>::smem);
   // the register split adds up only if the kernels were built with the launch's count
   auto check = [&](auto* f) {
     cudaFuncAttributes at{};
     if (e == cudaSuccess) e = cudaFuncGetAttributes(&at, f);
     if (e == cudaSuccess && at.numRegs != REGS) e = cudaErrorInvalidConfiguration;
   };
-  check(window_attention_kernel<true, 64>);
-  check(window_attention_kernel<false, 64>);
-  check(window_attention_kernel<true, 128>);
-  check(window_attention_kernel<false, 128>);
+  auto both = [&](auto* one, auto* split, int bytes) {
+    set(one, bytes);
+    set(split, bytes);
+    check(one);
+    check(split);
+  };
+  both(window_attention_kernel<true, 64, false>, window_attention_kernel<true, 64, true>, Shape<64>::smem);
+  both(window_attention_kernel<false, 64, false>, window_attention_kernel<false, 64, true>, Shape<64>::smem);
+  both(window_attention_kernel<true, 128, false>, window_attention_kernel<true, 128, true>, Shape<128>::smem);
+  both(window_attention_kernel<false, 128, false>, window_attention_kernel<false, 128, true>, Shape<128>::smem);
   return e;
 }
 
@@ -827,6 +954,12 @@ elasto_status window_attention_launch(const elasto_window_attention_args& u, int
     return ELASTO_ERR_UNSUPPORTED;
   }
   a.qtiles = static_cast<int>(qtiles);
+  // Few queries against many keys: the key tiles of an item shared out over a cluster, two at least for each CTA.
+  long long keys = a.max_keys;  // of an item at most
+  if (a.causal || a.sinks == 0) keys = std::min(keys, (a.causal ? 1LL : 2LL) * a.window + a.qpt + a.sinks);
+  const long long key_tiles = (keys + KT - 1) / KT;
+  a.split = 1;
+  if (a.tiles == 1) a.split = static_cast<int>(std::max(1LL, std::min({static_cast<long long>(MAX_SPLIT), num_sms() / (qtiles * per), key_tiles / 2})));
   a.items = static_cast<int>(qtiles * per);
   a.per_q = Divisor(static_cast<unsigned>(per)), a.by_nsub = Divisor(a.nsub), a.by_heads_kv = Divisor(a.heads_kv);
   const bool bf = u.dtype == ELASTO_BF16;

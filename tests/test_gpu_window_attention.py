@@ -123,6 +123,24 @@ def test_chunks_behind_a_cache(nq, heads, heads_kv, d):
     Case([nq], [400], heads, heads_kv, d, packed=False).check()
 
 
+@pytest.mark.parametrize("nq,nk,heads,heads_kv,d", [(2, 5000, 1, 1, 64), (33, 3001, 8, 2, 128), (7, 2049, 6, 1, 96), (128, 4100, 2, 2, 64),
+                                                    (300, 1300, 2, 1, 128), (16, 1024, 24, 1, 40)])
+def test_few_queries_many_keys(nq, nk, heads, heads_kv, d):
+    """Items that several CTAs share."""
+    Case([nq], [nk], heads, heads_kv, d, packed=False, room=3, tail=2).check()
+    Case([nq, max(1, nq // 2), 1], [nk, nk // 3, 1], heads, heads_kv, d, window=nk // 2, sinks=70, packed=False).check()
+    Case([nq, 0, nq], [nk - 5, 9, nq // 2], heads, heads_kv, d, window=900, sinks=3, packed=False, dtype=torch.float16).check()
+    Case([nq], [nk], heads, heads_kv, d, causal=False, window=700, sinks=0).check()
+
+
+@pytest.mark.parametrize("at", [0, 700, 1999])
+def test_bad_value_with_few_queries(at):
+    c = Case([20], [2000], 2, 1, 64, window=1400, sinks=1, packed=False)
+    c.v[0, at, 0, 5], c.v[0, 650, 0, 7] = INF, -INF
+    c.v[0, 1990, 0, 9] = NAN
+    c.check()
+
+
 @pytest.mark.parametrize("nk", [1, 2, 15, 16, 17, 63, 64, 65, 128, 200, 513, 1000, 2047])
 @pytest.mark.parametrize("window,sinks", [(-1, 0), (0, 0), (0, 3), (63, 4), (500, 0), (100, 300)])
 def test_single_tokens(nk, window, sinks):
