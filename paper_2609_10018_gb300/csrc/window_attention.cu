@@ -30,6 +30,7 @@
 // everything), so the grid has a block for each and the blocks that run take over
 // those not yet started (cluster launch control), the longest first.
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "common.h"
@@ -901,6 +902,34 @@ cudaError_t launch(const CUtensorMap (&tm)[6], const Args& a, cudaStream_t s) {
   return cudaLaunchKernelEx(&cfg, window_attention_kernel<BF, DP, true>, tm[0], tm[1], tm[2], tm[3], tm[4], tm[5], a);
 }
 
+// Clusters of n CTAs of the split kernels that the current device runs at once (one CTA takes an SM; asked for
+// once a device and size).
+cudaError_t max_clusters(int n, int* clusters) {
+  static std::atomic<int> known[64][MAX_SPLIT + 1];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  *clusters = known[dev][n].load(std::memory_order_relaxed);
+  if (*clusters > 0) return cudaSuccess;
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = n;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.gridDim = dim3(n * (num_sms() / n));
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = Shape<128>::smem;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  e = cudaOccupancyMaxActiveClusters(clusters, window_attention_kernel<true, 128, true>, &cfg);
+  if (e != cudaSuccess) return e;
+  if (*clusters <= 0) return cudaErrorInvalidConfiguration;
+  known[dev][n].store(*clusters, std::memory_order_relaxed);
+  return cudaSuccess;
+}
+
 }  // namespace
 
 cudaError_t window_attention_init_attributes() {
@@ -958,8 +987,14 @@ elasto_status window_attention_launch(const elasto_window_attention_args& u, int
   long long keys = a.max_keys;  // of an item at most
   if (a.causal || a.sinks == 0) keys = std::min(keys, (a.causal ? 1LL : 2LL) * a.window + a.qpt + a.sinks);
   const long long key_tiles = (keys + KT - 1) / KT;
+  // (As many as run at once: 16 clusters of 8 do not, and took 30 us where 16 of 7 take 18.)
   a.split = 1;
-  if (a.tiles == 1) a.split = static_cast<int>(std::max(1LL, std::min({static_cast<long long>(MAX_SPLIT), num_sms() / (qtiles * per), key_tiles / 2})));
+  if (a.tiles == 1)
+    for (int n = static_cast<int>(std::min<long long>({MAX_SPLIT, num_sms() / (qtiles * per), key_tiles / 2})); n > 1 && a.split == 1; --n) {
+      int clusters = 0;
+      ELASTO_CUDA_TRY(max_clusters(n, &clusters));
+      if (qtiles * per <= clusters) a.split = n;
+    }
   a.items = static_cast<int>(qtiles * per);
   a.per_q = Divisor(static_cast<unsigned>(per)), a.by_nsub = Divisor(a.nsub), a.by_heads_kv = Divisor(a.heads_kv);
   const bool bf = u.dtype == ELASTO_BF16;
