@@ -129,7 +129,7 @@ elasto_status elasto_op_gemm_fp8(void* stream, const void* A, long long lda, con
  * of its mean square (plus eps), multiplied by the gain of its channel, and its
  * first rot_dim channels rotated by the row's position; all in fp32, rounded
  * once. Keys, and values unchanged, optionally go to the rows of a cache.
- *   y = x * rsqrt(mean(x^2) + eps) * gain
+ *   y = x * rsqrt(mean(x^2) + eps) * gain      (a head of zeros with eps 0: NaN)
  *   pair j of rot_dim / 2: channels (j, j + rot_dim / 2), or (2 j, 2 j + 1) if
  *   interleaved != 0, (a, b) -> (a c - b s, b c + a s), with c and s from row
  *   positions[r] of cos_sin: rot_dim / 2 cosines, then rot_dim / 2 sines.
@@ -183,14 +183,17 @@ elasto_status elasto_op_qk_norm_rope(void* stream, const elasto_qk_norm_rope_arg
  * head_dim: a multiple of 8 up to 128. Softmax statistics and sums in fp32; the
  * probabilities are rounded to the operand type for the product with v.
  * Queries: sequence b has the rows q_start[b] to q_start[b + 1] of q and out, at
- *   most max_queries; q_start NULL: max_queries rows each. q and out have q_rows rows.
+ *   most max_queries; q_start NULL: max_queries rows each. q and out have q_rows rows
+ *   (at most 2^30, as kv_rows).
  * Keys: packed, the rows kv_start[b] to kv_start[b + 1] of k and v, which have
  *   kv_rows rows; or (kv_start NULL) in a cache of kv_rows rows per sequence, k_batch
  *   and v_batch apart, the first kv_len[b] of them (kv_len NULL: max_keys). At most
  *   max_keys each; max_keys <= kv_rows.
  * Lengths on the device past these limits are cut to them; nothing is read or
  * written outside them. Rows of out that belong to no sequence are left as they were.
- * max_queries == 1 runs the single-token form.
+ * max_queries == 1 runs the single-token form; few queries against many keys, and single
+ * tokens, share the keys out over several SMs and join their results in a fixed order.
+ * *status_device is set to ELASTO_ERR_TIMEOUT if a device-side wait gives up.
  * Strides of q, k, v and out are multiples of 8, the data is 16-byte aligned.
  * out may not overlap the inputs. */
 typedef struct {

@@ -512,7 +512,7 @@ elasto_status gemm_fp8_launch(const Fp8Gemm& g, cudaStream_t s) {
     set_error("elasto_op_gemm_fp8: output too large");
     return ELASTO_ERR_UNSUPPORTED;
   }
-  const int nkb = (g.K + BK - 1) / BK;
+  const int nkb = static_cast<int>((g.K + BK - 1LL) / BK);
   int bn = 64;
   for (int n : {128, 256})
     if (tile_cost(g, nkb, n) < tile_cost(g, nkb, bn)) bn = n;

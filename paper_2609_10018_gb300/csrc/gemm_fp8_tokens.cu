@@ -299,7 +299,7 @@ double gemm_fp8_tokens_cost(const Fp8Gemm& g, int nkb) {
 }
 
 elasto_status gemm_fp8_tokens_launch(const Fp8Gemm& g, cudaStream_t s) {
-  const int nt = rows_of_tile(g.M), nkb = (g.K + BK - 1) / BK;
+  const int nt = rows_of_tile(g.M), nkb = static_cast<int>((g.K + BK - 1LL) / BK);
   const long long tiles = tiles_of(g, nt);
   const int cluster = cluster_of(tiles, nt, nkb);
   CUtensorMap tw, ta;

@@ -246,7 +246,7 @@ elasto_status elasto_op_window_attention(void* stream, const elasto_window_atten
     return refuse("elasto_op_window_attention: q or out (null, alignment or strides)");
   if (!tensor16(a.k, a.k_row, a.k_head) || !tensor16(a.v, a.v_row, a.v_head) || !strides8(a.k_batch, a.v_batch))
     return refuse("elasto_op_window_attention: k or v (null, alignment or strides)");
-  if (a.q_rows <= 0 || a.kv_rows <= 0 || a.q_rows > 0x7fffffffLL || a.kv_rows > 0x7fffffffLL || a.max_keys > a.kv_rows)
+  if (a.q_rows <= 0 || a.kv_rows <= 0 || a.q_rows > 1 << 30 || a.kv_rows > 1 << 30 || a.max_keys > a.kv_rows)
     return refuse("elasto_op_window_attention: q_rows or kv_rows");
   if (!a.q_start && static_cast<long long>(a.batch) * a.max_queries > a.q_rows)
     return refuse("elasto_op_window_attention: q_rows is less than batch * max_queries");

@@ -963,7 +963,7 @@ elasto_status window_attention_launch(const elasto_window_attention_args& u, int
   a.window = u.window < 0 || u.window > u.max_keys ? u.max_keys : u.window;
   a.sinks = u.sinks > u.max_keys ? u.max_keys : u.sinks;
   a.scale_log2 = u.scale * 1.4426950408889634f;
-  a.max_queries = u.max_queries, a.q_rows = static_cast<int>(u.q_rows), a.q_start = u.q_start;
+  a.max_queries = static_cast<int>(std::min<long long>(u.max_queries, u.q_rows)), a.q_rows = static_cast<int>(u.q_rows), a.q_start = u.q_start;
   a.out = u.out, a.out_row = u.out_row, a.out_head = u.out_head;
   a.max_keys = u.max_keys, a.kv_rows = static_cast<int>(u.kv_rows), a.kv_start = u.kv_start, a.kv_len = u.kv_len;
   a.v = static_cast<const uint16_t*>(u.v), a.v_batch = u.v_batch, a.v_row = u.v_row, a.v_head = u.v_head;

@@ -84,7 +84,7 @@ def _attention(lib, **kw):
 
 @pytest.mark.parametrize("kw", [dict(dtype=binding.F32), dict(batch=0), dict(heads=0), dict(heads_kv=0), dict(heads_kv=3),
                                 dict(max_queries=0), dict(max_keys=0), dict(max_keys=13), dict(kv_rows=0), dict(q_rows=9),
-                                dict(q_rows=0), dict(sinks=-1), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.nan),
+                                dict(q_rows=0), dict(q_rows=(1 << 30) + 1), dict(kv_rows=(1 << 30) + 1), dict(sinks=-1), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.nan),
                                 dict(scale=math.inf), dict(q=None), dict(out=None), dict(k=None), dict(v=None), dict(q=P + 8),
                                 dict(out_row=250), dict(k_batch=1), dict(v_head=-8), dict(kv_start=P, kv_len=P),
                                 dict(q_start=P + 1), dict(kv_start=P + 2), dict(kv_len=P + 3)])
