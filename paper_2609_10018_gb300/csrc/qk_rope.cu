@@ -127,9 +127,11 @@ __global__ void __launch_bounds__(THREADS, MIN_CTAS)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float2 o = INTERLEAVED ? make_float2(v[j].y, v[j].x) : unpack2<BF>(__shfl_sync(0xffffffffu, ws[j], partner & 31));
-        // the partner's term only where there is one: an infinity there times 0 would be NaN
-        float2 z = mul2(mul2(v[j], make_float2(r, r)), own[j]);
-        if (turns) z = fma2(mul2(o, make_float2(r, r)), other[j], z);
+        // (where nothing turns `other` is 0 and `o` the value itself or its neighbour: an infinite one, whose head
+        // has r = 0, must not reach the neighbour as 0 * infinity)
+        float2 z = mul2(v[j], own[j]);
+        if (!INTERLEAVED || turns) z = fma2(o, other[j], z);
+        z = mul2(z, make_float2(r, r));
         out[j] = BF ? pack_bf16x2(z.x, z.y) : pack_f16x2(z.x, z.y);
       }
       if (on && h < n) *reinterpret_cast<uint4*>(y + h * y_head) = make_uint4(out[0], out[1], out[2], out[3]);
