@@ -120,7 +120,8 @@ __device__ __forceinline__ T of(const T (&x)[2], int g) {
   return g ? x[1] : x[0];
 }
 
-// What every role derives alike for a work item. Key tile t holds the keys from base(t) on, width(t) of them.
+// What every role derives alike for a work item. Key tile t holds the keys from base(t) on, width(t) of them; where
+// `lead` is not 0 the first `lead` columns of tile 0 hold the first keys (the sinks) and only the rest follow base(0).
 struct Item {
   int b, kvh, head0, nheads;    // first query head and how many of the tile's
   int q0, nq, k0, nk;
@@ -128,6 +129,7 @@ struct Item {
   int tiles;                    // key tiles
   int sink_tiles, base0;        // those of the sinks alone, the first key of the others
   int sink_width, last_width;   // of the first of the sinks' and of the last tile (the others have KT keys)
+  int lead;                     // columns of tile 0 for the sinks, in front of the band's first keys
   int with_sinks;               // tiles [0, with_sinks) hold sinks
   int from[2], to[2];           // and tiles [from, to] the keys that the group's rows see besides (none: to < from)
   int whole_from[2], whole_to[2];  // every row of the group sees every key of tiles [whole_from, whole_to]
@@ -137,6 +139,7 @@ struct Item {
   __device__ __forceinline__ int width(int t) const {
     return t == tiles - 1 ? last_width : t < sink_tiles ? sink_width : KT;
   }
+  __device__ __forceinline__ int key(int t, int col) const { return t == 0 && col < lead ? col : base(t) + col; }
   // The first and the last of the CTA's tiles that the group needs (none: last < first).
   __device__ __forceinline__ int first_tile(int g) const {
     const int f = of(from, g);
@@ -185,10 +188,15 @@ __device__ __forceinline__ Item make_item(const Args& a, int id, int rank) {
     }
     low = min(low, lo[g]), high = max(high, hi[g]);
   }
-  it.sink_tiles = 0;
+  // The sinks: in the band's tiles where these begin close to them, else in the first columns of the band's first
+  // tile where that saves a tile, else in tiles of their own.
+  it.sink_tiles = it.lead = 0;
   if (sinks > 0) {
-    if (low <= ((sinks + 31) & ~31))
+    const int cols = (sinks + 31) & ~31;
+    if (low <= cols)
       low = 0;
+    else if (cols < KT && (high - low) % KT + cols < KT)
+      it.lead = cols, low -= cols;
     else
       it.sink_tiles = (sinks + KT - 1) / KT;
   }
@@ -207,7 +215,7 @@ __device__ __forceinline__ Item make_item(const Args& a, int id, int rank) {
     if (pmin < 0) continue;
     // keys [pmax - window, until] (floor divisions: the differences may be negative)
     const int until = a.causal ? pmin : min(it.nk - 1, pmin + a.window);
-    it.whole_from[g] = it.sink_tiles + max(0, (pmax - a.window - low + KT - 1) >> 7);
+    it.whole_from[g] = it.sink_tiles + max(it.lead > 0 ? 1 : 0, (pmax - a.window - low + KT - 1) >> 7);
     it.whole_to[g] = it.sink_tiles + ((until + 1 - low) >> 7) - 1;
   }
   it.begin = it.tiles * rank / a.split, it.end = it.tiles * (rank + 1) / a.split;
@@ -234,7 +242,7 @@ __device__ __forceinline__ Seen seen_columns(const Args& a, const Item& it, int 
   if (p < 0) hi = -1, sinks = 0;
   s.a0 = lo - base;
   s.a1 = t < it.sink_tiles || hi < 0 ? -1 : hi - base;
-  s.b1 = sinks - 1 - base;
+  s.b1 = sinks - 1 - (t == 0 && it.lead > 0 ? 0 : base);
   return s;
 }
 
@@ -307,7 +315,7 @@ __device__ __noinline__ void add_bad_values(const Args& a, const Item& it, int g
       const Seen s = seen_columns(a, it, t, p);
       for (int col = 0; col < it.width(t); ++col) {
         if (!(s.word(col >> 5) >> (col & 31) & 1)) continue;
-        const long long key = it.k0 + it.base(t) + col;
+        const long long key = it.k0 + it.key(t, col);
         const uint16_t* v = a.v + (a.kv_start ? 0 : it.b * a.v_batch) + key * a.v_row + it.kvh * a.v_head;
         for (int c = 2 * lane; c < a.head_dim; c += 64) {
           const uint32_t w = *reinterpret_cast<const uint32_t*>(v + c), bad = bad16<BF>(w);
@@ -486,7 +494,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         const int batch = a.kv_start ? 0 : it.b;
         for (int t = SPLIT ? it.begin : 0; t < (SPLIT ? it.end : it.tiles) && ok; ++t) {
-          const int width = it.width(t), row = it.k0 + it.base(t);
+          const int width = it.width(t), row = it.k0 + it.base(t), lead = t == 0 ? it.lead : 0;
           for (int kv = 0; kv < 2 && ok; ++kv, ++seq) {
             const uint32_t slot = seq % S::slots;
             ok = mbar_wait(&empty[slot], ((seq / S::slots) & 1) ^ 1);
@@ -494,11 +502,11 @@ __global__ void __launch_bounds__(THREADS, 1)
             uint8_t* dst = ring + slot * S::tile;
             mbar_expect_tx(&full[slot], S::halves * width * 128);
             for (int h = 0; h < S::halves; ++h) {
-              if (width == KT) {
+              if (width == KT && lead == 0) {
                 tma_load_4d(dst + h * HALF, kv ? &tmV : &tmK, &full[slot], 64 * h, it.kvh, row, batch);
               } else {
                 for (int c = 0; c < width; c += 32)
-                  tma_load_4d(dst + h * HALF + c * 128, kv ? &tmV32 : &tmK32, &full[slot], 64 * h, it.kvh, row + c, batch);
+                  tma_load_4d(dst + h * HALF + c * 128, kv ? &tmV32 : &tmK32, &full[slot], 64 * h, it.kvh, (c < lead ? it.k0 : row) + c, batch);
               }
             }
           }
