@@ -176,6 +176,45 @@ def test_many_items_with_uneven_tiles(n, causal, window, sinks, d):
     Case(lens, lens, 4, 4, d, causal=causal, window=window, sinks=sinks).check()
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("window,sinks", [(255, 1), (224, 32), (300, 33), (199, 64), (130, 96), (160, 97), (270, 4), (31, 5)])
+@pytest.mark.parametrize("heads,heads_kv,batch", [(2, 2, 1), (8, 2, 1), (8, 8, 12)])
+def test_first_keys_far_from_the_window(causal, window, sinks, heads, heads_kv, batch):
+    """The first keys stand alone or in front of the window's, with every remainder of its length."""
+    lens = [730 - 41 * i for i in range(batch)]
+    Case(lens, lens, heads, heads_kv, 64, causal=causal, window=window, sinks=sinks).check()
+
+
+@pytest.mark.parametrize("nq,nk", [(700, 700), (650, 652), (640, 740), (700, 650), (700, 300), (129, 1000)])
+@pytest.mark.parametrize("sinks", [1, 3, 60, 150])
+@pytest.mark.parametrize("heads,heads_kv,batch,d", [(2, 2, 1, 64), (6, 6, 9, 64), (12, 3, 14, 128), (14, 2, 3, 96)])
+def test_queries_that_see_everything(nq, nk, sinks, heads, heads_kv, batch, d):
+    """Both directions: the first queries see all keys, the others a window; keys and queries of different numbers."""
+    nq, nk = [nq - 9 * i for i in range(batch)], [nk - 9 * i for i in range(batch)]
+    nq[-1] = nk[-1] = max(1, nk[-1] // 7)  # a short one among them
+    Case(nq, nk, heads, heads_kv, d, causal=False, window=25, sinks=sinks, packed=batch % 2 == 1).check()
+
+
+@pytest.mark.parametrize("value", [NAN, INF])
+@pytest.mark.parametrize("at", [0, 2, 5, 130, 500, 639, 640, 676])
+@pytest.mark.parametrize("causal", [True, False])
+def test_bad_value_in_many_items(value, at, causal):
+    """As below, where the first keys share a tile with the window's and queries that see everything share their keys."""
+    c = Case([677] * 7, [677] * 7, 6, 6, 64, causal=causal, window=40, sinks=3)
+    c.v[2 * 677 + at, 1, 5] = value
+    c.check()
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_hidden_keys_beside_the_first(causal):
+    """NaN in keys and values right behind the first ones, which share a load with them."""
+    c = Case([300] * 3, [900] * 3, 8, 8, 128, causal=causal, window=40, sinks=3)
+    for b in range(3):
+        c.k[900 * b + 3:900 * b + 500] = NAN
+        c.v[900 * b + 3:900 * b + 500] = NAN
+    c.check()
+
+
 def test_long_sequence():
     Case([2900], [2900], 2, 1, 128, window=300, sinks=4).check()
     Case([1500], [1500], 1, 1, 64, causal=False, window=100, sinks=1).check()
