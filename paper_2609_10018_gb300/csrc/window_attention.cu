@@ -496,7 +496,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint64_t* q_full = empty + S::slots;  // [group]
   uint64_t* q_empty = q_full + 2;
   uint64_t* s_full = q_empty + 2;        // [group]
-  uint64_t* p_full = s_full + 2;         // [group] 128 arrivals
+  uint64_t* p_full = s_full + 2;         // [group] four arrivals, of the warps
   uint64_t* o_full = p_full + 2;         // [group]
   uint64_t* drain = o_full + 2;          // [MMA warp]
   uint64_t* item_full = drain + 2;       // [2] item n is in items[n & 1]
@@ -525,7 +525,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_init(&q_full[g], 1);
       mbar_init(&q_empty[g], 1);
       mbar_init(&s_full[g], 1);
-      mbar_init(&p_full[g], 128);
+      mbar_init(&p_full[g], 4);
       mbar_init(&o_full[g], 1);
       mbar_init(&item_full[g], 1);
       mbar_init(&item_empty[g], 11);
@@ -862,7 +862,8 @@ __global__ void __launch_bounds__(THREADS, 1)
         sum += (add[0].x + add[0].y) + (add[1].x + add[1].y);
         tmem_st_wait();
         tc_fence_before();
-        mbar_arrive(&p_full[g]);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_full[g]);
         return true;
       };
       for (int t = SPLIT ? it.begin : 0; t < (SPLIT ? it.end : it.tiles) && ok; ++t) {
