@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         const int m0 = t / nt * T::tm + rank * BM, n0 = t % nt * BN + rank * (T::half / 2);
         for (int kb = 0; kb < nkb; ++kb, ++seq) {
           const uint32_t s = seq % S;
-          ok = mbar_wait(&empty[s], ((seq / S) & 1) ^ 1);
+          ok = mbar_wait<true>(&empty[s], ((seq / S) & 1) ^ 1);
           if (!ok) break;
           if constexpr (PAIR) {
             const uint32_t lead = cluster_map(smem_addr(&full[s]), 0);
@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       if (!ok) record_status(a.status, ELASTO_ERR_TIMEOUT);
       // all copies have landed before the CTA exits (a pair's are counted on the even CTA's barriers)
       if (rank == 0)
-        for (uint32_t q = seq > S ? seq - S : 0; q < seq; ++q) mbar_wait(&full[q % S], (q / S) & 1);
+        for (uint32_t q = seq > S ? seq - S : 0; q < seq; ++q) mbar_wait<true>(&full[q % S], (q / S) & 1);
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer
@@ -283,13 +283,13 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (int t = t_start; t < tiles && ok; t += t_stride)
         for (int kb = 0; kb < nkb; ++kb, ++seq) {
           const uint32_t s = seq % S, acc = seq % T::accs;
-          ok = mbar_wait_warp(&full[s], (seq / S) & 1);
+          ok = mbar_wait_warp<true>(&full[s], (seq / S) & 1);
           if (!ok) break;
           const uint32_t a_lo = sdesc_lo(smem_addr(sA + s * A_STAGE), 16), b_lo = sdesc_lo(smem_addr(sB + s * T::b_stage), 16);
 #pragma unroll
           for (int h = 0; h < T::halves; ++h) {
             const uint32_t i = acc * T::halves + h;
-            ok = mbar_wait_warp(&tempty[i], ((seq / T::accs) & 1) ^ 1);
+            ok = mbar_wait_warp<true>(&tempty[i], ((seq / T::accs) & 1) ^ 1);
             if (!ok) break;
             tc_fence_after();
 #pragma unroll
@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         } else {
           tc_commit_warp(drain);
         }
-        mbar_wait_warp(drain, 0);
+        mbar_wait_warp<true>(drain, 0);
       }
     }
   } else if (warp >= 4) {
@@ -355,7 +355,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (int kb = 0; kb < nkb; ++kb, ++seq) {
         const uint32_t p = seq % T::accs, pb = T::halves == 2 ? 2 * p + h : p;  // accumulator, and its barrier
         const float sa = kb + 2 < nkb ? __ldg(as + (kb + 2) * a.lds) : 0.0f, sw = kb + 2 < nkb ? __ldg(ws + kb + 2) : 0.0f;
-        ok = __all_sync(0xffffffffu, mbar_wait(&tfull[pb], (seq / T::accs) & 1));
+        ok = __all_sync(0xffffffffu, mbar_wait<true>(&tfull[pb], (seq / T::accs) & 1));
         if (!ok) break;
         tc_fence_after();
         const float2 s2 = make_float2(s0, s0);

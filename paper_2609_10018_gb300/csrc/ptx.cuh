@@ -55,9 +55,21 @@ __device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
 }
 // try_wait with a suspend-time hint: the thread sleeps in hardware until the
 // phase completes (or the hint expires) instead of spinning on issue slots.
+// BRISK: without the hint, for a time of the hardware's choosing. It then wakes sooner (a
+// round trip between two warps 203 clocks in place of 271: windowed attention 262 -> 251 us, e4m3 products 203 -> 200),
+// but the small steps of a one-image forward took 454 us with it in place of 444.
 constexpr uint32_t kSuspendHintNs = 1000000;
+template <bool BRISK = false>
 __device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
   uint32_t ok;
+  if constexpr (BRISK) {
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok)
+        : "r"(smem_addr(bar)), "r"(parity)
+        : "memory");
+    return ok != 0;
+  }
   asm volatile(
       "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}\n"
       : "=r"(ok)
@@ -66,22 +78,24 @@ __device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
   return ok != 0;
 }
 // Wait until the phase with the given parity has completed; false on timeout.
+template <bool BRISK = false>
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity) {
-  if (mbar_test(bar, parity)) return true;
+  if (mbar_test<BRISK>(bar, parity)) return true;
   const uint64_t t0 = global_timer_ns();
   for (uint32_t i = 1;; ++i) {
-    if (mbar_test(bar, parity)) return true;
+    if (mbar_test<BRISK>(bar, parity)) return true;
     if (global_timer_ns() - t0 > kWaitLimitNs) return false;
   }
 }
 
 // The wait by a whole converged warp; the result is the same in all its
 // threads, and known to the compiler to be.
+template <bool BRISK = false>
 __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity) {
-  if (__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
+  if (__all_sync(0xffffffffu, mbar_test<BRISK>(bar, parity))) return true;
   const uint64_t t0 = global_timer_ns();
   for (;;) {
-    if (__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
+    if (__all_sync(0xffffffffu, mbar_test<BRISK>(bar, parity))) return true;
     if (__any_sync(0xffffffffu, global_timer_ns() - t0 > kWaitLimitNs)) return false;
   }
 }

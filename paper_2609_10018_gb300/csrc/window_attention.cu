@@ -432,21 +432,21 @@ __device__ __noinline__ bool give(uint32_t o_tm, float2 stat, uint8_t* stage, ui
     uint32_t o[32];
     tmem_ld_32x32b_x32(o_tm + c, o);
     tmem_ld_wait();
-    if (!__all_sync(0xffffffffu, mbar_wait(taken, n & 1))) return false;
+    if (!__all_sync(0xffffffffu, mbar_wait<true>(taken, n & 1))) return false;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       *reinterpret_cast<uint4*>(row + ((j ^ (lane & 7)) << 4)) = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
     mbar_arrive(given);
   }
   tc_fence_before();
-  return __all_sync(0xffffffffu, mbar_wait(taken, n & 1));
+  return __all_sync(0xffffffffu, mbar_wait<true>(taken, n & 1));
 }
 template <int DP>
 __device__ __noinline__ float2 take_in(uint32_t o_tm, float2 own, float sc, const uint8_t* stage, uint64_t* given,
                                        uint64_t* taken, uint32_t n) {
   const int lane = threadIdx.x & 31;
   const uint8_t* const row = stage + lane * 128;
-  if (!__all_sync(0xffffffffu, mbar_wait(given, n & 1))) return make_float2(0.0f, 0.0f);
+  if (!__all_sync(0xffffffffu, mbar_wait<true>(given, n & 1))) return make_float2(0.0f, 0.0f);
   const float2 other = *reinterpret_cast<const float2*>(row);
   mbar_arrive(taken);
   ++n;
@@ -457,7 +457,7 @@ __device__ __noinline__ float2 take_in(uint32_t o_tm, float2 own, float sc, cons
     uint32_t o[32];
     tmem_ld_32x32b_x32(o_tm + c, o);
     tmem_ld_wait();
-    if (!__all_sync(0xffffffffu, mbar_wait(given, n & 1))) return make_float2(0.0f, 0.0f);
+    if (!__all_sync(0xffffffffu, mbar_wait<true>(given, n & 1))) return make_float2(0.0f, 0.0f);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const uint4 x = *reinterpret_cast<const uint4*>(row + ((j ^ (lane & 7)) << 4));
@@ -550,7 +550,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 
   // Item n for a warp (all its lanes call): false after the last one, or when the wait gave up.
   auto take = [&](uint32_t n, Item& it) -> bool {
-    if (!__all_sync(0xffffffffu, mbar_wait(&item_full[n & 1], (n >> 1) & 1))) {
+    if (!__all_sync(0xffffffffu, mbar_wait<true>(&item_full[n & 1], (n >> 1) & 1))) {
       if (lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
       return false;
     }
@@ -570,7 +570,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       bool ok = true;
       int id = SPLIT ? static_cast<int>(blockIdx.x) / a.split : static_cast<int>(blockIdx.x);
       for (uint32_t n = 0; ok; ++n) {
-        ok = mbar_wait(&item_empty[n & 1], ((n >> 1) & 1) ^ 1);
+        ok = mbar_wait<true>(&item_empty[n & 1], ((n >> 1) & 1) ^ 1);
         if (!ok) break;
         Item it;
         it.tiles = -1;
@@ -581,7 +581,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
           if (!ok || it.last_tile(g) < it.first_tile(g)) continue;
-          ok = mbar_wait(&q_empty[g], (nq[g] & 1) ^ 1);
+          ok = mbar_wait<true>(&q_empty[g], (nq[g] & 1) ^ 1);
           if (!ok) continue;
           mbar_expect_tx(&q_full[g], S::halves * a.hg * a.qpt * 128);
           for (int h = 0; h < S::halves; ++h)
@@ -593,7 +593,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           const int width = it.width(t), row = it.k0 + it.base(t), lead = t == 0 ? it.lead : 0;
           for (int kv = 0; kv < 2 && ok; ++kv, ++seq) {
             const uint32_t slot = seq % S::slots;
-            ok = mbar_wait(&empty[slot], ((seq / S::slots) & 1) ^ 1);
+            ok = mbar_wait<true>(&empty[slot], ((seq / S::slots) & 1) ^ 1);
             if (!ok) break;
             uint8_t* dst = ring + slot * S::tile;
             mbar_expect_tx(&full[slot], S::halves * width * 128);
@@ -616,14 +616,14 @@ __global__ void __launch_bounds__(THREADS, 1)
         fence_async_smem();  // (the last answer has been read)
         mbar_expect_tx(answered, 16);
         request_block(answer, answered);
-        ok = mbar_wait(answered, n & 1);
+        ok = mbar_wait<true>(answered, n & 1);
         id = requested_block(answer);
       }
       if (!ok) record_status(a.status, ELASTO_ERR_TIMEOUT);
       // all copies have landed before the CTA exits
-      for (uint32_t s = seq > S::slots ? seq - S::slots : 0; s < seq; ++s) mbar_wait(&full[s % S::slots], (s / S::slots) & 1);
+      for (uint32_t s = seq > S::slots ? seq - S::slots : 0; s < seq; ++s) mbar_wait<true>(&full[s % S::slots], (s / S::slots) & 1);
       for (int g = 0; g < 2; ++g)
-        if (nq[g] > 0) mbar_wait(&q_full[g], (nq[g] - 1) & 1);
+        if (nq[g] > 0) mbar_wait<true>(&q_full[g], (nq[g] - 1) & 1);
     }
   } else if (warp <= S::issuers) {
     // ------------------------------------------------------------ MMA issuer
@@ -656,7 +656,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
       auto width = [&](int t) { return t == tiles - 1 ? last_width : t < sink_tiles ? sink_width : KT; };
       auto landed = [&](uint32_t s) {
-        ok = ok && mbar_wait_warp(&full[s % S::slots], (s / S::slots) & 1);
+        ok = ok && mbar_wait_warp<true>(&full[s % S::slots], (s / S::slots) & 1);
         tc_fence_after();
       };
       auto scores = [&](auto group, int t) {
@@ -666,7 +666,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (S::issuers == 2 || g == 0) landed(seq + 2 * (t - begin));
         if (ok && ((t ^ g) & pair) == 0 && (t < with_sinks[g] || (t >= from[g] && t <= to[g]))) {
           if (t == first[g]) {
-            ok = mbar_wait_warp(&q_full[g], nq[g] & 1);
+            ok = mbar_wait_warp<true>(&q_full[g], nq[g] & 1);
             if (!ok) return;
             ++nq[g];
             tc_fence_after();
@@ -689,8 +689,8 @@ __global__ void __launch_bounds__(THREADS, 1)
         const uint32_t s = seq + 2 * (t - begin) + 1, slot = s % S::slots;
         if (S::issuers == 2 || g == 0) landed(s);
         if (ok && ((t ^ g) & pair) == 0 && (t < with_sinks[g] || (t >= from[g] && t <= to[g]))) {
-          if (t < whole_from[g] || t > whole_to[g]) ok = mbar_wait_warp(&v_ready[slot], (s / S::slots) & 1);
-          ok = ok && mbar_wait_warp(&p_full[g], np[g] & 1);
+          if (t < whole_from[g] || t > whole_to[g]) ok = mbar_wait_warp<true>(&v_ready[slot], (s / S::slots) & 1);
+          ok = ok && mbar_wait_warp<true>(&p_full[g], np[g] & 1);
           if (!ok) return;
           ++np[g];
           tc_fence_after();
@@ -734,7 +734,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     if (!ok && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
     if (issued) {
       tc_commit_warp(&drain[warp - 1]);
-      mbar_wait_warp(&drain[warp - 1], 0);
+      mbar_wait_warp<true>(&drain[warp - 1], 0);
     }
   } else if (warp < 4) {
     // ------------------------------------------------------------ a look through the V tiles with masks
@@ -746,7 +746,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (int t = begin; t < end && ok; ++t) {
         // (every V tile is waited for and given back, so that no slot is ever two tiles ahead)
         const uint32_t vs = seq + 2 * (t - begin) + 1, slot = vs % S::slots;
-        ok = mbar_wait_warp(&full[slot], (vs / S::slots) & 1);
+        ok = mbar_wait_warp<true>(&full[slot], (vs / S::slots) & 1);
         if (!ok) break;
         const bool masked = (it.template needs<FORM>(0, t) && !it.whole(0, t)) || (it.template needs<FORM>(1, t) && !it.whole(1, t));
         if (masked) clear_bad_values<BF, DP, 32 * S::lookers>(ring + slot * S::tile, it.width(t), (warp - 4 + S::lookers) * 32 + lane, n, &bad_seq[n & 7]);
@@ -783,7 +783,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       auto tile = [&](auto masked, int t) -> bool {
         constexpr int NC = KT / 32;
         constexpr bool MASKED = decltype(masked)::value;
-        if (!__all_sync(0xffffffffu, mbar_wait(&s_full[g], ns & 1))) return false;
+        if (!__all_sync(0xffffffffu, mbar_wait<true>(&s_full[g], ns & 1))) return false;
         ++ns;
         tc_fence_after();
         uint32_t v[NC][32];
@@ -871,7 +871,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
       // ------------------------------------------------------------ result rows
       if (ok && any) {
-        ok = __all_sync(0xffffffffu, mbar_wait(&o_full[g], no & 1));
+        ok = __all_sync(0xffffffffu, mbar_wait<true>(&o_full[g], no & 1));
         ++no;
         tc_fence_after();
       }
