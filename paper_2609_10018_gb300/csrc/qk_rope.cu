@@ -4,16 +4,19 @@
 //
 // q, k (and v) are read and written once, everything between in fp32 registers. A
 // head lies in LANES = head_dim / 8 lanes, rounded up to a power of two, 16 bytes
-// each; a warp holds 32 / LANES heads of one row at a time and walks over the
-// heads. q, and k with v, have CTAs of their own: a lane's cosines, sines and gains
-// are then one set, read once a row and multiplied together before the heads are
-// walked over. The partner channel of the half-split form is rot_dim / 16 lanes away
-// (rot_dim / 2 is a multiple of 8).
+// each; a warp walks over the heads of one row, 32 / LANES at a time, or of several
+// rows at once. q, and k with v, have CTAs of their own: a lane's cosines, sines and
+// gains are then one set, read once a row and multiplied together before the heads
+// are walked over. The partner channel of the half-split form is rot_dim / 16 lanes
+// away (rot_dim / 2 is a multiple of 8).
 //
-// Bound by memory with issue slots close behind (69 %: unpacking, the norm's
-// shuffles and the partners'). 32776 rows of 12 + 12 heads of 64: 42.3 us,
-// 4.8 TB/s of the 203 MB it reads and writes; the copy's 6.8 would take 29.9 us.
-// Single tokens (64 rows): 3 us, the latency of one chain of loads.
+// Bound by memory, with the loads a row needs before its heads (position, angles,
+// gains) and issue slots (unpacking, the norm's and the partners' shuffles) close
+// behind. 32776 rows of 12 + 12 heads of 64: 40.4 us, 5.0 TB/s of the 203 MB it reads
+// and writes; the copy's 6.8 would take 29.9 us. Single tokens (64 rows): 3 us, the
+// latency of one chain of loads.
+#include <type_traits>
+
 #include "common.h"
 #include "ptx.cuh"
 
@@ -29,20 +32,29 @@ __device__ __forceinline__ float2 unpack2(uint32_t w) {
             : __half22float2(*reinterpret_cast<const __half2*>(&w));
 }
 
-// chunks: warps that share a row, each taking every chunks-th group of heads.
-template <bool BF, int LANES, bool INTERLEAVED>
+// Rows of a warp: 1 (its 32 / LANES groups of lanes take as many heads of it) or, SHARED, 2 to the rows_log
+// (each row has its own groups). chunks: warps that share a row, each taking every chunks-th step of heads.
+template <bool BF, int LANES, bool INTERLEAVED, bool SHARED>
 __global__ void __launch_bounds__(THREADS, MIN_CTAS)
-    qk_norm_rope_kernel(const __grid_constant__ elasto_qk_norm_rope_args a, int chunks, int* status) {
+    qk_norm_rope_kernel(const __grid_constant__ elasto_qk_norm_rope_args a, int rows_of_warp, int chunks, int* status) {
   pdl_wait();
   pdl_trigger();
   constexpr int HPW = 32 / LANES;
+  const int rows_log = SHARED ? rows_of_warp : 0;
   const int lane = threadIdx.x & 31, l = lane % LANES, sub = lane / LANES;
   const bool both = a.heads_q > 0 && a.heads_k > 0;
   const bool keys = both ? blockIdx.x & 1 : a.heads_k > 0;  // this CTA's heads: k (and v), or q
   const unsigned unit = (both ? blockIdx.x >> 1 : blockIdx.x) * WARPS + (threadIdx.x >> 5);
-  const unsigned row = chunks == 1 ? unit : unit / chunks;
-  const int chunk = chunks == 1 ? 0 : static_cast<int>(unit - row * chunks);
-  if (row >= static_cast<unsigned>(a.rows)) return;
+  const unsigned first = (chunks == 1 ? unit : unit / chunks) << rows_log;  // of the warp's rows
+  const int chunk = chunks == 1 ? 0 : static_cast<int>(unit - first * chunks);  // (chunks > 1 only with one row a warp)
+  if (first >= static_cast<unsigned>(a.rows)) return;
+  unsigned row = first;
+  bool live = true;
+  if constexpr (SHARED) {  // lanes of rows past the last go along, for the shuffles
+    row = min(first + (sub & ((1u << rows_log) - 1)), static_cast<unsigned>(a.rows) - 1);
+    live = row == first + (sub & ((1u << rows_log) - 1));
+  }
+  const int step = HPW >> rows_log, hsub = sub >> rows_log;  // heads of a row at a time, and this lane's
   const int e = 8 * l;  // first channel of this lane
   const bool on = e < a.head_dim, turns = e < a.rot_dim;
   const int half = a.rot_dim / 2;
@@ -60,18 +72,23 @@ __global__ void __launch_bounds__(THREADS, MIN_CTAS)
   auto request = [&](int h0) {
 #pragma unroll
     for (int i = 0; i < BATCH; ++i) {
-      const int h = h0 + i * chunks * HPW + sub;
+      const int h = h0 + i * chunks * step + hsub;
       w[i] = make_uint4(0u, 0u, 0u, 0u);
       if (on && h < n) w[i] = __ldcs(reinterpret_cast<const uint4*>(x + h * x_head));
     }
   };
-  request(chunk * HPW);
+  request(chunk * step);
   if ((a.rot_dim > 0 && static_cast<unsigned>(pos) >= static_cast<unsigned>(a.n_positions)) ||
       (a.slots && a.heads_k > 0 && slot >= a.n_slots)) {
-    if (lane == 0) record_status(status, ELASTO_ERR_INVALID_ARG);
-    return;
+    if (live && (SHARED ? l == 0 : lane == 0)) record_status(status, ELASTO_ERR_INVALID_ARG);
+    if constexpr (!SHARED) return;
+    live = false;
+    pos = 0;
   }
-  if (keys && slot < 0) return;
+  if (keys && slot < 0) {
+    if constexpr (!SHARED) return;
+    live = false;
+  }
   const float inv_d = 1.0f / static_cast<float>(a.head_dim);
 
   // y = r (x own + partner's x * other), r = rsqrt(mean(x^2) + eps): the row's angles at this lane's
@@ -112,11 +129,11 @@ __global__ void __launch_bounds__(THREADS, MIN_CTAS)
   }
   const long long y_head = keys ? a.k_out_head : a.q_out_head;
   uint16_t* const y = static_cast<uint16_t*>(keys ? a.k_out : a.q_out) + (keys ? slot * a.k_out_row : static_cast<long long>(row) * a.q_out_row) + e;
-  for (int h0 = chunk * HPW; h0 < n; h0 += BATCH * chunks * HPW) {
-    if (h0 != chunk * HPW) request(h0);
+  for (int h0 = chunk * step; h0 < n; h0 += BATCH * chunks * step) {
+    if (h0 != chunk * step) request(h0);
 #pragma unroll
     for (int i = 0; i < BATCH; ++i) {
-      const int hb = h0 + i * chunks * HPW, h = hb + sub;
+      const int hb = h0 + i * chunks * step, h = hb + hsub;
       if (hb >= n) break;
       const uint32_t ws[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
       float2 v[4], ss = make_float2(0.0f, 0.0f);
@@ -140,33 +157,43 @@ __global__ void __launch_bounds__(THREADS, MIN_CTAS)
         z = mul2(z, make_float2(r, r));
         out[j] = BF ? pack_bf16x2(z.x, z.y) : pack_f16x2(z.x, z.y);
       }
-      if (on && h < n) *reinterpret_cast<uint4*>(y + h * y_head) = make_uint4(out[0], out[1], out[2], out[3]);
+      if (on && live && h < n) *reinterpret_cast<uint4*>(y + h * y_head) = make_uint4(out[0], out[1], out[2], out[3]);
     }
   }
   if (keys && a.v) {
     const uint16_t* const xv = static_cast<const uint16_t*>(a.v) + static_cast<long long>(row) * a.v_row + e;
     uint16_t* const yv = static_cast<uint16_t*>(a.v_out) + slot * a.v_out_row + e;
 #pragma unroll 4
-    for (int h = chunk * HPW + sub; h < n; h += chunks * HPW)
-      if (on) *reinterpret_cast<uint4*>(yv + h * a.v_out_head) = __ldcs(reinterpret_cast<const uint4*>(xv + h * a.v_head));
+    for (int h = chunk * step + hsub; h < n; h += chunks * step)
+      if (on && live) *reinterpret_cast<uint4*>(yv + h * a.v_out_head) = __ldcs(reinterpret_cast<const uint4*>(xv + h * a.v_head));
   }
 }
 
 template <int LANES>
 cudaError_t launch(const elasto_qk_norm_rope_args& a, int* status, cudaStream_t s) {
-  // as many warps a row as leave each at least one group of heads, where the rows alone are few
+  // As many warps a row as leave each at least one step of heads, where the rows alone are few; as many rows a warp as
+  // leave 32 warps for each SM and a lane eight heads, where they are many (what a lane sets up for a row then serves more
+  // heads: 60000 rows of 1 + 1 heads of 64 41.7 -> 14.0 us, 32776 of 12 + 12 42.4 -> 40.4; with 16 heads a lane, 10000
+  // rows of 32 + 8 of 128, 50.1 -> 52.8).
   const int heads = a.heads_q > a.heads_k ? a.heads_q : a.heads_k, groups = (heads + 32 / LANES - 1) / (32 / LANES);
   const long long wanted = 32LL * (num_sms() > 0 ? num_sms() : 152);
-  int chunks = static_cast<int>(wanted / a.rows);
+  int chunks = static_cast<int>(wanted / a.rows), rows_log = 0;
   chunks = chunks < 1 ? 1 : chunks > groups ? groups : chunks;
-  const unsigned units = static_cast<unsigned>(a.rows) * chunks;  // (rows, or at most 32 warps an SM)
+  while ((LANES << rows_log) < 32 && (static_cast<long long>(a.rows) >> (rows_log + 1)) >= wanted &&
+         (heads << rows_log) <= 8 * (32 / LANES))
+    ++rows_log;
+  const unsigned units = ((static_cast<unsigned>(a.rows) - 1) / (1u << rows_log) + 1) * chunks;  // (or at most 32 warps an SM)
   const dim3 grid((units + WARPS - 1) / WARPS * (a.heads_q > 0 && a.heads_k > 0 ? 2 : 1)), block(THREADS);
-  const bool bf = a.dtype == ELASTO_BF16;
-  if (a.interleaved)
-    return bf ? launch_pdl(qk_norm_rope_kernel<true, LANES, true>, grid, block, 0, s, a, chunks, status)
-              : launch_pdl(qk_norm_rope_kernel<false, LANES, true>, grid, block, 0, s, a, chunks, status);
-  return bf ? launch_pdl(qk_norm_rope_kernel<true, LANES, false>, grid, block, 0, s, a, chunks, status)
-            : launch_pdl(qk_norm_rope_kernel<false, LANES, false>, grid, block, 0, s, a, chunks, status);
+  auto start = [&](auto bf, auto interleaved) {
+    if constexpr (LANES < 32)
+      if (rows_log > 0)
+        return launch_pdl(qk_norm_rope_kernel<bf.value, LANES, interleaved.value, true>, grid, block, 0, s, a, rows_log, chunks, status);
+    return launch_pdl(qk_norm_rope_kernel<bf.value, LANES, interleaved.value, false>, grid, block, 0, s, a, 0, chunks, status);
+  };
+  const std::true_type yes;
+  const std::false_type no;
+  if (a.dtype == ELASTO_BF16) return a.interleaved ? start(yes, yes) : start(yes, no);
+  return a.interleaved ? start(no, yes) : start(no, no);
 }
 
 }  // namespace

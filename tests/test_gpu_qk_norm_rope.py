@@ -172,6 +172,39 @@ def test_bad_index_leaves_its_row_out(what):
         assert (t[n].cpu()[[2, 4]] == 9.0).all()
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("rows,hq,hk,d,rot", [(20003, 5, 2, 64, 64), (9999, 3, 3, 128, 64), (19999, 1, 1, 40, 32), (40001, 2, 1, 32, 0),
+                                              (160001, 1, 1, 8, 0), (80002, 3, 0, 16, 16)])
+def test_several_rows_a_warp(rows, hq, hk, d, rot, interleaved):
+    """Many rows, the last warps' short of some; every 7th is left out by its slot, and some have bad positions."""
+    c = Case(rows, hq, hk, d, rot, interleaved)
+    slots = torch.arange(rows, dtype=torch.int32).flip(0)
+    slots[::7] = -1
+    bad = torch.zeros(rows, dtype=torch.bool)
+    if rot:
+        bad[[0, 5, rows // 2, rows - 1]] = True
+        c.pos[bad] = c.n
+    t = c.device(v=hk > 0)
+    for n in ("q_out", "k_out", "v_out"):
+        if t[n] is not None:
+            t[n].fill_(9.0)
+    ds = slots.cuda()
+    assert _run(c.args(t, slots=ds.data_ptr(), n_slots=rows)) == (binding.ERR_INVALID_ARG if rot else 0)
+    c.pos.clamp_(0, c.n - 1)
+    q, k, v = c.want()
+    got = t["q_out"].cpu()
+    c.near(got[~bad], q[~bad])
+    assert (got[bad] == 9.0).all()
+    if hk:
+        there = ~bad & (slots >= 0)
+        at = slots[there].long()
+        c.near(t["k_out"].cpu()[at], k[there])
+        assert torch.equal(t["v_out"].cpu()[at], v[there])
+        rest = torch.ones(rows, dtype=torch.bool)
+        rest[at] = False
+        assert (t["k_out"].cpu()[rest] == 9.0).all() and (t["v_out"].cpu()[rest] == 9.0).all()
+
+
 def test_zero_and_tiny_rows():
     """A head of zeros gives zeros, one of subnormals stays finite."""
     c = Case(3, 2, 1, 64, 64)
