@@ -12,9 +12,9 @@
 //
 // Bound by memory, with the loads a row needs before its heads (position, angles,
 // gains) and issue slots (unpacking, the norm's and the partners' shuffles) close
-// behind. 32776 rows of 12 + 12 heads of 64: 40.4 us, 5.0 TB/s of the 203 MB it reads
-// and writes; the copy's 6.8 would take 29.9 us. Single tokens (64 rows): 3 us, the
-// latency of one chain of loads.
+// behind. 32776 rows of 12 + 12 heads of 64: 36.0 us, 5.6 TB/s of the 203 MB it reads
+// and writes; the copy's 6.8 would take 29.9 us. (CTAs of 256 threads with three heads in flight a lane: 40.4; of
+// 128 with six: 37.4.) Single tokens (64 rows): 2.7 us, the latency of one chain of loads.
 #include <type_traits>
 
 #include "common.h"
@@ -24,7 +24,7 @@ namespace elasto {
 
 namespace {
 
-constexpr int THREADS = 256, WARPS = THREADS / 32, MIN_CTAS = 4, BATCH = 3;
+constexpr int THREADS = 128, WARPS = THREADS / 32, MIN_CTAS = 7, BATCH = 4;
 
 template <bool BF>
 __device__ __forceinline__ float2 unpack2(uint32_t w) {
@@ -74,7 +74,7 @@ __global__ void __launch_bounds__(THREADS, MIN_CTAS)
     for (int i = 0; i < BATCH; ++i) {
       const int h = h0 + i * chunks * step + hsub;
       w[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (on && h < n) w[i] = __ldcs(reinterpret_cast<const uint4*>(x + h * x_head));
+      if (on && h < n) w[i] = *reinterpret_cast<const uint4*>(x + h * x_head);
     }
   };
   request(chunk * step);
@@ -173,8 +173,8 @@ template <int LANES>
 cudaError_t launch(const elasto_qk_norm_rope_args& a, int* status, cudaStream_t s) {
   // As many warps a row as leave each at least one step of heads, where the rows alone are few; as many rows a warp as
   // leave 32 warps for each SM and a lane eight heads, where they are many (what a lane sets up for a row then serves more
-  // heads: 60000 rows of 1 + 1 heads of 64 41.7 -> 14.0 us, 32776 of 12 + 12 42.4 -> 40.4; with 16 heads a lane, 10000
-  // rows of 32 + 8 of 128, 50.1 -> 52.8).
+  // heads: 60000 rows of 1 + 1 heads of 64 41.7 -> 14.0 us, 32776 of 12 + 12 42.4 -> 40.4, on CTAs of 256; with 16
+  // heads a lane, 10000 rows of 32 + 8 of 128, 50.1 -> 52.8).
   const int heads = a.heads_q > a.heads_k ? a.heads_q : a.heads_k, groups = (heads + 32 / LANES - 1) / (32 / LANES);
   const long long wanted = 32LL * (num_sms() > 0 ? num_sms() : 152);
   int chunks = static_cast<int>(wanted / a.rows), rows_log = 0;
