@@ -31,14 +31,14 @@
 // those not yet started (cluster launch control), the longest first.
 //
 // Measured on a GB300 (captured calls): prompts of 8192, 7150 and 4140 tokens, 32 / 8 heads of 128, causal
-// with a window of 1024: 264 us, 1.14 PFLOP/s of visible pairs. A pair of
-// tiles costs ~2500 clocks a key tile where its products alone cost 2048 (the waits
+// with a window of 1024: 250 us, 1.21 PFLOP/s of visible pairs. A pair of
+// tiles costs ~2400 clocks a key tile where its products alone cost 2080 (the waits
 // between S, softmax and PV that the other tile does not cover); the masked tiles at
 // the window's two ends and an item's start and end are the rest. Four sequences
-// of 4097 tokens, 12 heads of 64, 256 keys to either side and a class token: 78 us (58
+// of 4097 tokens, 12 heads of 64, 256 keys to either side and a class token: 76 us (58
 // without the class token: 7 more for its key tile in every item, the rest for its query, which sees all keys). A
 // group's five tiles of the window are cut by it at both ends, and the softmax warps' chain (scores from TMEM, mask,
-// maximum, exp2, P back) sets the pace, not the tensor cores (19 %).
+// maximum, exp2, P back) sets the pace, not the tensor cores (21 %).
 // 16 queries against 8192 keys, 32 / 8 heads of 128: 19 us on clusters, 86 us without (Args::split).
 #include <algorithm>
 #include <atomic>
@@ -71,8 +71,8 @@ template <int DP>
 struct Shape {
   static constexpr int halves = DP / 64, tile = halves * HALF;
   static constexpr int slots = DP == 128 ? 4 : 8;
-  // MMA warps: at 64 channels one for each group, which then needs no step of the other (four images 84.9 -> 82.8
-  // us); at 128, where the tensor cores have twice the work, two fell into step (prefill 272 -> 316 us).
+  // MMA warps: at 64 channels one for each group, which then needs no step of the other (four images of 4097
+  // tokens 84.9 -> 82.8 us); at 128, where the tensor cores have twice the work, two fell into step (prefill 272 -> 316 us).
   static constexpr int issuers = DP == 128 ? 1 : 2, lookers = 3 - issuers;
   static constexpr int smem = 1024 + (2 + slots) * tile + STAGING + TAIL;
 };
