@@ -418,8 +418,9 @@ __device__ __forceinline__ void join(const Args& a, const Item& it, int rank, in
 }
 
 // A pair's second group hands its rows' maxima, sums and O to the first, 32 channels at a time through its staging
-// (a row a thread, 16-byte pieces swizzled by the row), and the first adds them to its own (the joint sum, and 0 for a wait that gave up). n: pieces handed over
-// so far. Out of line: they are rare, and the kernel's code has to fit the instruction caches.
+// (a row a thread, 16-byte pieces swizzled by the row); the first adds them to its own and returns the joint sum,
+// and 0 beside it for a wait that gave up. n: pieces handed over so far. Out of line: they are rare, and the
+// kernel's code has to fit the instruction caches.
 template <int DP>
 __device__ __noinline__ bool give(uint32_t o_tm, float2 stat, uint8_t* stage, uint64_t* given, uint64_t* taken, uint32_t n) {
   const int lane = threadIdx.x & 31;
