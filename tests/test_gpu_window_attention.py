@@ -362,3 +362,30 @@ def test_same_result_every_call_and_streams(nq):
     graph.replay()
     torch.cuda.synchronize()
     c.check(c.out.cpu())
+
+
+@pytest.mark.parametrize("causal,sinks", [(False, 2), (True, 3)])
+def test_graph_replay_reads_new_lengths(causal, sinks):
+    """Captured with full lengths, replayed with shorter ones; calls on two streams beside it."""
+    c = Case([700] * 9, [700] * 9, 6, 6, 64, causal=causal, window=25, sinks=sinks)
+    c.check()
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        binding.elasto_op_window_attention(stream_handle(), c.args(), st.data_ptr())
+    lens = [700, 1, 0, 333, 128, 699, 2, 257, 64]
+    c.nq = c.nk = lens
+    c.q_start.copy_(c.starts(lens))
+    c.kv_start.copy_(c.starts(lens))
+    c.out.fill_(9.0)
+    graph.replay()
+    torch.cuda.synchronize()
+    got = c.out.cpu()
+    c.check(got)
+    outs, streams = [torch.full_like(c.out, 9.0) for _ in range(4)], [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for i, out in enumerate(outs):
+        binding.elasto_op_window_attention(streams[i % 2].cuda_stream, c.args(out=out.data_ptr()), st.data_ptr())
+    torch.cuda.synchronize()
+    assert all(torch.equal(out.cpu(), got) for out in outs) and int(st.item()) == 0
