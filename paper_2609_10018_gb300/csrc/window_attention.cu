@@ -778,6 +778,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       const int qi = first + own, head = r - own * a.hg;
       const bool mine = own < a.qpt && qi <= last && head < it.nheads;
       const int shift = it.nk - it.nq, p = shift + qi;
+      const float lazy = mine ? kLazy : INFINITY;
       float m = -INFINITY, sum = 0.0f;
       bool any = false;
       // one key tile; MASKED: some row does not see some of its keys, or it has less than KT
@@ -813,8 +814,10 @@ __global__ void __launch_bounds__(THREADS, 1)
             t4[(j >> 1) & 3] = max3(t4[(j >> 1) & 3], __uint_as_float(v[i][j]), __uint_as_float(v[i][j + 1]));
         }
         const float top = fmaxf(m, fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])));
-        if (__any_sync(0xffffffffu, (top - m) * sc > kLazy)) {
-          // (top - m is NaN while both are -inf: nothing seen yet, nothing to rescale)
+        // (Rows without a query of this item have no vote: they hold a neighbour's values, or what an earlier kernel left in
+        // shared memory, and a rescaling rounds every row's P anew. top - m is NaN while both are -inf: nothing seen yet,
+        // nothing to rescale.)
+        if (__any_sync(0xffffffffu, (top - m) * sc > lazy)) {
           const float keep = m == -INFINITY ? 0.0f : ex2_approx((m - top) * sc);
           if (any) {
             uint32_t o[32];
