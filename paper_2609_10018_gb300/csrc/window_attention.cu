@@ -645,13 +645,12 @@ __global__ void __launch_bounds__(THREADS, 1)
       const int sink_width = warp_uniform(it.sink_width), last_width = warp_uniform(it.last_width);
       const int begin = SPLIT ? warp_uniform(it.begin) : 0, end = SPLIT ? warp_uniform(it.end) : tiles;
       const int pair = FORM == WIDE ? warp_uniform(it.pair) : 0;
-      int from[2], to[2], with_sinks[2], whole_from[2], whole_to[2], first[2], last[2];
+      int from[2], to[2], with_sinks[2], first[2], last[2];
       bool begun[2] = {false, false};
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
         from[g] = warp_uniform(it.from[g]), to[g] = warp_uniform(it.to[g]);
         with_sinks[g] = warp_uniform(to[g] < from[g] ? 0 : it.with_sinks);
-        whole_from[g] = warp_uniform(it.whole_from[g]), whole_to[g] = warp_uniform(it.whole_to[g]);
         first[g] = SPLIT ? warp_uniform(it.first_tile(g)) : with_sinks[g] > 0 ? 0 : from[g];
         last[g] = SPLIT ? warp_uniform(it.last_tile(g)) : max(to[g], with_sinks[g] - 1);
       }
@@ -688,10 +687,14 @@ __global__ void __launch_bounds__(THREADS, 1)
         constexpr int g = decltype(group)::value;
         if (!ok) return;
         const uint32_t s = seq + 2 * (t - begin) + 1, slot = s % S::slots;
-        if (S::issuers == 2 || g == 0) landed(s);
+        if (S::issuers == 2 || g == 0) {
+          landed(s);
+          // (also where this group sees the tile wholly: what the other group sees in part is changed in place)
+          ok = ok && mbar_wait_warp<true>(&v_ready[slot], (s / S::slots) & 1);
+          tc_fence_after();
+        }
         if (ok && ((t ^ g) & pair) == 0 && (t < with_sinks[g] || (t >= from[g] && t <= to[g]))) {
-          if (t < whole_from[g] || t > whole_to[g]) ok = mbar_wait_warp<true>(&v_ready[slot], (s / S::slots) & 1);
-          ok = ok && mbar_wait_warp<true>(&p_full[g], np[g] & 1);
+          ok = mbar_wait_warp<true>(&p_full[g], np[g] & 1);
           if (!ok) return;
           ++np[g];
           tc_fence_after();

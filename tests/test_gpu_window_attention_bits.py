@@ -54,3 +54,34 @@ def test_bits_do_not_depend_on_the_next_sequence(nq, heads, heads_kv):
         c.dq[nq:] = (c.q[nq:].float() * factor).to(c.dtype).cuda()
         c.out.fill_(9.0)
         assert torch.equal(c.run()[:nq], first), factor
+
+
+INF = float("inf")
+
+
+def _improbable(c, key, value, channel, head=0):
+    """`value` at a key whose score is 240 below all others, so that its probability rounds to 0 in 16 and in 32 bits."""
+    c.q[..., 0], c.k[..., 0] = 32.0, 0.0
+    c.q[..., 1:].mul_(0.25)
+    k, v = (c.k, c.v) if c.packed else (c.k[0], c.v[0])
+    k[key, head, 0] = -7.5 * c.d ** 0.5
+    v[key, head, channel] = value
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("value", [INF, -INF])
+@pytest.mark.parametrize("at", [5, 130, 300, 511, 600])
+def test_improbable_infinity_seen_in_part_by_one_tile(at, value, dtype):
+    """Causal, two tiles of queries an item: the key tile of the first one's diagonal is whole for the second."""
+    n, b = 677, 3
+    c = Case([n] * 7, [n] * 7, 6, 6, 64, dtype=dtype)
+    _improbable(c, b * n + at, value, 9, 2)
+    c.device()
+    first = c.run()
+    c.check(first)
+    rows = first[b * n:(b + 1) * n, 2, 9]
+    sharers = [r for r in range(at, n) if r // 256 == at // 256]  # queries of the item whose diagonal tile holds the key
+    assert (rows[sharers].float() == value).all()
+    for _ in range(5):
+        c.out.fill_(9.0)
+        assert torch.equal(c.run().view(torch.int16), first.view(torch.int16))
