@@ -178,7 +178,9 @@ elasto_status elasto_op_qk_norm_rope(void* stream, const elasto_qk_norm_rope_arg
  * window < 0: no limit. A query before the first key (p < 0) sees nothing.
  *   out = softmax over the visible keys of (scale q . k), times v;
  * a query that sees nothing gets zeros. Keys and values that no query sees, and
- * NaN or infinite ones at places hidden from a query, do not change its result.
+ * NaN or infinite ones at places hidden from a query, do not change its result. A
+ * channel in which a query sees infinite or NaN values gets the sum of these, however
+ * small their probabilities (NaN in any case where a score is NaN or +infinity, or all are -infinity).
  * heads is a multiple of heads_kv: head h reads key head h / (heads / heads_kv).
  * head_dim: a multiple of 8 up to 128. Softmax statistics and sums in fp32; the
  * probabilities are rounded to the operand type for the product with v.

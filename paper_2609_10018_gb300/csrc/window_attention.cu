@@ -23,8 +23,9 @@
 // Key tiles have 128 keys, the last one and the one of the sinks 32 or 64 where
 // that is enough; one that no row of a group sees is skipped for it. Tiles that all
 // rows see wholly take no mask. In the others values that are not finite are set to
-// zero before the product, since 0 * NaN would reach rows that do not see them; the
-// rows that do see them get them added at the end.
+// zero before the product, since 0 * NaN would reach rows that do not see them. Rows
+// that see such values get them at the end (put_bad_values): after such a tile, or
+// where a result is not finite.
 //
 // Items differ in length (ragged sequences, causal rows, class tokens that see
 // everything), so the grid has a block for each and the blocks that run take over
@@ -332,31 +333,42 @@ __device__ __forceinline__ void clear_bad_values(uint8_t* v, int rows, int r, in
   fence_async_smem();
 }
 
-// Values that are not finite were left out of the products: adds those that a row sees to its result, for
-// rows [row0, row1) (rare, so by the warp row by row and key by key).
+// A channel in which a row sees an infinite or NaN value gets the sum of these, whatever their probabilities: the
+// products leave them out where a tile is seen in part, and in other tiles make NaN of an infinity whose probability
+// has rounded to 0. Rows [row0, row1) with their bit in `good` set (rare, so by the warp row by row and key by key).
 template <bool BF>
-__device__ __noinline__ void add_bad_values(const Args& a, const Item& it, int g, int row0, int row1, int lane) {
+__device__ __noinline__ void put_bad_values(const Args& a, const Item& it, int g, int row0, int row1, uint32_t good, int lane) {
   __syncwarp();
   for (int r = row0; r < row1; ++r) {
     const int q = r * a.by_hg >> 16, h = r - q * a.hg, qi = of(it.first, g) + q, p = it.nk - it.nq + qi;
-    if (q >= a.qpt || qi > of(it.last, g) || h >= it.nheads || p < 0) continue;
-    uint16_t* const out = static_cast<uint16_t*>(a.out) + static_cast<long long>(it.q0 + qi) * a.out_row +
-                          static_cast<long long>(it.head0 + h) * a.out_head;
+    if (!(good >> (r - row0) & 1) || q >= a.qpt || qi > of(it.last, g) || h >= it.nheads || p < 0) continue;
+    uint32_t found[2] = {0u, 0u};  // of channels 2 lane and 2 lane + 64, and the next
+    float2 sum[2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
     for (int t = 0; t < it.tiles; ++t) {
       const Seen s = seen_columns(a, it, t, p);
       for (int col = 0; col < it.width(t); ++col) {
         if (!(s.word(col >> 5) >> (col & 31) & 1)) continue;
         const long long key = it.k0 + it.key(t, col);
         const uint16_t* v = a.v + (a.kv_start ? 0 : it.b * a.v_batch) + key * a.v_row + it.kvh * a.v_head;
-        for (int c = 2 * lane; c < a.head_dim; c += 64) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int c = 64 * i + 2 * lane;
+          if (c >= a.head_dim) continue;
           const uint32_t w = *reinterpret_cast<const uint32_t*>(v + c), bad = bad16<BF>(w);
-          if (!bad) continue;
-          uint32_t* const o = reinterpret_cast<uint32_t*>(out + c);
-          const float2 x = unpack16<BF>(w), y = unpack16<BF>(*o);
-          *o = pack16<BF>(bad & 0xffffu ? x.x + y.x : y.x, bad >> 16 ? x.y + y.y : y.y);
+          const float2 x = unpack16<BF>(w & bad);
+          found[i] |= bad;
+          sum[i].x += x.x, sum[i].y += x.y;
         }
       }
     }
+    uint16_t* const out = static_cast<uint16_t*>(a.out) + static_cast<long long>(it.q0 + qi) * a.out_row +
+                          static_cast<long long>(it.head0 + h) * a.out_head + 2 * lane;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (found[i]) {
+        uint32_t* const o = reinterpret_cast<uint32_t*>(out + 64 * i);
+        *o = (*o & ~found[i]) | (pack16<BF>(sum[i].x, sum[i].y) & found[i]);
+      }
   }
   __syncwarp();
 }
@@ -405,7 +417,7 @@ __device__ __forceinline__ void join(const Args& a, const Item& it, int rank, in
                                                       static_cast<long long>(it.head0 + h) * a.out_head + 4 * piece);
     *reinterpret_cast<uint2*>(out) = make_uint2(pack16<BF>(y[0] * inv, y[1] * inv), pack16<BF>(y[2] * inv, y[3] * inv));
   }
-  bool bad = false;
+  bool bad = false;  // some CTA left values out, or has a sum that is not finite
   for (int k = 0; k < a.split; ++k) {
     int v;
     asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(cluster_map(smem_addr(bad_seq), k)));
@@ -414,7 +426,11 @@ __device__ __forceinline__ void join(const Args& a, const Item& it, int rank, in
   if (!bad) return;
   named_bar_sync(1, 256);
   const Item copy = it;
-  for (int r = row0 + (thread >> 5); r < row1; r += 8) add_bad_values<BF>(a, copy, 0, r, r + 1, thread & 31);
+  for (int r = row0 + (thread >> 5); r < row1; r += 8) {
+    float total = 0.0f;  // (whether it is 0 or NaN: the parts' weights do not matter)
+    for (int k = 0; k < a.split; ++k) total += cluster_load2(cluster_map(smem_addr(stat + r), k)).y;
+    put_bad_values<BF>(a, copy, 0, r, r + 1, total > 0.0f, thread & 31);
+  }
 }
 
 // A pair's second group hands its rows' maxima, sums and O to the first, 32 channels at a time through its staging
@@ -771,6 +787,15 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint32_t s_tm = tmem + lanes + g * KT, o_tm = tmem + lanes + O_COL + g * DP;
     const float sc = a.scale_log2;
     uint8_t* const stage = staging + (warp - 4) * (STAGING / 8);
+    // O's columns past those that the products write: zeros, so that the look for results that are not finite needs no
+    // bound (with one prompts took 258 us in place of 251)
+    for (int c = (a.head_dim + 15) & ~15; c < DP; c += 16) {
+      uint32_t zero[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) zero[j] = 0u;
+      tmem_st_16(o_tm + c, zero);
+    }
+    tmem_st_wait();
     uint32_t ns = 0, no = 0, nj = 0;  // score tiles and items of this group, pieces of results given or taken
     bool ok = true;
     Item it;
@@ -901,6 +926,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         // this CTA's maximum, sum and O of each row, for the cluster (the ring is done with: O is complete)
         float* const part = reinterpret_cast<float*>(ring) + r * DP;
         reinterpret_cast<float2*>(staging)[r] = make_float2(any ? m : -INFINITY, sum);
+        float look = 0.0f;  // NaN after a value that is not finite
 #pragma unroll 1
         for (int c = 0; c < DP; c += 32) {
           uint32_t o[32];
@@ -914,12 +940,16 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
           for (int j = 0; j < 8; ++j)  // (16-byte pieces swizzled by the row: no bank conflicts)
             *reinterpret_cast<uint4*>(part + ((((c >> 2) + j) ^ (r & 7)) << 2)) = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) look = fmaf(__uint_as_float(o[j]), 0.0f, look);
         }
+        if (sees && look != look && sum == sum) *bad_seq = static_cast<int>(nth);
         continue;
       }
       // the warp's 32 rows are whole queries of all the tile's heads
       const bool boxed = a.box_q > 0 && first + ((warp & 3) + 1) * a.box_q - 1 <= last && it.nheads == a.hg;
       const float inv = sees ? 1.0f / sum : 0.0f;  // (O of a row that sees nothing is 0)
+      uint32_t look = 0u;  // NaN after a result that is not finite
       // (loops that are not unrolled: the kernel's code has to fit the instruction caches, where twice the code
       // made every part of it slower)
 #pragma unroll 1
@@ -946,6 +976,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             for (int i = 0; i < 4; ++i) {
               const float2 x = mul2(make_float2(__uint_as_float(o[8 * j + 2 * i]), __uint_as_float(o[8 * j + 2 * i + 1])), make_float2(inv, inv));
               pk[i] = pack16<BF>(x.x, x.y);
+              look16<BF>(pk[i], look);
             }
             *reinterpret_cast<uint4*>(stage + lane * 128 + ((((c >> 3) + j) ^ (lane & 7)) << 4)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
           }
@@ -973,13 +1004,15 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         __syncwarp();
       }
-      if (any && bad_seq[nth & 7] == static_cast<int>(nth)) {
+      // (a row whose sum is 0 or NaN has NaN in all channels)
+      const uint32_t good = __ballot_sync(0xffffffffu, sees && sum > 0.0f);
+      if (any && __any_sync(0xffffffffu, bad_seq[nth & 7] == static_cast<int>(nth) || ((good >> lane & 1) && bad16<BF>(look)))) {
         if (boxed) {
           if (elect_one()) bulk_wait_all();
           __syncwarp();
         }
         const Item copy = it;  // (in memory, which `it` itself is not)
-        add_bad_values<BF>(a, copy, g, (warp & 3) * 32, (warp & 3) * 32 + 32, lane);
+        put_bad_values<BF>(a, copy, g, (warp & 3) * 32, (warp & 3) * 32 + 32, good, lane);
       }
       tc_fence_before();
     }

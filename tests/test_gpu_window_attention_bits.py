@@ -85,3 +85,37 @@ def test_improbable_infinity_seen_in_part_by_one_tile(at, value, dtype):
     for _ in range(5):
         c.out.fill_(9.0)
         assert torch.equal(c.run().view(torch.int16), first.view(torch.int16))
+
+
+def _check_not_finite(c):
+    """Values that are not finite as the definition has them; the others within the usual bound."""
+    got = c.device().run()
+    c.check(got)
+    for b in range(len(c.nq)):
+        want, _ = c.want(b)
+        g = got[sum(c.nq[:b]):sum(c.nq[:b + 1])].double()
+        odd = ~want.isfinite()
+        assert odd.any() or b > 0
+        assert torch.equal(g[odd].isnan(), want[odd].isnan())
+        assert torch.equal(g[odd].nan_to_num(nan=0.0), want[odd].nan_to_num(nan=0.0))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("d", [64, 72, 128])
+@pytest.mark.parametrize("at", [0, 40, 333, 640])
+@pytest.mark.parametrize("nq,nk,heads,kw", [
+    ([677], [677], 2, dict()),                                                         # a tile an item
+    ([677] * 7, [677] * 7, 6, dict(window=500, sinks=2)),                              # two tiles an item
+    ([677] * 5, [677] * 5, 6, dict(causal=False, window=40, sinks=3)),                 # queries that see everything
+    ([20], [2000], 2, dict(packed=False)),                                             # keys shared out over a cluster
+    ([20, 3], [1999, 700], 2, dict(packed=False, window=1500, sinks=1)),
+], ids=["one", "two", "wide", "split", "split_window"])
+def test_improbable_infinity(nq, nk, heads, kw, at, d, dtype):
+    """An infinite value behind a probability that rounds to 0 reaches who sees it, in every form and tile; with its
+    opposite in the same channel NaN; a query of NaN stays NaN."""
+    c = Case(nq, nk, heads, heads, d, dtype=dtype, **kw)
+    _improbable(c, at, INF, 9, 1)
+    _improbable(c, at + 9, -INF, 40, 1)
+    (c.v if c.packed else c.v[0])[at + 11, 1, 40] = INF
+    c.q[5, 1] = float("nan")
+    _check_not_finite(c)
