@@ -47,6 +47,8 @@ struct Args {
   const int* kv_len;
   const uint16_t* q;
   long long q_row, q_head;
+  const uint16_t* v;
+  long long v_batch, v_row, v_head;
   uint16_t* out;
   long long out_row, out_head;
   int nsub, rows;  // parts of a head group, heads of a part
@@ -85,6 +87,20 @@ __device__ __forceinline__ float cluster_load(uint32_t addr) {
   float v;
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr));
   return v;
+}
+
+// The sum of the infinite and NaN values of a channel that the token sees, `y` where there are none. v: the channel
+// of key 0; keys [0, sinks) and [lo, nk) are visible. (Rare, so by the thread key by key.)
+template <bool BF>
+__device__ __noinline__ float bad_values(const uint16_t* v, long long row, int sinks, int lo, int nk, float y) {
+  float sum = 0.0f;
+#pragma unroll 8
+  for (int j = 0; j < sinks + nk - lo; ++j) {
+    const uint16_t w = v[(j < sinks ? j : lo + j - sinks) * row];
+    const float x = BF ? __uint_as_float(static_cast<uint32_t>(w) << 16) : __half2float(__ushort_as_half(w));
+    if (!(fabsf(x) < INFINITY)) sum += x;
+  }
+  return sum == 0.0f ? y : sum;
 }
 
 template <bool BF, int DP>
@@ -314,6 +330,9 @@ __global__ void __launch_bounds__(THREADS)
       }
     if (ch < a.head_dim) {
       y = nk > 0 ? y / total : 0.0f;
+      // (an infinite value whose probability has rounded to 0 gave NaN; where the sum is 0 or NaN all channels are NaN)
+      if (!(fabsf(y) < INFINITY) && total > 0.0f)
+        y = bad_values<BF>(a.v + (a.kv_start ? 0 : b * a.v_batch) + k0 * a.v_row + kvh * a.v_head + ch, a.v_row, sinks, lo, nk, y);
       a.out[static_cast<long long>(q0) * a.out_row + (head0 + h) * a.out_head + ch] =
           BF ? __bfloat16_as_ushort(__float2bfloat16_rn(y)) : __half_as_ushort(__float2half_rn(y));
     }
@@ -364,6 +383,7 @@ elasto_status window_decode_launch(const elasto_window_attention_args& u, int* s
   a.q_rows = static_cast<int>(u.q_rows), a.max_keys = u.max_keys, a.kv_rows = static_cast<int>(u.kv_rows);
   a.q_start = u.q_start, a.kv_start = u.kv_start, a.kv_len = u.kv_len;
   a.q = static_cast<const uint16_t*>(u.q), a.q_row = u.q_row, a.q_head = u.q_head;
+  a.v = static_cast<const uint16_t*>(u.v), a.v_batch = u.v_batch, a.v_row = u.v_row, a.v_head = u.v_head;
   a.out = static_cast<uint16_t*>(u.out), a.out_row = u.out_row, a.out_head = u.out_head;
   a.nsub = (a.group + ROWS - 1) / ROWS;
   a.rows = (a.group + a.nsub - 1) / a.nsub;

@@ -119,3 +119,27 @@ def test_improbable_infinity(nq, nk, heads, kw, at, d, dtype):
     (c.v if c.packed else c.v[0])[at + 11, 1, 40] = INF
     c.q[5, 1] = float("nan")
     _check_not_finite(c)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("d", [64, 72, 128])
+@pytest.mark.parametrize("at", [0, 40, 333, 2040])
+@pytest.mark.parametrize("nk,kw", [(2100, dict(packed=False, room=3)), (2100, dict(window=2070, sinks=2)), (2052, dict(packed=False, window=20, sinks=400))],
+                         ids=["all", "window", "sinks"])
+def test_improbable_infinity_single_token(nk, kw, at, d, dtype):
+    """As test_improbable_infinity, for the form of single tokens; three query heads share each key head."""
+    c = Case([1], [nk], 6, 2, d, dtype=dtype, **kw)
+    _improbable(c, at, INF, 9, 1)
+    _improbable(c, at + 9, -INF, 40, 1)
+    (c.v if c.packed else c.v[0])[at + 11, 1, 40] = INF
+    (c.v if c.packed else c.v[0])[nk - 1, 0, 7] = float("nan")
+    c.q[0, 5] = float("nan")
+    _check_not_finite(c)
+
+
+def test_infinity_hidden_from_a_single_token():
+    """Not found by the search for visible ones either."""
+    c = Case([1], [500], 2, 1, 64, window=100, sinks=3, packed=False, room=8)
+    _improbable(c, 450, INF, 9)
+    c.v[0, 3:399, 0, 9], c.v[0, 500:, 0, 9] = -INF, -INF
+    _check_not_finite(c)
