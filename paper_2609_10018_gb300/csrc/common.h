@@ -364,6 +364,14 @@ cudaError_t gemm_fp8_init_attributes();
 cudaError_t qk_norm_rope_launch(const elasto_qk_norm_rope_args& a, int* status, cudaStream_t s);
 elasto_status window_attention_launch(const elasto_window_attention_args& a, int* status, cudaStream_t s);
 cudaError_t window_attention_init_attributes();
+// The windowed attentions sum p v before they divide by the sum of p, and p may be 2^8 (a running maximum that lags):
+// bf16 values near the type's end, which is fp32's, would overflow. A power of two off every p, cancelled by the division,
+// holds the sum of up to `keys` of them below 1. f16 values cannot overflow (2^30 keys of 2^8 * 2^16).
+inline float sum_headroom(bool bf, int keys) {
+  int log2 = 0;
+  while ((1LL << log2) < keys) ++log2;
+  return bf ? 9.0f + log2 : 0.0f;
+}
 // The single-token form (max_queries == 1).
 elasto_status window_decode_launch(const elasto_window_attention_args& a, int* status, cudaStream_t s);
 cudaError_t window_decode_init_attributes();

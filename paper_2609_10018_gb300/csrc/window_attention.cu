@@ -82,7 +82,7 @@ static_assert(Shape<128>::smem <= SMEM_LIMIT && Shape<64>::smem <= SMEM_LIMIT, "
 struct Args {
   int batch, heads, heads_kv, group, head_dim;
   int causal, window, sinks;  // window and sinks cut to max_keys
-  float scale_log2;
+  float scale_log2, down;  // P is 2^-down times the probability over the running maximum (sum_headroom)
   int max_queries, q_rows;
   const int* q_start;
   void* out;
@@ -870,7 +870,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           m = top;
         }
         any = true;
-        const float neg = m == -INFINITY ? 0.0f : -m * sc;
+        const float neg = m == -INFINITY ? 0.0f : fmaf(-m, sc, -a.down);
         const float2 sc2 = make_float2(sc, sc), neg2 = make_float2(neg, neg);
         float2 add[2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
 #pragma unroll
@@ -1137,6 +1137,7 @@ elasto_status window_attention_launch(const elasto_window_attention_args& u, int
   a.window = u.window < 0 || u.window > u.max_keys ? u.max_keys : u.window;
   a.sinks = u.sinks > u.max_keys ? u.max_keys : u.sinks;
   a.scale_log2 = u.scale * 1.4426950408889634f;
+  a.down = sum_headroom(u.dtype == ELASTO_BF16, u.max_keys);
   a.max_queries = static_cast<int>(std::min<long long>(u.max_queries, u.q_rows)), a.q_rows = static_cast<int>(u.q_rows), a.q_start = u.q_start;
   a.out = u.out, a.out_row = u.out_row, a.out_head = u.out_head;
   a.max_keys = u.max_keys, a.kv_rows = static_cast<int>(u.kv_rows), a.kv_start = u.kv_start, a.kv_len = u.kv_len;

@@ -40,7 +40,7 @@ struct Shape {
 struct Args {
   int batch, heads_kv, group, head_dim;
   int window, sinks;
-  float scale_log2;
+  float scale_log2, down;  // P is 2^-down times the probability over the running maximum (sum_headroom)
   int q_rows, max_keys, kv_rows;
   const int* q_start;
   const int* kv_start;
@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(THREADS)
         uint32_t p[4];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const float neg = m[h] == -INFINITY ? 0.0f : -m[h] * sc;
+          const float neg = m[h] == -INFINITY ? 0.0f : fmaf(-m[h], sc, -a.down);
           float e[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) e[j] = ex2_approx(fmaf(x[j >> 1][2 * h + (j & 1)], sc, neg));
@@ -380,6 +380,7 @@ elasto_status window_decode_launch(const elasto_window_attention_args& u, int* s
   a.window = u.window < 0 || u.window > u.max_keys ? u.max_keys : u.window;
   a.sinks = u.sinks > u.max_keys ? u.max_keys : u.sinks;
   a.scale_log2 = u.scale * 1.4426950408889634f;
+  a.down = sum_headroom(u.dtype == ELASTO_BF16, u.max_keys);
   a.q_rows = static_cast<int>(u.q_rows), a.max_keys = u.max_keys, a.kv_rows = static_cast<int>(u.kv_rows);
   a.q_start = u.q_start, a.kv_start = u.kv_start, a.kv_len = u.kv_len;
   a.q = static_cast<const uint16_t*>(u.q), a.q_row = u.q_row, a.q_head = u.q_head;

@@ -143,3 +143,29 @@ def test_infinity_hidden_from_a_single_token():
     _improbable(c, 450, INF, 9)
     c.v[0, 3:399, 0, 9], c.v[0, 500:, 0, 9] = -INF, -INF
     _check_not_finite(c)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_large_finite_values_are_not_taken_for_infinities(dtype):
+    """The type's largest value, seen by all with probability 1 / 2 and 1."""
+    for nq, nk, packed in ((300, 300, True), (20, 2000, False)):
+        c = Case([nq], [nk], 2, 2, 64, dtype=dtype, packed=packed)
+        c.q.zero_()
+        c.v.zero_()
+        v = c.v if packed else c.v[0]
+        v[:2, 0, 3], v[:, 1, 5] = torch.finfo(dtype).max / 512, -torch.finfo(dtype).max / 512
+        c.check()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("nq,nk,heads,kw", [([300] * 4, [300] * 4, 4, dict()), ([677] * 7, [677] * 7, 6, dict(window=500, sinks=2)),
+                                            ([677] * 5, [677] * 5, 6, dict(causal=False, window=40, sinks=3)),
+                                            ([20], [2000], 2, dict(packed=False)), ([1, 1], [1999, 70], 2, dict(packed=False))],
+                         ids=["one", "two", "wide", "split", "single"])
+def test_values_near_the_end_of_the_type(nq, nk, heads, kw, dtype):
+    """Weighted means of values of half the type's largest, whose sums are past fp32's for bf16; scores that grow
+    along the keys."""
+    c = _growing(Case(nq, nk, heads, heads, 64, dtype=dtype, **kw))
+    c.v.copy_((c.v.float().clamp(-4, 4) / 8 * torch.finfo(dtype).max).to(dtype))
+    c.v[..., 3] = torch.finfo(dtype).max / 2
+    c.check()
