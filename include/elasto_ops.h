@@ -202,7 +202,7 @@ typedef struct {
   int dtype; /* of q, k, v and out: ELASTO_BF16 or ELASTO_F16 */
   int batch, heads, heads_kv, head_dim;
   int causal, window, sinks;
-  float scale; /* > 0 */
+  float scale; /* > 0, at most 2.3e38 */
   int max_queries;
   long long q_rows;
   const int32_t* q_start; /* [batch + 1] or NULL */

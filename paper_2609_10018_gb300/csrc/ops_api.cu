@@ -241,7 +241,7 @@ elasto_status elasto_op_window_attention(void* stream, const elasto_window_atten
     return refuse("elasto_op_window_attention: batch, heads, max_queries or max_keys");
   if (a.head_dim <= 0 || a.head_dim % 8 != 0 || a.head_dim > 128)
     return refuse("elasto_op_window_attention: head_dim must be a multiple of 8 up to 128", ELASTO_ERR_UNSUPPORTED);
-  if (a.sinks < 0 || !(a.scale > 0.0f) || a.scale > 3.0e38f) return refuse("elasto_op_window_attention: sinks or scale");
+  if (a.sinks < 0 || !(a.scale > 0.0f) || a.scale > 2.3e38f) return refuse("elasto_op_window_attention: sinks or scale");
   if (!tensor16(a.q, a.q_row, a.q_head) || !tensor16(a.out, a.out_row, a.out_head))
     return refuse("elasto_op_window_attention: q or out (null, alignment or strides)");
   if (!tensor16(a.k, a.k_row, a.k_head) || !tensor16(a.v, a.v_row, a.v_head) || !strides8(a.k_batch, a.v_batch))

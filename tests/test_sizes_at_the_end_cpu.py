@@ -1,0 +1,13 @@
+"""Sizes and numbers at the ends of their types in the calls for long sequences: refused on the host. CPU only."""
+import pytest
+
+from paper_2609_10018_gb300 import binding
+from test_abi_cpu import lib  # noqa: F401  (builds the library where it is stale)
+from test_long_sequence_ops_cpu import _attention
+
+
+@pytest.mark.parametrize("scale", [2.4e38, 2.9e38])
+def test_scale_times_log2_e_past_fp32(lib, scale):  # noqa: F811
+    """Scores are held in units of log2: the factor itself would be infinite, and every result NaN."""
+    assert _attention(lib, scale=scale) == binding.ERR_INVALID_ARG
+    assert "elasto_op_window_attention: sinks or scale" in binding.elasto_last_error()
