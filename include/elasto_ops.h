@@ -105,8 +105,8 @@ enum { ELASTO_F16 = 2 };
  *   q = x * (448 / a) rounded to the nearest e4m3 (ties to even),
  * so x is about q * scale. A NaN in a block makes its scale and all its values
  * NaN; an infinity makes its scale infinite, its own value NaN and the others 0.
- * ldx, ldq >= cols: row strides; lds >= rows: stride of scale's rows. Columns
- * past cols are neither read nor written. x, q and scale need their types'
+ * ldx, ldq >= cols: row strides; lds >= rows: stride of scale's rows. At most 2^31 - 128
+ * columns and 2^31 - 1 blocks. Columns past cols are neither read nor written. x, q and scale need their types'
  * alignment; 16-byte rows of x and 8-byte rows of q are read and written wide. */
 elasto_status elasto_op_quantize_fp8(void* stream, const void* x, int x_type, long long ldx, void* q, long long ldq,
                                      float* scale, long long lds, int rows, int cols);

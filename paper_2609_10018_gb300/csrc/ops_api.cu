@@ -168,6 +168,8 @@ elasto_status elasto_op_quantize_fp8(void* stream, const void* x, int x_type, lo
     return refuse("elasto_op_quantize_fp8: x or scale misaligned for its type");
   if (static_cast<long long>(rows) * ((cols + 127LL) / 128) > 0x7fffffffLL)
     return refuse("elasto_op_quantize_fp8: more than 2^31 blocks", ELASTO_ERR_UNSUPPORTED);
+  if (cols > 0x7fffffff - 127)  // (the last block's columns would pass an int)
+    return refuse("elasto_op_quantize_fp8: more than 2^31 - 128 columns", ELASTO_ERR_UNSUPPORTED);
   elasto_status st = check_device();
   if (st != ELASTO_OK) return st;
   ELASTO_CUDA_TRY(quantize_fp8_launch(x, x_type, ldx, static_cast<uint8_t*>(q), ldq, scale, lds, rows, cols,
