@@ -118,7 +118,7 @@ elasto_status elasto_op_quantize_fp8(void* stream, const void* x, int x_type, lo
  * stride ldw) with w_scale fp32 [ceil(N / 128), ceil(K / 128)], dense; bias fp32 [N] or
  * NULL. epilogue: ELASTO_EPI_BIAS_BF16, _BIAS_GELU_BF16, _BIAS_F32, or
  * _BIAS_RESID_F32 (out += acc + bias); out has row stride ldo >= N.
- * M, N, K >= 1, of any size; A and W 16-byte aligned with lda and ldw multiples of
+ * M, N, K >= 1, M and N at most 2^31 - 256, of any remainder; A and W 16-byte aligned with lda and ldw multiples of
  * 16 (>= K); columns past K are not read. The result does not depend on lda, ldw,
  * ldo, and is the same in every call. */
 elasto_status elasto_op_gemm_fp8(void* stream, const void* A, long long lda, const float* a_scale, long long lds,

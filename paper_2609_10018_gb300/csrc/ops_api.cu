@@ -183,6 +183,8 @@ elasto_status elasto_op_gemm_fp8(void* stream, const void* A, long long lda, con
   clear_error();
   if (!A || !a_scale || !W || !w_scale || !out || M <= 0 || N <= 0 || K <= 0 || lda < K || ldw < K || lds < M || ldo < N)
     return refuse("elasto_op_gemm_fp8: null pointer, size or stride");
+  if (M > 0x7fffffff - 255 || N > 0x7fffffff - 255)  // (a last tile's rows and columns would pass an int)
+    return refuse("elasto_op_gemm_fp8: M or N above 2^31 - 256", ELASTO_ERR_UNSUPPORTED);
   if (!aligned(A, 16) || !aligned(W, 16) || lda % 16 != 0 || ldw % 16 != 0)
     return refuse("elasto_op_gemm_fp8: A and W need 16-byte aligned rows");
   if (epilogue != ELASTO_EPI_BIAS_BF16 && epilogue != ELASTO_EPI_BIAS_GELU_BF16 && epilogue != ELASTO_EPI_BIAS_RESID_F32 &&
