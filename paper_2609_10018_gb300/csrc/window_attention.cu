@@ -1172,9 +1172,12 @@ elasto_status window_attention_launch(const elasto_window_attention_args& u, int
     }
   // Items for queries that see everything, where the keys are more than three times those in an item's window: 4 x 4097
   // tokens with a window of 256 84.6 -> 77.9 us, 16000 tokens 216 -> 110; 4 x 2400 51.3 -> 50.9, but 8 x 1600 65.4 -> 67.7.
-  if (a.split == 1 && !a.causal && a.sinks > 0 && a.max_keys > 3 * (2LL * a.window + a.tiles * a.qpt)) {
-    a.wide = (std::min(a.sinks, a.max_queries) + a.qpt - 1) / a.qpt;
-    qtiles += a.wide;
+  // (Only while the items with them, and queries' numbers behind them, stay within an int.)
+  const long long wide = (std::min(a.sinks, a.max_queries) + a.qpt - 1LL) / a.qpt;
+  if (a.split == 1 && !a.causal && a.sinks > 0 && a.max_keys > 3 * (2LL * a.window + a.tiles * a.qpt) &&
+      (qtiles + wide) * per <= 0x3fffffffLL && a.sinks + static_cast<long long>(a.max_queries) <= 1 << 30) {
+    a.wide = static_cast<int>(wide);
+    qtiles += wide;
   }
   a.items = static_cast<int>(qtiles * per);
   a.per_q = Divisor(static_cast<unsigned>(per)), a.by_nsub = Divisor(a.nsub), a.by_heads_kv = Divisor(a.heads_kv);
