@@ -41,29 +41,20 @@ bool tables_ok(const int32_t* idx, int n, int limit) {
   return true;
 }
 
-std::once_flag g_attr_once[64];
-cudaError_t g_attr_err[64];
-
 }  // namespace
 
+// Of the kernels that models run; the operators for long sequences set up their own when they are first called.
 cudaError_t ensure_kernel_attributes() {
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-  std::call_once(g_attr_once[dev], [dev] {
+  static DeviceOnce once;
+  return once([] {
     cudaError_t r = gemm_init_attributes();
     if (r == cudaSuccess) r = halo_init_attributes();
     if (r == cudaSuccess) r = attn_init_attributes();
     if (r == cudaSuccess) r = cnn_init_attributes();
     if (r == cudaSuccess) r = head_init_attributes();
     if (r == cudaSuccess) r = pk_init_attributes();
-    if (r == cudaSuccess) r = gemm_fp8_init_attributes();
-    if (r == cudaSuccess) r = window_attention_init_attributes();
-    if (r == cudaSuccess) r = window_decode_init_attributes();
-    g_attr_err[dev] = r;
+    return r;
   });
-  return g_attr_err[dev];
 }
 
 elasto_status check_device() {

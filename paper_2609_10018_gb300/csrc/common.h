@@ -6,6 +6,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <mutex>
 #include <string>
 
 #include "elasto.h"
@@ -330,6 +331,25 @@ cudaError_t convert_to_bf16(const void* src, int src_dtype, size_t n, bf16* dst,
 cudaError_t convert_to_bf16_lo(const void* src, int src_dtype, size_t n, bf16* dst, cudaStream_t s);
 cudaError_t convert_to_f32(const void* src, int src_dtype, size_t n, float* dst, cudaStream_t s);
 
+// Runs an initialisation once for each device; every call returns its result.
+class DeviceOnce {
+ public:
+  template <typename F>
+  cudaError_t operator()(F init) {
+    int dev = 0;
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= kDevices) return cudaErrorInvalidDevice;
+    std::call_once(flag_[dev], [&] { result_[dev] = init(); });
+    return result_[dev];
+  }
+
+ private:
+  static constexpr int kDevices = 64;
+  std::once_flag flag_[kDevices];
+  cudaError_t result_[kDevices] = {};
+};
+
 // n / d for n < 2^31 (Granlund and Montgomery's multiplication by a reciprocal).
 struct Divisor {
   unsigned d = 1, mul = 1, shift = 0;
@@ -360,10 +380,8 @@ struct Fp8Gemm {
   int* status;
 };
 elasto_status gemm_fp8_launch(const Fp8Gemm& g, cudaStream_t s);
-cudaError_t gemm_fp8_init_attributes();
 cudaError_t qk_norm_rope_launch(const elasto_qk_norm_rope_args& a, int* status, cudaStream_t s);
 elasto_status window_attention_launch(const elasto_window_attention_args& a, int* status, cudaStream_t s);
-cudaError_t window_attention_init_attributes();
 // The windowed attentions sum p v before they divide by the sum of p, and p may be 2^8 (a running maximum that lags):
 // bf16 values near the type's end, which is fp32's, would overflow. A power of two off every p, cancelled by the division,
 // holds the sum of up to `keys` of them below 1. f16 values cannot overflow (2^30 keys of 2^8 * 2^16).
@@ -374,6 +392,5 @@ inline float sum_headroom(bool bf, int keys) {
 }
 // The single-token form (max_queries == 1).
 elasto_status window_decode_launch(const elasto_window_attention_args& a, int* status, cudaStream_t s);
-cudaError_t window_decode_init_attributes();
 
 }  // namespace elasto

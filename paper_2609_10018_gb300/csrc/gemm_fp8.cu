@@ -506,9 +506,7 @@ double tile_cost(const Fp8Gemm& g, int nkb, int bn) {
   return 2.2 + waves * (nkb * block + epilogue);
 }
 
-}  // namespace
-
-cudaError_t gemm_fp8_init_attributes() {
+cudaError_t init_attributes() {
   cudaError_t e = cudaSuccess;
   set_attributes_of<true, 256>(&e);
   set_attributes_of<false, 128>(&e);
@@ -516,11 +514,15 @@ cudaError_t gemm_fp8_init_attributes() {
   return e == cudaSuccess ? gemm_fp8_tokens_init_attributes() : e;
 }
 
+}  // namespace
+
 elasto_status gemm_fp8_launch(const Fp8Gemm& g, cudaStream_t s) {
   if ((g.M + BM - 1LL) / BM * ((g.N + 63LL) / 64) > 0x7fffffffLL) {
     set_error("elasto_op_gemm_fp8: output too large");
     return ELASTO_ERR_UNSUPPORTED;
   }
+  static DeviceOnce once;
+  ELASTO_CUDA_TRY(once(init_attributes));
   const int nkb = static_cast<int>((g.K + BK - 1LL) / BK);
   int bn = 64;
   for (int n : {128, 256})

@@ -1099,9 +1099,7 @@ cudaError_t max_clusters(int n, int* clusters) {
   return cudaSuccess;
 }
 
-}  // namespace
-
-cudaError_t window_attention_init_attributes() {
+cudaError_t init_attributes() {
   cudaError_t e = cudaSuccess;
   auto set = [&](auto* f, int bytes) {
     if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
@@ -1130,7 +1128,11 @@ cudaError_t window_attention_init_attributes() {
   return e;
 }
 
+}  // namespace
+
 elasto_status window_attention_launch(const elasto_window_attention_args& u, int* status, cudaStream_t s) {
+  static DeviceOnce once;
+  ELASTO_CUDA_TRY(once(init_attributes));
   Args a{};
   a.batch = u.batch, a.heads = u.heads, a.heads_kv = u.heads_kv, a.group = u.heads / u.heads_kv, a.head_dim = u.head_dim;
   a.causal = u.causal != 0;

@@ -359,9 +359,7 @@ cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const Args& a, 
   return cudaLaunchKernelEx(&cfg, window_decode_kernel<BF, DP>, tk, tv, a);
 }
 
-}  // namespace
-
-cudaError_t window_decode_init_attributes() {
+cudaError_t init_attributes() {
   cudaError_t e = cudaSuccess;
   auto set = [&](auto* f, int bytes) {
     if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
@@ -374,7 +372,11 @@ cudaError_t window_decode_init_attributes() {
   return e;
 }
 
+}  // namespace
+
 elasto_status window_decode_launch(const elasto_window_attention_args& u, int* status, cudaStream_t s) {
+  static DeviceOnce once;
+  ELASTO_CUDA_TRY(once(init_attributes));
   Args a{};
   a.batch = u.batch, a.heads_kv = u.heads_kv, a.group = u.heads / u.heads_kv, a.head_dim = u.head_dim;
   a.window = u.window < 0 || u.window > u.max_keys ? u.max_keys : u.window;
