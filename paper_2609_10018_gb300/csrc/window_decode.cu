@@ -16,9 +16,11 @@
 // 64 sequences of up to 8192 keys, 32 / 8 heads of 128, window 4095: 150 us, 6.3 TB/s (of 6.8 measured
 // for a copy). One sequence: 5.6 us, the chain of launch, loads and the two joins.
 #include <algorithm>
+#include <atomic>
 
 #include "common.h"
 #include "ptx.cuh"
+#include "window_cluster.h"
 
 namespace elasto {
 
@@ -359,6 +361,34 @@ cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const Args& a, 
   return cudaLaunchKernelEx(&cfg, window_decode_kernel<BF, DP>, tk, tv, a);
 }
 
+// 16 where the current device runs a cluster of that many of these CTAs, which not every one (or part of one) does, else
+// 8, which all do. Asked for once a device.
+int largest_cluster(bool narrow) {
+  static std::atomic<int> known[64][2];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 8;
+  int n = known[dev][narrow].load(std::memory_order_relaxed);
+  if (n > 0) return n;
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = MAX_CLUSTER;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.gridDim = dim3(MAX_CLUSTER);
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = narrow ? Shape<64>::smem : Shape<128>::smem;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int clusters = 0;
+  const cudaError_t e = narrow ? cudaOccupancyMaxActiveClusters(&clusters, window_decode_kernel<true, 64>, &cfg)
+                               : cudaOccupancyMaxActiveClusters(&clusters, window_decode_kernel<true, 128>, &cfg);
+  if (e != cudaSuccess) cudaGetLastError();  // (a size that the device does not know)
+  n = e == cudaSuccess && clusters > 0 ? MAX_CLUSTER : 8;
+  known[dev][narrow].store(n, std::memory_order_relaxed);
+  return n;
+}
+
 cudaError_t init_attributes() {
   cudaError_t e = cudaSuccess;
   auto set = [&](auto* f, int bytes) {
@@ -393,13 +423,8 @@ elasto_status window_decode_launch(const elasto_window_attention_args& u, int* s
   a.status = status;
   const long long units = static_cast<long long>(a.batch) * a.heads_kv * a.nsub;
   const long long keys = std::min<long long>(u.max_keys, static_cast<long long>(a.window) + 1 + a.sinks);
-  // CTAs of a unit: until the SMs have two each (down to 128 keys a CTA), and where keys are many
-  // until there are enough CTAs to even out sequences of different lengths
-  const int sms = num_sms();
-  a.cluster = 1;
-  while (a.cluster < MAX_CLUSTER && ((units * a.cluster < 2 * sms && keys >= 256LL * a.cluster) ||
-                                     (units * a.cluster < 8 * sms && keys >= 2048LL * a.cluster)))
-    a.cluster *= 2;
+  a.cluster = single_token_cluster(units, keys, num_sms(), MAX_CLUSTER);
+  if (a.cluster > 8) a.cluster = single_token_cluster(units, keys, num_sms(), largest_cluster(u.head_dim <= 64));
   if (units * a.cluster > 0x7fffffffLL) {
     set_error("elasto_op_window_attention: too many sequences");
     return ELASTO_ERR_UNSUPPORTED;
