@@ -125,6 +125,16 @@ elasto_status elasto_op_gemm_fp8(void* stream, const void* A, long long lda, con
                                  const void* W, long long ldw, const float* w_scale, const float* bias, void* out,
                                  long long ldo, int M, int N, int K, int epilogue, int* status_device);
 
+/* The tiles that elasto_op_gemm_fp8 cuts a call of this size into on the current
+ * device. Nothing is launched. */
+typedef struct {
+  int rows;    /* of A in a tile */
+  int columns; /* of out */
+  int pair;    /* 1: a pair of CTAs shares a tile */
+  int split;   /* few rows of A: CTAs (a cluster) that share a tile's blocks of K; 0: the form for many rows */
+} elasto_fp8_tile;
+elasto_status elasto_op_gemm_fp8_tile(int M, int N, int K, elasto_fp8_tile* tile);
+
 /* Queries and keys of `rows` tokens: each head of each row divided by the root
  * of its mean square (plus eps), multiplied by the gain of its channel, and its
  * first rot_dim channels rotated by the row's position; all in fp32, rounded

@@ -142,6 +142,7 @@ def lib() -> ctypes.CDLL:
                                    c_int, c_int],
         "elasto_op_gemm_fp8": [c_void_p, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p,
                                c_void_p, c_void_p, c_longlong, c_int, c_int, c_int, c_int, c_void_p],
+        "elasto_op_gemm_fp8_tile": [c_int, c_int, c_int, c_void_p],
         "elasto_op_qk_norm_rope": [c_void_p, ctypes.POINTER(QkNormRope), c_void_p],
         "elasto_op_window_attention": [c_void_p, ctypes.POINTER(WindowAttention), c_void_p],
         "elasto_op_bounded_wait": [c_void_p, c_int, c_void_p, c_void_p],
@@ -455,6 +456,20 @@ def elasto_op_gemm_fp8(stream, A, lda, a_scale, lds, W, ldw, w_scale, bias, out,
                        status=0) -> None:
     _check(lib().elasto_op_gemm_fp8(stream, A, lda, a_scale, lds, W, ldw, w_scale, bias, out, ldo, M, N, K, epilogue,
                                     status), "elasto_op_gemm_fp8")
+
+
+class Fp8Tile(ctypes.Structure):
+    """elasto_fp8_tile: how an e4m3 product is cut up."""
+    _fields_ = [("rows", c_int), ("columns", c_int), ("pair", c_int), ("split", c_int)]
+
+    def fields(self):
+        return self.rows, self.columns, self.pair, self.split
+
+
+def elasto_op_gemm_fp8_tile(M, N, K) -> Fp8Tile:
+    t = Fp8Tile()
+    _check(lib().elasto_op_gemm_fp8_tile(M, N, K, ctypes.byref(t)), "elasto_op_gemm_fp8_tile")
+    return t
 
 
 def elasto_op_qk_norm_rope(stream, args: QkNormRope, status=0) -> None:

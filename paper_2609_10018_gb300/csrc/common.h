@@ -379,6 +379,7 @@ struct Fp8Gemm {
   int M, N, K, epi;
   int* status;
 };
+elasto_fp8_tile gemm_fp8_tile(const Fp8Gemm& g);  // (of its sizes alone)
 elasto_status gemm_fp8_launch(const Fp8Gemm& g, cudaStream_t s);
 cudaError_t qk_norm_rope_launch(const elasto_qk_norm_rope_args& a, int* status, cudaStream_t s);
 elasto_status window_attention_launch(const elasto_window_attention_args& a, int* status, cudaStream_t s);

@@ -16,6 +16,7 @@ __device__ __forceinline__ void fp8_store_one(void* out, long long at, float x) 
 
 // For few rows of A (gemm_fp8_tokens.cu), and its estimated microseconds (nkb: blocks of 128 of K).
 double gemm_fp8_tokens_cost(const Fp8Gemm& g, int nkb);
+elasto_fp8_tile gemm_fp8_tokens_tile(const Fp8Gemm& g, int nkb);
 elasto_status gemm_fp8_tokens_launch(const Fp8Gemm& g, cudaStream_t s);
 cudaError_t gemm_fp8_tokens_init_attributes();
 

@@ -506,6 +506,13 @@ double tile_cost(const Fp8Gemm& g, int nkb, int bn) {
   return 2.2 + waves * (nkb * block + epilogue);
 }
 
+int tile_columns(const Fp8Gemm& g, int nkb) {
+  int bn = 64;
+  for (int n : {128, 256})
+    if (tile_cost(g, nkb, n) < tile_cost(g, nkb, bn)) bn = n;
+  return bn;
+}
+
 cudaError_t init_attributes() {
   cudaError_t e = cudaSuccess;
   set_attributes_of<true, 256>(&e);
@@ -516,6 +523,12 @@ cudaError_t init_attributes() {
 
 }  // namespace
 
+elasto_fp8_tile gemm_fp8_tile(const Fp8Gemm& g) {
+  const int nkb = static_cast<int>((g.K + BK - 1LL) / BK), bn = tile_columns(g, nkb);
+  if (gemm_fp8_tokens_cost(g, nkb) < tile_cost(g, nkb, bn)) return gemm_fp8_tokens_tile(g, nkb);
+  return {bn == 256 ? 256 : 128, bn, bn == 256, 0};
+}
+
 elasto_status gemm_fp8_launch(const Fp8Gemm& g, cudaStream_t s) {
   if ((g.M + BM - 1LL) / BM * ((g.N + 63LL) / 64) > 0x7fffffffLL) {
     set_error("elasto_op_gemm_fp8: output too large");
@@ -524,9 +537,7 @@ elasto_status gemm_fp8_launch(const Fp8Gemm& g, cudaStream_t s) {
   static DeviceOnce once;
   ELASTO_CUDA_TRY(once(init_attributes));
   const int nkb = static_cast<int>((g.K + BK - 1LL) / BK);
-  int bn = 64;
-  for (int n : {128, 256})
-    if (tile_cost(g, nkb, n) < tile_cost(g, nkb, bn)) bn = n;
+  const int bn = tile_columns(g, nkb);
   if (gemm_fp8_tokens_cost(g, nkb) < tile_cost(g, nkb, bn)) return gemm_fp8_tokens_launch(g, s);
   Args a{};
   a.M = g.M, a.N = g.N, a.K = g.K, a.nkb = nkb;

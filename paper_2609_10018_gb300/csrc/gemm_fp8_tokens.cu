@@ -300,6 +300,11 @@ double gemm_fp8_tokens_cost(const Fp8Gemm& g, int nkb) {
   return 2.6 + 0.03 * nt + (0.3 + 0.0016 * nt) * ((nkb + cluster - 1) / cluster) * waves;
 }
 
+elasto_fp8_tile gemm_fp8_tokens_tile(const Fp8Gemm& g, int nkb) {
+  const int nt = rows_of_tile(g.M);
+  return {nt, BM, 0, cluster_of(tiles_of(g, nt), nt, nkb)};
+}
+
 elasto_status gemm_fp8_tokens_launch(const Fp8Gemm& g, cudaStream_t s) {
   const int nt = rows_of_tile(g.M), nkb = static_cast<int>((g.K + BK - 1LL) / BK);
   const long long tiles = tiles_of(g, nt);

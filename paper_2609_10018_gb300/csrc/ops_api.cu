@@ -200,6 +200,19 @@ elasto_status elasto_op_gemm_fp8(void* stream, const void* A, long long lda, con
                          static_cast<cudaStream_t>(stream));
 }
 
+elasto_status elasto_op_gemm_fp8_tile(int M, int N, int K, elasto_fp8_tile* tile) {
+  clear_error();
+  if (!tile || M <= 0 || N <= 0 || K <= 0) return refuse("elasto_op_gemm_fp8_tile: null pointer or size");
+  if (M > 0x7fffffff - 255 || N > 0x7fffffff - 255)
+    return refuse("elasto_op_gemm_fp8_tile: M or N above 2^31 - 256", ELASTO_ERR_UNSUPPORTED);
+  elasto_status st = check_device();
+  if (st != ELASTO_OK) return st;
+  Fp8Gemm g{};
+  g.M = M, g.N = N, g.K = K;
+  *tile = gemm_fp8_tile(g);
+  return ELASTO_OK;
+}
+
 elasto_status elasto_op_qk_norm_rope(void* stream, const elasto_qk_norm_rope_args* args, int* status_device) {
   clear_error();
   if (!args) return refuse("elasto_op_qk_norm_rope: null arguments");
