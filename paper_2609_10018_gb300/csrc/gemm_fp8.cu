@@ -417,8 +417,15 @@ __global__ void __launch_bounds__(THREADS, 1)
             x[j + 1] = add2(x[j + 1], make_float2(b4.z, b4.w));
           }
         }
-        if (part == 0) {  // the piece's last store has read it
-          if (elect_one()) bulk_wait_read<1>();
+        if (part == 0) {
+          // The piece's last store has read it. The two pieces take turns within a tile only: the tile before may have
+          // ended in this one (one piece a tile, or an odd number at the last columns).
+          if (elect_one()) {
+            if (c == 0)
+              bulk_wait_read<0>();
+            else
+              bulk_wait_read<1>();
+          }
           __syncwarp();
         }
         store_chunk<EPI, narrow>(a, &tmC, piece, piece + (c / per & 1) * PIECE, part, lane, row0, col, x);
