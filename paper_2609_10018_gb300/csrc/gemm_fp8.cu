@@ -64,7 +64,7 @@ struct Args {
   const float* bias;
   void* out;
   long long ldo;
-  int tma;  // rows of out start on 16 bytes: tiles leave by TMA
+  int tma_cols;  // pieces of columns that end by this one leave by TMA (0: rows of out do not start on 16 bytes)
   int* status;
 };
 
@@ -130,15 +130,15 @@ __device__ __forceinline__ void store_rows(const Args& a, const uint32_t* t, int
 
 // 32 finished columns of a warp's 32 rows, a row a lane: out[row0 + lane, col .. col + 32). part: which
 // 64 bytes of a 128-byte staging row (16-bit types take two chunks). NARROW: one chunk of a 16-bit
-// type is all the warp has; its rows are 64 bytes, not swizzled.
+// type is all the warp has; its rows are 64 bytes, not swizzled. tma: the piece leaves by TMA, else from `base`.
 template <int EPI, bool NARROW>
-__device__ __forceinline__ void store_chunk(const Args& a, const CUtensorMap* tmC, uint8_t* base, uint8_t* piece, int part, int lane,
-                                            int row0, int col, float2 (&x)[16]) {
+__device__ __forceinline__ void store_chunk(const Args& a, const CUtensorMap* tmC, bool tma, uint8_t* base, uint8_t* piece, int part,
+                                            int lane, int row0, int col, float2 (&x)[16]) {
   if constexpr (EPI == EPI_BIAS_GELU_BF16) {
 #pragma unroll
     for (int j = 0; j < 16; ++j) x[j] = gelu2(x[j]);
   }
-  if (!a.tma) {
+  if (!tma) {
     uint32_t* const t = reinterpret_cast<uint32_t*>(base);
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
@@ -417,18 +417,19 @@ __global__ void __launch_bounds__(THREADS, 1)
             x[j + 1] = add2(x[j + 1], make_float2(b4.z, b4.w));
           }
         }
+        const bool tma = col - 32 * part + 32 * per <= a.tma_cols;
         if (part == 0) {
           // The piece's last store has read it. The two pieces take turns within a tile only: the tile before may have
           // ended in this one (one piece a tile, or an odd number at the last columns).
           if (elect_one()) {
-            if (c == 0)
+            if (c == 0 || !tma)
               bulk_wait_read<0>();
             else
               bulk_wait_read<1>();
           }
           __syncwarp();
         }
-        store_chunk<EPI, narrow>(a, &tmC, piece, piece + (c / per & 1) * PIECE, part, lane, row0, col, x);
+        store_chunk<EPI, narrow>(a, &tmC, tma, piece, piece + (c / per & 1) * PIECE, part, lane, row0, col, x);
       }
     }
     if (elect_one()) bulk_wait_all();
@@ -552,12 +553,14 @@ elasto_status gemm_fp8_launch(const Fp8Gemm& g, cudaStream_t s) {
   a.out = g.out, a.ldo = g.ldo, a.status = g.status;
   const int size = g.epi == EPI_BIAS_RESID_F32 || g.epi == EPI_BIAS_F32 ? 4 : 2;
   const uintptr_t starts = reinterpret_cast<uintptr_t>(g.out) | static_cast<uintptr_t>(g.ldo * size);
-  a.tma = starts % 16 == 0;
+  // (TMA stores whole 16-byte words of a row: where the last column is inside one, its piece leaves value by value)
+  const bool tma = starts % 16 == 0;
+  a.tma_cols = !tma ? 0 : static_cast<uintptr_t>(g.N) * size % 16 == 0 ? 0x7fffffff : g.N;
   CUtensorMap ta, tb, tc{};
   const uint64_t od[2] = {static_cast<uint64_t>(g.N), static_cast<uint64_t>(g.M)}, os[1] = {static_cast<uint64_t>(g.ldo) * size};
   const bool narrow = bn == 64 && size == 2;
   const uint32_t ob[2] = {narrow ? 32u : 128u / size, 32};
-  if ((a.tma && !encode_tmap_plain(&tc, g.out, 2, od, os, ob, size == 4, !narrow)) ||
+  if ((tma && !encode_tmap_plain(&tc, g.out, 2, od, os, ob, size == 4, !narrow)) ||
       !encode_tmap_8(&ta, g.A, g.K, g.M, g.lda, BM) || !encode_tmap_8(&tb, g.W, g.K, g.N, g.ldw, bn == 256 ? 64 : bn)) {
     set_error("elasto_op_gemm_fp8: cuTensorMapEncodeTiled failed (alignment or size)");
     return ELASTO_ERR_UNSUPPORTED;

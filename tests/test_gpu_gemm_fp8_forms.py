@@ -67,3 +67,14 @@ def test_staging_of_the_tile_before(M, N, K, want, epi):
     for o in outs:
         _call(a, sa, w, sw, b, o, N, M, N, K, epi)
     assert all(torch.equal(o, outs[0]) for o in outs)
+
+
+@pytest.mark.parametrize("M,N,K,want", [(2200, 2001, 392, PAIR), (2200, 2041, 392, PAIR), (18701, 251, 777, PAIR), (5000, 1027, 777, (128, 128, 0, 0)),
+                                        (5000, 1131, 100, (128, 64, 0, 0)), (300, 97, 260, (128, 64, 0, 0)), (300, 70, 260, (128, 64, 0, 0))])
+@pytest.mark.parametrize("epi", [BF16, GELU, RESID, F32])
+def test_columns_behind_the_last_are_left_alone(M, N, K, want, epi):
+    """Rows that start on 16 bytes and end inside 16 bytes: what lies behind them is another tensor's."""
+    _tile(M, N, K, want)
+    unit = 4 if epi in (RESID, F32) else 8
+    _check(M, N, K, epi, pad=-N % unit)
+    _check(M, N, K, epi, pad=-N % unit + unit)
