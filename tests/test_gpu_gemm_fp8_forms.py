@@ -78,3 +78,26 @@ def test_columns_behind_the_last_are_left_alone(M, N, K, want, epi):
     unit = 4 if epi in (RESID, F32) else 8
     _check(M, N, K, epi, pad=-N % unit)
     _check(M, N, K, epi, pad=-N % unit + unit)
+
+
+@pytest.mark.parametrize("M,N,K,rows,split", [
+    (7, 9999, 100, 16, 1), (16, 300, 392, 16, 2), (7, 100, 1000, 16, 4), (13, 130, 2100, 16, 8),
+    (27, 20001, 100, 32, 1), (32, 9999, 392, 32, 2), (27, 131, 1000, 32, 4), (17, 300, 2100, 32, 8),
+    (50, 40001, 100, 64, 1), (50, 9999, 1500, 64, 2), (64, 100, 1500, 64, 4), (33, 300, 2100, 64, 8),
+    (300, 33987, 100, 128, 1), (90, 2484, 4000, 128, 4), (150, 1292, 4000, 128, 4), (90, 301, 2500, 128, 8), (150, 100, 2500, 128, 8)])
+@pytest.mark.parametrize("epi", [BF16, GELU, RESID, F32])
+def test_few_rows(M, N, K, rows, split, epi):
+    """Each height of a tile, with its blocks of K shared out over 1 to 8 CTAs; outputs of any row stride."""
+    _tile(M, N, K, (rows, 128, 0, split))
+    _check(M, N, K, epi)
+    if N < 2500:
+        _check(M, N, K, epi, extra=1, pad=5, bias=False)
+
+
+@pytest.mark.parametrize("M,N,K", [(50, 100, 2000), (90, 301, 2500), (27, 131, 1000), (7, 100, 392)])
+def test_few_rows_same_bits(M, N, K):
+    a, sa, w, sw, b = (t.cuda() for t in _problem(M, N, K, 19))
+    outs = [torch.empty((M, N + 3 * i), device="cuda") for i in range(4)]
+    for o in outs:
+        _call(a, sa, w, sw, b, o, o.shape[1], M, N, K, F32)
+    assert all(torch.equal(o[:, :N], outs[0]) for o in outs)
