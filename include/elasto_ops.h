@@ -1,14 +1,15 @@
 /*
- * elasto_ops.h -- stateless kernel-level entry points of libelasto. Each is
- * one step of the DN forward (Section 4.1, Eq. 2-7) that elasto_forward
- * composes; they exist so that every kernel can be checked on its own
- * against the fp64 definition of that step.
+ * elasto_ops.h -- stateless kernel-level entry points of libelasto. The first
+ * part has the steps of the DN forward (Section 4.1, Eq. 2-7) that elasto_forward
+ * composes, so that every kernel can be checked on its own against the fp64
+ * definition of that step. The second part has operators for a caller's own attention
+ * sublayers over long sequences with 8-bit weights; no model call runs them.
  *
- * All pointers are CUDA device memory of the current device, 16-byte aligned,
- * row-major, caller-owned. Calls are asynchronous on `stream` (void* =
+ * All pointers are CUDA device memory of the current device, row-major,
+ * caller-owned; in the first part 16-byte aligned, in the second as each call says. Calls are asynchronous on `stream` (void* =
  * cudaStream_t). `status_device` (nullable) is an int the kernels set to
- * ELASTO_ERR_TIMEOUT if one of their bounded device-side waits gives up.
- * Errors: ELASTO_ERR_INVALID_ARG for null pointers, non-positive or
+ * ELASTO_ERR_TIMEOUT if one of their bounded device-side waits gives up (and to
+ * what else a call says of it). Errors: ELASTO_ERR_INVALID_ARG for null pointers, non-positive or
  * unsupported sizes; ELASTO_ERR_CUDA for launch failures.
  */
 #ifndef ELASTO_OPS_H
@@ -23,7 +24,8 @@ extern "C" {
 /* Epilogues fused into the tensor-core GEMM (acc = A W^T in fp32). */
 typedef enum {
   ELASTO_EPI_BIAS_BF16 = 0,       /* out bf16 = acc + bias                  (QKV, Eq. 2) */
-  ELASTO_EPI_BIAS_GELU_BF16 = 1,  /* out bf16 = GELU(acc + bias)            (FC1, Eq. 5) */
+  ELASTO_EPI_BIAS_GELU_BF16 = 1,  /* out bf16 = GELU(acc + bias)            (FC1, Eq. 5): x Phi(x) in a fitted form,
+                                     off by at most 2.52e-5 (more than rounding where the result is small) */
   ELASTO_EPI_BIAS_RESID_F32 = 2,  /* out fp32 += acc + bias                 (proj, FC2: residual) */
   ELASTO_EPI_BIAS_F32 = 3,        /* out fp32 = acc + bias */
   ELASTO_EPI_BIAS_RELU_BF16 = 4,  /* out bf16 = ReLU(acc + bias)            (conv + folded BN) */
@@ -116,8 +118,8 @@ elasto_status elasto_op_quantize_fp8(void* stream, const void* x, int x_type, lo
  * in fp32. A e4m3 [M, K] (row stride lda) with a_scale fp32 [ceil(K / 128), M]
  * (row stride lds >= M), as elasto_op_quantize_fp8 makes them; W e4m3 [N, K] (row
  * stride ldw) with w_scale fp32 [ceil(N / 128), ceil(K / 128)], dense; bias fp32 [N] or
- * NULL. epilogue: ELASTO_EPI_BIAS_BF16, _BIAS_GELU_BF16, _BIAS_F32, or
- * _BIAS_RESID_F32 (out += acc + bias); out has row stride ldo >= N.
+ * NULL. epilogue: ELASTO_EPI_BIAS_BF16, _BIAS_GELU_BF16 (the same fitted GELU), _BIAS_F32, or
+ * _BIAS_RESID_F32 (out += acc + bias); out has row stride ldo >= N, columns past N are left alone.
  * M, N, K >= 1, M and N at most 2^31 - 256, of any remainder; A and W 16-byte aligned with lda and ldw multiples of
  * 16 (>= K); columns past K are not read. The result does not depend on lda, ldw,
  * ldo, and is the same in every call. */
@@ -192,8 +194,9 @@ elasto_status elasto_op_qk_norm_rope(void* stream, const elasto_qk_norm_rope_arg
  * channel in which a query sees infinite or NaN values gets the sum of these, however
  * small their probabilities (NaN in any case where a score is NaN or +infinity, or all are -infinity).
  * heads is a multiple of heads_kv: head h reads key head h / (heads / heads_kv).
- * head_dim: a multiple of 8 up to 128. Softmax statistics and sums in fp32; the
- * probabilities are rounded to the operand type for the product with v.
+ * head_dim: a multiple of 8 up to 128. Scores, softmax statistics and sums in fp32, exp2 by
+ * the hardware's approximation; the probabilities are rounded to the operand type for the
+ * product with v, their sum is of the unrounded ones.
  * Queries: sequence b has the rows q_start[b] to q_start[b + 1] of q and out, at
  *   most max_queries; q_start NULL: max_queries rows each. q and out have q_rows rows
  *   (at most 2^30, as kv_rows).

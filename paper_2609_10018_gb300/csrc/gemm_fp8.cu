@@ -14,8 +14,8 @@
 //
 // Large products run on CTA pairs (256 x 256 tiles: each SM loads half of W's tile),
 // others on 128 x 128 and 128 x 64; tile_cost estimates which is quickest.
-// 8192 x 8192 x 4096: 198.5 us, 2.8 PFLOP/s (e4m3's rate is about twice the 1.87 measured for bf16). A
-// block of K costs ~760 clocks where its MMAs take 512: MMA, commit, read-out and
+// 8192 x 8192 x 4096: 199 us captured in a graph, 2.8 PFLOP/s (e4m3's rate is about twice the 1.87 measured for bf16);
+// called with new inputs each time 215. A block of K costs ~760 clocks where its MMAs take 512: MMA, commit, read-out and
 // release follow one another, with only two accumulators in TMEM to overlap them.
 // The column halves shorten that chain (207 -> 202 us). 50432 x 2304 x 768 to bf16: 104
 // us, of which the last read-out and store of each tile are ~2 us in 6 blocks of K;

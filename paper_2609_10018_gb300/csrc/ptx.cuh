@@ -56,7 +56,7 @@ __device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
 // try_wait with a suspend-time hint: the thread sleeps in hardware until the
 // phase completes (or the hint expires) instead of spinning on issue slots.
 // BRISK: without the hint, for a time of the hardware's choosing. It then wakes sooner (a
-// round trip between two warps 203 clocks in place of 271: windowed attention 262 -> 251 us, e4m3 products 203 -> 200),
+// round trip between two warps 203 clocks in place of 271: windowed attention 262 -> 250 us, e4m3 products 203 -> 198.5),
 // but the small steps of a one-image forward took 454 us with it in place of 444.
 constexpr uint32_t kSuspendHintNs = 1000000;
 template <bool BRISK = false>

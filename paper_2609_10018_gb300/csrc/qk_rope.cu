@@ -14,7 +14,8 @@
 // gains) and issue slots (unpacking, the norm's and the partners' shuffles) close
 // behind. 32776 rows of 12 + 12 heads of 64: 36.0 us, 5.6 TB/s of the 203 MB it reads
 // and writes; the copy's 6.8 would take 29.9 us. (CTAs of 256 threads with three heads in flight a lane: 40.4; of
-// 128 with six: 37.4.) Single tokens (64 rows): 2.7 us, the latency of one chain of loads.
+// 128 with six: 37.4.) With values, into a cache: 10000 rows of 32 + 8 heads of 128 46.6 us (36.9 by their
+// bytes at a copy's rate), 32776 of 12 + 12 of 64 64.0 (45.7). Single tokens (64 rows): 2.7 to 3.0 us, the latency of one chain of loads.
 #include <type_traits>
 
 #include "common.h"
@@ -173,8 +174,8 @@ template <int LANES>
 cudaError_t launch(const elasto_qk_norm_rope_args& a, int* status, cudaStream_t s) {
   // As many warps a row as leave each at least one step of heads, where the rows alone are few; as many rows a warp as
   // leave 32 warps for each SM and a lane eight heads, where they are many (what a lane sets up for a row then serves more
-  // heads: 60000 rows of 1 + 1 heads of 64 41.7 -> 14.0 us, 32776 of 12 + 12 42.4 -> 40.4, on CTAs of 256; with 16
-  // heads a lane, 10000 rows of 32 + 8 of 128, 50.1 -> 52.8).
+  // heads: 60000 rows of 1 + 1 heads of 64 42.1 -> 13.0 us, 32776 of 12 + 12 41.6 -> 35.7; with 16 heads a lane, 10000 rows
+  // of 32 + 8 of 128, 46.5 -> 48.9).
   const int heads = a.heads_q > a.heads_k ? a.heads_q : a.heads_k, groups = (heads + 32 / LANES - 1) / (32 / LANES);
   const long long wanted = 32LL * (num_sms() > 0 ? num_sms() : 152);
   int chunks = static_cast<int>(wanted / a.rows), rows_log = 0;

@@ -17,7 +17,8 @@
 // While one group works on its scores the tensor cores run the other's products.
 // O stays in TMEM; it is rescaled by its group only when a row's maximum has
 // grown by more than 2^8 (else P simply is up to 2^8: exact in the sums, and the
-// division at the end cancels it). S(t) is issued after PV(t - 1), so its arrival
+// division at the end cancels it, as it does the power of two that keeps bf16 sums
+// from overflowing). S(t) is issued after PV(t - 1), so its arrival
 // also says that O is at rest.
 //
 // Key tiles have 128 keys, the last one and the one of the sinks 32 or 64 where
@@ -32,11 +33,11 @@
 // those not yet started (cluster launch control), the longest first.
 //
 // Measured on a GB300 (captured calls): prompts of 8192, 7150 and 4140 tokens, 32 / 8 heads of 128, causal
-// with a window of 1024: 250 us, 1.21 PFLOP/s of visible pairs. A pair of
+// with a window of 1024: 249 us, 1.21 PFLOP/s of visible pairs. A pair of
 // tiles costs ~2400 clocks a key tile where its products alone cost 2080 (the waits
 // between S, softmax and PV that the other tile does not cover); the masked tiles at
 // the window's two ends and an item's start and end are the rest. Four sequences
-// of 4097 tokens, 12 heads of 64, 256 keys to either side and a class token: 76 us (58
+// of 4097 tokens, 12 heads of 64, 256 keys to either side and a class token: 77.5 us (when it was 76: 58
 // without the class token: 7 more for its key tile in every item, the rest for its query, which sees all keys). A
 // group's five tiles of the window are cut by it at both ends, and the softmax warps' chain (scores from TMEM, mask,
 // maximum, exp2, P back) sets the pace, not the tensor cores (21 %).
