@@ -169,3 +169,21 @@ def test_values_near_the_end_of_the_type(nq, nk, heads, kw, dtype):
     c.v.copy_((c.v.float().clamp(-4, 4) / 8 * torch.finfo(dtype).max).to(dtype))
     c.v[..., 3] = torch.finfo(dtype).max / 2
     c.check()
+
+
+@pytest.mark.parametrize("share", [0.002, 0.3])
+@pytest.mark.parametrize("nq,nk,heads,heads_kv,kw", [([300], [300], 6, 2, dict(window=40, sinks=5)), ([260] * 5, [300] * 5, 8, 8, dict(window=100)),
+                                                     ([300], [300], 6, 2, dict(causal=False, window=30, sinks=9)),
+                                                     ([400] * 4, [400] * 4, 10, 10, dict(causal=False, window=20, sinks=3)),
+                                                     ([40], [1100], 5, 1, dict(packed=False, window=600, sinks=3)),
+                                                     ([1, 1], [700, 90], 4, 2, dict(packed=False, window=300, sinks=3)),
+                                                     ([90], [70], 4, 2, dict(window=30, sinks=3))],
+                         ids=["grouped", "two", "both", "wide", "split", "single", "no_keys_first"])
+def test_many_values_that_are_not_finite(nq, nk, heads, heads_kv, kw, share):
+    """NaN and infinities of either sign all over the values: each row and channel gets the sum of those it sees."""
+    c = Case(nq, nk, heads, heads_kv, 72, dtype=torch.float16, **kw)
+    g = torch.Generator().manual_seed(5)
+    kind = torch.rand(c.v.shape, generator=g)
+    for i, value in enumerate((INF, -INF, float("nan"))):
+        c.v[(kind >= i * share / 3) & (kind < (i + 1) * share / 3) & (torch.arange(72) % (3 if i == 2 else 1) == 0)] = value
+    _check_not_finite(c)
