@@ -108,7 +108,8 @@ enum { ELASTO_F16 = 2 };
  * so x is about q * scale. A NaN in a block makes its scale and all its values
  * NaN; an infinity makes its scale infinite, its own value NaN and the others 0.
  * ldx, ldq >= cols: row strides; lds >= rows: stride of scale's rows. At most 2^31 - 128
- * columns and 2^31 - 1 blocks. Columns past cols are neither read nor written. x, q and scale need their types'
+ * columns and 2^31 - 1 blocks. Columns past cols are neither read nor written. q and scale
+ * may not overlap x. x, q and scale need their types'
  * alignment; 16-byte rows of x and 8-byte rows of q are read and written wide. */
 elasto_status elasto_op_quantize_fp8(void* stream, const void* x, int x_type, long long ldx, void* q, long long ldq,
                                      float* scale, long long lds, int rows, int cols);
@@ -119,7 +120,8 @@ elasto_status elasto_op_quantize_fp8(void* stream, const void* x, int x_type, lo
  * (row stride lds >= M), as elasto_op_quantize_fp8 makes them; W e4m3 [N, K] (row
  * stride ldw) with w_scale fp32 [ceil(N / 128), ceil(K / 128)], dense; bias fp32 [N] or
  * NULL. epilogue: ELASTO_EPI_BIAS_BF16, _BIAS_GELU_BF16 (the same fitted GELU), _BIAS_F32, or
- * _BIAS_RESID_F32 (out += acc + bias); out has row stride ldo >= N, columns past N are left alone.
+ * _BIAS_RESID_F32 (out += acc + bias); out has row stride ldo >= N, columns past N are left alone,
+ * and may not overlap the inputs.
  * M, N, K >= 1, M and N at most 2^31 - 256, of any remainder; A and W 16-byte aligned with lda and ldw multiples of
  * 16 (>= K); columns past K are not read. The result does not depend on lda, ldw,
  * ldo, and is the same in every call. */

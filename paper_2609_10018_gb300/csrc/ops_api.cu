@@ -170,6 +170,7 @@ elasto_status elasto_op_quantize_fp8(void* stream, const void* x, int x_type, lo
     return refuse("elasto_op_quantize_fp8: more than 2^31 blocks", ELASTO_ERR_UNSUPPORTED);
   if (cols > 0x7fffffff - 127)  // (the last block's columns would pass an int)
     return refuse("elasto_op_quantize_fp8: more than 2^31 - 128 columns", ELASTO_ERR_UNSUPPORTED);
+  if (q == x || scale == x || scale == q) return refuse("elasto_op_quantize_fp8: an output that is x or the other output");
   elasto_status st = check_device();
   if (st != ELASTO_OK) return st;
   ELASTO_CUDA_TRY(quantize_fp8_launch(x, x_type, ldx, static_cast<uint8_t*>(q), ldq, scale, lds, rows, cols,
@@ -193,6 +194,8 @@ elasto_status elasto_op_gemm_fp8(void* stream, const void* A, long long lda, con
   const bool f32 = epilogue == ELASTO_EPI_BIAS_RESID_F32 || epilogue == ELASTO_EPI_BIAS_F32;
   if (!aligned(out, f32 ? 4 : 2) || !aligned(a_scale, 4) || !aligned(w_scale, 4) || !aligned(bias, 4))
     return refuse("elasto_op_gemm_fp8: out, a scale or the bias misaligned for its type");
+  if (out == A || out == W || out == a_scale || out == w_scale || out == bias)
+    return refuse("elasto_op_gemm_fp8: out is one of the inputs");
   elasto_status st = check_device();
   if (st != ELASTO_OK) return st;
   return gemm_fp8_launch({static_cast<const uint8_t*>(A), lda, a_scale, lds, static_cast<const uint8_t*>(W), ldw, w_scale,

@@ -1,9 +1,10 @@
-"""Sizes and numbers at the ends of their types in the calls for long sequences: refused on the host. CPU only."""
+"""Refusals on the host by the calls for long sequences: sizes and numbers at the ends of their types, outputs that
+are inputs. CPU only."""
 import pytest
 
 from paper_2609_10018_gb300 import binding
 from test_abi_cpu import lib  # noqa: F401  (builds the library where it is stale)
-from test_long_sequence_ops_cpu import _attention, _gemm, _quantize
+from test_long_sequence_ops_cpu import P, _attention, _gemm, _quantize
 
 
 @pytest.mark.parametrize("scale", [2.4e38, 2.9e38])
@@ -24,3 +25,17 @@ def test_quantize_last_block_past_an_int(lib, cols):  # noqa: F811
 def test_gemm_fp8_last_tile_past_an_int(lib, kw):  # noqa: F811
     assert _gemm(lib, **kw) == binding.ERR_UNSUPPORTED
     assert "2^31" in binding.elasto_last_error()
+
+
+@pytest.mark.parametrize("kw", [dict(q=P, scale=3 * P), dict(q=2 * P, scale=P), dict(q=2 * P, scale=2 * P)])
+def test_quantize_in_place(lib, kw):  # noqa: F811
+    """A block's codes would be written where another's values have not been read."""
+    assert _quantize(lib, **kw) == binding.ERR_INVALID_ARG
+    assert "an output that is" in binding.elasto_last_error()
+
+
+@pytest.mark.parametrize("of", ["A", "a_scale", "W", "w_scale", "bias"])
+def test_gemm_fp8_into_an_input(lib, of):  # noqa: F811
+    kw = dict(A=2 * P, a_scale=3 * P, W=4 * P, w_scale=5 * P, bias=6 * P)
+    assert _gemm(lib, **kw | {of: P}) == binding.ERR_INVALID_ARG
+    assert "one of the inputs" in binding.elasto_last_error()
