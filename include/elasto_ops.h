@@ -97,8 +97,8 @@ elasto_status elasto_op_attention(void* stream, const void* qkv, void* out, int 
  * Strides are in elements. A call allocates nothing and keeps nothing; it may
  * be captured into a graph. */
 
-/* Operand type of these calls besides ELASTO_F32 and ELASTO_BF16: IEEE f16. */
-enum { ELASTO_F16 = 2 };
+/* Operand types of these calls besides ELASTO_F32 and ELASTO_BF16: IEEE f16, and (where a call says so) e4m3. */
+enum { ELASTO_F16 = 2, ELASTO_E4M3 = 3 };
 
 /* q e4m3 [rows, cols] and scale fp32 [ceil(cols / 128), rows]: each row of x
  * (x_type ELASTO_F32, _BF16 or _F16) in blocks of 128 columns, the last block
@@ -235,6 +235,109 @@ typedef struct {
   long long v_batch, v_row, v_head;
 } elasto_window_attention_args;
 elasto_status elasto_op_window_attention(void* stream, const elasto_window_attention_args* args, int* status_device);
+
+/* The norms of elasto_op_residual_norm, over the columns of a row:
+ *   RMS    v / sqrt(mean(v^2) + eps)
+ *   LAYER  (v - mean) / sqrt(mean((v - mean)^2) + eps)
+ * each times the gain of its column (NULL: 1) plus the bias (NULL: 0). NONE: v, no gain and no bias. */
+enum { ELASTO_NORM_NONE = 0, ELASTO_NORM_RMS = 1, ELASTO_NORM_LAYER = 2 };
+
+/* The sum at a block's end and the norm before the next block. For each row
+ *   u = post_norm(y)
+ *   s = x_factor x + y_scale gate u           x_out = s
+ *   z = pre_norm(s) (1 + scale) + shift
+ * in fp32, each output rounded once; z takes s as it was before its rounding to x_out.
+ * x and x_out are the stream (x_type ELASTO_F32, _BF16 or _F16); y (the block's output) has y_type, one of the same.
+ * y NULL: s = x_factor x. x_out NULL: the sum is not stored; z NULL: nothing is normed (one of them is needed).
+ * x_out may be x (the same row stride).
+ * z_type ELASTO_F32, _BF16, _F16, or ELASTO_E4M3: rows and z_scale [ceil(cols / 128), rows] (row stride
+ * z_scale_row >= rows) as elasto_op_quantize_fp8 makes them of the fp32 z.
+ * y_scale: a factor for each column. gate, shift and scale (each may be NULL; mod_type ELASTO_F32, _BF16 or _F16) are tables
+ * [groups, cols] with row stride mod_row: row r takes row group[r] of them (group NULL: row 0). groups 0: no tables. A row
+ * with a group outside [0, groups) is left out, and *status_device is set to ELASTO_ERR_INVALID_ARG.
+ * Squares are summed in fp32: from about 1e19 on they overflow, and the norm gives 0, or NaN for an infinity.
+ * cols: 1 to 16384. Row strides are at least cols. Data needs its types' alignment; rows whose starts are multiples of
+ * eight values in memory are read and written wide. Outputs may not overlap the inputs (but x_out, x) or one another. */
+typedef struct {
+  int rows, cols;
+  float eps;      /* >= 0 */
+  float x_factor; /* finite */
+  int x_type;
+  const void* x;
+  long long x_row;
+  void* x_out;
+  long long x_out_row;
+  int y_type;
+  const void* y;
+  long long y_row;
+  int post_norm;
+  const float* post_gain; /* [cols], or NULL */
+  const float* post_bias;
+  const float* y_scale;
+  int pre_norm;
+  const float* pre_gain;
+  const float* pre_bias;
+  int groups;
+  const int32_t* group; /* [rows], or NULL */
+  int mod_type;
+  long long mod_row;
+  const void* gate;
+  const void* shift;
+  const void* scale;
+  int z_type;
+  void* z;
+  long long z_row;
+  float* z_scale;
+  long long z_scale_row;
+} elasto_residual_norm_args;
+elasto_status elasto_op_residual_norm(void* stream, const elasto_residual_norm_args* args, int* status_device);
+
+/* Which channels of a head elasto_op_qk_norm_rope_axes turns together; pair j of rot_dim / 2 is
+ *   HALF        (j, j + rot_dim / 2)
+ *   NEIGHBOURS  (2 j, 2 j + 1)
+ *   AXIS        halves of each axis's own channels: with pairs s to s + n - 1 of the axis, (s + j, s + j + n). */
+enum { ELASTO_PAIRS_HALF = 0, ELASTO_PAIRS_NEIGHBOURS = 1, ELASTO_PAIRS_AXIS = 2 };
+
+/* elasto_op_qk_norm_rope with positions on several axes (time, height and width of a
+ * patch): pair j is turned by the row's position on axis axis_of[j],
+ *   (a, b) -> (a c - b s, b c + a s),  c, s = cos_sin[p][j], cos_sin[p][rot_dim / 2 + j],
+ *   p = positions[r * positions_row + axis_of[j] * positions_axis],
+ * so the frequencies of all axes lie side by side in one table. norm 1: each head divided by the root of its mean square
+ * (plus eps) first; 0: not. Gains in both cases. A row with any of its `axes` positions outside
+ * [0, n_positions) is left out, as one with a slot >= n_slots is, and *status_device is set to ELASTO_ERR_INVALID_ARG.
+ * Everything else, refusals too, is as elasto_op_qk_norm_rope has it. Refused besides: axes not 1 to 4; an axis_of
+ * that is not below axes; with AXIS pairs, runs of pairs of an axis that are no multiples of 8, or an axis with two runs;
+ * negative strides of positions. */
+typedef struct {
+  int dtype; /* of q, k, v and the outputs: ELASTO_BF16 or ELASTO_F16 */
+  int rows, heads_q, heads_k, head_dim, rot_dim;
+  int pairing;
+  int norm;
+  float eps; /* >= 0 */
+  const void* q; /* heads_q heads (0: no queries, q and q_out are not used) */
+  long long q_row, q_head;
+  const void* k; /* heads_k heads (0: no keys and values) */
+  long long k_row, k_head;
+  const void* v; /* heads_k heads, copied to v_out; or NULL */
+  long long v_row, v_head;
+  void* q_out;
+  long long q_out_row, q_out_head;
+  void* k_out;
+  long long k_out_row, k_out_head;
+  void* v_out;
+  long long v_out_row, v_out_head;
+  const float* q_gain; /* [head_dim], or NULL: ones */
+  const float* k_gain;
+  const float* cos_sin; /* [n_positions, rot_dim], 16-byte aligned (rot_dim 0: not used, nor are positions and axes) */
+  int n_positions;
+  int axes;
+  const unsigned char* axis_of; /* [rot_dim / 2], HOST memory, read during the call */
+  const int32_t* positions;
+  long long positions_row, positions_axis;
+  const int32_t* slots; /* [rows], or NULL */
+  int n_slots;
+} elasto_qk_norm_rope_axes_args;
+elasto_status elasto_op_qk_norm_rope_axes(void* stream, const elasto_qk_norm_rope_axes_args* args, int* status_device);
 
 /* Self-test of the bounded device-side wait that every kernel above (and the
  * forward's kernels) uses instead of an unbounded spin: one thread waits on an

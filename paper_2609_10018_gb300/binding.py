@@ -20,13 +20,15 @@ LIB_PATH = os.path.join(_HERE, "libelasto.so")
 
 ARCH_VIT, ARCH_RESNET50 = 1, 2
 F32, BF16 = 0, 1
-F16 = 2  # operand type of the calls for long sequences (models are stored as F32 or BF16)
+F16, E4M3 = 2, 3  # operand types of the calls for long sequences (models are stored as F32 or BF16)
 OK, ERR_INVALID_ARG, ERR_BAD_TABLE, ERR_BAD_MODE, ERR_OOM, ERR_CUDA, ERR_UNSUPPORTED, ERR_TIMEOUT, ERR_GUARD = (
     0, -1, -2, -3, -4, -5, -6, -7, -8)
 Q_N_MODES, Q_PACKED_BYTES, Q_SHARED_BYTES, Q_WORKSPACE_BYTES, Q_ARENA_BYTES, Q_MODE_MACS, Q_LAUNCHES = range(7)
 Q_PACKED_TOTAL, Q_PREFIX_SHARED, Q_GUARD_ZONES, Q_ONE_LAUNCH = 7, 8, 9, 10
 EPI_BIAS_BF16, EPI_BIAS_GELU_BF16, EPI_BIAS_RESID_F32, EPI_BIAS_F32, EPI_BIAS_RELU_BF16, EPI_BIAS_RESID_RELU_BF16 = range(6)
 EPI_BIAS_RELU_F16, EPI_BIAS_F16, EPI_BIAS_RESID_RELU_F16 = range(6, 9)  # A, W, resid, out in IEEE f16
+NORM_NONE, NORM_RMS, NORM_LAYER = range(3)
+PAIRS_HALF, PAIRS_NEIGHBOURS, PAIRS_AXIS = range(3)
 
 c_int, c_void_p, c_size_t, c_int64 = ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int64
 c_longlong = ctypes.c_longlong
@@ -87,6 +89,27 @@ class WindowAttention(ctypes.Structure):
                                                        ("_head", c_longlong))])
 
 
+class ResidualNorm(ctypes.Structure):
+    """elasto_residual_norm_args."""
+    _fields_ = [("rows", c_int), ("cols", c_int), ("eps", ctypes.c_float), ("x_factor", ctypes.c_float),
+                ("x_type", c_int), ("x", c_void_p), ("x_row", c_longlong), ("x_out", c_void_p), ("x_out_row", c_longlong),
+                ("y_type", c_int), ("y", c_void_p), ("y_row", c_longlong),
+                ("post_norm", c_int), ("post_gain", c_void_p), ("post_bias", c_void_p), ("y_scale", c_void_p),
+                ("pre_norm", c_int), ("pre_gain", c_void_p), ("pre_bias", c_void_p),
+                ("groups", c_int), ("group", c_void_p), ("mod_type", c_int), ("mod_row", c_longlong),
+                ("gate", c_void_p), ("shift", c_void_p), ("scale", c_void_p),
+                ("z_type", c_int), ("z", c_void_p), ("z_row", c_longlong), ("z_scale", c_void_p), ("z_scale_row", c_longlong)]
+
+
+class QkNormRopeAxes(ctypes.Structure):
+    """elasto_qk_norm_rope_axes_args. axis_of: a ctypes array of c_uint8 (host memory)."""
+    _fields_ = ([(f, c_int) for f in ("dtype", "rows", "heads_q", "heads_k", "head_dim", "rot_dim", "pairing", "norm")] +
+                [("eps", ctypes.c_float)] + _strided("q", "k", "v", "q_out", "k_out", "v_out") +
+                [("q_gain", c_void_p), ("k_gain", c_void_p), ("cos_sin", c_void_p), ("n_positions", c_int), ("axes", c_int),
+                 ("axis_of", ctypes.POINTER(ctypes.c_uint8)), ("positions", c_void_p), ("positions_row", c_longlong),
+                 ("positions_axis", c_longlong), ("slots", c_void_p), ("n_slots", c_int)])
+
+
 class ElastoError(RuntimeError):
     def __init__(self, status: int, where: str, msg: str):
         super().__init__(f"{where} failed with status {status}: {msg}")
@@ -144,6 +167,8 @@ def lib() -> ctypes.CDLL:
                                c_void_p, c_void_p, c_longlong, c_int, c_int, c_int, c_int, c_void_p],
         "elasto_op_gemm_fp8_tile": [c_int, c_int, c_int, c_void_p],
         "elasto_op_qk_norm_rope": [c_void_p, ctypes.POINTER(QkNormRope), c_void_p],
+        "elasto_op_residual_norm": [c_void_p, ctypes.POINTER(ResidualNorm), c_void_p],
+        "elasto_op_qk_norm_rope_axes": [c_void_p, ctypes.POINTER(QkNormRopeAxes), c_void_p],
         "elasto_op_window_attention": [c_void_p, ctypes.POINTER(WindowAttention), c_void_p],
         "elasto_op_bounded_wait": [c_void_p, c_int, c_void_p, c_void_p],
         "elasto_op_grid_barrier": [c_void_p, c_int, c_void_p, c_void_p, c_void_p],
@@ -474,6 +499,14 @@ def elasto_op_gemm_fp8_tile(M, N, K) -> Fp8Tile:
 
 def elasto_op_qk_norm_rope(stream, args: QkNormRope, status=0) -> None:
     _check(lib().elasto_op_qk_norm_rope(stream, args, status), "elasto_op_qk_norm_rope")
+
+
+def elasto_op_residual_norm(stream, args: ResidualNorm, status=0) -> None:
+    _check(lib().elasto_op_residual_norm(stream, args, status), "elasto_op_residual_norm")
+
+
+def elasto_op_qk_norm_rope_axes(stream, args: QkNormRopeAxes, status=0) -> None:
+    _check(lib().elasto_op_qk_norm_rope_axes(stream, args, status), "elasto_op_qk_norm_rope_axes")
 
 
 def elasto_op_window_attention(stream, args: WindowAttention, status=0) -> None:

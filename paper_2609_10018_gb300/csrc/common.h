@@ -382,6 +382,8 @@ struct Fp8Gemm {
 elasto_fp8_tile gemm_fp8_tile(const Fp8Gemm& g);  // (of its sizes alone)
 elasto_status gemm_fp8_launch(const Fp8Gemm& g, cudaStream_t s);
 cudaError_t qk_norm_rope_launch(const elasto_qk_norm_rope_args& a, int* status, cudaStream_t s);
+cudaError_t qk_norm_rope_axes_launch(const elasto_qk_norm_rope_axes_args& a, int* status, cudaStream_t s);
+cudaError_t residual_norm_launch(const elasto_residual_norm_args& a, int* status, cudaStream_t s);
 elasto_status window_attention_launch(const elasto_window_attention_args& a, int* status, cudaStream_t s);
 // The windowed attentions sum p v before they divide by the sum of p, and p may be 2^8 (a running maximum that lags):
 // bf16 values near the type's end, which is fp32's, would overflow. A power of two off every p, cancelled by the division,

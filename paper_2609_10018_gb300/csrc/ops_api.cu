@@ -19,6 +19,39 @@ elasto_status refuse(const char* what, elasto_status st = ELASTO_ERR_INVALID_ARG
   return st;
 }
 
+// What elasto_op_qk_norm_rope and its form for several axes refuse alike.
+template <typename ROPE>
+elasto_status check_qk_norm_rope(const ROPE& a, const char* call) {
+  auto no = [&](const char* what, elasto_status st = ELASTO_ERR_INVALID_ARG) { return refuse((std::string(call) + what).c_str(), st); };
+  if (a.dtype != ELASTO_BF16 && a.dtype != ELASTO_F16) return no(": dtype");
+  if (a.rows <= 0 || a.heads_q < 0 || a.heads_k < 0 || a.heads_q + static_cast<long long>(a.heads_k) <= 0 ||
+      a.heads_q + 2LL * a.heads_k > 65536)
+    return no(": rows or heads");
+  if (a.head_dim <= 0 || a.head_dim % 8 != 0 || a.head_dim > 256)
+    return no(": head_dim must be a multiple of 8 up to 256", ELASTO_ERR_UNSUPPORTED);
+  if (a.rot_dim < 0 || a.rot_dim % 16 != 0 || a.rot_dim > a.head_dim)
+    return no(": rot_dim must be a multiple of 16 up to head_dim", ELASTO_ERR_UNSUPPORTED);
+  if (!(a.eps >= 0.0f) || a.eps > 3.0e38f) return no(": eps");
+  if (a.heads_q > 0 && (!tensor16(a.q, a.q_row, a.q_head) || !tensor16(a.q_out, a.q_out_row, a.q_out_head)))
+    return no(": q or q_out (null, alignment or strides)");
+  if (a.heads_k > 0 && (!tensor16(a.k, a.k_row, a.k_head) || !tensor16(a.k_out, a.k_out_row, a.k_out_head)))
+    return no(": k or k_out (null, alignment or strides)");
+  if (a.heads_k > 0 && (a.v || a.v_out) &&
+      (!tensor16(a.v, a.v_row, a.v_head) || !tensor16(a.v_out, a.v_out_row, a.v_out_head)))
+    return no(": v or v_out (null, alignment or strides)");
+  if (a.heads_k > 0 && a.slots && (a.k == a.k_out || (a.v && a.v == a.v_out)))
+    return no(": slots with an output that is its own input");
+  if ((a.q == a.q_out && a.heads_q > 0 && (a.q_row != a.q_out_row || a.q_head != a.q_out_head)) ||
+      (a.k == a.k_out && a.heads_k > 0 && (a.k_row != a.k_out_row || a.k_head != a.k_out_head)) ||
+      (a.v && a.v == a.v_out && a.heads_k > 0 && (a.v_row != a.v_out_row || a.v_head != a.v_out_head)))
+    return no(": an output that is its own input has other strides");
+  if (!aligned(a.q_gain, 16) || !aligned(a.k_gain, 16)) return no(": gains misaligned");
+  if (a.rot_dim > 0 && (!a.cos_sin || !aligned(a.cos_sin, 16) || !a.positions || !aligned(a.positions, 4) || a.n_positions <= 0))
+    return no(": cos_sin, positions or n_positions");
+  if (a.slots && (a.n_slots <= 0 || !aligned(a.slots, 4))) return no(": slots or n_slots");
+  return ELASTO_OK;
+}
+
 // The bounded wait every kernel uses (mbar_wait: a time limit, then false),
 // on an mbarrier of one arrival. armed != 0: that arrival is made first, so
 // the wait returns at once; armed == 0: nothing ever arrives, the wait gives
@@ -220,35 +253,85 @@ elasto_status elasto_op_qk_norm_rope(void* stream, const elasto_qk_norm_rope_arg
   clear_error();
   if (!args) return refuse("elasto_op_qk_norm_rope: null arguments");
   const elasto_qk_norm_rope_args& a = *args;
-  if (a.dtype != ELASTO_BF16 && a.dtype != ELASTO_F16) return refuse("elasto_op_qk_norm_rope: dtype");
-  if (a.rows <= 0 || a.heads_q < 0 || a.heads_k < 0 || a.heads_q + static_cast<long long>(a.heads_k) <= 0 ||
-      a.heads_q + 2LL * a.heads_k > 65536)
-    return refuse("elasto_op_qk_norm_rope: rows or heads");
-  if (a.head_dim <= 0 || a.head_dim % 8 != 0 || a.head_dim > 256)
-    return refuse("elasto_op_qk_norm_rope: head_dim must be a multiple of 8 up to 256", ELASTO_ERR_UNSUPPORTED);
-  if (a.rot_dim < 0 || a.rot_dim % 16 != 0 || a.rot_dim > a.head_dim)
-    return refuse("elasto_op_qk_norm_rope: rot_dim must be a multiple of 16 up to head_dim", ELASTO_ERR_UNSUPPORTED);
-  if (!(a.eps >= 0.0f) || a.eps > 3.0e38f) return refuse("elasto_op_qk_norm_rope: eps");
-  if (a.heads_q > 0 && (!tensor16(a.q, a.q_row, a.q_head) || !tensor16(a.q_out, a.q_out_row, a.q_out_head)))
-    return refuse("elasto_op_qk_norm_rope: q or q_out (null, alignment or strides)");
-  if (a.heads_k > 0 && (!tensor16(a.k, a.k_row, a.k_head) || !tensor16(a.k_out, a.k_out_row, a.k_out_head)))
-    return refuse("elasto_op_qk_norm_rope: k or k_out (null, alignment or strides)");
-  if (a.heads_k > 0 && (a.v || a.v_out) &&
-      (!tensor16(a.v, a.v_row, a.v_head) || !tensor16(a.v_out, a.v_out_row, a.v_out_head)))
-    return refuse("elasto_op_qk_norm_rope: v or v_out (null, alignment or strides)");
-  if (a.heads_k > 0 && a.slots && (a.k == a.k_out || (a.v && a.v == a.v_out)))
-    return refuse("elasto_op_qk_norm_rope: slots with an output that is its own input");
-  if ((a.q == a.q_out && a.heads_q > 0 && (a.q_row != a.q_out_row || a.q_head != a.q_out_head)) ||
-      (a.k == a.k_out && a.heads_k > 0 && (a.k_row != a.k_out_row || a.k_head != a.k_out_head)) ||
-      (a.v && a.v == a.v_out && a.heads_k > 0 && (a.v_row != a.v_out_row || a.v_head != a.v_out_head)))
-    return refuse("elasto_op_qk_norm_rope: an output that is its own input has other strides");
-  if (!aligned(a.q_gain, 16) || !aligned(a.k_gain, 16)) return refuse("elasto_op_qk_norm_rope: gains misaligned");
-  if (a.rot_dim > 0 && (!a.cos_sin || !aligned(a.cos_sin, 16) || !a.positions || !aligned(a.positions, 4) || a.n_positions <= 0))
-    return refuse("elasto_op_qk_norm_rope: cos_sin, positions or n_positions");
-  if (a.slots && (a.n_slots <= 0 || !aligned(a.slots, 4))) return refuse("elasto_op_qk_norm_rope: slots or n_slots");
-  elasto_status st = check_device();
+  elasto_status st = check_qk_norm_rope(a, "elasto_op_qk_norm_rope");
+  if (st != ELASTO_OK) return st;
+  st = check_device();
   if (st != ELASTO_OK) return st;
   ELASTO_CUDA_TRY(qk_norm_rope_launch(a, status_device, static_cast<cudaStream_t>(stream)));
+  return ELASTO_OK;
+}
+
+elasto_status elasto_op_qk_norm_rope_axes(void* stream, const elasto_qk_norm_rope_axes_args* args, int* status_device) {
+  clear_error();
+  if (!args) return refuse("elasto_op_qk_norm_rope_axes: null arguments");
+  const elasto_qk_norm_rope_axes_args& a = *args;
+  elasto_status st = check_qk_norm_rope(a, "elasto_op_qk_norm_rope_axes");
+  if (st != ELASTO_OK) return st;
+  if (a.pairing != ELASTO_PAIRS_HALF && a.pairing != ELASTO_PAIRS_NEIGHBOURS && a.pairing != ELASTO_PAIRS_AXIS)
+    return refuse("elasto_op_qk_norm_rope_axes: pairing");
+  if (a.norm != 0 && a.norm != 1) return refuse("elasto_op_qk_norm_rope_axes: norm");
+  if (a.rot_dim > 0) {
+    if (a.axes < 1 || a.axes > 4 || !a.axis_of) return refuse("elasto_op_qk_norm_rope_axes: axes or axis_of");
+    if (a.positions_row < 0 || a.positions_axis < 0) return refuse("elasto_op_qk_norm_rope_axes: strides of positions");
+    unsigned seen = 0;  // axes with a run of pairs already
+    for (int j = 0, run = 0; j < a.rot_dim / 2; ++j) {
+      if (a.axis_of[j] >= a.axes) return refuse("elasto_op_qk_norm_rope_axes: an axis_of that is not below axes");
+      if (a.pairing != ELASTO_PAIRS_AXIS) continue;
+      if (j == 0 || a.axis_of[j] != a.axis_of[j - 1]) {
+        if (run % 8 != 0 || (seen >> a.axis_of[j] & 1)) return refuse("elasto_op_qk_norm_rope_axes: runs of an axis's pairs");
+        seen |= 1u << a.axis_of[j];
+        run = 0;
+      }
+      ++run;
+    }
+  }
+  st = check_device();
+  if (st != ELASTO_OK) return st;
+  ELASTO_CUDA_TRY(qk_norm_rope_axes_launch(a, status_device, static_cast<cudaStream_t>(stream)));
+  return ELASTO_OK;
+}
+
+elasto_status elasto_op_residual_norm(void* stream, const elasto_residual_norm_args* args, int* status_device) {
+  clear_error();
+  if (!args) return refuse("elasto_op_residual_norm: null arguments");
+  const elasto_residual_norm_args& a = *args;
+  auto type = [](int t) { return t == ELASTO_F32 || t == ELASTO_BF16 || t == ELASTO_F16; };
+  auto size = [](int t) { return t == ELASTO_F32 ? 4u : t == ELASTO_E4M3 ? 1u : 2u; };
+  auto kind = [](int n) { return n == ELASTO_NORM_NONE || n == ELASTO_NORM_RMS || n == ELASTO_NORM_LAYER; };
+  if (a.rows <= 0 || a.cols <= 0) return refuse("elasto_op_residual_norm: rows or cols");
+  if (a.cols > 16384) return refuse("elasto_op_residual_norm: more than 16384 columns", ELASTO_ERR_UNSUPPORTED);
+  if (!(a.eps >= 0.0f) || a.eps > 3.0e38f || !(a.x_factor >= -3.0e38f && a.x_factor <= 3.0e38f))
+    return refuse("elasto_op_residual_norm: eps or x_factor");
+  if (!type(a.x_type) || !a.x || !aligned(a.x, size(a.x_type)) || a.x_row < a.cols) return refuse("elasto_op_residual_norm: x (type, null, alignment or stride)");
+  if (a.y && (!type(a.y_type) || !aligned(a.y, size(a.y_type)) || a.y_row < a.cols))
+    return refuse("elasto_op_residual_norm: y (type, alignment or stride)");
+  if (!a.x_out && !a.z) return refuse("elasto_op_residual_norm: no output");
+  if (a.x_out && (!aligned(a.x_out, size(a.x_type)) || a.x_out_row < a.cols)) return refuse("elasto_op_residual_norm: x_out (alignment or stride)");
+  if (a.z && ((!type(a.z_type) && a.z_type != ELASTO_E4M3) || !aligned(a.z, size(a.z_type)) || a.z_row < a.cols))
+    return refuse("elasto_op_residual_norm: z (type, alignment or stride)");
+  const bool fp8 = a.z && a.z_type == ELASTO_E4M3;
+  if (fp8 && (!a.z_scale || !aligned(a.z_scale, 4) || a.z_scale_row < a.rows))
+    return refuse("elasto_op_residual_norm: z_scale (null, alignment or stride)");
+  if (!kind(a.post_norm) || !kind(a.pre_norm)) return refuse("elasto_op_residual_norm: post_norm or pre_norm");
+  for (const float* p : {a.post_gain, a.post_bias, a.y_scale, a.pre_gain, a.pre_bias})
+    if (!aligned(p, 4)) return refuse("elasto_op_residual_norm: a gain, a bias or y_scale misaligned");
+  if (a.groups < 0 || !aligned(a.group, 4)) return refuse("elasto_op_residual_norm: groups or group");
+  if (a.groups == 0 && (a.group || a.gate || a.shift || a.scale)) return refuse("elasto_op_residual_norm: group or tables with groups 0");
+  if (a.gate || a.shift || a.scale) {
+    if (!type(a.mod_type) || a.mod_row < a.cols) return refuse("elasto_op_residual_norm: mod_type or mod_row");
+    for (const void* p : {a.gate, a.shift, a.scale})
+      if (!aligned(p, size(a.mod_type))) return refuse("elasto_op_residual_norm: gate, shift or scale misaligned");
+  }
+  if (a.x_out == a.x && a.x_out_row != a.x_row) return refuse("elasto_op_residual_norm: x_out is x with another row stride");
+  const void* const inputs[] = {a.x, a.y, a.post_gain, a.post_bias, a.y_scale, a.pre_gain, a.pre_bias, a.group, a.gate, a.shift, a.scale};
+  for (const void* p : inputs)
+    if (p && ((p == a.x_out && p != a.x) || p == a.z || (fp8 && p == a.z_scale)))
+      return refuse("elasto_op_residual_norm: an output that is an input");
+  if ((a.z && a.z == a.x_out) || (fp8 && (a.z_scale == a.z || a.z_scale == a.x_out)) || (a.y && a.y == a.x_out))
+    return refuse("elasto_op_residual_norm: two outputs, or y and x_out, are one");
+  elasto_status st = check_device();
+  if (st != ELASTO_OK) return st;
+  ELASTO_CUDA_TRY(residual_norm_launch(a, status_device, static_cast<cudaStream_t>(stream)));
   return ELASTO_OK;
 }
 
