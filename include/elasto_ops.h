@@ -15,6 +15,8 @@
 #ifndef ELASTO_OPS_H
 #define ELASTO_OPS_H
 
+#include <stddef.h>
+
 #include "elasto.h"
 
 #ifdef __cplusplus
@@ -338,6 +340,66 @@ typedef struct {
   int n_slots;
 } elasto_qk_norm_rope_axes_args;
 elasto_status elasto_op_qk_norm_rope_axes(void* stream, const elasto_qk_norm_rope_axes_args* args, int* status_device);
+
+/* Attention of `batch` sequences that share long prefixes: each sees all keys of its prefix, which are read once
+ * for all sequences that share it, and behind them keys of its own, causally. Query i of a sequence with nq queries and
+ * nk keys of its own sees prefix keys 0 to prefix_len - 1 and own keys j <= nk - nq + i (none where that is negative).
+ *   out = softmax over the visible keys of (scale q . k), times v;
+ * a query that sees nothing gets zeros. What lies behind prefix_len or at hidden places is not used, NaN and infinities
+ * included. A channel in which a query sees infinite or NaN values gets the sum of these, however
+ * small their probabilities (NaN in any case where a score is NaN or +infinity, or all are -infinity).
+ * Heads, types, scale and accuracy as elasto_op_window_attention has them.
+ * Queries: sequence b has the rows q_start[b] to q_start[b + 1] of q and out, at most max_queries; q_start NULL:
+ *   max_queries rows each, one sequence after another. q and out have q_rows rows (at most 2^30, as prefix_rows and kv_rows).
+ * Prefixes: prefix g is shared by sequences seq_start[g] to seq_start[g + 1] - 1 (seq_start NULL: one prefix, all
+ *   sequences); its keys are the first prefix_len[g] rows (NULL: max_prefix) of prefix_k + g * prefix_k_batch, and so on
+ *   for v. At most max_prefix of them, max_prefix <= prefix_rows. Sequences in no prefix's range have their own keys only.
+ * Own keys: packed, the rows kv_start[b] to kv_start[b + 1] of k and v, which have kv_rows rows; or (kv_start NULL) in
+ *   a cache of kv_rows rows per sequence, k_batch and v_batch apart, the first kv_len[b] of them (kv_len NULL: max_keys). At
+ *   most max_keys each; max_keys <= kv_rows. max_keys 0: none, and k, v, kv_rows and their strides are not used.
+ * q_start and seq_start ascend. Lengths on the device past these limits are cut to them; nothing is read or
+ * written outside them. Rows of out that belong to no sequence are left as they were.
+ * workspace: elasto_op_prefix_attention_workspace's bytes on the device, 16-byte aligned, for the results of the
+ * prefixes' parts; what is there before and after a call does not matter. Calls that may run at the same time (on
+ * several streams, in graphs replayed side by side) need workspaces of their own. Results are joined in a fixed order.
+ * *status_device is set to ELASTO_ERR_TIMEOUT if a device-side wait gives up.
+ * Strides of q, k, v and out are multiples of 8, the data is 16-byte aligned. out and the workspace may not overlap
+ * the inputs or one another. */
+typedef struct {
+  int dtype; /* of q, k, v and out: ELASTO_BF16 or ELASTO_F16 */
+  int batch, heads, heads_kv, head_dim;
+  float scale; /* > 0, at most 2.3e38 */
+  int max_queries;
+  long long q_rows;
+  const int32_t* q_start; /* [batch + 1] or NULL */
+  const void* q;
+  long long q_row, q_head;
+  void* out;
+  long long out_row, out_head;
+  int prefixes;
+  const int32_t* seq_start; /* [prefixes + 1], or NULL with one prefix */
+  int max_prefix;           /* >= 1 */
+  long long prefix_rows;
+  const int32_t* prefix_len; /* [prefixes] or NULL */
+  const void* prefix_k;
+  long long prefix_k_batch, prefix_k_row, prefix_k_head;
+  const void* prefix_v;
+  long long prefix_v_batch, prefix_v_row, prefix_v_head;
+  int max_keys;
+  long long kv_rows;
+  const int32_t* kv_start; /* [batch + 1] or NULL */
+  const int32_t* kv_len;   /* [batch] or NULL; only without kv_start */
+  const void* k;
+  long long k_batch, k_row, k_head;
+  const void* v;
+  long long v_batch, v_row, v_head;
+  void* workspace;
+  size_t workspace_bytes;
+} elasto_prefix_attention_args;
+elasto_status elasto_op_prefix_attention(void* stream, const elasto_prefix_attention_args* args, int* status_device);
+/* The bytes of workspace that a call with these sizes needs on the current device (of args the sizes alone are
+ * read, no pointer but whether seq_start is NULL). Nothing is launched. */
+elasto_status elasto_op_prefix_attention_workspace(const elasto_prefix_attention_args* args, size_t* bytes);
 
 /* Self-test of the bounded device-side wait that every kernel above (and the
  * forward's kernels) uses instead of an unbounded spin: one thread waits on an

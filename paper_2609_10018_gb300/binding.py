@@ -110,6 +110,22 @@ class QkNormRopeAxes(ctypes.Structure):
                  ("positions_axis", c_longlong), ("slots", c_void_p), ("n_slots", c_int)])
 
 
+def _keys(*names):
+    """(data, stride of sequences, of rows, of heads) fields of each tensor of keys or values."""
+    return [f for n in names for f in ((n, c_void_p), (n + "_batch", c_longlong), (n + "_row", c_longlong), (n + "_head", c_longlong))]
+
+
+class PrefixAttention(ctypes.Structure):
+    """elasto_prefix_attention_args."""
+    _fields_ = ([(f, c_int) for f in ("dtype", "batch", "heads", "heads_kv", "head_dim")] +
+                [("scale", ctypes.c_float), ("max_queries", c_int), ("q_rows", c_longlong), ("q_start", c_void_p)] +
+                _strided("q", "out") +
+                [("prefixes", c_int), ("seq_start", c_void_p), ("max_prefix", c_int), ("prefix_rows", c_longlong), ("prefix_len", c_void_p)] +
+                _keys("prefix_k", "prefix_v") +
+                [("max_keys", c_int), ("kv_rows", c_longlong), ("kv_start", c_void_p), ("kv_len", c_void_p)] + _keys("k", "v") +
+                [("workspace", c_void_p), ("workspace_bytes", c_size_t)])
+
+
 class ElastoError(RuntimeError):
     def __init__(self, status: int, where: str, msg: str):
         super().__init__(f"{where} failed with status {status}: {msg}")
@@ -170,6 +186,8 @@ def lib() -> ctypes.CDLL:
         "elasto_op_residual_norm": [c_void_p, ctypes.POINTER(ResidualNorm), c_void_p],
         "elasto_op_qk_norm_rope_axes": [c_void_p, ctypes.POINTER(QkNormRopeAxes), c_void_p],
         "elasto_op_window_attention": [c_void_p, ctypes.POINTER(WindowAttention), c_void_p],
+        "elasto_op_prefix_attention": [c_void_p, ctypes.POINTER(PrefixAttention), c_void_p],
+        "elasto_op_prefix_attention_workspace": [ctypes.POINTER(PrefixAttention), ctypes.POINTER(c_size_t)],
         "elasto_op_bounded_wait": [c_void_p, c_int, c_void_p, c_void_p],
         "elasto_op_grid_barrier": [c_void_p, c_int, c_void_p, c_void_p, c_void_p],
     }
@@ -511,6 +529,16 @@ def elasto_op_qk_norm_rope_axes(stream, args: QkNormRopeAxes, status=0) -> None:
 
 def elasto_op_window_attention(stream, args: WindowAttention, status=0) -> None:
     _check(lib().elasto_op_window_attention(stream, args, status), "elasto_op_window_attention")
+
+
+def elasto_op_prefix_attention(stream, args: PrefixAttention, status=0) -> None:
+    _check(lib().elasto_op_prefix_attention(stream, args, status), "elasto_op_prefix_attention")
+
+
+def elasto_op_prefix_attention_workspace(args: PrefixAttention) -> int:
+    n = c_size_t()
+    _check(lib().elasto_op_prefix_attention_workspace(args, ctypes.byref(n)), "elasto_op_prefix_attention_workspace")
+    return n.value
 
 
 def elasto_op_bounded_wait(stream, armed: bool, status, elapsed_ns) -> None:

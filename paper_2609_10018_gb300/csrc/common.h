@@ -393,6 +393,8 @@ inline float sum_headroom(bool bf, int keys) {
   while ((1LL << log2) < keys) ++log2;
   return bf ? 9.0f + log2 : 0.0f;
 }
+elasto_status prefix_attention_launch(const elasto_prefix_attention_args& a, int* status, cudaStream_t s);
+elasto_status prefix_attention_workspace(const elasto_prefix_attention_args& a, size_t* bytes);
 // The single-token form (max_queries == 1).
 elasto_status window_decode_launch(const elasto_window_attention_args& a, int* status, cudaStream_t s);
 

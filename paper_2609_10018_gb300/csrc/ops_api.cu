@@ -52,6 +52,21 @@ elasto_status check_qk_norm_rope(const ROPE& a, const char* call) {
   return ELASTO_OK;
 }
 
+// The sizes of a call with shared prefixes (what its workspace depends on).
+elasto_status check_prefix_sizes(const elasto_prefix_attention_args& a, const char* call) {
+  auto no = [&](const char* what, elasto_status st = ELASTO_ERR_INVALID_ARG) { return refuse((std::string(call) + what).c_str(), st); };
+  if (a.dtype != ELASTO_BF16 && a.dtype != ELASTO_F16) return no(": dtype");
+  if (a.batch <= 0 || a.heads <= 0 || a.heads_kv <= 0 || a.heads % a.heads_kv != 0 || a.max_queries <= 0 || a.max_prefix <= 0 || a.max_keys < 0)
+    return no(": batch, heads, max_queries, max_prefix or max_keys");
+  if (a.head_dim <= 0 || a.head_dim % 8 != 0 || a.head_dim > 128)
+    return no(": head_dim must be a multiple of 8 up to 128", ELASTO_ERR_UNSUPPORTED);
+  if (a.prefixes <= 0 || (a.prefixes > 1 && !a.seq_start)) return no(": prefixes, or several without seq_start");
+  if (a.q_rows <= 0 || a.q_rows > 1 << 30 || a.prefix_rows <= 0 || a.prefix_rows > 1 << 30 || a.max_prefix > a.prefix_rows)
+    return no(": q_rows or prefix_rows");
+  if (a.max_keys > 0 && (a.kv_rows <= 0 || a.kv_rows > 1 << 30 || a.max_keys > a.kv_rows)) return no(": kv_rows");
+  return ELASTO_OK;
+}
+
 // The bounded wait every kernel uses (mbar_wait: a time limit, then false),
 // on an mbarrier of one arrival. armed != 0: that arrival is made first, so
 // the wait returns at once; armed == 0: nothing ever arrives, the wait gives
@@ -360,6 +375,48 @@ elasto_status elasto_op_window_attention(void* stream, const elasto_window_atten
   if (st != ELASTO_OK) return st;
   if (a.max_queries == 1) return window_decode_launch(a, status_device, static_cast<cudaStream_t>(stream));
   return window_attention_launch(a, status_device, static_cast<cudaStream_t>(stream));
+}
+
+elasto_status elasto_op_prefix_attention_workspace(const elasto_prefix_attention_args* args, size_t* bytes) {
+  clear_error();
+  if (!args || !bytes) return refuse("elasto_op_prefix_attention_workspace: null arguments");
+  elasto_status st = check_prefix_sizes(*args, "elasto_op_prefix_attention_workspace");
+  if (st != ELASTO_OK) return st;
+  st = check_device();
+  if (st != ELASTO_OK) return st;
+  return prefix_attention_workspace(*args, bytes);
+}
+
+elasto_status elasto_op_prefix_attention(void* stream, const elasto_prefix_attention_args* args, int* status_device) {
+  clear_error();
+  if (!args) return refuse("elasto_op_prefix_attention: null arguments");
+  const elasto_prefix_attention_args& a = *args;
+  elasto_status st = check_prefix_sizes(a, "elasto_op_prefix_attention");
+  if (st != ELASTO_OK) return st;
+  if (!(a.scale > 0.0f) || a.scale > 2.3e38f) return refuse("elasto_op_prefix_attention: scale");
+  if (!tensor16(a.q, a.q_row, a.q_head) || !tensor16(a.out, a.out_row, a.out_head))
+    return refuse("elasto_op_prefix_attention: q or out (null, alignment or strides)");
+  if (!tensor16(a.prefix_k, a.prefix_k_row, a.prefix_k_head) || !tensor16(a.prefix_v, a.prefix_v_row, a.prefix_v_head) ||
+      !strides8(a.prefix_k_batch, a.prefix_v_batch))
+    return refuse("elasto_op_prefix_attention: prefix_k or prefix_v (null, alignment or strides)");
+  if (!a.q_start && static_cast<long long>(a.batch) * a.max_queries > a.q_rows)
+    return refuse("elasto_op_prefix_attention: q_rows is less than batch * max_queries");
+  if (a.max_keys > 0) {
+    if (!tensor16(a.k, a.k_row, a.k_head) || !tensor16(a.v, a.v_row, a.v_head) || !strides8(a.k_batch, a.v_batch))
+      return refuse("elasto_op_prefix_attention: k or v (null, alignment or strides)");
+    if (a.kv_start && a.kv_len) return refuse("elasto_op_prefix_attention: kv_start and kv_len exclude one another");
+    if (a.out == a.k || a.out == a.v || a.workspace == a.k || a.workspace == a.v)
+      return refuse("elasto_op_prefix_attention: out or the workspace is an input");
+  }
+  if (!aligned(a.q_start, 4) || !aligned(a.seq_start, 4) || !aligned(a.prefix_len, 4) || !aligned(a.kv_start, 4) || !aligned(a.kv_len, 4))
+    return refuse("elasto_op_prefix_attention: starts or lengths misaligned");
+  if (a.out == a.q || a.out == a.prefix_k || a.out == a.prefix_v || a.workspace == a.out || a.workspace == a.q || a.workspace == a.prefix_k ||
+      a.workspace == a.prefix_v)
+    return refuse("elasto_op_prefix_attention: out or the workspace is an input, or both are one");
+  if (!a.workspace || !aligned(a.workspace, 16)) return refuse("elasto_op_prefix_attention: workspace (null or alignment)");
+  st = check_device();
+  if (st != ELASTO_OK) return st;
+  return prefix_attention_launch(a, status_device, static_cast<cudaStream_t>(stream));
 }
 
 elasto_status elasto_op_softmax(void* stream, const float* x, float* y, int rows, int cols) {

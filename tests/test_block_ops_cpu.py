@@ -99,3 +99,62 @@ def test_reference_rotation_by_axes(pairing):
     assert abs(a - b) <= 1e-12 * abs(a) + 1e-12 and abs(a - c) > 1e-6
     channels = sorted(c for pair in block.channels(axis_of, pairing) for c in pair)
     assert channels == list(range(48))
+
+
+def _prefix(lib, call="elasto_op_prefix_attention", **kw):
+    a = dict(dtype=binding.BF16, batch=2, heads=4, heads_kv=2, head_dim=64, scale=0.125, max_queries=5, q_rows=10, q=P, q_row=256,
+             q_head=64, out=2 * P, out_row=256, out_head=64, prefixes=2, seq_start=3 * P, max_prefix=9, prefix_rows=12, prefix_k=4 * P,
+             prefix_k_batch=2048, prefix_k_row=128, prefix_k_head=64, prefix_v=5 * P, prefix_v_batch=2048, prefix_v_row=128, prefix_v_head=64,
+             max_keys=9, kv_rows=12, k=6 * P, k_batch=2048, k_row=128, k_head=64, v=7 * P, v_batch=2048, v_row=128, v_head=64,
+             workspace=8 * P, workspace_bytes=1 << 30) | kw
+    return lib.elasto_op_prefix_attention(None, ctypes.byref(binding.PrefixAttention(**a)), None)
+
+
+SIZES = [dict(dtype=binding.F32), dict(batch=0), dict(heads=0), dict(heads_kv=0), dict(heads_kv=3), dict(max_queries=0), dict(max_prefix=0),
+         dict(max_prefix=13), dict(max_keys=-1), dict(max_keys=13), dict(kv_rows=0), dict(q_rows=0), dict(q_rows=(1 << 30) + 1),
+         dict(prefix_rows=0), dict(prefix_rows=(1 << 30) + 1), dict(kv_rows=(1 << 30) + 1), dict(prefixes=0), dict(seq_start=None)]
+
+
+@pytest.mark.parametrize("kw", SIZES + [
+    dict(q_rows=9), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.nan), dict(scale=2.4e38), dict(q=None), dict(out=None),
+    dict(prefix_k=None), dict(prefix_v=None), dict(k=None), dict(v=None), dict(q=P + 8), dict(out_row=250), dict(prefix_k_row=1),
+    dict(prefix_v_batch=4), dict(prefix_k_head=-8), dict(k_batch=1), dict(v_head=-8), dict(kv_start=P, kv_len=P), dict(q_start=P + 1),
+    dict(seq_start=P + 2), dict(prefix_len=P + 1), dict(kv_start=P + 2), dict(kv_len=P + 3), dict(workspace=None), dict(workspace=8 * P + 8),
+    dict(out=P), dict(out=4 * P), dict(out=5 * P), dict(out=6 * P), dict(out=7 * P), dict(workspace=P), dict(workspace=2 * P),
+    dict(workspace=4 * P), dict(workspace=7 * P)])
+def test_prefix_attention_refusals(lib, kw):  # noqa: F811
+    assert _prefix(lib, **kw) == binding.ERR_INVALID_ARG
+    assert "elasto_op_prefix_attention" in binding.elasto_last_error()
+
+
+@pytest.mark.parametrize("kw", [dict(head_dim=60), dict(head_dim=136), dict(head_dim=0)])
+def test_prefix_attention_unsupported(lib, kw):  # noqa: F811
+    assert _prefix(lib, **kw) == binding.ERR_UNSUPPORTED
+    assert lib.elasto_op_prefix_attention(None, None, None) == binding.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("kw", SIZES)
+def test_prefix_workspace_refusals(lib, kw):  # noqa: F811
+    a = dict(dtype=binding.BF16, batch=2, heads=4, heads_kv=2, head_dim=64, max_queries=5, q_rows=10, prefixes=2, seq_start=P, max_prefix=9,
+             prefix_rows=12, max_keys=9, kv_rows=12) | kw
+    n = ctypes.c_size_t()
+    assert lib.elasto_op_prefix_attention_workspace(ctypes.byref(binding.PrefixAttention(**a)), ctypes.byref(n)) == binding.ERR_INVALID_ARG
+    assert "elasto_op_prefix_attention_workspace" in binding.elasto_last_error()
+    assert lib.elasto_op_prefix_attention_workspace(None, ctypes.byref(n)) == binding.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("nq,nk,p", [(1, 5, 7), (4, 4, 3), (6, 2, 5), (3, 0, 4), (2, 1, 0)])
+def test_reference_prefix_attention(nq, nk, p):
+    """Behind a prefix whose keys are the first of one sequence: torch's own attention with that mask."""
+    g = torch.Generator().manual_seed(3)
+    q, k, v = (torch.randn((n, h, 8), generator=g, dtype=torch.float64) for n, h in ((nq, 4), (nk, 2), (nk, 2)))
+    pk, pv = torch.randn((p, 2, 8), generator=g, dtype=torch.float64), torch.randn((p, 2, 8), generator=g, dtype=torch.float64)
+    got, _ = block.prefix_attention(q, k, v, pk, pv, 0.5)
+    j = torch.arange(p + nk)
+    seen = j[None] <= (p + nk - nq + torch.arange(nq))[:, None]
+    seen[:, :p] = True
+    kk, vv = torch.cat([pk, k]).repeat_interleave(2, 1), torch.cat([pv, v]).repeat_interleave(2, 1)
+    rows = seen.any(1)
+    want = torch.nn.functional.scaled_dot_product_attention(q.transpose(0, 1)[:, rows], kk.transpose(0, 1), vv.transpose(0, 1), seen[rows], scale=0.5)
+    assert torch.allclose(got[rows], want.transpose(0, 1), atol=1e-12)
+    assert (got[~rows] == 0).all()
