@@ -3,8 +3,8 @@
 //
 //   m = max_j s_j,  l = sum_j exp(s_j - m),  o = sum_j exp(s_j - m) v_j,  s_j = scale q . k_j
 //
-// over a part of the prefix's keys, for every query head of every sequence; prefix_own.cu joins the parts with the
-// sequences' own keys. All queries see all keys of their prefix, so there are no masks but at its end, and the queries of
+// over a part of the prefix's keys, for every query head of every sequence; prefix_own.cu does the same with the
+// sequences' own keys and joins the parts. All queries see all keys of their prefix, so there are no masks but at its end, and the queries of
 // all its sequences are rows of the same tiles.
 //
 // A tile is 128 rows of Q: the hg query heads that share a key head, times 128 / hg consecutive queries. An item is two
@@ -29,7 +29,7 @@ namespace {
 
 constexpr int THREADS = 384;
 // Registers of a thread: at launch, of the four producer and MMA warps, of the eight softmax warps.
-constexpr int REGS = 168, REGS_FEW = 56, REGS_MANY = 224;
+constexpr int REGS = 168, REGS_FEW = 88, REGS_MANY = 208;
 static_assert(128 * REGS_FEW + 256 * REGS_MANY <= THREADS * REGS, "register split");
 constexpr int QT = kPrefixTile, KT = kPrefixTile;
 constexpr int HALF = 128 * 128;  // bytes of 128 rows of 64 16-bit values
@@ -168,9 +168,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   const int len = warp_uniform(found->len), tiles = (len + KT - 1) / KT;
   const int begin = prefix < 0 ? 0 : split_from(tiles, rank, a.split), end = prefix < 0 ? 0 : split_from(tiles, rank + 1, a.split);
   const int pair = a.pair;
-  // group g takes key tile t, and which rows: from + g * qpt on (pair: the same)
+  // group g's rows: from + g * qpt on (pair: the same rows, every other key tile)
   const bool second = pair || from + a.qpt < to;  // group 1 has rows
-  auto needs = [&](int g, int t) { return pair ? ((t - begin) & 1) == g : g == 0 || second; };
   const int left = len - (end - 1) * KT;  // keys of the last tile, where it is the prefix's
   const bool cut = end == tiles && left < KT;
 
@@ -308,9 +307,18 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t s_tm = tmem + lanes + g * KT, o_tm = tmem + lanes + O_COL + g * DP;
     const float sc = a.scale_log2;
-    const int q = r * a.by_hg >> 16, head = r - q * a.hg, first = from + (pair ? 0 : g) * a.qpt;
-    const bool mine = q < a.qpt && first + q < to && head < nheads;
-    const float lazy = mine ? kLazy : INFINITY;  // (rows without a query have no vote on rescaling)
+    auto place = [&](int& query, int& head) {  // of this row; false: it has none
+      const int q = r * a.by_hg >> 16;
+      head = r - q * a.hg, query = from + (pair ? 0 : g) * a.qpt + q;
+      return q < a.qpt && query < to && head < nheads;
+    };
+    float lazy = kLazy;
+    {
+      int query, head;
+      if (!place(query, head)) lazy = INFINITY;  // (rows without a query have no vote on rescaling)
+    }
+    const uint32_t count = pair ? (end - begin + 1 - g) / 2 : g == 0 || second ? end - begin : 0;  // of this group's key tiles
+    const bool last_cut = cut && count > 0 && (!pair || ((end - 1 - begin) & 1) == g);
     float m = -INFINITY, sum = 0.0f;
     uint32_t ns = 0;
     bool ok = true;
@@ -385,17 +393,20 @@ __global__ void __launch_bounds__(THREADS, 1)
       if (lane == 0) mbar_arrive(&p_full[g]);
       return true;
     };
-    for (int t = begin; t < end && ok; ++t)
-      if (needs(g, t)) ok = cut && t == end - 1 ? tile(std::true_type()) : tile(std::false_type());
+    for (uint32_t n = last_cut ? 1 : 0; n < count && ok; ++n) ok = tile(std::false_type());
+    if (last_cut && ok) ok = tile(std::true_type());
     // ------------------------------------------------------------ the part's results
     if (ok && ns > 0) {
       ok = __all_sync(0xffffffffu, mbar_wait<true>(&o_full[g], 0));
       tc_fence_after();
     }
     if (ok && ns > 0) {
+      int query, head;
+      const bool mine = place(query, head);
       const int part = pair ? 2 * rank + g : rank;
-      const long long rho = static_cast<long long>(first + q) * a.hg + head;
+      const long long rho = static_cast<long long>(query) * a.hg + head;
       if (mine) *reinterpret_cast<float2*>(a.parts.stat + a.parts.stat_at(part, h, rho)) = make_float2(m, sum);
+      float* const sums = a.parts.sums + a.parts.sums_at(part, h, rho);
 #pragma unroll 1
       for (int c = 0; c < DP; c += 32) {
         uint32_t o[32];
@@ -404,7 +415,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
         for (int j = 0; j < 8; ++j)
           if (mine && c + 4 * j < a.head_dim)
-            *reinterpret_cast<uint4*>(a.parts.sums + a.parts.sums_at(part, h, c / 4 + j, rho)) = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+            *reinterpret_cast<uint4*>(sums + (c / 4 + j) * kQuadStep) = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
       }
       tc_fence_before();
     }
@@ -440,15 +451,20 @@ int64_t queries(const elasto_prefix_attention_args& u) {
   return u.q_start ? u.q_rows : std::min<int64_t>(most, u.q_rows);
 }
 PrefixPlan plan_of(const elasto_prefix_attention_args& u) {
-  const int64_t most = queries(u), rows = std::min<int64_t>(most, static_cast<int64_t>(u.batch) * u.max_queries);
-  return prefix_plan(rows, most, u.prefixes, u.heads / u.heads_kv, u.heads_kv, u.max_prefix, u.head_dim, num_sms() > 0 ? num_sms() : 152);
+  PrefixSizes z;
+  z.most = queries(u), z.rows = std::min<int64_t>(z.most, static_cast<int64_t>(u.batch) * u.max_queries);
+  z.batch = u.batch, z.max_queries = static_cast<int>(std::min<int64_t>(u.max_queries, u.q_rows)), z.prefixes = u.prefixes;
+  z.group = u.heads / u.heads_kv, z.heads_kv = u.heads_kv, z.head_dim = u.head_dim;
+  z.max_prefix = u.max_prefix, z.max_keys = u.max_keys, z.sms = num_sms() > 0 ? num_sms() : 152;
+  return prefix_plan(z);
 }
+int64_t part_rows(const elasto_prefix_attention_args& u, const PrefixPlan& p) { return (queries(u) * p.hg + 31) & ~int64_t(31); }
 // Floats of the parts' statistics and sums.
 int64_t stat_floats(const elasto_prefix_attention_args& u, const PrefixPlan& p) {
-  return (2 * p.parts() * static_cast<int64_t>(u.heads_kv) * p.nsub * queries(u) * p.hg + 3) & ~int64_t(3);
+  return 2 * p.parts() * static_cast<int64_t>(u.heads_kv) * p.nsub * part_rows(u, p);
 }
 int64_t sums_floats(const elasto_prefix_attention_args& u, const PrefixPlan& p) {
-  return p.parts() * static_cast<int64_t>(u.heads_kv) * p.nsub * queries(u) * p.hg * u.head_dim;
+  return p.parts() * static_cast<int64_t>(u.heads_kv) * p.nsub * part_rows(u, p) * u.head_dim;
 }
 
 }  // namespace
@@ -461,6 +477,10 @@ elasto_status prefix_attention_workspace(const elasto_prefix_attention_args& u, 
 
 elasto_status prefix_attention_launch(const elasto_prefix_attention_args& u, int* status, cudaStream_t s) {
   static DeviceOnce once;
+  if (static_cast<int64_t>(std::min<int64_t>(u.max_queries, u.q_rows)) * (u.heads / u.heads_kv) > 0x3fffffff) {
+    set_error("elasto_op_prefix_attention: too many queries");
+    return ELASTO_ERR_UNSUPPORTED;
+  }
   const PrefixPlan p = plan_of(u);
   size_t bytes = 0;
   prefix_attention_workspace(u, &bytes);
@@ -484,7 +504,7 @@ elasto_status prefix_attention_launch(const elasto_prefix_attention_args& u, int
     return ELASTO_ERR_UNSUPPORTED;
   }
   a.by_items = Divisor(static_cast<unsigned>(p.items)), a.by_hs = Divisor(hs);
-  a.parts = {static_cast<float*>(u.workspace) + stat_floats(u, p), static_cast<float*>(u.workspace), queries(u) * p.hg, hs, u.head_dim / 4};
+  a.parts = {static_cast<float*>(u.workspace) + stat_floats(u, p), static_cast<float*>(u.workspace), part_rows(u, p), hs, u.head_dim / 4};
   a.status = status;
   const bool bf = u.dtype == ELASTO_BF16;
   auto keys = [&](CUtensorMap* tm, const void* data, long long head_s, long long row_s, long long batch_s) {
@@ -503,7 +523,7 @@ elasto_status prefix_attention_launch(const elasto_prefix_attention_args& u, int
     set_error("elasto_op_prefix_attention: cuTensorMapEncodeTiled failed (alignment, strides or size)");
     return ELASTO_ERR_UNSUPPORTED;
   }
-  // (the second kernel's checks come before the first is launched)
+  // (the other kernels' checks come before the first is launched)
   PrefixOwn own;
   elasto_status st = prefix_own_plan(u, p, a.parts, a.down, status, &own);
   if (st != ELASTO_OK) return st;

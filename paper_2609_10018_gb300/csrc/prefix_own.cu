@@ -1,22 +1,21 @@
-// Attention behind shared prefixes: the sequences' own keys, joined with the parts that prefix_attention.cu left.
+// Attention behind shared prefixes: the sequences' own keys, and the join of all parts.
 //
-// A block is 16 or 64 rows (query, head) of one sequence and key head; a cluster of CTAs takes it, the own keys in tiles
-// of 64 shared out over the CTAs. In a CTA warp 4 streams K and V tiles by TMA through a ring, and warps 0-3 form
-// S = Q K^T and O += P V by m16n8k16 products, running maximum and sum of the softmax for themselves:
+// prefix_own_kernel: a block is 16 or 64 rows (query, head) of one sequence and key head; its own keys, in tiles of 64, are
+// shared out over own_split CTAs, each of which leaves a part as prefix_attention.cu's CTAs do. Warp 4 streams K and V
+// tiles by TMA through a ring, and warps 0-3 form S = Q K^T and O += P V by m16n8k16 products, running maximum and sum
+// of the softmax for themselves:
 //   16 rows (single tokens and few): a warp takes 16 keys of each tile, all rows;
 //   64 rows (longer runs of tokens): a warp takes 16 rows, all keys.
-// (tcgen05 would need 128 rows of one sequence: the prefix, where most of the work lies, has them.) Then the warps' results
-// are joined in shared memory, the CTAs' through distributed shared memory, and the prefix's parts, in a fixed order.
-// This kernel starts while the prefixes' runs out (programmatic launch) and waits for it only before it reads the parts.
+// (tcgen05 would need 128 rows of one sequence: the prefix, where most of the work lies, has them.) It does not wait for
+// the prefixes' kernel: both run at the same time, that one bound by its products, this one by reading the keys and values
+// once. Only its last CTA waits before it ends, so that what waits for this kernel waits for both.
 //
-// Bound by reading the own keys and values once.
+// prefix_join_kernel: out = sum over parts of o exp(m - top) / sum of l exp(m - top), four channels a thread, in a fixed order.
 #include <algorithm>
-#include <atomic>
 #include <type_traits>
 
 #include "prefix_own.h"
 #include "ptx.cuh"
-#include "window_cluster.h"
 
 namespace elasto {
 
@@ -24,14 +23,17 @@ namespace {
 
 constexpr int KT = 64, WARPS = 4, THREADS = 32 * (WARPS + 1);
 constexpr int HALF = KT * 128;  // bytes of 64 keys of 64 channels
-constexpr int MAX_CLUSTER = 8;
+constexpr int JOIN_THREADS = 256;
+static_assert(4 * 64 * (2 * kPrefixSplit + kOwnSplit) <= 40 * 1024, "the join's weights");
 constexpr float kLazy = 8.0f;  // log2 of how far a maximum may grow before O is rescaled
 
 template <int DP, bool MANY>
 struct Shape {
   static constexpr int rows = MANY ? 64 : 16;
   static constexpr int halves = DP / 64, tile = halves * HALF, stage = 2 * tile;
-  static constexpr int stages = DP == 128 ? 3 : 6;  // two CTAs an SM
+  // CTAs an SM: three, of the blocks of 64 rows (whose registers do not allow for it) two
+  static constexpr int ctas = MANY ? 2 : 3;
+  static constexpr int stages = (DP == 128 ? 1 : 2) * (MANY ? 3 : 2);
   static constexpr int smem = 1024 + stages * stage + 256;
   static constexpr int part = MANY ? 0 : WARPS * 16 * DP;  // floats of the warps' O, of the block's
   static_assert(stages * stage >= (part + rows * DP + 2 * rows + (MANY ? 0 : WARPS * 32)) * 4, "the results take the ring's place");
@@ -71,20 +73,13 @@ __device__ __forceinline__ uint32_t bad16(uint32_t w) {
   const uint32_t x = (w & e) ^ e;
   return ((x & 0xffffu) == 0 ? 0xffffu : 0u) | ((x >> 16) == 0 ? 0xffff0000u : 0u);
 }
-__device__ __forceinline__ float4 cluster_load4(uint32_t addr) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
-  return v;
-}
-__device__ __forceinline__ float2 cluster_load2(uint32_t addr) {
-  float2 v;
-  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr));
-  return v;
-}
-__device__ __forceinline__ int cluster_load_int(uint32_t addr) {
-  int v;
-  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(addr));
-  return v;
+// acc + 0 * w: NaN from the first infinite or NaN value on.
+template <bool BF>
+__device__ __forceinline__ void look16(uint32_t w, uint32_t& acc) {
+  if constexpr (BF)
+    asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(acc) : "r"(w), "r"(0u));
+  else
+    asm("fma.rn.f16x2 %0, %1, %2, %0;" : "+r"(acc) : "r"(w), "r"(0u));
 }
 
 // The sum of the infinite and NaN values among n keys of a channel (v: its first key).
@@ -100,25 +95,23 @@ __device__ __noinline__ float bad_values(const uint16_t* v, long long row, int n
   return sum;
 }
 
-// A softmax's running maximum, sum and four channels of its weighted sum.
-struct Joined {
-  float top, total;
-  float4 y;
-  // (a part without a finite score has sums of zeros, or NaN that must stay)
-  __device__ __forceinline__ void add(float2 st, float4 o, float f) {
-    const float w = st.x == -INFINITY ? 1.0f : f;
-    total = fmaf(st.y, w, total);
-    y.x = fmaf(o.x, w, y.x), y.y = fmaf(o.y, w, y.y), y.z = fmaf(o.z, w, y.z), y.w = fmaf(o.w, w, y.w);
+// Rows of q and own keys of sequence b, cut to what the host allows.
+__device__ __forceinline__ void sequence(const PrefixOwnArgs& a, int b, int& q0, int& nq, int& k0, int& nk) {
+  q0 = b * a.max_queries, nq = a.max_queries, k0 = 0, nk = a.max_keys;
+  if (a.q_start) {
+    q0 = min(max(a.q_start[b], 0), a.q_rows);
+    nq = min(max(min(a.q_start[b + 1], a.q_rows) - q0, 0), a.max_queries);
   }
-  __device__ __forceinline__ void rise(float to, float sc) {  // the maximum to at least `to`
-    const float t = fmaxf(top, to), f = top == -INFINITY ? 1.0f : ex2_approx((top - t) * sc);
-    total *= f, y.x *= f, y.y *= f, y.z *= f, y.w *= f;
-    top = t;
+  if (a.kv_start) {
+    k0 = min(max(a.kv_start[b], 0), a.kv_rows);
+    nk = min(max(min(a.kv_start[b + 1], a.kv_rows) - k0, 0), a.max_keys);
+  } else if (a.kv_len) {
+    nk = min(max(a.kv_len[b], 0), a.max_keys);
   }
-};
+}
 
 template <bool BF, int DP, bool MANY>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, Shape<DP, MANY>::ctas)
     prefix_own_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                       const __grid_constant__ PrefixOwnArgs a) {
   using T = Shape<DP, MANY>;
@@ -129,8 +122,7 @@ __global__ void __launch_bounds__(THREADS)
   uint64_t* empty = full + S;
   int* bad = reinterpret_cast<int*>(empty + S);  // values that some row sees have been left out
   const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
-  const int rank = static_cast<int>(blockIdx.x) % a.cluster;
-  const int unit = static_cast<int>(blockIdx.x) / a.cluster;
+  const int unit = static_cast<int>(a.by_split.quotient(blockIdx.x)), rank = static_cast<int>(blockIdx.x) - unit * a.own_split;
   const int u1 = static_cast<int>(a.by_blocks.quotient(unit)), blk = unit - u1 * a.blocks;
   const int b = static_cast<int>(a.by_heads_kv.quotient(u1)), kvh = u1 - b * a.heads_kv;
   if (threadIdx.x == 0) {
@@ -145,47 +137,21 @@ __global__ void __launch_bounds__(THREADS)
   }
   __syncthreads();
   pdl_trigger();
-  // Nothing but the parts is written by the kernel before, and that one waited for what came before it: the inputs may be
-  // read at once.
-
-  // the sequence, cut to what the host allows
-  int q0 = b * a.max_queries, nq = a.max_queries, k0 = 0, nk = a.max_keys;
-  if (a.q_start) {
-    q0 = min(max(a.q_start[b], 0), a.q_rows);
-    nq = min(max(min(a.q_start[b + 1], a.q_rows) - q0, 0), a.max_queries);
-  }
-  if (a.kv_start) {
-    k0 = min(max(a.kv_start[b], 0), a.kv_rows);
-    nk = min(max(min(a.kv_start[b + 1], a.kv_rows) - k0, 0), a.max_keys);
-  } else if (a.kv_len) {
-    nk = min(max(a.kv_len[b], 0), a.max_keys);
-  }
+  // The kernel before writes nothing but its parts, and waited for what came before it: the inputs may be read at once.
+  int q0, nq, k0, nk;
+  sequence(a, b, q0, nq, k0, nk);
   const int row0 = blk * ROWS, nrows = min(nq * a.group - row0, ROWS);
-  if (nrows <= 0) return;  // (the whole cluster)
-  // its prefix: the last g with seq_start[g] <= b
-  int prefix = 0, len = a.max_prefix;
-  if (a.seq_start) {
-    int lo = 0, hi = a.prefixes;  // seq_start[lo] <= b < seq_start[hi], if there is one
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (a.seq_start[mid] <= b)
-        lo = mid;
-      else
-        hi = mid;
-    }
-    prefix = a.seq_start[lo] <= b && b < a.seq_start[lo + 1] ? lo : -1;
+  if (nrows <= 0) {
+    if (blockIdx.x == gridDim.x - 1) pdl_wait();
+    return;
   }
-  if (prefix < 0)
-    len = 0;
-  else if (a.prefix_len)
-    len = min(max(a.prefix_len[prefix], 0), a.max_prefix);
 
   // visible own keys of a row of the block
   auto query = [&](int row) { return static_cast<int>(a.by_group.quotient(row0 + row)); };
   auto visible = [&](int row) { return row < nrows ? min(max(nk - nq + query(row) + 1, 0), nk) : 0; };
   const int most = visible(nrows - 1), least = visible(0);
   const int tiles = (most + KT - 1) / KT;
-  const int t0 = split_from(tiles, rank, a.cluster), t1 = split_from(tiles, rank + 1, a.cluster);
+  const int t0 = split_from(tiles, rank, a.own_split), t1 = split_from(tiles, rank + 1, a.own_split);
 
   float o[DP / 8][4], m[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f};
 #pragma unroll
@@ -245,22 +211,27 @@ __global__ void __launch_bounds__(THREADS)
       // do: 0 * NaN would reach those. (The rows that see these get them at the end.)
       if (whole < 16 * NS && left > 0) {
         const int from = max(whole, 0), thread = MANY ? static_cast<int>(threadIdx.x) : lane, threads = MANY ? 32 * WARPS : 32;
-        bool any = false;
-        for (int e = thread; e < (16 * NS - from) * (DP / 8); e += threads) {
-          const int key = from + e / (DP / 8), row = sub0 + key, piece = e % (DP / 8);
-          uint4* const p = reinterpret_cast<uint4*>(kb + T::tile + (piece >> 3) * HALF + row * 128 + (((piece & 7) ^ (row & 7)) << 4));
-          if (key >= left) {
+        auto piece = [&](int e) {
+          const int row = sub0 + from + e / (DP / 8), at = e % (DP / 8);
+          return reinterpret_cast<uint4*>(kb + T::tile + (at >> 3) * HALF + row * 128 + (((at & 7) ^ (row & 7)) << 4));
+        };
+        const int seen = (min(left, 16 * NS) - from) * (DP / 8), all = (16 * NS - from) * (DP / 8);
+        uint32_t acc = 0u;
+        for (int e = thread; e < all; e += threads) {
+          uint4* const p = piece(e);
+          if (e < seen)
+            look16<BF>(p->x, acc), look16<BF>(p->y, acc), look16<BF>(p->z, acc), look16<BF>(p->w, acc);
+          else
             *p = make_uint4(0u, 0u, 0u, 0u);
-          } else {
+        }
+        if (bad16<BF>(acc) != 0u) {
+          *bad = 1;
+          for (int e = thread; e < seen; e += threads) {
+            uint4* const p = piece(e);
             const uint4 w = *p;
-            const uint4 x = make_uint4(bad16<BF>(w.x), bad16<BF>(w.y), bad16<BF>(w.z), bad16<BF>(w.w));
-            if ((x.x | x.y | x.z | x.w) != 0u) {
-              *p = make_uint4(w.x & ~x.x, w.y & ~x.y, w.z & ~x.z, w.w & ~x.w);
-              any = true;
-            }
+            *p = make_uint4(w.x & ~bad16<BF>(w.x), w.y & ~bad16<BF>(w.y), w.z & ~bad16<BF>(w.z), w.w & ~bad16<BF>(w.w));
           }
         }
-        if (any) *bad = 1;
         fence_async_smem();  // (before the next tile is copied there)
         if (MANY)
           named_bar_sync(1, 32 * WARPS);
@@ -364,117 +335,217 @@ __global__ void __launch_bounds__(THREADS)
   __syncthreads();
   const int quads = a.head_dim / 4;
   const float sc = a.scale_log2;
-  if constexpr (!MANY) {
-    for (int e = threadIdx.x; e < quads * nrows; e += THREADS) {
-      const int quad = e / nrows, row = e - quad * nrows;
-      Joined x = {-INFINITY, 0.0f, make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
+  const bool left_out = *bad != 0;
+  // (a thread keeps its row: what the addresses of a row take is reckoned once)
+  const int row = threadIdx.x & (ROWS - 1);
+  if (row < nrows && threadIdx.x < THREADS / ROWS * ROWS) {
+    const int qi = query(row), head = row0 + row - qi * a.group, sub = head / a.hg, h = kvh * a.nsub + sub;
+    const long long rho = static_cast<long long>(q0 + qi) * a.hg + (head - sub * a.hg);
+    float* const sums = a.parts.sums + a.parts.sums_at(a.prefix_parts + rank, h, rho);
+    float f[WARPS];
+    float top = -INFINITY, total = 0.0f;
+    if constexpr (MANY) {
+      const float2 st = *reinterpret_cast<const float2*>(cta + 2 * row);
+      top = st.x, total = st.y;
+    } else {
 #pragma unroll
-      for (int w = 0; w < WARPS; ++w) x.top = fmaxf(x.top, stat[32 * w + 2 * row]);
+      for (int w = 0; w < WARPS; ++w) top = fmaxf(top, stat[32 * w + 2 * row]);
 #pragma unroll
       for (int w = 0; w < WARPS; ++w) {
         const float2 st = *reinterpret_cast<const float2*>(stat + 32 * w + 2 * row);
-        x.add(st, *reinterpret_cast<const float4*>(part + w * 16 * DP + (quad * ROWS + row) * 4), ex2_approx((st.x - x.top) * sc));
+        // (a part without a finite score has sums of zeros, or NaN that must stay)
+        f[w] = st.x == -INFINITY ? 1.0f : ex2_approx((st.x - top) * sc);
+        total = fmaf(st.y, f[w], total);
       }
-      *reinterpret_cast<float4*>(whole + (quad * ROWS + row) * 4) = x.y;
-      if (quad == 0) *reinterpret_cast<float2*>(cta + 2 * row) = make_float2(x.top, x.total);
     }
+    if (threadIdx.x < ROWS)
+      *reinterpret_cast<float2*>(a.parts.stat + a.parts.stat_at(a.prefix_parts + rank, h, rho)) = make_float2(top, left_out ? -total : total);
+    if (top != -INFINITY)
+      for (int quad = threadIdx.x / ROWS; quad < quads; quad += THREADS / ROWS) {
+        float4 y;
+        if constexpr (MANY) {
+          y = *reinterpret_cast<const float4*>(whole + (quad * ROWS + row) * 4);
+        } else {
+          y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+          for (int w = 0; w < WARPS; ++w) {
+            const float4 o4 = *reinterpret_cast<const float4*>(part + w * 16 * DP + (quad * ROWS + row) * 4);
+            y.x = fmaf(o4.x, f[w], y.x), y.y = fmaf(o4.y, f[w], y.y), y.z = fmaf(o4.z, f[w], y.z), y.w = fmaf(o4.w, f[w], y.w);
+          }
+        }
+        *reinterpret_cast<float4*>(sums + quad * kQuadStep) = y;
+      }
   }
-  if (a.cluster > 1)
-    cluster_sync_all();
-  else
-    __syncthreads();
-  pdl_wait();  // the prefix's parts
-  bool left_out = *bad != 0;
-  for (int k = 0; k < a.cluster && a.cluster > 1; ++k) left_out |= cluster_load_int(cluster_map(smem_addr(bad), k)) != 0;
-  const int key_tiles = (len + kPrefixTile - 1) / kPrefixTile, parts = a.pair ? 2 * a.split : a.split;
-  // (a part without key tiles has not been written)
-  auto written = [&](int part) {
-    const int r = a.pair ? part >> 1 : part, n = split_from(key_tiles, r + 1, a.split) - split_from(key_tiles, r, a.split);
-    return n > (a.pair ? part & 1 : 0);
-  };
-  for (int e = rank * THREADS + threadIdx.x; e < quads * nrows; e += a.cluster * THREADS) {
-    const int quad = e / nrows, row = e - quad * nrows, qi = query(row), head = row0 + row - qi * a.group;
-    const uint32_t ms = smem_addr(cta + 2 * row), ys = smem_addr(whole + (quad * ROWS + row) * 4);
-    Joined x = {-INFINITY, 0.0f, make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
-    if (a.cluster > 1) {
-      float2 st[MAX_CLUSTER];
-      float4 y[MAX_CLUSTER];
-#pragma unroll
-      for (int k = 0; k < MAX_CLUSTER; ++k)
-        if (k < a.cluster) st[k] = cluster_load2(cluster_map(ms, k)), y[k] = cluster_load4(cluster_map(ys, k));
-#pragma unroll
-      for (int k = 0; k < MAX_CLUSTER; ++k)
-        if (k < a.cluster) x.top = fmaxf(x.top, st[k].x);
-#pragma unroll
-      for (int k = 0; k < MAX_CLUSTER; ++k)
-        if (k < a.cluster) x.add(st[k], y[k], ex2_approx((st[k].x - x.top) * sc));
-    } else {
-      const float2 st = *reinterpret_cast<const float2*>(cta + 2 * row);
-      x = {st.x, st.y, *reinterpret_cast<const float4*>(whole + (quad * ROWS + row) * 4)};
+  if (blockIdx.x == gridDim.x - 1) pdl_wait();
+}
+
+// A CTA has ROWS rows (query, head) of one sequence, over all its heads. First the weight of each part in each row, then
+// the weighted sums, four channels of a row a thread: four neighbouring threads have a row, so that whole sectors of the
+// parts and of out move.
+template <bool BF, int ROWS>
+__global__ void __launch_bounds__(JOIN_THREADS)
+    prefix_join_kernel(const __grid_constant__ PrefixOwnArgs a) {
+  constexpr int GROUPS = JOIN_THREADS / ROWS;  // threads that share a row's parts
+  extern __shared__ float weight[];            // [part][ROWS]: times 1 / the joint sum; -1: not to be read
+  __shared__ float2 partial[GROUPS][ROWS];     // maximum and sum of a thread's parts (the sign: values left out)
+  __shared__ float base[ROWS];                 // 0, or NaN in rows without a sum above 0
+  __shared__ int look[ROWS];                   // 1: values that the row may see have been left out
+  const int b = static_cast<int>(a.by_join.quotient(blockIdx.x)), blk = static_cast<int>(blockIdx.x) - b * a.join_blocks;
+  pdl_trigger();
+  // (the inputs may be read before the wait, as by prefix_own_kernel)
+  int q0, nq, k0, nk;
+  sequence(a, b, q0, nq, k0, nk);
+  // its prefix: the last g with seq_start[g] <= b
+  int prefix = 0, len = a.max_prefix;
+  if (a.seq_start) {
+    int lo = 0, hi = a.prefixes;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (a.seq_start[mid] <= b)
+        lo = mid;
+      else
+        hi = mid;
     }
-    if (key_tiles > 0) {
-      const int sub = head / a.hg, h = kvh * a.nsub + sub;
-      const long long rho = static_cast<long long>(q0 + qi) * a.hg + (head - sub * a.hg);
-      constexpr int N = 8;  // parts on the way at once
+    prefix = a.seq_start[lo] <= b && b < a.seq_start[lo + 1] ? lo : -1;
+    if (prefix < 0) len = 0;
+  }
+  if (prefix >= 0 && a.prefix_len) len = min(max(a.prefix_len[prefix], 0), a.max_prefix);
+  const int heads = a.heads_kv * a.group, row0 = blk * ROWS, nrows = min(nq * heads - row0, ROWS);
+  if (nrows <= 0) return;
+  const int key_tiles = (len + kPrefixTile - 1) / kPrefixTile, parts = a.prefix_parts + (a.max_keys > 0 ? a.own_split : 0);
+  auto written = [&](int p) {  // (a part without key tiles of its prefix is not)
+    const int r = a.pair ? p >> 1 : p;
+    return p >= a.prefix_parts || split_from(key_tiles, r + 1, a.split) - split_from(key_tiles, r, a.split) > (a.pair ? p & 1 : 0);
+  };
+  struct Row {
+    int query, head, h;
+    long long rho;
+  };
+  auto place = [&](int row) {
+    Row r;
+    r.query = static_cast<int>(a.by_heads.quotient(row0 + row)), r.head = row0 + row - r.query * heads;
+    const int kvh = static_cast<int>(a.by_group.quotient(r.head)), in = r.head - kvh * a.group, sub = in / a.hg;
+    r.h = kvh * a.nsub + sub;
+    r.rho = static_cast<long long>(q0 + r.query) * a.hg + (in - sub * a.hg);
+    return r;
+  };
+  const float sc = a.scale_log2;
+  auto factor = [&](float m, float top) { return m == -INFINITY ? 1.0f : ex2_approx((m - top) * sc); };
+  {
+    // (a part without a finite score has a sum of 0, or NaN that must stay)
+    const int row = threadIdx.x & (ROWS - 1), g = threadIdx.x / ROWS;
+    const Row r = place(min(row, nrows - 1));
+    const float* const st = a.parts.stat + a.parts.stat_at(0, r.h, r.rho);
+    const long long step = a.parts.stat_at(1, 0, 0);
+    float top = -INFINITY, total = 0.0f;
+    bool left_out = false;
+    pdl_wait();
+#pragma unroll 4
+    for (int p = g; p < parts; p += GROUPS) {
+      const float2 v = written(p) ? *reinterpret_cast<const float2*>(st + p * step) : make_float2(-INFINITY, 0.0f);
+      left_out |= __float_as_int(v.y) < 0;
+      const float up = fmaxf(top, v.x);
+      total = total * factor(top, up) + fabsf(v.y) * factor(v.x, up);
+      top = up;
+      weight[p * ROWS + row] = v.x;
+    }
+    partial[g][row] = make_float2(top, left_out ? -total : total);
+    __syncthreads();
+    top = -INFINITY, total = 0.0f, left_out = false;
+#pragma unroll
+    for (int k = 0; k < GROUPS; ++k) top = fmaxf(top, partial[k][row].x);
+#pragma unroll
+    for (int k = 0; k < GROUPS; ++k) {
+      const float2 v = partial[k][row];
+      left_out |= __float_as_int(v.y) < 0;
+      total += fabsf(v.y) * factor(v.x, top);
+    }
+    const float inv = 1.0f / total;
+    for (int p = g; p < parts; p += GROUPS) {
+      const float m = weight[p * ROWS + row];
+      weight[p * ROWS + row] = m == -INFINITY ? -1.0f : ex2_approx((m - top) * sc) * inv;
+    }
+    if (g == 0) {
+      const bool sees = len > 0 || min(nk - nq + r.query + 1, nk) > 0;
+      base[row] = sees && !(total > 0.0f) ? __int_as_float(0x7fc00000) : 0.0f;
+      look[row] = left_out;
+    }
+    __syncthreads();
+  }
+  const int row = (threadIdx.x >> 2) & (ROWS - 1);
+  if (row >= nrows) return;
+  const Row r = place(row);
+  const int kvh = r.h / a.nsub, quads = a.head_dim / 4;
+  const float* const sums = a.parts.sums + a.parts.sums_at(0, r.h, r.rho);
+  const long long y_step = a.parts.sums_at(1, 0, 0);
+  const float none = base[row];
+  uint16_t* const out = a.out + static_cast<long long>(q0 + r.query) * a.out_row + static_cast<long long>(r.head) * a.out_head;
+  // U times four channels at once, N parts on the way
+  auto run = [&](auto un, auto pn) {
+    constexpr int U = un.value, N = pn.value, STEP = JOIN_THREADS / ROWS;
+    for (int quad0 = 4 * (threadIdx.x / (4 * ROWS)) + (threadIdx.x & 3); quad0 < quads; quad0 += U * STEP) {
+      float4 y[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) y[u] = make_float4(none, none, none, none);
       for (int p0 = 0; p0 < parts; p0 += N) {
-        float2 st[N];
-        float4 y[N];
-        float top = x.top;
+        float w[N];
+        float4 o[N][U];
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-          st[k] = make_float2(-INFINITY, 0.0f), y[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-          if (p0 + k < parts && written(p0 + k)) {
-            st[k] = *reinterpret_cast<const float2*>(a.parts.stat + a.parts.stat_at(p0 + k, h, rho));
-            y[k] = *reinterpret_cast<const float4*>(a.parts.sums + a.parts.sums_at(p0 + k, h, quad, rho));
+          w[k] = p0 + k < parts ? weight[(p0 + k) * ROWS + row] : -1.0f;
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            o[k][u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (w[k] != -1.0f && quad0 + u * STEP < quads)
+              o[k][u] = *reinterpret_cast<const float4*>(sums + (p0 + k) * y_step + (quad0 + u * STEP) * kQuadStep);
           }
         }
 #pragma unroll
-        for (int k = 0; k < N; ++k) top = fmaxf(top, st[k].x);
-        x.rise(top, sc);
+        for (int k = 0; k < N; ++k)
 #pragma unroll
-        for (int k = 0; k < N; ++k) x.add(st[k], y[k], ex2_approx((st[k].x - x.top) * sc));
+          for (int u = 0; u < U; ++u)
+            y[u].x = fmaf(o[k][u].x, w[k], y[u].x), y[u].y = fmaf(o[k][u].y, w[k], y[u].y), y[u].z = fmaf(o[k][u].z, w[k], y[u].z),
+            y[u].w = fmaf(o[k][u].w, w[k], y[u].w);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int quad = quad0 + u * STEP;
+        if (quad >= quads) continue;
+        float z[4] = {y[u].x, y[u].y, y[u].z, y[u].w};
+        // (an infinite value whose probability has rounded to 0 gave NaN)
+        const float odd = fmaf(z[0], 0.0f, fmaf(z[1], 0.0f, fmaf(z[2], 0.0f, z[3] * 0.0f)));
+        if ((odd != 0.0f || look[row]) && none == 0.0f) {
+          const int seen = min(max(nk - nq + r.query + 1, 0), nk);  // of the own keys
+#pragma unroll 1
+          for (int j = 0; j < 4; ++j) {
+            const float was = j == 0 ? z[0] : j == 1 ? z[1] : j == 2 ? z[2] : z[3];
+            float s = 0.0f;
+            if (seen > 0) s += bad_values<BF>(a.v + (a.kv_start ? 0 : b * a.v_batch) + k0 * a.v_row + kvh * a.v_head + 4 * quad + j, a.v_row, seen);
+            if (!(fabsf(was) < INFINITY) && len > 0)
+              s += bad_values<BF>(a.pv + prefix * a.pv_batch + kvh * a.pv_head + 4 * quad + j, a.pv_row, len);
+            if (s != 0.0f) z[0] = j == 0 ? s : z[0], z[1] = j == 1 ? s : z[1], z[2] = j == 2 ? s : z[2], z[3] = j == 3 ? s : z[3];  // (NaN too)
+          }
+        }
+        *reinterpret_cast<uint2*>(out + 4 * quad) = make_uint2(pack16<BF>(z[0], z[1]), pack16<BF>(z[2], z[3]));
       }
     }
-    const int seen = visible(row);
-    float y[4] = {x.y.x, x.y.y, x.y.z, x.y.w};
-    const float inv = 1.0f / x.total;
-    uint32_t w[2];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      // (an infinite value whose probability has rounded to 0 gave NaN; where the sum is 0 or NaN all channels are NaN)
-      y[j] = seen > 0 || len > 0 ? y[j] * inv : 0.0f;
-      const bool odd = !(fabsf(y[j]) < INFINITY);
-      if ((odd || left_out) && x.total > 0.0f) {
-        float s = 0.0f;
-        if (seen > 0) s += bad_values<BF>(a.v + (a.kv_start ? 0 : b * a.v_batch) + k0 * a.v_row + kvh * a.v_head + 4 * quad + j, a.v_row, seen);
-        if (odd && len > 0) s += bad_values<BF>(a.pv + prefix * a.pv_batch + kvh * a.pv_head + 4 * quad + j, a.pv_row, len);
-        if (s != 0.0f) y[j] = s;  // (NaN too)
-      }
-    }
-    w[0] = pack16<BF>(y[0], y[1]), w[1] = pack16<BF>(y[2], y[3]);
-    *reinterpret_cast<uint2*>(a.out + static_cast<long long>(q0 + qi) * a.out_row + static_cast<long long>(kvh * a.group + head) * a.out_head + 4 * quad) =
-        make_uint2(w[0], w[1]);
-  }
-  if (a.cluster > 1) cluster_sync_all();  // the peers have read this CTA's results
+  };
+  if (parts <= 2)
+    run(std::integral_constant<int, ROWS == 64 ? 4 : 2>(), std::integral_constant<int, 2>());
+  else
+    run(std::integral_constant<int, 1>(), std::integral_constant<int, 16>());
 }
 
 template <bool BF, int DP, bool MANY>
 cudaError_t launch(const PrefixOwn& own, cudaStream_t s) {
-  cudaLaunchConfig_t cfg{};
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // see launch_pdl
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = own.a.cluster;
-  attr[1].val.clusterDim.y = 1;
-  attr[1].val.clusterDim.z = 1;
-  cfg.gridDim = dim3(static_cast<unsigned>(own.units * own.a.cluster));
-  cfg.blockDim = dim3(THREADS);
-  cfg.dynamicSmemBytes = Shape<DP, MANY>::smem;
-  cfg.stream = s;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, prefix_own_kernel<BF, DP, MANY>, own.k, own.v, own.a);
+  cudaError_t e = cudaSuccess;
+  if (own.keys)
+    e = launch_pdl(prefix_own_kernel<BF, DP, MANY>, dim3(static_cast<unsigned>(own.units * own.a.own_split)), dim3(THREADS), Shape<DP, MANY>::smem, s,
+                   own.k, own.v, own.a);
+  if (e != cudaSuccess) return e;
+  const int parts = own.a.prefix_parts + (own.keys ? own.a.own_split : 0), rows = own.join_rows;
+  return launch_pdl(rows == 64 ? prefix_join_kernel<BF, 64> : prefix_join_kernel<BF, 16>, dim3(static_cast<unsigned>(own.a.batch) * own.a.join_blocks),
+                    dim3(JOIN_THREADS), 4 * parts * rows, s, own.a);
 }
 
 cudaError_t init_attributes() {
@@ -512,20 +583,26 @@ elasto_status prefix_own_plan(const elasto_prefix_attention_args& u, const Prefi
   a.prefixes = u.prefixes, a.max_prefix = u.max_prefix, a.seq_start = u.seq_start, a.prefix_len = u.prefix_len;
   a.pv = static_cast<const uint16_t*>(u.prefix_v), a.pv_batch = u.prefix_v_batch, a.pv_row = u.prefix_v_row, a.pv_head = u.prefix_v_head;
   a.hg = p.hg, a.nsub = p.nsub, a.pair = p.pair, a.split = p.split, a.parts = parts;
+  a.prefix_parts = p.prefix_parts(), a.own_split = p.own_split;
   a.status = status;
-  // 16 rows where a sequence has no more, or one query; else 64
-  const int64_t rows = static_cast<int64_t>(a.max_queries) * a.group;
-  own->many = a.max_queries > 1 && rows > 16;
-  const int of = own->many ? 64 : 16;
-  const int64_t blocks = (rows + of - 1) / of;
-  own->units = blocks * a.batch * a.heads_kv;
-  if (rows > 0x3fffffff || own->units > 0x7fffffffLL / MAX_CLUSTER) {
+  own->many = p.many != 0, own->keys = u.max_keys > 0;
+  own->units = static_cast<int64_t>(p.blocks) * a.batch * a.heads_kv;
+  if (own->units * a.own_split > 0x7fffffffLL) {
     set_error("elasto_op_prefix_attention: too many sequences or queries");
     return ELASTO_ERR_UNSUPPORTED;
   }
-  a.blocks = static_cast<int>(blocks);
-  a.cluster = u.max_keys > 0 ? single_token_cluster(own->units, u.max_keys, num_sms(), MAX_CLUSTER) : 1;
-  a.by_blocks = Divisor(a.blocks), a.by_heads_kv = Divisor(a.heads_kv), a.by_group = Divisor(a.group);
+  a.blocks = p.blocks;
+  // the join: 64 rows a CTA where these fill the SMs, else 16
+  const int64_t all = static_cast<int64_t>(a.max_queries) * u.heads;
+  own->join_rows = (all + 63) / 64 * a.batch >= 2LL * num_sms() ? 64 : 16;
+  const int64_t join_blocks = (all + own->join_rows - 1) / own->join_rows;
+  if (join_blocks * a.batch > 0x7fffffffLL || all > 0x3fffffff) {
+    set_error("elasto_op_prefix_attention: too many sequences or queries");
+    return ELASTO_ERR_UNSUPPORTED;
+  }
+  a.join_blocks = static_cast<int>(join_blocks);
+  a.by_join = Divisor(a.join_blocks), a.by_heads = Divisor(u.heads);
+  a.by_split = Divisor(a.own_split), a.by_blocks = Divisor(a.blocks), a.by_heads_kv = Divisor(a.heads_kv), a.by_group = Divisor(a.group);
   own->a = a, own->bf = u.dtype == ELASTO_BF16;
   auto map_of = [&](CUtensorMap* tm, const void* data, long long head_s, long long row_s, long long batch_s) {
     const uint64_t dims[4] = {static_cast<uint64_t>(u.head_dim), static_cast<uint64_t>(u.heads_kv), static_cast<uint64_t>(u.kv_rows),

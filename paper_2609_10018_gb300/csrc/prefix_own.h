@@ -1,4 +1,4 @@
-// The second kernel of attention behind shared prefixes, as the first one's file starts it.
+// The second and third kernel of attention behind shared prefixes, as the first one's file starts them.
 #pragma once
 #include "common.h"
 #include "prefix_parts.h"
@@ -24,17 +24,20 @@ struct PrefixOwnArgs {
   const uint16_t* pv;
   long long pv_batch, pv_row, pv_head;
   int hg, nsub, pair, split;
+  int prefix_parts, own_split;
   PrefixParts parts;
-  int blocks;   // of rows, of a sequence and key head
-  int cluster;  // CTAs that share a block's keys
-  Divisor by_blocks, by_heads_kv, by_group;
+  int blocks;  // of rows, of a sequence and key head
+  int join_blocks;  // of rows of a sequence over all heads, for the join
+  Divisor by_join, by_heads;
+  Divisor by_split, by_blocks, by_heads_kv, by_group;
   int* status;
 };
 struct PrefixOwn {
   PrefixOwnArgs a;
   CUtensorMap k, v;
   int64_t units;
-  bool bf, many;  // many: blocks of 64 rows
+  int join_rows;  // of a CTA of the join
+  bool bf, many, keys;  // many: blocks of 64 rows; keys: there are own ones
 };
 elasto_status prefix_own_plan(const elasto_prefix_attention_args& u, const PrefixPlan& p, const PrefixParts& parts, float down, int* status,
                               PrefixOwn* own);

@@ -1,11 +1,18 @@
-// What the two kernels of attention behind shared prefixes agree on: how the keys of a prefix are cut, and where the
-// results of the parts lie. (Host code too: the plan is tested without a GPU.)
+// What the kernels of attention behind shared prefixes agree on: how the keys of a prefix and of the sequences are cut, and
+// where the results of the parts lie. (No CUDA here but the attributes: the plan is tested on the host.)
 #pragma once
 #include <stdint.h>
 
+#ifdef __CUDACC__
+#define ELASTO_HD __host__ __device__
+#else
+#define ELASTO_HD
+#endif
+
 namespace elasto {
 
-constexpr int kPrefixTile = 128;  // rows of Q, and keys, of a tile
+constexpr int kPrefixTile = 128;                 // rows of Q, and keys, of a tile
+constexpr int kPrefixSplit = 64, kOwnSplit = 16;  // CTAs that share keys at most
 
 // A row is a query head at a query: rho = q row * hg + head of the tile. An item is one or two tiles of 128 rows of
 // one prefix and key head (or part of its query heads); its key tiles are shared out over `split` CTAs. With one tile of
@@ -15,59 +22,78 @@ struct PrefixPlan {
   int pair;           // 1: items of one tile of rows
   int split;          // CTAs of an item
   int64_t items;      // for each key head and part of its heads, at most (those that there are not end at once)
-  int parts() const { return pair ? 2 * split : split; }
+  int many;           // 1: blocks of 64 rows of a sequence's own attention, 0: of 16
+  int blocks;         // of a sequence and key head
+  int own_split;      // CTAs that share a block's own keys, each leaving a part behind the prefix's
+  int prefix_parts() const { return pair ? 2 * split : split; }
+  int parts() const { return prefix_parts() + own_split; }
 };
 
-// rows: the queries that are to be expected; most: as many as there may be.
-inline PrefixPlan prefix_plan(int64_t rows, int64_t most, int prefixes, int group, int heads_kv, int64_t max_prefix, int head_dim, int sms) {
+struct PrefixSizes {
+  int64_t rows, most;  // queries that are to be expected, and as many as there may be
+  int batch, max_queries, prefixes, group, heads_kv, head_dim;
+  int64_t max_prefix, max_keys;
+  int sms;
+};
+
+inline PrefixPlan prefix_plan(const PrefixSizes& z) {
   PrefixPlan p;
-  p.nsub = (group + 31) / 32;
-  p.hg = (group + p.nsub - 1) / p.nsub;
+  p.nsub = (z.group + 31) / 32;
+  p.hg = (z.group + p.nsub - 1) / p.nsub;
   p.qpt = kPrefixTile / p.hg;
-  p.pair = rows <= static_cast<int64_t>(prefixes) * p.qpt;
+  p.pair = z.rows <= static_cast<int64_t>(z.prefixes) * p.qpt;
   const int64_t step = p.pair ? p.qpt : 2LL * p.qpt;
   auto items = [&](int64_t n) {  // of n rows: each prefix's last item may be short, and each has a row at least
-    const int64_t k = prefixes == 1 ? (n + step - 1) / step : n / step + prefixes;
+    const int64_t k = z.prefixes == 1 ? (n + step - 1) / step : n / step + z.prefixes;
     return k < n ? k : n;
   };
-  p.items = items(most);
-  const int64_t tiles = (max_prefix + kPrefixTile - 1) / kPrefixTile, ctas = items(rows) * heads_kv * p.nsub;
-  // Microseconds: of a CTA's start and end, of a key tile, and of writing and reading a part of all rows.
-  const double start = 4.0, tile = (p.pair ? 0.65 : 1.25) * (head_dim > 64 ? 1.0 : 0.7);
-  const double part = static_cast<double>(rows) * group * heads_kv * (8.0 * head_dim + 16) * (p.pair ? 2 : 1) / 8e6;
+  p.items = items(z.most);
+  // The sequences' own keys: blocks of 64 rows where a sequence has more than three of 16 and several queries. CTAs until the SMs have six
+  // each, with four tiles of 64 keys at least, so that sequences of different lengths even out.
+  const int64_t rows = static_cast<int64_t>(z.max_queries) * z.group;
+  p.many = z.max_queries > 1 && rows > 48;
+  const int64_t of = p.many ? 64 : 16;
+  p.blocks = static_cast<int>((rows + of - 1) / of);
+  const int64_t units = static_cast<int64_t>(p.blocks) * z.batch * z.heads_kv;
+  p.own_split = 1;
+  while (p.own_split < kOwnSplit && units * p.own_split < 6LL * z.sms && z.max_keys >= 512LL * p.own_split) p.own_split *= 2;
+  // How many CTAs share a prefix's keys. Both kernels run at the same time, the prefixes' with an SM a CTA, the other
+  // on what is left: in microseconds, of a CTA's start and end, of a key tile, of a part of all rows written and read,
+  // and of the own keys (about 0.6 of the longest each) at the memory's rate, which takes 60 SMs.
+  const int64_t tiles = (z.max_prefix + kPrefixTile - 1) / kPrefixTile, ctas = items(z.rows) * z.heads_kv * p.nsub;
+  const double start = 5.0, tile = (p.pair ? 0.7 : 1.4) * (z.head_dim > 64 ? 1.0 : 0.7);
+  const double part = static_cast<double>(z.rows) * z.group * z.heads_kv * (8.0 * z.head_dim + 16) * (p.pair ? 2 : 1) / 8e6;
+  const double own = 0.6 * 4.0 * z.head_dim * z.heads_kv * static_cast<double>(z.batch) * z.max_keys / 6.5e6;
   double best = 0.0;
   p.split = 1;
-  for (int n = 1; n <= 64 && n <= tiles; ++n) {
-    const double waves = static_cast<double>((ctas * n + sms - 1) / sms);
-    const double cost = waves * (start + static_cast<double>((tiles + n - 1) / n) * tile) + n * part;
+  for (int n = 1; n <= kPrefixSplit && n <= tiles; ++n) {
+    const int64_t waves = (ctas * n + z.sms - 1) / z.sms;
+    const double prefix = static_cast<double>(waves) * (start + static_cast<double>((tiles + n - 1) / n) * tile);
+    const double left = waves > 1 ? 0.0 : static_cast<double>(z.sms - ctas * n), rate = left < 60 ? left / 60 : 1.0;
+    const double both = rate * prefix >= own ? prefix : prefix + (own - rate * prefix);
+    const double cost = both + n * part;
     if (n == 1 || cost < best) best = cost, p.split = n;
   }
   return p;
 }
 
-// Parts of the results: stat [part][key head x nsub][rho] (maximum and sum of each row) and
-// sums [part][key head x nsub][channels / 4][rho] of four channels.
+// Parts of the results, those of the prefix and then those of the own keys: stat [part][key head x nsub][rho] (maximum and
+// sum of each row; of an own part the sum with its sign turned where values that some row sees were left out) and
+// sums [part][key head x nsub][rho / 32][channels / 4][rho % 32] of four channels (not written where the maximum is
+// -infinity): what a warp writes or reads of 32 rows lies together, all channels of them in one piece of 16 KB at most.
 struct PrefixParts {
   float* sums;
   float* stat;
-  int64_t rho;  // rows
+  int64_t rho;    // rows, a multiple of 32
   int hs, quads;  // key heads x nsub, head_dim / 4
-#ifdef __CUDACC__
-  __host__ __device__
-#endif
-  int64_t stat_at(int part, int h, int64_t row) const { return 2 * ((static_cast<int64_t>(part) * hs + h) * rho + row); }
-#ifdef __CUDACC__
-  __host__ __device__
-#endif
-  int64_t sums_at(int part, int h, int quad, int64_t row) const {
-    return 4 * (((static_cast<int64_t>(part) * hs + h) * quads + quad) * rho + row);
+  ELASTO_HD int64_t stat_at(int part, int h, int64_t row) const { return 2 * ((static_cast<int64_t>(part) * hs + h) * rho + row); }
+  ELASTO_HD int64_t sums_at(int part, int h, int64_t row) const {  // of the first four channels, 128 floats from four to the next
+    return 4 * (((static_cast<int64_t>(part) * hs + h) * (rho >> 5) + (row >> 5)) * quads * 32 + (row & 31));
   }
 };
+constexpr int kQuadStep = 128;
 
-// The key tiles [first, last) of a CTA.
-#ifdef __CUDACC__
-__host__ __device__
-#endif
-inline int split_from(int tiles, int rank, int split) { return static_cast<int>(static_cast<int64_t>(tiles) * rank / split); }
+// The first key tile of a CTA (at most 2^24 tiles, and 64 CTAs).
+ELASTO_HD inline int split_from(int tiles, int rank, int split) { return tiles * rank / split; }
 
 }  // namespace elasto

@@ -304,7 +304,9 @@ __global__ void __launch_bounds__(LOG == 9 ? 512 : CTA_THREADS, 1)
 #pragma unroll
       for (int j = 0; j < 4; ++j) sum = fma2(v[i][j], v[i][j], sum);
     });
-    return rsqrtf(fmaf(row_sum(sum, slot + 1), inv_n, a.eps));
+    // (rsqrtf is off by up to two units in the last place; one step of Newton's method leaves half of one)
+    const float m = fmaf(row_sum(sum, slot + 1), inv_n, a.eps), rs = rsqrtf(m), e = fmaf(-m * rs, rs, 1.0f);
+    return fabsf(e) < 1.0f ? fmaf(0.5f * rs, e, rs) : rs;
   };
 
   bool failed = false;
