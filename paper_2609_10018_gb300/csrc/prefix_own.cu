@@ -1,16 +1,18 @@
 // Attention behind shared prefixes: the sequences' own keys, and the join of all parts.
 //
-// prefix_own_kernel: a block is 16 or 64 rows (query, head) of one sequence and key head; its own keys, in tiles of 64, are
-// shared out over own_split CTAs, each of which leaves a part as prefix_attention.cu's CTAs do. Warp 4 streams K and V
-// tiles by TMA through a ring, and warps 0-3 form S = Q K^T and O += P V by m16n8k16 products, running maximum and sum
-// of the softmax for themselves:
-//   16 rows (single tokens and few): a warp takes 16 keys of each tile, all rows;
-//   64 rows (longer runs of tokens): a warp takes 16 rows, all keys.
-// (tcgen05 would need 128 rows of one sequence: the prefix, where most of the work lies, has them.) It does not wait for
-// the prefixes' kernel: both run at the same time, that one bound by its products, this one by reading the keys and values
-// once. Only its last CTA waits before it ends, so that what waits for this kernel waits for both.
+// A block is 16 or 64 rows (query, head) of one sequence and key head; S = Q K^T and O += P V by m16n8k16 products (tcgen05
+// would need 128 rows of one sequence: the prefix, where most of the work lies, has them), running maximum and sum of the
+// softmax in one pass. The own keys of a block are shared out over own_split CTAs, each of which leaves a part as
+// prefix_attention.cu's CTAs do.
+//   prefix_few_kernel    16 rows, single tokens and few: a CTA is one warp, which streams 16 keys at a time by TMA through
+//     a ring of its own. Nothing is shared between warps, and while one of an SM's nine CTAs starts or ends the others load.
+//   prefix_many_kernel   64 rows, longer runs of tokens: four warps with 16 rows each, a fifth loads tiles of 64 keys.
+// Neither waits for the prefixes' kernel: that one is bound by its products, these by reading the keys and values
+// once, and both run at the same time. Only the last CTA waits before it ends, so that what waits for this kernel waits
+// for both.
 //
-// prefix_join_kernel: out = sum over parts of o exp(m - top) / sum of l exp(m - top), four channels a thread, in a fixed order.
+// prefix_join_kernel: out = sum over parts of o exp(m - top) / sum of l exp(m - top), four channels a thread, in a fixed
+// order.
 #include <algorithm>
 #include <type_traits>
 
@@ -21,22 +23,26 @@ namespace elasto {
 
 namespace {
 
-constexpr int KT = 64, WARPS = 4, THREADS = 32 * (WARPS + 1);
-constexpr int HALF = KT * 128;  // bytes of 64 keys of 64 channels
-constexpr int JOIN_THREADS = 256;
-static_assert(4 * 64 * (2 * kPrefixSplit + kOwnSplit) <= 40 * 1024, "the join's weights");
 constexpr float kLazy = 8.0f;  // log2 of how far a maximum may grow before O is rescaled
+constexpr int JOIN_THREADS = 256;
 
-template <int DP, bool MANY>
-struct Shape {
-  static constexpr int rows = MANY ? 64 : 16;
+// A CTA of one warp and its ring.
+template <int DP>
+struct Few {
+  static constexpr int halves = DP / 64, half = 16 * 128, tile = halves * half, stage = 2 * tile;  // 16 keys of 64 channels
+  static constexpr int stages = 24 * 1024 / stage;
+  static constexpr int smem = 1024 + stages * stage + 64;
+};
+
+constexpr int KT = 64, WARPS = 4, THREADS = 32 * (WARPS + 1), ROWS = 64;
+constexpr int HALF = KT * 128;                 // bytes of 64 keys of 64 channels
+constexpr int QUAD = 4 * ROWS + 8;             // floats from four channels of all rows to the next four (no bank conflicts)
+template <int DP>
+struct Many {
   static constexpr int halves = DP / 64, tile = halves * HALF, stage = 2 * tile;
-  // CTAs an SM: three, of the blocks of 64 rows (whose registers do not allow for it) two
-  static constexpr int ctas = MANY ? 2 : 3;
-  static constexpr int stages = (DP == 128 ? 1 : 2) * (MANY ? 3 : 2);
+  static constexpr int stages = DP == 128 ? 2 : 4;  // three CTAs an SM
   static constexpr int smem = 1024 + stages * stage + 256;
-  static constexpr int part = MANY ? 0 : WARPS * 16 * DP;  // floats of the warps' O, of the block's
-  static_assert(stages * stage >= (part + rows * DP + 2 * rows + (MANY ? 0 : WARPS * 32)) * 4, "the results take the ring's place");
+  static_assert(stages * stage >= (DP / 4 * QUAD + 2 * ROWS) * 4, "the results take the ring's place");
 };
 
 __device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&r)[4]) {
@@ -95,6 +101,25 @@ __device__ __noinline__ float bad_values(const uint16_t* v, long long row, int n
   return sum;
 }
 
+// The results y of four channels of a row that sees `seen` own keys and `len` of its prefix: a channel in which the row sees
+// values that are not finite gets their sum. (An infinite value whose probability has rounded to 0 gave NaN; left_out: some have
+// been set to 0 because other rows do not see them.)
+template <bool BF>
+__device__ __forceinline__ float4 put_bad_values(const PrefixOwnArgs& a, float4 y, int b, int kvh, int k0, int seen, int prefix, int len, int quad,
+                                                 bool left_out) {
+  const float odd = fmaf(y.x, 0.0f, fmaf(y.y, 0.0f, fmaf(y.z, 0.0f, y.w * 0.0f)));
+  if (odd == 0.0f && !left_out) return y;
+#pragma unroll 1
+  for (int j = 0; j < 4; ++j) {
+    const float was = j == 0 ? y.x : j == 1 ? y.y : j == 2 ? y.z : y.w;
+    float s = 0.0f;
+    if (seen > 0) s += bad_values<BF>(a.v + (a.kv_start ? 0 : b * a.v_batch) + k0 * a.v_row + kvh * a.v_head + 4 * quad + j, a.v_row, seen);
+    if (!(fabsf(was) < INFINITY) && len > 0) s += bad_values<BF>(a.pv + prefix * a.pv_batch + kvh * a.pv_head + 4 * quad + j, a.pv_row, len);
+    if (s != 0.0f) y.x = j == 0 ? s : y.x, y.y = j == 1 ? s : y.y, y.z = j == 2 ? s : y.z, y.w = j == 3 ? s : y.w;  // (NaN too)
+  }
+  return y;
+}
+
 // Rows of q and own keys of sequence b, cut to what the host allows.
 __device__ __forceinline__ void sequence(const PrefixOwnArgs& a, int b, int& q0, int& nq, int& k0, int& nk) {
   q0 = b * a.max_queries, nq = a.max_queries, k0 = 0, nk = a.max_keys;
@@ -110,12 +135,242 @@ __device__ __forceinline__ void sequence(const PrefixOwnArgs& a, int b, int& q0,
   }
 }
 
-template <bool BF, int DP, bool MANY>
-__global__ void __launch_bounds__(THREADS, Shape<DP, MANY>::ctas)
-    prefix_own_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                      const __grid_constant__ PrefixOwnArgs a) {
-  using T = Shape<DP, MANY>;
-  constexpr int S = T::stages, ROWS = T::rows, NS = MANY ? KT / 16 : 1;  // sub-tiles of 16 keys that a warp takes
+// Whether part p of a prefix has key tiles.
+__device__ __forceinline__ bool has_keys(const PrefixOwnArgs& a, int p, int len) {
+  const int r = a.pair ? p >> 1 : p, key_tiles = (len + kPrefixTile - 1) / kPrefixTile;
+  return split_from(key_tiles, r + 1, a.split) - split_from(key_tiles, r, a.split) > (a.pair ? p & 1 : 0);
+}
+
+// The running softmax of a warp's 16 rows (this lane's: r and r + 8, r = lane / 4) over N blocks of 16 keys, and the
+// products. q: the rows; ks, vs: this lane's rows of the K and V tiles for ldmatrix; half: bytes from 64 channels to
+// the next; left: keys that some row sees; vis: keys that the two rows see (MASKED: not all of them all).
+template <bool BF, int DP>
+struct Softmax {
+  float o[DP / 8][4], m[2], sum[2];
+  __device__ __forceinline__ Softmax() {
+    m[0] = m[1] = -INFINITY, sum[0] = sum[1] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < DP / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
+  }
+  template <int N>
+  __device__ __forceinline__ void step(const uint32_t (&q)[DP / 16][4], uint32_t ks, uint32_t vs, int half, int left, bool masked, const int (&vis)[2],
+                                       float sc, float down, int lane) {
+    const int c2 = 2 * (lane & 3), kswap = lane & 7, kpiece = (lane >> 3) & 1, vpiece = lane >> 4;
+    float x[2 * N][4];
+#pragma unroll
+    for (int n = 0; n < 2 * N; ++n) x[n][0] = x[n][1] = x[n][2] = x[n][3] = 0.0f;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      if (16 * n >= left) continue;
+#pragma unroll
+      for (int k = 0; k < DP / 16; ++k) {
+        uint32_t bk[4];
+        ldmatrix4(ks + n * 2048 + (k >> 2) * half + (((2 * (k & 3) + kpiece) ^ kswap) << 4), bk);
+        mma16816<BF>(x[2 * n], q[k], bk[0], bk[1]);
+        mma16816<BF>(x[2 * n + 1], q[k], bk[2], bk[3]);
+      }
+    }
+    if (masked) {
+#pragma unroll
+      for (int n = 0; n < 2 * N; ++n)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (8 * n + c2 + (j & 1) >= vis[j >> 1]) x[n][j] = -INFINITY;
+    }
+    float top[2], keep[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float v = -INFINITY;
+#pragma unroll
+      for (int n = 0; n < 2 * N; ++n) v = max3(v, x[n][2 * h], x[n][2 * h + 1]);
+      v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
+      v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
+      top[h] = fmaxf(m[h], v);
+    }
+    if (__any_sync(0xffffffffu, (top[0] - m[0]) * sc > kLazy || (top[1] - m[1]) * sc > kLazy)) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        keep[h] = m[h] == -INFINITY ? 0.0f : ex2_approx((m[h] - top[h]) * sc);
+        sum[h] *= keep[h];
+        m[h] = top[h];
+      }
+#pragma unroll
+      for (int j = 0; j < DP / 8; ++j) o[j][0] *= keep[0], o[j][1] *= keep[0], o[j][2] *= keep[1], o[j][3] *= keep[1];
+    }
+    uint32_t p[N][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float neg = m[h] == -INFINITY ? 0.0f : fmaf(-m[h], sc, -down);
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        float e[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) e[j] = ex2_approx(fmaf(x[2 * n + (j >> 1)][2 * h + (j & 1)], sc, neg));
+        sum[h] += (e[0] + e[1]) + (e[2] + e[3]);
+        p[n][h] = pack16<BF>(e[0], e[1]);
+        p[n][2 + h] = pack16<BF>(e[2], e[3]);
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      if (16 * n >= left) continue;
+#pragma unroll
+      for (int k = 0; k < DP / 16; ++k) {
+        uint32_t bv[4];
+        ldmatrix4_trans(vs + n * 2048 + (k >> 2) * half + (((2 * (k & 3) + vpiece) ^ kswap) << 4), bv);
+        mma16816<BF>(o[2 * k], p[n], bv[0], bv[1]);
+        mma16816<BF>(o[2 * k + 1], p[n], bv[2], bv[3]);
+      }
+    }
+  }
+  // the four lanes of a row: its sum
+  __device__ __forceinline__ void finish() {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      sum[h] += __shfl_xor_sync(0xffffffffu, sum[h], 1);
+      sum[h] += __shfl_xor_sync(0xffffffffu, sum[h], 2);
+    }
+  }
+};
+
+// Values of the V tile at v (64 channels of `half` bytes, `keys` keys, 128 bytes each) that no row sees, from key `left` on,
+// become 0, and from key `from` on, where some rows do not see them, those that are not finite: 0 * NaN
+// would reach these rows. (The rows that see them get them at the end.) Whether there were any; thread `t` of `threads`.
+template <bool BF, int DP>
+__device__ __forceinline__ bool clear_values(uint8_t* v, int half, int keys, int from, int left, int t, int threads) {
+  auto piece = [&](int e) {
+    const int row = from + e / (DP / 8), at = e % (DP / 8);
+    return reinterpret_cast<uint4*>(v + (at >> 3) * half + row * 128 + ((at & 7) << 4));  // (the swizzle stays within a row)
+  };
+  const int seen = (min(left, keys) - from) * (DP / 8), all = (keys - from) * (DP / 8);
+  uint32_t acc = 0u;
+  for (int e = t; e < all; e += threads) {
+    uint4* const p = piece(e);
+    if (e < seen)
+      look16<BF>(p->x, acc), look16<BF>(p->y, acc), look16<BF>(p->z, acc), look16<BF>(p->w, acc);
+    else
+      *p = make_uint4(0u, 0u, 0u, 0u);
+  }
+  const bool bad = bad16<BF>(acc) != 0u;
+  if (bad)
+    for (int e = t; e < seen; e += threads) {
+      uint4* const p = piece(e);
+      const uint4 w = *p;
+      *p = make_uint4(w.x & ~bad16<BF>(w.x), w.y & ~bad16<BF>(w.y), w.z & ~bad16<BF>(w.z), w.w & ~bad16<BF>(w.w));
+    }
+  fence_async_smem();  // (before the next tile is copied there)
+  return bad;
+}
+
+template <bool BF, int DP>
+__global__ void __launch_bounds__(32)
+    prefix_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ PrefixOwnArgs a) {
+  using T = Few<DP>;
+  constexpr int S = T::stages;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + S * T::stage);
+  const int lane = threadIdx.x;
+  const int unit = static_cast<int>(a.by_split.quotient(blockIdx.x)), rank = static_cast<int>(blockIdx.x) - unit * a.own_split;
+  const int u1 = static_cast<int>(a.by_blocks.quotient(unit)), blk = unit - u1 * a.blocks;
+  const int b = static_cast<int>(a.by_heads_kv.quotient(u1)), kvh = u1 - b * a.heads_kv;
+  if (lane == 0) {
+    for (int i = 0; i < S; ++i) mbar_init(&full[i], 1);
+    fence_barrier_init();
+    tma_prefetch_desc(&tmK);
+    tma_prefetch_desc(&tmV);
+  }
+  __syncwarp();
+  pdl_trigger();
+  // The kernel before writes nothing but its parts, and waited for what came before it: the inputs may be read at once.
+  int q0, nq, k0, nk;
+  sequence(a, b, q0, nq, k0, nk);
+  const int row0 = blk * 16, nrows = min(nq * a.group - row0, 16);
+  if (nrows > 0) {
+    auto query = [&](int row) { return static_cast<int>(a.by_group.quotient(row0 + row)); };
+    auto visible = [&](int row) { return row < nrows ? min(max(nk - nq + query(row) + 1, 0), nk) : 0; };
+    const int most = visible(nrows - 1), least = visible(0), subs = (most + 15) / 16;
+    const int t0 = split_from(subs, rank, a.own_split), n = split_from(subs, rank + 1, a.own_split) - t0;
+    auto request = [&](int i) {  // (one lane)
+      uint8_t* const dst = smem + i % S * T::stage;
+      mbar_expect_tx(&full[i % S], T::stage);
+      for (int h = 0; h < T::halves; ++h) {
+        tma_load_4d(dst + h * T::half, &tmK, &full[i % S], 64 * h, kvh, k0 + (t0 + i) * 16, a.kv_start ? 0 : b);
+        tma_load_4d(dst + T::tile + h * T::half, &tmV, &full[i % S], 64 * h, kvh, k0 + (t0 + i) * 16, a.kv_start ? 0 : b);
+      }
+    };
+    int asked = min(n, S);
+    if (elect_one())
+      for (int i = 0; i < asked; ++i) request(i);
+    __syncwarp();
+    const int r = lane >> 2, c2 = 2 * (lane & 3);
+    uint32_t q[DP / 16][4];  // the rows r and r + 8
+    int vis[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int row = r + 8 * h, qi = query(row), head = row0 + row - qi * a.group;
+      vis[h] = visible(row);
+      const uint16_t* const p = a.q + static_cast<long long>(q0 + qi) * a.q_row + static_cast<long long>(kvh * a.group + head) * a.q_head;
+#pragma unroll
+      for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int ch = 16 * k + c2 + 8 * j;
+          q[k][h + 2 * j] = row < nrows && ch < a.head_dim ? *reinterpret_cast<const uint32_t*>(p + ch) : 0u;
+        }
+    }
+    const float sc = a.scale_log2;
+    const int krow = (lane & 7) + (lane >> 4) * 8, vrow = lane & 15;  // this lane's in the ldmatrix loads of K and of V
+    Softmax<BF, DP> x;
+    bool ok = true, left_out = false;
+    for (int i = 0; i < n; ++i) {
+      const int s = i % S, key0 = (t0 + i) * 16;
+      ok = mbar_wait_warp(&full[s], (i / S) & 1);
+      if (!ok) break;
+      uint8_t* const kb = smem + s * T::stage;
+      const int whole = least - key0, left = most - key0;  // of these keys: those that all rows see, and that some row sees
+      if (whole < 16) {
+        left_out |= clear_values<BF, DP>(kb + T::tile, T::half, 16, max(whole, 0), left, lane, 32);
+        __syncwarp();
+      }
+      const int seen[2] = {vis[0] - key0, vis[1] - key0};
+      x.template step<1>(q, smem_addr(kb) + krow * 128, smem_addr(kb + T::tile) + vrow * 128, T::half, left, whole < 16, seen, sc, a.down, lane);
+      __syncwarp();
+      if (i + S < n) {
+        if (elect_one()) request(i + S);
+        __syncwarp();
+        ++asked;
+      }
+    }
+    if (!ok) {  // (the copies in flight land before the CTA exits)
+      if (lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
+      for (int i = max(0, asked - S); i < asked; ++i) mbar_wait_warp(&full[i % S], (i / S) & 1);
+    }
+    x.finish();
+    left_out = __any_sync(0xffffffffu, left_out);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int row = r + 8 * h;
+      if (row >= nrows) continue;
+      const int qi = query(row), head = row0 + row - qi * a.group, sub = head / a.hg, hs = kvh * a.nsub + sub;
+      const long long rho = static_cast<long long>(q0 + qi) * a.hg + (head - sub * a.hg);
+      if ((lane & 3) == 0)
+        *reinterpret_cast<float2*>(a.parts.stat + a.parts.stat_at(a.prefix_parts + rank, hs, rho)) = make_float2(x.m[h], left_out ? -x.sum[h] : x.sum[h]);
+      if (x.m[h] == -INFINITY) continue;
+      float* const sums = a.parts.sums + a.parts.sums_at(a.prefix_parts + rank, hs, rho) + (c2 & 3) + (c2 >> 2) * kQuadStep;
+#pragma unroll
+      for (int j = 0; j < DP / 8; ++j)
+        if (8 * j < a.head_dim) *reinterpret_cast<float2*>(sums + 2 * j * kQuadStep) = make_float2(x.o[j][2 * h], x.o[j][2 * h + 1]);
+    }
+  }
+  if (blockIdx.x == gridDim.x - 1) pdl_wait();
+}
+
+template <bool BF, int DP>
+__global__ void __launch_bounds__(THREADS, 3)
+    prefix_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ PrefixOwnArgs a) {
+  using T = Many<DP>;
+  constexpr int S = T::stages;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + S * T::stage);
@@ -137,7 +392,7 @@ __global__ void __launch_bounds__(THREADS, Shape<DP, MANY>::ctas)
   }
   __syncthreads();
   pdl_trigger();
-  // The kernel before writes nothing but its parts, and waited for what came before it: the inputs may be read at once.
+  // (the inputs may be read at once, as by prefix_few_kernel)
   int q0, nq, k0, nk;
   sequence(a, b, q0, nq, k0, nk);
   const int row0 = blk * ROWS, nrows = min(nq * a.group - row0, ROWS);
@@ -145,18 +400,14 @@ __global__ void __launch_bounds__(THREADS, Shape<DP, MANY>::ctas)
     if (blockIdx.x == gridDim.x - 1) pdl_wait();
     return;
   }
-
-  // visible own keys of a row of the block
   auto query = [&](int row) { return static_cast<int>(a.by_group.quotient(row0 + row)); };
   auto visible = [&](int row) { return row < nrows ? min(max(nk - nq + query(row) + 1, 0), nk) : 0; };
   const int most = visible(nrows - 1), least = visible(0);
   const int tiles = (most + KT - 1) / KT;
   const int t0 = split_from(tiles, rank, a.own_split), t1 = split_from(tiles, rank + 1, a.own_split);
 
-  float o[DP / 8][4], m[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f};
-#pragma unroll
-  for (int i = 0; i < DP / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
-  const int base = MANY ? 16 * warp : 0;  // of the warp's rows
+  Softmax<BF, DP> x;
+  const int r = lane >> 2, c2 = 2 * (lane & 3), base = 16 * warp;  // (of the warp's rows)
   if (warp == WARPS) {
     if (elect_one()) {
       bool ok = true;
@@ -177,7 +428,6 @@ __global__ void __launch_bounds__(THREADS, Shape<DP, MANY>::ctas)
     }
     __syncwarp();
   } else if (t0 < t1) {
-    const int r = lane >> 2, c2 = 2 * (lane & 3);
     uint32_t q[DP / 16][4];  // the rows base + r and base + r + 8
     int vis[2];
 #pragma unroll
@@ -194,118 +444,24 @@ __global__ void __launch_bounds__(THREADS, Shape<DP, MANY>::ctas)
         }
     }
     const float sc = a.scale_log2;
-    // this lane's row and 16-byte piece in the ldmatrix loads of K and of V
-    const int sub0 = MANY ? 0 : 16 * warp;
-    const int krow = sub0 + (lane & 7) + (lane >> 4) * 8, kpiece = (lane >> 3) & 1;
-    const int vrow = sub0 + (lane & 15), vpiece = lane >> 4;
+    const int krow = (lane & 7) + (lane >> 4) * 8, vrow = lane & 15;
     bool ok = true;
     int i = 0;
     for (int t = t0; t < t1 && ok; ++t, ++i) {
-      const int s = i % S, key0 = t * KT + sub0;
+      const int s = i % S, key0 = t * KT;
       ok = mbar_wait_warp(&full[s], (i / S) & 1);
       if (!ok) break;
       uint8_t* const kb = smem + s * T::stage;
-      const int left = most - key0;   // of the warp's keys, those that some row sees
-      const int whole = least - key0;  // and those that all rows see
-      // Values that no row sees become 0, and where some rows do not see them values that are not finite
-      // do: 0 * NaN would reach those. (The rows that see these get them at the end.)
-      if (whole < 16 * NS && left > 0) {
-        const int from = max(whole, 0), thread = MANY ? static_cast<int>(threadIdx.x) : lane, threads = MANY ? 32 * WARPS : 32;
-        auto piece = [&](int e) {
-          const int row = sub0 + from + e / (DP / 8), at = e % (DP / 8);
-          return reinterpret_cast<uint4*>(kb + T::tile + (at >> 3) * HALF + row * 128 + (((at & 7) ^ (row & 7)) << 4));
-        };
-        const int seen = (min(left, 16 * NS) - from) * (DP / 8), all = (16 * NS - from) * (DP / 8);
-        uint32_t acc = 0u;
-        for (int e = thread; e < all; e += threads) {
-          uint4* const p = piece(e);
-          if (e < seen)
-            look16<BF>(p->x, acc), look16<BF>(p->y, acc), look16<BF>(p->z, acc), look16<BF>(p->w, acc);
-          else
-            *p = make_uint4(0u, 0u, 0u, 0u);
-        }
-        if (bad16<BF>(acc) != 0u) {
-          *bad = 1;
-          for (int e = thread; e < seen; e += threads) {
-            uint4* const p = piece(e);
-            const uint4 w = *p;
-            *p = make_uint4(w.x & ~bad16<BF>(w.x), w.y & ~bad16<BF>(w.y), w.z & ~bad16<BF>(w.z), w.w & ~bad16<BF>(w.w));
-          }
-        }
-        fence_async_smem();  // (before the next tile is copied there)
-        if (MANY)
-          named_bar_sync(1, 32 * WARPS);
-        else
-          __syncwarp();
+      const int whole = least - key0, left = most - key0;
+      if (whole < KT) {
+        if (clear_values<BF, DP>(kb + T::tile, HALF, KT, max(whole, 0), left, threadIdx.x, 32 * WARPS)) *bad = 1;
+        named_bar_sync(1, 32 * WARPS);
       }
-      if (left > 0) {
-        float x[2 * NS][4];
-#pragma unroll
-        for (int n = 0; n < 2 * NS; ++n) x[n][0] = x[n][1] = x[n][2] = x[n][3] = 0.0f;
-        const uint32_t ks = smem_addr(kb) + krow * 128, vs = smem_addr(kb + T::tile) + vrow * 128;
-#pragma unroll
-        for (int n = 0; n < NS; ++n) {
-          if (16 * n >= left) continue;
-#pragma unroll
-          for (int k = 0; k < DP / 16; ++k) {
-            uint32_t bk[4];
-            ldmatrix4(ks + n * 2048 + (k >> 2) * HALF + (((2 * (k & 3) + kpiece) ^ (krow & 7)) << 4), bk);
-            mma16816<BF>(x[2 * n], q[k], bk[0], bk[1]);
-            mma16816<BF>(x[2 * n + 1], q[k], bk[2], bk[3]);
-          }
-        }
-        if (whole < 16 * NS) {
-#pragma unroll
-          for (int n = 0; n < 2 * NS; ++n)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (key0 + 8 * n + c2 + (j & 1) >= vis[j >> 1]) x[n][j] = -INFINITY;
-        }
-        float top[2], keep[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float v = -INFINITY;
-#pragma unroll
-          for (int n = 0; n < 2 * NS; ++n) v = max3(v, x[n][2 * h], x[n][2 * h + 1]);
-          v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
-          v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
-          top[h] = fmaxf(m[h], v);
-        }
-        if (__any_sync(0xffffffffu, (top[0] - m[0]) * sc > kLazy || (top[1] - m[1]) * sc > kLazy)) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            keep[h] = m[h] == -INFINITY ? 0.0f : ex2_approx((m[h] - top[h]) * sc);
-            sum[h] *= keep[h];
-            m[h] = top[h];
-          }
-#pragma unroll
-          for (int j = 0; j < DP / 8; ++j) o[j][0] *= keep[0], o[j][1] *= keep[0], o[j][2] *= keep[1], o[j][3] *= keep[1];
-        }
-        uint32_t p[NS][4];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float neg = m[h] == -INFINITY ? 0.0f : fmaf(-m[h], sc, -a.down);
-#pragma unroll
-          for (int n = 0; n < NS; ++n) {
-            float e[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) e[j] = ex2_approx(fmaf(x[2 * n + (j >> 1)][2 * h + (j & 1)], sc, neg));
-            sum[h] += (e[0] + e[1]) + (e[2] + e[3]);
-            p[n][h] = pack16<BF>(e[0], e[1]);
-            p[n][2 + h] = pack16<BF>(e[2], e[3]);
-          }
-        }
-#pragma unroll
-        for (int n = 0; n < NS; ++n) {
-          if (16 * n >= left) continue;
-#pragma unroll
-          for (int k = 0; k < DP / 16; ++k) {
-            uint32_t bv[4];
-            ldmatrix4_trans(vs + n * 2048 + (k >> 2) * HALF + (((2 * (k & 3) + vpiece) ^ (vrow & 7)) << 4), bv);
-            mma16816<BF>(o[2 * k], p[n], bv[0], bv[1]);
-            mma16816<BF>(o[2 * k + 1], p[n], bv[2], bv[3]);
-          }
-        }
+#pragma unroll 1
+      for (int n = 0; n < KT && n < left; n += 32) {  // (32 keys at a time: with 64 the registers do for two CTAs an SM)
+        const int seen[2] = {vis[0] - key0 - n, vis[1] - key0 - n};
+        x.template step<2>(q, smem_addr(kb) + (n + krow) * 128, smem_addr(kb + T::tile) + (n + vrow) * 128, HALF, left - n, whole < n + 32, seen, sc,
+                           a.down, lane);
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&empty[s]);
@@ -313,68 +469,33 @@ __global__ void __launch_bounds__(THREADS, Shape<DP, MANY>::ctas)
     if (!ok && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
   }
   __syncthreads();  // all tiles are consumed: the ring's memory takes the results, [channels / 4][row] of four channels
-  float* const whole = reinterpret_cast<float*>(smem);  // of this CTA's block
-  float* const cta = whole + ROWS * DP;                 // [row][maximum, sum]
-  float* const part = cta + 2 * ROWS;                   // [warp] of 16 rows, and
-  float* const stat = part + T::part;                   // [warp][row][maximum, sum]
+  float* const sums = reinterpret_cast<float*>(smem);
+  float* const stat = sums + DP / 4 * QUAD;  // [row][maximum, sum]
   if (warp < WARPS) {
-    const int r = lane >> 2, c2 = 2 * (lane & 3);
-    float* const to = MANY ? whole : part + warp * 16 * DP;
-    float* const st = MANY ? cta : stat + warp * 32;
+    x.finish();
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      sum[h] += __shfl_xor_sync(0xffffffffu, sum[h], 1);
-      sum[h] += __shfl_xor_sync(0xffffffffu, sum[h], 2);
       const int row = base + r + 8 * h;
-      if ((lane & 3) == 0) *reinterpret_cast<float2*>(st + 2 * row) = make_float2(m[h], sum[h]);
+      if ((lane & 3) == 0) *reinterpret_cast<float2*>(stat + 2 * row) = make_float2(x.m[h], x.sum[h]);
 #pragma unroll
       for (int j = 0; j < DP / 8; ++j)
-        *reinterpret_cast<float2*>(to + ((2 * j + (c2 >> 2)) * ROWS + row) * 4 + (c2 & 3)) = make_float2(o[j][2 * h], o[j][2 * h + 1]);
+        *reinterpret_cast<float2*>(sums + (2 * j + (c2 >> 2)) * QUAD + 4 * row + (c2 & 3)) = make_float2(x.o[j][2 * h], x.o[j][2 * h + 1]);
     }
   }
   __syncthreads();
   const int quads = a.head_dim / 4;
-  const float sc = a.scale_log2;
   const bool left_out = *bad != 0;
-  // (a thread keeps its row: what the addresses of a row take is reckoned once)
+  // a row a thread: what the addresses of a row take is reckoned once
   const int row = threadIdx.x & (ROWS - 1);
-  if (row < nrows && threadIdx.x < THREADS / ROWS * ROWS) {
-    const int qi = query(row), head = row0 + row - qi * a.group, sub = head / a.hg, h = kvh * a.nsub + sub;
+  if (row < nrows && threadIdx.x < 2 * ROWS) {
+    const int qi = query(row), head = row0 + row - qi * a.group, sub = head / a.hg, hs = kvh * a.nsub + sub;
     const long long rho = static_cast<long long>(q0 + qi) * a.hg + (head - sub * a.hg);
-    float* const sums = a.parts.sums + a.parts.sums_at(a.prefix_parts + rank, h, rho);
-    float f[WARPS];
-    float top = -INFINITY, total = 0.0f;
-    if constexpr (MANY) {
-      const float2 st = *reinterpret_cast<const float2*>(cta + 2 * row);
-      top = st.x, total = st.y;
-    } else {
-#pragma unroll
-      for (int w = 0; w < WARPS; ++w) top = fmaxf(top, stat[32 * w + 2 * row]);
-#pragma unroll
-      for (int w = 0; w < WARPS; ++w) {
-        const float2 st = *reinterpret_cast<const float2*>(stat + 32 * w + 2 * row);
-        // (a part without a finite score has sums of zeros, or NaN that must stay)
-        f[w] = st.x == -INFINITY ? 1.0f : ex2_approx((st.x - top) * sc);
-        total = fmaf(st.y, f[w], total);
-      }
-    }
-    if (threadIdx.x < ROWS)
-      *reinterpret_cast<float2*>(a.parts.stat + a.parts.stat_at(a.prefix_parts + rank, h, rho)) = make_float2(top, left_out ? -total : total);
-    if (top != -INFINITY)
-      for (int quad = threadIdx.x / ROWS; quad < quads; quad += THREADS / ROWS) {
-        float4 y;
-        if constexpr (MANY) {
-          y = *reinterpret_cast<const float4*>(whole + (quad * ROWS + row) * 4);
-        } else {
-          y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-          for (int w = 0; w < WARPS; ++w) {
-            const float4 o4 = *reinterpret_cast<const float4*>(part + w * 16 * DP + (quad * ROWS + row) * 4);
-            y.x = fmaf(o4.x, f[w], y.x), y.y = fmaf(o4.y, f[w], y.y), y.z = fmaf(o4.z, f[w], y.z), y.w = fmaf(o4.w, f[w], y.w);
-          }
-        }
-        *reinterpret_cast<float4*>(sums + quad * kQuadStep) = y;
-      }
+    const float2 st = *reinterpret_cast<const float2*>(stat + 2 * row);
+    float* const to = a.parts.sums + a.parts.sums_at(a.prefix_parts + rank, hs, rho);
+    if (threadIdx.x < ROWS) *reinterpret_cast<float2*>(a.parts.stat + a.parts.stat_at(a.prefix_parts + rank, hs, rho)) = make_float2(st.x, left_out ? -st.y : st.y);
+    if (st.x != -INFINITY)
+      for (int quad = threadIdx.x / ROWS; quad < quads; quad += 2)
+        *reinterpret_cast<float4*>(to + quad * kQuadStep) = *reinterpret_cast<const float4*>(sums + quad * QUAD + 4 * row);
   }
   if (blockIdx.x == gridDim.x - 1) pdl_wait();
 }
@@ -383,7 +504,7 @@ __global__ void __launch_bounds__(THREADS, Shape<DP, MANY>::ctas)
 // the weighted sums, four channels of a row a thread: four neighbouring threads have a row, so that whole sectors of the
 // parts and of out move.
 template <bool BF, int ROWS>
-__global__ void __launch_bounds__(JOIN_THREADS)
+__global__ void __launch_bounds__(JOIN_THREADS, ROWS == 64 ? 4 : 2)
     prefix_join_kernel(const __grid_constant__ PrefixOwnArgs a) {
   constexpr int GROUPS = JOIN_THREADS / ROWS;  // threads that share a row's parts
   extern __shared__ float weight[];            // [part][ROWS]: times 1 / the joint sum; -1: not to be read
@@ -395,37 +516,30 @@ __global__ void __launch_bounds__(JOIN_THREADS)
   // (the inputs may be read before the wait, as by prefix_own_kernel)
   int q0, nq, k0, nk;
   sequence(a, b, q0, nq, k0, nk);
-  // its prefix: the last g with seq_start[g] <= b
-  int prefix = 0, len = a.max_prefix;
-  if (a.seq_start) {
-    int lo = 0, hi = a.prefixes;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (a.seq_start[mid] <= b)
-        lo = mid;
-      else
-        hi = mid;
-    }
-    prefix = a.seq_start[lo] <= b && b < a.seq_start[lo + 1] ? lo : -1;
-    if (prefix < 0) len = 0;
+  // its prefix (-1: none) and the number of its keys: a prefix a thread, so that all loads are on the way at once
+  __shared__ int found[2];
+  if (threadIdx.x == 0) found[0] = a.seq_start ? -1 : 0, found[1] = a.seq_start ? 0 : a.max_prefix;
+  __syncthreads();
+  for (int g = threadIdx.x; g < a.prefixes; g += JOIN_THREADS) {
+    const int n = a.prefix_len ? min(max(a.prefix_len[g], 0), a.max_prefix) : a.max_prefix;
+    if (!a.seq_start || (a.seq_start[g] <= b && b < a.seq_start[g + 1])) found[0] = g, found[1] = n;
   }
-  if (prefix >= 0 && a.prefix_len) len = min(max(a.prefix_len[prefix], 0), a.max_prefix);
+  __syncthreads();
+  const int prefix = found[0], len = found[1];
   const int heads = a.heads_kv * a.group, row0 = blk * ROWS, nrows = min(nq * heads - row0, ROWS);
   if (nrows <= 0) return;
-  const int key_tiles = (len + kPrefixTile - 1) / kPrefixTile, parts = a.prefix_parts + (a.max_keys > 0 ? a.own_split : 0);
-  auto written = [&](int p) {  // (a part without key tiles of its prefix is not)
-    const int r = a.pair ? p >> 1 : p;
-    return p >= a.prefix_parts || split_from(key_tiles, r + 1, a.split) - split_from(key_tiles, r, a.split) > (a.pair ? p & 1 : 0);
-  };
+  const int parts = a.prefix_parts + (a.max_keys > 0 ? a.own_split : 0);
   struct Row {
     int query, head, h;
     long long rho;
   };
   auto place = [&](int row) {
+    // (the rows of a key head together, as in the parts)
     Row r;
-    r.query = static_cast<int>(a.by_heads.quotient(row0 + row)), r.head = row0 + row - r.query * heads;
-    const int kvh = static_cast<int>(a.by_group.quotient(r.head)), in = r.head - kvh * a.group, sub = in / a.hg;
-    r.h = kvh * a.nsub + sub;
+    const int each = nq * a.group, kvh = (row0 + row) / each, own = row0 + row - kvh * each;
+    r.query = static_cast<int>(a.by_group.quotient(own));
+    const int in = own - r.query * a.group, sub = in / a.hg;
+    r.head = kvh * a.group + in, r.h = kvh * a.nsub + sub;
     r.rho = static_cast<long long>(q0 + r.query) * a.hg + (in - sub * a.hg);
     return r;
   };
@@ -442,7 +556,7 @@ __global__ void __launch_bounds__(JOIN_THREADS)
     pdl_wait();
 #pragma unroll 4
     for (int p = g; p < parts; p += GROUPS) {
-      const float2 v = written(p) ? *reinterpret_cast<const float2*>(st + p * step) : make_float2(-INFINITY, 0.0f);
+      const float2 v = p >= a.prefix_parts || has_keys(a, p, len) ? *reinterpret_cast<const float2*>(st + p * step) : make_float2(-INFINITY, 0.0f);
       left_out |= __float_as_int(v.y) < 0;
       const float up = fmaxf(top, v.x);
       total = total * factor(top, up) + fabsf(v.y) * factor(v.x, up);
@@ -511,41 +625,33 @@ __global__ void __launch_bounds__(JOIN_THREADS)
       for (int u = 0; u < U; ++u) {
         const int quad = quad0 + u * STEP;
         if (quad >= quads) continue;
-        float z[4] = {y[u].x, y[u].y, y[u].z, y[u].w};
-        // (an infinite value whose probability has rounded to 0 gave NaN)
-        const float odd = fmaf(z[0], 0.0f, fmaf(z[1], 0.0f, fmaf(z[2], 0.0f, z[3] * 0.0f)));
-        if ((odd != 0.0f || look[row]) && none == 0.0f) {
-          const int seen = min(max(nk - nq + r.query + 1, 0), nk);  // of the own keys
-#pragma unroll 1
-          for (int j = 0; j < 4; ++j) {
-            const float was = j == 0 ? z[0] : j == 1 ? z[1] : j == 2 ? z[2] : z[3];
-            float s = 0.0f;
-            if (seen > 0) s += bad_values<BF>(a.v + (a.kv_start ? 0 : b * a.v_batch) + k0 * a.v_row + kvh * a.v_head + 4 * quad + j, a.v_row, seen);
-            if (!(fabsf(was) < INFINITY) && len > 0)
-              s += bad_values<BF>(a.pv + prefix * a.pv_batch + kvh * a.pv_head + 4 * quad + j, a.pv_row, len);
-            if (s != 0.0f) z[0] = j == 0 ? s : z[0], z[1] = j == 1 ? s : z[1], z[2] = j == 2 ? s : z[2], z[3] = j == 3 ? s : z[3];  // (NaN too)
-          }
-        }
-        *reinterpret_cast<uint2*>(out + 4 * quad) = make_uint2(pack16<BF>(z[0], z[1]), pack16<BF>(z[2], z[3]));
+        float4 z = y[u];
+        if (none == 0.0f) z = put_bad_values<BF>(a, z, b, kvh, k0, min(max(nk - nq + r.query + 1, 0), nk), prefix, len, quad, look[row]);
+        *reinterpret_cast<uint2*>(out + 4 * quad) = make_uint2(pack16<BF>(z.x, z.y), pack16<BF>(z.z, z.w));
       }
     }
   };
-  if (parts <= 2)
-    run(std::integral_constant<int, ROWS == 64 ? 4 : 2>(), std::integral_constant<int, 2>());
+  if constexpr (ROWS == 16)
+    run(std::integral_constant<int, 2>(), std::integral_constant<int, 8>());
+  else if (parts <= 2)
+    run(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
   else
-    run(std::integral_constant<int, 1>(), std::integral_constant<int, 16>());
+    run(std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
 }
 
-template <bool BF, int DP, bool MANY>
+template <bool BF, int DP>
 cudaError_t launch(const PrefixOwn& own, cudaStream_t s) {
+  const PrefixOwnArgs& a = own.a;
   cudaError_t e = cudaSuccess;
-  if (own.keys)
-    e = launch_pdl(prefix_own_kernel<BF, DP, MANY>, dim3(static_cast<unsigned>(own.units * own.a.own_split)), dim3(THREADS), Shape<DP, MANY>::smem, s,
-                   own.k, own.v, own.a);
+  const dim3 grid(static_cast<unsigned>(own.units * a.own_split));
+  if (own.many)
+    e = launch_pdl(prefix_many_kernel<BF, DP>, grid, dim3(THREADS), Many<DP>::smem, s, own.k, own.v, a);
+  else if (a.max_keys > 0)
+    e = launch_pdl(prefix_few_kernel<BF, DP>, grid, dim3(32), Few<DP>::smem, s, own.k, own.v, a);
   if (e != cudaSuccess) return e;
-  const int parts = own.a.prefix_parts + (own.keys ? own.a.own_split : 0), rows = own.join_rows;
-  return launch_pdl(rows == 64 ? prefix_join_kernel<BF, 64> : prefix_join_kernel<BF, 16>, dim3(static_cast<unsigned>(own.a.batch) * own.a.join_blocks),
-                    dim3(JOIN_THREADS), 4 * parts * rows, s, own.a);
+  const int parts = a.prefix_parts + (a.max_keys > 0 ? a.own_split : 0), rows = own.join_rows;
+  return launch_pdl(rows == 64 ? prefix_join_kernel<BF, 64> : prefix_join_kernel<BF, 16>, dim3(static_cast<unsigned>(a.batch) * a.join_blocks),
+                    dim3(JOIN_THREADS), 4 * parts * rows, s, a);
 }
 
 cudaError_t init_attributes() {
@@ -553,15 +659,17 @@ cudaError_t init_attributes() {
   auto set = [&](auto* f, int bytes) {
     if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   };
-  auto both = [&](auto many) {
-    constexpr bool M = many.value;
-    set(prefix_own_kernel<true, 64, M>, Shape<64, M>::smem);
-    set(prefix_own_kernel<false, 64, M>, Shape<64, M>::smem);
-    set(prefix_own_kernel<true, 128, M>, Shape<128, M>::smem);
-    set(prefix_own_kernel<false, 128, M>, Shape<128, M>::smem);
+  auto all = [&](auto bf) {
+    constexpr bool B = bf.value;
+    set(prefix_few_kernel<B, 64>, Few<64>::smem);
+    set(prefix_few_kernel<B, 128>, Few<128>::smem);
+    set(prefix_many_kernel<B, 64>, Many<64>::smem);
+    set(prefix_many_kernel<B, 128>, Many<128>::smem);
+    set(prefix_join_kernel<B, 16>, 4 * 16 * kMaxParts);
+    set(prefix_join_kernel<B, 64>, 4 * 64 * kMaxParts);
   };
-  both(std::false_type());
-  both(std::true_type());
+  all(std::false_type());
+  all(std::true_type());
   return e;
 }
 
@@ -585,7 +693,7 @@ elasto_status prefix_own_plan(const elasto_prefix_attention_args& u, const Prefi
   a.hg = p.hg, a.nsub = p.nsub, a.pair = p.pair, a.split = p.split, a.parts = parts;
   a.prefix_parts = p.prefix_parts(), a.own_split = p.own_split;
   a.status = status;
-  own->many = p.many != 0, own->keys = u.max_keys > 0;
+  own->many = p.many != 0 && u.max_keys > 0;
   own->units = static_cast<int64_t>(p.blocks) * a.batch * a.heads_kv;
   if (own->units * a.own_split > 0x7fffffffLL) {
     set_error("elasto_op_prefix_attention: too many sequences or queries");
@@ -601,14 +709,14 @@ elasto_status prefix_own_plan(const elasto_prefix_attention_args& u, const Prefi
     return ELASTO_ERR_UNSUPPORTED;
   }
   a.join_blocks = static_cast<int>(join_blocks);
-  a.by_join = Divisor(a.join_blocks), a.by_heads = Divisor(u.heads);
+  a.by_join = Divisor(a.join_blocks);
   a.by_split = Divisor(a.own_split), a.by_blocks = Divisor(a.blocks), a.by_heads_kv = Divisor(a.heads_kv), a.by_group = Divisor(a.group);
   own->a = a, own->bf = u.dtype == ELASTO_BF16;
   auto map_of = [&](CUtensorMap* tm, const void* data, long long head_s, long long row_s, long long batch_s) {
     const uint64_t dims[4] = {static_cast<uint64_t>(u.head_dim), static_cast<uint64_t>(u.heads_kv), static_cast<uint64_t>(u.kv_rows),
                               static_cast<uint64_t>(u.kv_start ? 1 : u.batch)};
     const uint64_t strides[3] = {static_cast<uint64_t>(head_s) * 2, static_cast<uint64_t>(row_s) * 2, u.kv_start ? 0 : static_cast<uint64_t>(batch_s) * 2};
-    const uint32_t box[4] = {64, 1, KT, 1};
+    const uint32_t box[4] = {64, 1, own->many ? KT : 16u, 1};
     return encode_tmap_16(tm, data, own->bf, 4, dims, strides, box);
   };
   own->k = CUtensorMap{}, own->v = CUtensorMap{};
@@ -620,11 +728,8 @@ elasto_status prefix_own_plan(const elasto_prefix_attention_args& u, const Prefi
 }
 
 elasto_status prefix_own_launch(const PrefixOwn& own, cudaStream_t s) {
-  auto run = [&](auto bf, auto many) {
-    return own.a.head_dim <= 64 ? launch<bf.value, 64, many.value>(own, s) : launch<bf.value, 128, many.value>(own, s);
-  };
-  auto typed = [&](auto many) { return own.bf ? run(std::true_type(), many) : run(std::false_type(), many); };
-  ELASTO_CUDA_TRY(own.many ? typed(std::true_type()) : typed(std::false_type()));
+  auto run = [&](auto bf) { return own.a.head_dim <= 64 ? launch<bf.value, 64>(own, s) : launch<bf.value, 128>(own, s); };
+  ELASTO_CUDA_TRY(own.bf ? run(std::true_type()) : run(std::false_type()));
   return ELASTO_OK;
 }
 

@@ -28,7 +28,7 @@ struct PrefixOwnArgs {
   PrefixParts parts;
   int blocks;  // of rows, of a sequence and key head
   int join_blocks;  // of rows of a sequence over all heads, for the join
-  Divisor by_join, by_heads;
+  Divisor by_join;
   Divisor by_split, by_blocks, by_heads_kv, by_group;
   int* status;
 };
@@ -37,7 +37,7 @@ struct PrefixOwn {
   CUtensorMap k, v;
   int64_t units;
   int join_rows;  // of a CTA of the join
-  bool bf, many, keys;  // many: blocks of 64 rows; keys: there are own ones
+  bool bf, many;  // many: blocks of 64 rows
 };
 elasto_status prefix_own_plan(const elasto_prefix_attention_args& u, const PrefixPlan& p, const PrefixParts& parts, float down, int* status,
                               PrefixOwn* own);

@@ -12,7 +12,8 @@
 namespace elasto {
 
 constexpr int kPrefixTile = 128;                 // rows of Q, and keys, of a tile
-constexpr int kPrefixSplit = 64, kOwnSplit = 16;  // CTAs that share keys at most
+constexpr int kPrefixSplit = 64, kOwnSplit = 64;  // CTAs that share keys at most
+constexpr int kMaxParts = 2 * kPrefixSplit + kOwnSplit;
 
 // A row is a query head at a query: rho = q row * hg + head of the tile. An item is one or two tiles of 128 rows of
 // one prefix and key head (or part of its query heads); its key tiles are shared out over `split` CTAs. With one tile of
@@ -48,30 +49,41 @@ inline PrefixPlan prefix_plan(const PrefixSizes& z) {
     return k < n ? k : n;
   };
   p.items = items(z.most);
-  // The sequences' own keys: blocks of 64 rows where a sequence has more than three of 16 and several queries. CTAs until the SMs have six
-  // each, with four tiles of 64 keys at least, so that sequences of different lengths even out.
+  // The sequences' own keys: blocks of 64 rows where a sequence has more than three of 16 and several queries, in CTAs
+  // until the SMs have six each, with four tiles of 64 keys at least; else of 16 rows, in CTAs of a warp until the SMs have
+  // fourteen, with 256 keys at least: sequences of different lengths even out.
   const int64_t rows = static_cast<int64_t>(z.max_queries) * z.group;
   p.many = z.max_queries > 1 && rows > 48;
-  const int64_t of = p.many ? 64 : 16;
+  const int64_t of = p.many ? 64 : 16, enough = (p.many ? 6LL : 14LL) * z.sms;
   p.blocks = static_cast<int>((rows + of - 1) / of);
   const int64_t units = static_cast<int64_t>(p.blocks) * z.batch * z.heads_kv;
   p.own_split = 1;
-  while (p.own_split < kOwnSplit && units * p.own_split < 6LL * z.sms && z.max_keys >= 512LL * p.own_split) p.own_split *= 2;
+  while (p.own_split < kOwnSplit && units * p.own_split < enough && z.max_keys >= 512LL * p.own_split) p.own_split *= 2;
+  while (!p.many && p.own_split < 4 && units * p.own_split < z.sms && z.max_keys >= 64LL * p.own_split) p.own_split *= 2;
   // How many CTAs share a prefix's keys. Both kernels run at the same time, the prefixes' with an SM a CTA, the other
-  // on what is left: in microseconds, of a CTA's start and end, of a key tile, of a part of all rows written and read,
-  // and of the own keys (about 0.6 of the longest each) at the memory's rate, which takes 60 SMs.
-  const int64_t tiles = (z.max_prefix + kPrefixTile - 1) / kPrefixTile, ctas = items(z.rows) * z.heads_kv * p.nsub;
+  // on what is left. In microseconds: of a prefix's CTA its start and end and its key tiles (which wait longer for their
+  // keys, where it alone reads them, while the other kernel reads at the memory's rate: 64 sequences behind 8192 keys took
+  // 48 us with five CTAs a key head, 35 with ten); of a part of all rows, written and read; of the own keys (about 0.6 of
+  // the longest each) the memory's time, and an SM's for all their CTAs.
+  const int64_t tiles = (z.max_prefix + kPrefixTile - 1) / kPrefixTile, each = items(z.rows), ctas = each * z.heads_kv * p.nsub;
   const double start = 5.0, tile = (p.pair ? 0.7 : 1.4) * (z.head_dim > 64 ? 1.0 : 0.7);
-  const double part = static_cast<double>(z.rows) * z.group * z.heads_kv * (8.0 * z.head_dim + 16) * (p.pair ? 2 : 1) / 8e6;
-  const double own = 0.6 * 4.0 * z.head_dim * z.heads_kv * static_cast<double>(z.batch) * z.max_keys / 6.5e6;
+  const double part = (static_cast<double>(z.rows) * z.group * z.heads_kv * (8.0 * z.head_dim + 16) / 8e6 + 0.15) * (p.pair ? 2 : 1);
+  const double keys = 0.6 * static_cast<double>(z.max_keys);
+  const double memory = keys * 4.0 * z.head_dim * z.heads_kv * z.batch / 6.5e6;
+  const double sm = static_cast<double>(units) * p.own_split * (4.0 + 0.03 * keys / p.own_split) / (p.many ? 3 : 9);
+  auto own_rate = [&](double sms) {  // of all own keys, a microsecond
+    const double t = z.max_keys == 0 ? 0.0 : sms <= 0.0 ? 1e9 : sm / sms > memory ? sm / sms : memory;
+    return t > 0.01 ? 1.0 / t : 100.0;
+  };
   double best = 0.0;
   p.split = 1;
   for (int n = 1; n <= kPrefixSplit && n <= tiles; ++n) {
     const int64_t waves = (ctas * n + z.sms - 1) / z.sms;
-    const double prefix = static_cast<double>(waves) * (start + static_cast<double>((tiles + n - 1) / n) * tile);
-    const double left = waves > 1 ? 0.0 : static_cast<double>(z.sms - ctas * n), rate = left < 60 ? left / 60 : 1.0;
-    const double both = rate * prefix >= own ? prefix : prefix + (own - rate * prefix);
-    const double cost = both + n * part;
+    const double left = waves > 1 ? 0.0 : static_cast<double>(z.sms - ctas * n);
+    const double slow = 1.0 + (memory > 10.0 && left > 0.0 ? 0.6 * (left < 60 ? left / 60 : 1.0) : 0.0) * z.prefixes / static_cast<double>(each);
+    const double prefix = static_cast<double>(waves) * (start + static_cast<double>((tiles + n - 1) / n) * tile * slow);
+    const double done = prefix * own_rate(left);  // of the own keys
+    const double cost = prefix + (done < 1.0 ? (1.0 - done) / own_rate(z.sms) : 0.0) + n * part;
     if (n == 1 || cost < best) best = cost, p.split = n;
   }
   return p;
