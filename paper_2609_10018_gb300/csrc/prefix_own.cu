@@ -11,7 +11,7 @@
 // once, and both run at the same time. Only the last CTA waits before it ends, so that what waits for this kernel waits
 // for both.
 //
-// prefix_join_kernel: out = sum over parts of o exp(m - top) / sum of l exp(m - top), four channels a thread, in a fixed
+// prefix_join_few_kernel, prefix_join_many_kernel: out = sum over parts of o exp(m - top) / sum of l exp(m - top), four channels a thread, in a fixed
 // order.
 #include <algorithm>
 #include <type_traits>
@@ -500,55 +500,138 @@ __global__ void __launch_bounds__(THREADS, 3)
   if (blockIdx.x == gridDim.x - 1) pdl_wait();
 }
 
-// A CTA has ROWS rows (query, head) of one sequence, over all its heads. First the weight of each part in each row, then
+// Where a row (query, head) of a sequence is: its rows over all heads, those of a key head together as in the parts.
+struct JoinRow {
+  int query, head, kvh, h;
+  long long rho;
+};
+__device__ __forceinline__ JoinRow join_row(const PrefixOwnArgs& a, int q0, int nq, int row) {
+  JoinRow r;
+  const int each = nq * a.group;
+  r.kvh = row / each;
+  const int own = row - r.kvh * each;
+  r.query = static_cast<int>(a.by_group.quotient(own));
+  const int in = own - r.query * a.group, sub = in / a.hg;
+  r.head = r.kvh * a.group + in, r.h = r.kvh * a.nsub + sub;
+  r.rho = static_cast<long long>(q0 + r.query) * a.hg + (in - sub * a.hg);
+  return r;
+}
+// The prefix of sequence b (-1: none) and the number of its keys, by a CTA, a prefix a thread, so that all loads are on the
+// way at once; and which parts have results, as bits.
+struct Found {
+  int prefix, len;
+  uint32_t written[(kMaxParts + 31) / 32];
+};
+__device__ __forceinline__ void find_prefix(const PrefixOwnArgs& a, int b, int parts, Found& found) {
+  if (threadIdx.x == 0) found.prefix = a.seq_start ? -1 : 0, found.len = a.seq_start ? 0 : a.max_prefix;
+  __syncthreads();
+  for (int g = threadIdx.x; g < a.prefixes; g += JOIN_THREADS) {
+    const int n = a.prefix_len ? min(max(a.prefix_len[g], 0), a.max_prefix) : a.max_prefix;
+    if (!a.seq_start || (a.seq_start[g] <= b && b < a.seq_start[g + 1])) found.prefix = g, found.len = n;
+  }
+  __syncthreads();
+  if (threadIdx.x < (parts + 31) / 32 * 32) {
+    const int p = threadIdx.x;
+    const uint32_t bits = __ballot_sync(0xffffffffu, p < a.prefix_parts ? has_keys(a, p, found.len) : p < parts);
+    if ((p & 31) == 0) found.written[p >> 5] = bits;
+  }
+  __syncthreads();
+}
+
+// The join of few rows: 32 rows of a sequence and 32 channels a CTA, four channels of a row a thread, which asks for all
+// its parts' statistics and sums (N at a time) at once.
+template <bool BF, int N>
+__global__ void __launch_bounds__(JOIN_THREADS)
+    prefix_join_few_kernel(const __grid_constant__ PrefixOwnArgs a) {
+  __shared__ Found found;
+  const int b = static_cast<int>(a.by_join.quotient(blockIdx.x)), blk = static_cast<int>(blockIdx.x) - b * a.join_blocks;
+  pdl_trigger();
+  // (the inputs may be read before the wait, as by prefix_few_kernel)
+  int q0, nq, k0, nk;
+  sequence(a, b, q0, nq, k0, nk);
+  const int parts = a.prefix_parts + (a.max_keys > 0 ? a.own_split : 0);
+  find_prefix(a, b, parts, found);
+  const int prefix = found.prefix, len = found.len;
+  const int row = 32 * blk + (threadIdx.x >> 3), quads = a.head_dim / 4;
+  if (row >= nq * a.heads_kv * a.group) return;
+  const JoinRow r = join_row(a, q0, nq, row);
+  const float* const st0 = a.parts.stat + a.parts.stat_at(0, r.h, r.rho);
+  const float* const y0 = a.parts.sums + a.parts.sums_at(0, r.h, r.rho);
+  const long long st_step = a.parts.stat_at(1, 0, 0), y_step = a.parts.sums_at(1, 0, 0);
+  const float sc = a.scale_log2;
+  const int seen = min(max(nk - nq + r.query + 1, 0), nk);  // of the own keys
+  uint16_t* const out = a.out + static_cast<long long>(q0 + r.query) * a.out_row + static_cast<long long>(r.head) * a.out_head;
+  const int quad = 8 * blockIdx.y + (threadIdx.x & 7);
+  if (quad >= quads) return;
+  float top = -INFINITY, total = 0.0f;
+  float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  bool left_out = false;
+  pdl_wait();
+  for (int p0 = 0; p0 < parts; p0 += N) {
+    const uint32_t bits = found.written[p0 >> 5] >> (p0 & 31);
+    float2 st[N];
+    float4 o[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      st[k] = make_float2(-INFINITY, 0.0f), o[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (bits >> k & 1) {
+        st[k] = *reinterpret_cast<const float2*>(st0 + (p0 + k) * st_step);
+        o[k] = *reinterpret_cast<const float4*>(y0 + (p0 + k) * y_step + quad * kQuadStep);
+      }
+    }
+    float up = top;
+#pragma unroll
+    for (int k = 0; k < N; ++k) up = fmaxf(up, st[k].x);
+    const float f = top == -INFINITY ? 1.0f : ex2_approx((top - up) * sc);
+    total *= f, y.x *= f, y.y *= f, y.z *= f, y.w *= f;
+    top = up;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      left_out |= __float_as_int(st[k].y) < 0;
+      // (a part without a finite score has a sum of 0, or NaN that must stay, and no weighted sums)
+      const bool none = st[k].x == -INFINITY;
+      const float w = none ? 1.0f : ex2_approx((st[k].x - top) * sc);
+      total = fmaf(fabsf(st[k].y), w, total);
+      y.x = none ? y.x : fmaf(o[k].x, w, y.x), y.y = none ? y.y : fmaf(o[k].y, w, y.y);
+      y.z = none ? y.z : fmaf(o[k].z, w, y.z), y.w = none ? y.w : fmaf(o[k].w, w, y.w);
+    }
+  }
+  const float inv = len > 0 || seen > 0 ? 1.0f / total : 0.0f;
+  y = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
+  if (total > 0.0f)
+    y = put_bad_values<BF>(a, y, b, r.kvh, k0, seen, prefix, len, quad, left_out);
+  else if (inv != 0.0f)  // (a sum of 0 or NaN over visible keys)
+    y.x = y.y = y.z = y.w = __int_as_float(0x7fc00000);
+  *reinterpret_cast<uint2*>(out + 4 * quad) = make_uint2(pack16<BF>(y.x, y.y), pack16<BF>(y.z, y.w));
+}
+
+// The join of many rows: a CTA has 64 of one sequence. First the weight of each part in each row, then
 // the weighted sums, four channels of a row a thread: four neighbouring threads have a row, so that whole sectors of the
 // parts and of out move.
-template <bool BF, int ROWS>
-__global__ void __launch_bounds__(JOIN_THREADS, ROWS == 64 ? 4 : 2)
-    prefix_join_kernel(const __grid_constant__ PrefixOwnArgs a) {
+template <bool BF>
+__global__ void __launch_bounds__(JOIN_THREADS, 4)
+    prefix_join_many_kernel(const __grid_constant__ PrefixOwnArgs a) {
   constexpr int GROUPS = JOIN_THREADS / ROWS;  // threads that share a row's parts
   extern __shared__ float weight[];            // [part][ROWS]: times 1 / the joint sum; -1: not to be read
   __shared__ float2 partial[GROUPS][ROWS];     // maximum and sum of a thread's parts (the sign: values left out)
   __shared__ float base[ROWS];                 // 0, or NaN in rows without a sum above 0
   __shared__ int look[ROWS];                   // 1: values that the row may see have been left out
+  __shared__ Found found;
   const int b = static_cast<int>(a.by_join.quotient(blockIdx.x)), blk = static_cast<int>(blockIdx.x) - b * a.join_blocks;
   pdl_trigger();
-  // (the inputs may be read before the wait, as by prefix_own_kernel)
   int q0, nq, k0, nk;
   sequence(a, b, q0, nq, k0, nk);
-  // its prefix (-1: none) and the number of its keys: a prefix a thread, so that all loads are on the way at once
-  __shared__ int found[2];
-  if (threadIdx.x == 0) found[0] = a.seq_start ? -1 : 0, found[1] = a.seq_start ? 0 : a.max_prefix;
-  __syncthreads();
-  for (int g = threadIdx.x; g < a.prefixes; g += JOIN_THREADS) {
-    const int n = a.prefix_len ? min(max(a.prefix_len[g], 0), a.max_prefix) : a.max_prefix;
-    if (!a.seq_start || (a.seq_start[g] <= b && b < a.seq_start[g + 1])) found[0] = g, found[1] = n;
-  }
-  __syncthreads();
-  const int prefix = found[0], len = found[1];
-  const int heads = a.heads_kv * a.group, row0 = blk * ROWS, nrows = min(nq * heads - row0, ROWS);
-  if (nrows <= 0) return;
   const int parts = a.prefix_parts + (a.max_keys > 0 ? a.own_split : 0);
-  struct Row {
-    int query, head, h;
-    long long rho;
-  };
-  auto place = [&](int row) {
-    // (the rows of a key head together, as in the parts)
-    Row r;
-    const int each = nq * a.group, kvh = (row0 + row) / each, own = row0 + row - kvh * each;
-    r.query = static_cast<int>(a.by_group.quotient(own));
-    const int in = own - r.query * a.group, sub = in / a.hg;
-    r.head = kvh * a.group + in, r.h = kvh * a.nsub + sub;
-    r.rho = static_cast<long long>(q0 + r.query) * a.hg + (in - sub * a.hg);
-    return r;
-  };
+  find_prefix(a, b, parts, found);
+  const int prefix = found.prefix, len = found.len;
+  const int row0 = blk * ROWS, nrows = min(nq * a.heads_kv * a.group - row0, ROWS);
+  if (nrows <= 0) return;
   const float sc = a.scale_log2;
   auto factor = [&](float m, float top) { return m == -INFINITY ? 1.0f : ex2_approx((m - top) * sc); };
   {
     // (a part without a finite score has a sum of 0, or NaN that must stay)
     const int row = threadIdx.x & (ROWS - 1), g = threadIdx.x / ROWS;
-    const Row r = place(min(row, nrows - 1));
+    const JoinRow r = join_row(a, q0, nq, row0 + min(row, nrows - 1));
     const float* const st = a.parts.stat + a.parts.stat_at(0, r.h, r.rho);
     const long long step = a.parts.stat_at(1, 0, 0);
     float top = -INFINITY, total = 0.0f;
@@ -556,7 +639,7 @@ __global__ void __launch_bounds__(JOIN_THREADS, ROWS == 64 ? 4 : 2)
     pdl_wait();
 #pragma unroll 4
     for (int p = g; p < parts; p += GROUPS) {
-      const float2 v = p >= a.prefix_parts || has_keys(a, p, len) ? *reinterpret_cast<const float2*>(st + p * step) : make_float2(-INFINITY, 0.0f);
+      const float2 v = found.written[p >> 5] >> (p & 31) & 1 ? *reinterpret_cast<const float2*>(st + p * step) : make_float2(-INFINITY, 0.0f);
       left_out |= __float_as_int(v.y) < 0;
       const float up = fmaxf(top, v.x);
       total = total * factor(top, up) + fabsf(v.y) * factor(v.x, up);
@@ -588,8 +671,8 @@ __global__ void __launch_bounds__(JOIN_THREADS, ROWS == 64 ? 4 : 2)
   }
   const int row = (threadIdx.x >> 2) & (ROWS - 1);
   if (row >= nrows) return;
-  const Row r = place(row);
-  const int kvh = r.h / a.nsub, quads = a.head_dim / 4;
+  const JoinRow r = join_row(a, q0, nq, row0 + row);
+  const int quads = a.head_dim / 4;
   const float* const sums = a.parts.sums + a.parts.sums_at(0, r.h, r.rho);
   const long long y_step = a.parts.sums_at(1, 0, 0);
   const float none = base[row];
@@ -626,14 +709,12 @@ __global__ void __launch_bounds__(JOIN_THREADS, ROWS == 64 ? 4 : 2)
         const int quad = quad0 + u * STEP;
         if (quad >= quads) continue;
         float4 z = y[u];
-        if (none == 0.0f) z = put_bad_values<BF>(a, z, b, kvh, k0, min(max(nk - nq + r.query + 1, 0), nk), prefix, len, quad, look[row]);
+        if (none == 0.0f) z = put_bad_values<BF>(a, z, b, r.kvh, k0, min(max(nk - nq + r.query + 1, 0), nk), prefix, len, quad, look[row]);
         *reinterpret_cast<uint2*>(out + 4 * quad) = make_uint2(pack16<BF>(z.x, z.y), pack16<BF>(z.z, z.w));
       }
     }
   };
-  if constexpr (ROWS == 16)
-    run(std::integral_constant<int, 2>(), std::integral_constant<int, 8>());
-  else if (parts <= 2)
+  if (parts <= 2)
     run(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
   else
     run(std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
@@ -649,9 +730,12 @@ cudaError_t launch(const PrefixOwn& own, cudaStream_t s) {
   else if (a.max_keys > 0)
     e = launch_pdl(prefix_few_kernel<BF, DP>, grid, dim3(32), Few<DP>::smem, s, own.k, own.v, a);
   if (e != cudaSuccess) return e;
-  const int parts = a.prefix_parts + (a.max_keys > 0 ? a.own_split : 0), rows = own.join_rows;
-  return launch_pdl(rows == 64 ? prefix_join_kernel<BF, 64> : prefix_join_kernel<BF, 16>, dim3(static_cast<unsigned>(a.batch) * a.join_blocks),
-                    dim3(JOIN_THREADS), 4 * parts * rows, s, a);
+  const int parts = a.prefix_parts + (a.max_keys > 0 ? a.own_split : 0);
+  const unsigned blocks = static_cast<unsigned>(a.batch) * a.join_blocks;
+  if (own.join_many) return launch_pdl(prefix_join_many_kernel<BF>, dim3(blocks), dim3(JOIN_THREADS), 4 * parts * ROWS, s, a);
+  const dim3 grid2(blocks, (a.head_dim + 31) / 32);
+  return launch_pdl(parts <= 4 ? prefix_join_few_kernel<BF, 4> : parts <= 8 ? prefix_join_few_kernel<BF, 8> : prefix_join_few_kernel<BF, 16>, grid2,
+                    dim3(JOIN_THREADS), 0, s, a);
 }
 
 cudaError_t init_attributes() {
@@ -665,8 +749,7 @@ cudaError_t init_attributes() {
     set(prefix_few_kernel<B, 128>, Few<128>::smem);
     set(prefix_many_kernel<B, 64>, Many<64>::smem);
     set(prefix_many_kernel<B, 128>, Many<128>::smem);
-    set(prefix_join_kernel<B, 16>, 4 * 16 * kMaxParts);
-    set(prefix_join_kernel<B, 64>, 4 * 64 * kMaxParts);
+    set(prefix_join_many_kernel<B>, 4 * ROWS * kMaxParts);
   };
   all(std::false_type());
   all(std::true_type());
@@ -700,10 +783,11 @@ elasto_status prefix_own_plan(const elasto_prefix_attention_args& u, const Prefi
     return ELASTO_ERR_UNSUPPORTED;
   }
   a.blocks = p.blocks;
-  // the join: 64 rows a CTA where these fill the SMs, else 16
+  // The join: 32 rows and channels a CTA, 64 rows and all channels from 40000 rows on (a small CTA's start then costs
+  // more than its loads).
   const int64_t all = static_cast<int64_t>(a.max_queries) * u.heads;
-  own->join_rows = (all + 63) / 64 * a.batch >= 2LL * num_sms() ? 64 : 16;
-  const int64_t join_blocks = (all + own->join_rows - 1) / own->join_rows;
+  own->join_many = all * a.batch > 40000;
+  const int64_t join_rows = own->join_many ? ROWS : 32, join_blocks = (all + join_rows - 1) / join_rows;
   if (join_blocks * a.batch > 0x7fffffffLL || all > 0x3fffffff) {
     set_error("elasto_op_prefix_attention: too many sequences or queries");
     return ELASTO_ERR_UNSUPPORTED;

@@ -36,8 +36,7 @@ struct PrefixOwn {
   PrefixOwnArgs a;
   CUtensorMap k, v;
   int64_t units;
-  int join_rows;  // of a CTA of the join
-  bool bf, many;  // many: blocks of 64 rows
+  bool bf, many, join_many;  // blocks of 64 rows; the join for many rows
 };
 elasto_status prefix_own_plan(const elasto_prefix_attention_args& u, const PrefixPlan& p, const PrefixParts& parts, float down, int* status,
                               PrefixOwn* own);
