@@ -105,7 +105,9 @@ struct PrefixParts {
 };
 constexpr int kQuadStep = 128;
 
-// The first key tile of a CTA (at most 2^24 tiles, and 64 CTAs).
-ELASTO_HD inline int split_from(int tiles, int rank, int split) { return tiles * rank / split; }
+// The first key tile of a CTA.
+ELASTO_HD inline int split_from(int tiles, int rank, int split) {
+  return static_cast<int>(static_cast<int64_t>(tiles) * rank / split);
+}
 
 }  // namespace elasto

@@ -1,0 +1,215 @@
+"""The operators of a transformer block together: an image's tokens go once through residual sum and norm (e4m3 rows), the QKV
+product and the rotation on two axes into the cache of a prefix; then prompts and single tokens of several sequences
+through the same and attention behind that prefix, the output product and the block's residual sum."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+import block_reference as block
+import sublayer_reference as ref
+from helpers import stream_handle
+from paper_2609_10018_gb300 import binding
+
+pytestmark = pytest.mark.gpu
+C, HEADS, HEADS_KV, D, GRID, CAP, BATCH = 256, 4, 2, 64, 12, 40, 3
+COLS, EPS = (HEADS + 2 * HEADS_KV) * D, 1e-6
+AXES = [0] * 16 + [1] * 16
+BF16 = torch.bfloat16
+
+
+def _i32(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+class Block:
+    def __init__(self):
+        g = torch.Generator().manual_seed(11)
+        rand = lambda *s: torch.randn(s, generator=g)  # noqa: E731
+        self.codes, self.scales, self.wide = {}, {}, {}
+        for n, shape in (("qkv", (COLS, C)), ("out", (C, HEADS * D))):
+            w = rand(*shape) / math.sqrt(shape[1])
+            _, s = ref.quantize(w)
+            s = s.t().reshape(ref.blocks(shape[0]), 128, -1).amax(1)
+            wide = s.repeat_interleave(128, 0).repeat_interleave(128, 1)
+            q = (w / wide).to(torch.float8_e4m3fn)
+            self.codes[n], self.scales[n], self.wide[n] = q.cuda(), s.contiguous().cuda(), q.double() * wide.double()
+        self.v = {n: (1 + 0.2 * rand(C) if n != "y_scale" else 0.5 * rand(C)) for n in ("post_gain", "pre_gain", "y_scale")}
+        self.mod = {n: 0.4 * rand(1 + BATCH, C) for n in ("gate", "shift", "scale")}  # the image's, and the sequences'
+        inv = 100.0 ** (-torch.arange(16, dtype=torch.float64).repeat(2) / 16)
+        angle = torch.arange(200, dtype=torch.float64)[:, None] * inv
+        self.table = torch.cat([angle.cos(), angle.sin()], 1).float()
+        self.gains = {n: 1 + 0.2 * rand(D) for n in ("q", "k")}
+        self.dev = {n: t.cuda() for d in (self.v, self.mod, {"table": self.table, "gq": self.gains["q"], "gk": self.gains["k"]}) for n, t in d.items()}
+        n = GRID * GRID
+        self.cache = {p + kv: torch.zeros((r, HEADS_KV, D), dtype=BF16, device="cuda") for p, r in (("p", n), ("o", BATCH * CAP)) for kv in "kv"}
+        self.st = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def norm(self, x, y, groups, first):
+        """x += gated y in place (y None: not), and the e4m3 rows of the modulated norm, or (not `first`) the sum alone."""
+        rows, d, s = x.shape[0], self.dev, stream_handle()
+        z = torch.empty((rows, C), dtype=torch.uint8, device="cuda")
+        scale = torch.empty((C // 128, rows), device="cuda")
+        group = _i32(groups)
+        binding.elasto_op_residual_norm(s, binding.ResidualNorm(
+            rows=rows, cols=C, eps=EPS, x_factor=1.0, x_type=binding.F32, x=x.data_ptr(), x_row=C, x_out=x.data_ptr() if y is not None else None,
+            x_out_row=C, y_type=binding.F32, y=None if y is None else y.data_ptr(), y_row=C, post_norm=binding.NORM_RMS,
+            post_gain=d["post_gain"].data_ptr(), y_scale=d["y_scale"].data_ptr(), pre_norm=binding.NORM_LAYER, pre_gain=d["pre_gain"].data_ptr(),
+            groups=1 + BATCH, group=group.data_ptr(), mod_type=binding.F32, mod_row=C, gate=d["gate"].data_ptr(), shift=d["shift"].data_ptr(),
+            scale=d["scale"].data_ptr(), z_type=binding.E4M3, z=z.data_ptr() if first else None, z_row=C,
+            z_scale=scale.data_ptr() if first else None, z_scale_row=rows), self.st.data_ptr())
+        return z, scale
+
+    def product(self, z, scale, name, out, epilogue):
+        w = self.codes[name]
+        binding.elasto_op_gemm_fp8(stream_handle(), z.data_ptr(), z.shape[1], scale.data_ptr(), scale.shape[1], w.data_ptr(), w.shape[1],
+                                   self.scales[name].data_ptr(), None, out.data_ptr(), out.shape[1], z.shape[0], w.shape[0], z.shape[1], epilogue,
+                                   self.st.data_ptr())
+
+    def rotate(self, qkv, positions, slots, cache):
+        at, rows, d = qkv.data_ptr(), qkv.shape[0], self.dev
+        pos, slot = _i32(positions), _i32(slots)
+        k, v = self.cache[cache + "k"], self.cache[cache + "v"]
+        binding.elasto_op_qk_norm_rope_axes(stream_handle(), binding.QkNormRopeAxes(
+            dtype=binding.BF16, rows=rows, heads_q=HEADS, heads_k=HEADS_KV, head_dim=D, rot_dim=D, pairing=binding.PAIRS_AXIS, norm=1, eps=EPS,
+            q=at, q_row=COLS, q_head=D, k=at + 2 * HEADS * D, k_row=COLS, k_head=D, v=at + 2 * (HEADS + HEADS_KV) * D, v_row=COLS, v_head=D,
+            q_out=at, q_out_row=COLS, q_out_head=D, k_out=k.data_ptr(), k_out_row=HEADS_KV * D, k_out_head=D,
+            v_out=v.data_ptr(), v_out_row=HEADS_KV * D, v_out_head=D, q_gain=d["gq"].data_ptr(), k_gain=d["gk"].data_ptr(),
+            cos_sin=d["table"].data_ptr(), n_positions=200, axes=2, axis_of=(ctypes.c_uint8 * 32)(*AXES), positions=pos.data_ptr(),
+            positions_row=2, positions_axis=1, slots=slot.data_ptr(), n_slots=k.shape[0]), self.st.data_ptr())
+
+    def image(self, x):
+        """The image's tokens into the prefix's cache."""
+        z, scale = self.norm(x, None, [0] * x.shape[0], True)
+        qkv = torch.empty((x.shape[0], COLS), dtype=BF16, device="cuda")
+        self.product(z, scale, "qkv", qkv, binding.EPI_BIAS_BF16)
+        self.rotate(qkv, [[i // GRID, i % GRID] for i in range(x.shape[0])], list(range(x.shape[0])), "p")
+
+    def step(self, x, counts, before):
+        """x fp32, in place: counts[b] new tokens of sequence b behind the image and before[b] tokens of its own."""
+        rows = x.shape[0]
+        groups = [1 + b for b in range(BATCH) for _ in range(counts[b])]
+        place = [(b, before[b] + i) for b in range(BATCH) for i in range(counts[b])]
+        z, scale = self.norm(x, None, groups, True)
+        qkv = torch.empty((rows, COLS), dtype=BF16, device="cuda")
+        self.product(z, scale, "qkv", qkv, binding.EPI_BIAS_BF16)
+        self.rotate(qkv, [[GRID + i, GRID + i] for _, i in place], [b * CAP + i for b, i in place], "o")
+        o = torch.empty((rows, HEADS * D), dtype=BF16, device="cuda")
+        starts, lens = _i32([sum(counts[:b]) for b in range(BATCH + 1)]), _i32([a + c for a, c in zip(before, counts)])
+        k = {n: t.data_ptr() for n, t in self.cache.items()}
+        n = GRID * GRID
+        args = binding.PrefixAttention(
+            dtype=binding.BF16, batch=BATCH, heads=HEADS, heads_kv=HEADS_KV, head_dim=D, scale=1 / math.sqrt(D), max_queries=max(counts),
+            q_rows=rows, q_start=starts.data_ptr(), q=qkv.data_ptr(), q_row=COLS, q_head=D, out=o.data_ptr(), out_row=HEADS * D, out_head=D,
+            prefixes=1, max_prefix=n, prefix_rows=n, prefix_k=k["pk"], prefix_k_row=HEADS_KV * D, prefix_k_head=D, prefix_v=k["pv"],
+            prefix_v_row=HEADS_KV * D, prefix_v_head=D, max_keys=CAP, kv_rows=CAP, kv_len=lens.data_ptr(), k=k["ok"], k_batch=CAP * HEADS_KV * D,
+            k_row=HEADS_KV * D, k_head=D, v=k["ov"], v_batch=CAP * HEADS_KV * D, v_row=HEADS_KV * D, v_head=D)
+        work = torch.empty(binding.elasto_op_prefix_attention_workspace(args), dtype=torch.uint8, device="cuda")
+        args.workspace, args.workspace_bytes = work.data_ptr(), work.numel()
+        binding.elasto_op_prefix_attention(stream_handle(), args, self.st.data_ptr())
+        oq, os = torch.empty((rows, HEADS * D), dtype=torch.uint8, device="cuda"), torch.empty((HEADS * D // 128, rows), device="cuda")
+        binding.elasto_op_quantize_fp8(stream_handle(), o.data_ptr(), binding.BF16, HEADS * D, oq.data_ptr(), HEADS * D, os.data_ptr(), rows, rows,
+                                       HEADS * D)
+        y = torch.empty((rows, C), device="cuda")
+        self.product(oq, os, "out", y, binding.EPI_BIAS_F32)
+        self.norm(x, y, groups, False)
+        torch.cuda.synchronize()
+        assert int(self.st.item()) == 0
+        return x
+
+    # ---------------------------------------------------------------- 64 bits, activations not rounded
+
+    def reference(self, image, x, b):
+        """One whole sequence behind the image: [n, C]."""
+        def qkv(t, group, positions):
+            z = block.residual_norm(t, None, pre=block.LAYER, pre_gain=self.v["pre_gain"], shift=self.mod["shift"], scale=self.mod["scale"],
+                                    group=torch.full((t.shape[0],), group), eps=EPS)[1]
+            w = (z @ self.wide["qkv"].t()).view(t.shape[0], -1, D)
+            f = lambda y, g: block.rope_axes(y, g, self.table, torch.tensor(positions), AXES, block.AXIS, True, EPS)  # noqa: E731
+            return f(w[:, :HEADS], self.gains["q"]), f(w[:, HEADS:HEADS + HEADS_KV], self.gains["k"]), w[:, HEADS + HEADS_KV:]
+        _, pk, pv = qkv(image, 0, [[i // GRID, i % GRID] for i in range(image.shape[0])])
+        q, k, v = qkv(x, 1 + b, [[GRID + i, GRID + i] for i in range(x.shape[0])])
+        o, _ = block.prefix_attention(q, k, v, pk, pv, 1 / math.sqrt(D))
+        y = o.flatten(1) @ self.wide["out"].t()
+        return block.residual_norm(x, y, post=block.RMS, post_gain=self.v["post_gain"], y_scale=self.v["y_scale"], gate=self.mod["gate"],
+                                   group=torch.full((x.shape[0],), 1 + b), eps=EPS)[0]
+
+
+def test_image_prompts_and_single_tokens():
+    """Prompts behind the image, then their tokens one at a time: the same rows as the whole sequences at once. Against 64 bits:
+    two roundings to e4m3 (2^-4 a value, independent, so about 2^-4 / sqrt(3) of the added term's norm each, and the scores'
+    change of the same order): within a fifth of its norm."""
+    g = torch.Generator().manual_seed(4)
+    image = torch.randn((GRID * GRID, C), generator=g)
+    lens, first = [20, 33, 9], [12, 25, 1]
+    x = [torch.randn((n, C), generator=g) for n in lens]
+    whole = Block()
+    whole.image(image.cuda())
+    at_once = whole.step(torch.cat(x).cuda(), lens, [0] * BATCH).cpu()
+    steps = Block()
+    steps.image(image.cuda())
+    got = steps.step(torch.cat([a[:f] for a, f in zip(x, first)]).cuda(), first, [0] * BATCH).cpu()
+    rows = [list(t) for t in got.split(first)]
+    for t in range(8):
+        y = steps.step(torch.stack([a[f + t] for a, f in zip(x, first)]).cuda(), [1] * BATCH, [f + t for f in first]).cpu()
+        for b in range(BATCH):
+            rows[b].append(y[b])
+    step_by_step = torch.cat([torch.stack(r) for r in rows])
+    added = (at_once - torch.cat(x)).norm()
+    # (the caches hold the same values; the attention's sums may differ by the roundings of P and of its result, which
+    # move one of e4m3 here and there)
+    assert (step_by_step - at_once).norm() <= 2.0 ** -5 * added
+    want = torch.cat([whole.reference(image, a, b) for b, a in enumerate(x)])
+    assert (at_once.double() - want).norm() <= 0.2 * (want - torch.cat(x).double()).norm()
+
+
+@pytest.mark.parametrize("queries", [1, 30])
+def test_keys_and_lengths_from_the_calls_before(queries):
+    """The kernels of the own keys and of the join read their inputs without waiting for the kernel right before them: what
+    the call before the whole writes has to be there all the same. A long product makes the keys, a copy the lengths."""
+    g = torch.Generator(device="cuda").manual_seed(queries)
+    batch, keys, prefix, depth = 16, 96, 256, 8192
+    rand = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    a = {n: (rand(r * HEADS_KV, depth) / depth ** 0.5).to(BF16) for n, r in (("k", batch * keys), ("v", batch * keys), ("pk", prefix), ("pv", prefix))}
+    w = rand(D, depth).to(BF16)
+    q = rand(batch * queries, HEADS, D).to(BF16)
+    out = torch.empty_like(q)
+    t = {n: torch.empty((x.shape[0], D), dtype=BF16, device="cuda") for n, x in a.items()}
+    lens, want_lens = _i32([1] * batch), _i32([queries + 3 * i % 60 for i in range(batch)])
+    row = HEADS_KV * D
+    args = binding.PrefixAttention(
+        dtype=binding.BF16, batch=batch, heads=HEADS, heads_kv=HEADS_KV, head_dim=D, scale=0.125, max_queries=queries, q_rows=q.shape[0],
+        q=q.data_ptr(), q_row=HEADS * D, q_head=D, out=out.data_ptr(), out_row=HEADS * D, out_head=D, prefixes=1, max_prefix=prefix,
+        prefix_rows=prefix, prefix_k=t["pk"].data_ptr(), prefix_k_row=row, prefix_k_head=D, prefix_v=t["pv"].data_ptr(), prefix_v_row=row,
+        prefix_v_head=D, max_keys=keys, kv_rows=keys, kv_len=lens.data_ptr(), k=t["k"].data_ptr(), k_batch=keys * row, k_row=row, k_head=D,
+        v=t["v"].data_ptr(), v_batch=keys * row, v_row=row, v_head=D)
+    work = torch.empty(binding.elasto_op_prefix_attention_workspace(args), dtype=torch.uint8, device="cuda")
+    args.workspace, args.workspace_bytes = work.data_ptr(), work.numel()
+
+    def make(n):
+        binding.elasto_op_gemm(stream_handle(), a[n].data_ptr(), w.data_ptr(), None, t[n].data_ptr(), None, a[n].shape[0], D, depth,
+                               binding.EPI_BIAS_BF16)
+
+    lens.copy_(want_lens)
+    for n in t:
+        make(n)
+    torch.cuda.synchronize()
+    binding.elasto_op_prefix_attention(stream_handle(), args)
+    torch.cuda.synchronize()
+    want = out.clone()
+    for last in ("k", "v", "pk", "pv"):
+        for _ in range(5):
+            for x in t.values():
+                x.fill_(float("nan"))
+            lens.fill_(0), work.fill_(255), out.fill_(0)
+            for n in sorted(t, key=lambda n: n == last):
+                make(n)
+            lens.copy_(want_lens)
+            if last == "v":  # (a call of the library right before)
+                make(last)
+            binding.elasto_op_prefix_attention(stream_handle(), args)
+            after = out.clone()
+            for x in t.values():
+                x.fill_(float("nan"))
+            assert torch.equal(after, want)
