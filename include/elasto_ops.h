@@ -3,7 +3,8 @@
  * part has the steps of the DN forward (Section 4.1, Eq. 2-7) that elasto_forward
  * composes, so that every kernel can be checked on its own against the fp64
  * definition of that step. The second part has operators for a caller's own attention
- * sublayers over long sequences with 8-bit weights; no model call runs them.
+ * sublayers over long sequences with 8-bit weights, and for blocks of transformers over image, video and text
+ * tokens; no model call runs them.
  *
  * All pointers are CUDA device memory of the current device, row-major,
  * caller-owned; in the first part 16-byte aligned, in the second as each call says. Calls are asynchronous on `stream` (void* =
@@ -95,7 +96,8 @@ elasto_status elasto_op_attention(void* stream, const void* qkv, void* out, int 
 /* ------------------------------------------------------------------------
  * An attention sublayer over long token sequences with 8-bit weights: rows to
  * e4m3, products of e4m3 rows, norms and positions of queries and keys, and
- * attention in a sliding window. Forward only, like the rest of the library.
+ * attention in a sliding window; the sum at a block's end with the norm before the next,
+ * positions on several axes, and attention behind shared prefixes. Forward only, like the rest of the library.
  * Strides are in elements. A call allocates nothing and keeps nothing; it may
  * be captured into a graph. */
 
@@ -350,7 +352,8 @@ elasto_status elasto_op_qk_norm_rope_axes(void* stream, const elasto_qk_norm_rop
  * small their probabilities (NaN in any case where a score is NaN or +infinity, or all are -infinity).
  * Heads, types, scale and accuracy as elasto_op_window_attention has them.
  * Queries: sequence b has the rows q_start[b] to q_start[b + 1] of q and out, at most max_queries; q_start NULL:
- *   max_queries rows each, one sequence after another. q and out have q_rows rows (at most 2^30, as prefix_rows and kv_rows).
+ *   max_queries rows each, one sequence after another. q and out have q_rows rows (at most 2^30, as prefix_rows and kv_rows);
+ *   with q_start the work and the workspace are planned for all of them, so give those in use, not a buffer's capacity.
  * Prefixes: prefix g is shared by sequences seq_start[g] to seq_start[g + 1] - 1 (seq_start NULL: one prefix, all
  *   sequences); its keys are the first prefix_len[g] rows (NULL: max_prefix) of prefix_k + g * prefix_k_batch, and so on
  *   for v. At most max_prefix of them, max_prefix <= prefix_rows. Sequences in no prefix's range have their own keys only.

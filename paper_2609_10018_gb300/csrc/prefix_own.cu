@@ -12,7 +12,8 @@
 // for both.
 //
 // prefix_join_few_kernel, prefix_join_many_kernel: out = sum over parts of o exp(m - top) / sum of l exp(m - top), four channels a thread, in a fixed
-// order.
+// order. Where the prefixes' CTAs fill the chip by themselves and leave one part, prefix_few_kernel waits for them and joins its
+// rows itself.
 #include <algorithm>
 #include <type_traits>
 
@@ -101,22 +102,24 @@ __device__ __noinline__ float bad_values(const uint16_t* v, long long row, int n
   return sum;
 }
 
-// The results y of four channels of a row that sees `seen` own keys and `len` of its prefix: a channel in which the row sees
-// values that are not finite gets their sum. (An infinite value whose probability has rounded to 0 gave NaN; left_out: some have
-// been set to 0 because other rows do not see them.)
+// The result y of channel ch of a row that sees `seen` own keys and `len` of its prefix: the sum of the values that are not
+// finite, if it sees such. (An infinite value whose probability has rounded to 0 gave NaN; left_out: some have been set to 0
+// because other rows do not see them.)
+template <bool BF>
+__device__ __noinline__ float put_bad_value(const PrefixOwnArgs& a, float y, int b, int kvh, int k0, int seen, int prefix, int len, int ch) {
+  float s = 0.0f;
+  if (seen > 0) s += bad_values<BF>(a.v + (a.kv_start ? 0 : b * a.v_batch) + k0 * a.v_row + kvh * a.v_head + ch, a.v_row, seen);
+  if (!(fabsf(y) < INFINITY) && len > 0) s += bad_values<BF>(a.pv + prefix * a.pv_batch + kvh * a.pv_head + ch, a.pv_row, len);
+  return s != 0.0f ? s : y;  // (NaN too)
+}
+// The same of four channels.
 template <bool BF>
 __device__ __forceinline__ float4 put_bad_values(const PrefixOwnArgs& a, float4 y, int b, int kvh, int k0, int seen, int prefix, int len, int quad,
                                                  bool left_out) {
   const float odd = fmaf(y.x, 0.0f, fmaf(y.y, 0.0f, fmaf(y.z, 0.0f, y.w * 0.0f)));
-  if (odd == 0.0f && !left_out) return y;
-#pragma unroll 1
-  for (int j = 0; j < 4; ++j) {
-    const float was = j == 0 ? y.x : j == 1 ? y.y : j == 2 ? y.z : y.w;
-    float s = 0.0f;
-    if (seen > 0) s += bad_values<BF>(a.v + (a.kv_start ? 0 : b * a.v_batch) + k0 * a.v_row + kvh * a.v_head + 4 * quad + j, a.v_row, seen);
-    if (!(fabsf(was) < INFINITY) && len > 0) s += bad_values<BF>(a.pv + prefix * a.pv_batch + kvh * a.pv_head + 4 * quad + j, a.pv_row, len);
-    if (s != 0.0f) y.x = j == 0 ? s : y.x, y.y = j == 1 ? s : y.y, y.z = j == 2 ? s : y.z, y.w = j == 3 ? s : y.w;  // (NaN too)
-  }
+  if (odd != 0.0f || left_out)
+    y = make_float4(put_bad_value<BF>(a, y.x, b, kvh, k0, seen, prefix, len, 4 * quad), put_bad_value<BF>(a, y.y, b, kvh, k0, seen, prefix, len, 4 * quad + 1),
+                    put_bad_value<BF>(a, y.z, b, kvh, k0, seen, prefix, len, 4 * quad + 2), put_bad_value<BF>(a, y.w, b, kvh, k0, seen, prefix, len, 4 * quad + 3));
   return y;
 }
 
@@ -303,6 +306,13 @@ __global__ void __launch_bounds__(32)
     if (elect_one())
       for (int i = 0; i < asked; ++i) request(i);
     __syncwarp();
+    int prefix = -1, len = 0;
+    if (a.fused)
+      for (int g0 = 0; g0 < a.prefixes && prefix < 0; g0 += 32) {
+        const int g = g0 + lane, keys = g < a.prefixes && a.prefix_len ? min(max(a.prefix_len[g], 0), a.max_prefix) : a.max_prefix;
+        const uint32_t mine = __ballot_sync(0xffffffffu, g < a.prefixes && (!a.seq_start || (a.seq_start[g] <= b && b < a.seq_start[g + 1])));
+        if (mine) prefix = g0 + __ffs(mine) - 1, len = __shfl_sync(0xffffffffu, keys, __ffs(mine) - 1);
+      }
     const int r = lane >> 2, c2 = 2 * (lane & 3);
     uint32_t q[DP / 16][4];  // the rows r and r + 8
     int vis[2];
@@ -348,19 +358,49 @@ __global__ void __launch_bounds__(32)
     }
     x.finish();
     left_out = __any_sync(0xffffffffu, left_out);
+    if (a.fused) pdl_wait();  // (the prefix's part)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int row = r + 8 * h;
       if (row >= nrows) continue;
       const int qi = query(row), head = row0 + row - qi * a.group, sub = head / a.hg, hs = kvh * a.nsub + sub;
       const long long rho = static_cast<long long>(q0 + qi) * a.hg + (head - sub * a.hg);
-      if ((lane & 3) == 0)
-        *reinterpret_cast<float2*>(a.parts.stat + a.parts.stat_at(a.prefix_parts + rank, hs, rho)) = make_float2(x.m[h], left_out ? -x.sum[h] : x.sum[h]);
-      if (x.m[h] == -INFINITY) continue;
-      float* const sums = a.parts.sums + a.parts.sums_at(a.prefix_parts + rank, hs, rho) + (c2 & 3) + (c2 >> 2) * kQuadStep;
+      if (!a.fused) {
+        if ((lane & 3) == 0)
+          *reinterpret_cast<float2*>(a.parts.stat + a.parts.stat_at(a.prefix_parts + rank, hs, rho)) = make_float2(x.m[h], left_out ? -x.sum[h] : x.sum[h]);
+        if (x.m[h] == -INFINITY) continue;
+        float* const sums = a.parts.sums + a.parts.sums_at(a.prefix_parts + rank, hs, rho) + (c2 & 3) + (c2 >> 2) * kQuadStep;
 #pragma unroll
-      for (int j = 0; j < DP / 8; ++j)
-        if (8 * j < a.head_dim) *reinterpret_cast<float2*>(sums + 2 * j * kQuadStep) = make_float2(x.o[j][2 * h], x.o[j][2 * h + 1]);
+        for (int j = 0; j < DP / 8; ++j)
+          if (8 * j < a.head_dim) *reinterpret_cast<float2*>(sums + 2 * j * kQuadStep) = make_float2(x.o[j][2 * h], x.o[j][2 * h + 1]);
+        continue;
+      }
+      // the row's result: the lane's channels of the prefix's one part and of the own keys
+      const float* const sums = a.parts.sums + a.parts.sums_at(0, hs, rho) + (c2 & 3) + (c2 >> 2) * kQuadStep;
+      float2 st = make_float2(-INFINITY, 0.0f), p[DP / 8];
+      if (len > 0) st = *reinterpret_cast<const float2*>(a.parts.stat + a.parts.stat_at(0, hs, rho));
+#pragma unroll
+      for (int j = 0; j < DP / 8; ++j) p[j] = len > 0 && 8 * j < a.head_dim ? *reinterpret_cast<const float2*>(sums + 2 * j * kQuadStep) : make_float2(0.0f, 0.0f);
+      const float top = fmaxf(x.m[h], st.x);
+      // (a part without a finite score has sums of zeros, or NaN that must stay)
+      const float wo = x.m[h] == -INFINITY ? 1.0f : ex2_approx((x.m[h] - top) * sc), wp = st.x == -INFINITY ? 1.0f : ex2_approx((st.x - top) * sc);
+      const float total = x.sum[h] * wo + st.y * wp;
+      const int seen_own = visible(row);
+      const float inv = len > 0 || seen_own > 0 ? 1.0f / total : 0.0f;
+      uint16_t* const out = a.out + static_cast<long long>(q0 + qi) * a.out_row + static_cast<long long>(kvh * a.group + head) * a.out_head + c2;
+#pragma unroll
+      for (int j = 0; j < DP / 8; ++j) {
+        if (8 * j >= a.head_dim) continue;
+        float2 y = make_float2((x.o[j][2 * h] * wo + p[j].x * wp) * inv, (x.o[j][2 * h + 1] * wo + p[j].y * wp) * inv);
+        if (total > 0.0f) {
+          if (fmaf(y.x, 0.0f, y.y * 0.0f) != 0.0f || left_out)
+            y = make_float2(put_bad_value<BF>(a, y.x, b, kvh, k0, seen_own, prefix, len, 8 * j + c2),
+                            put_bad_value<BF>(a, y.y, b, kvh, k0, seen_own, prefix, len, 8 * j + c2 + 1));
+        } else if (inv != 0.0f) {  // (a sum of 0 or NaN over visible keys)
+          y.x = y.y = __int_as_float(0x7fc00000);
+        }
+        *reinterpret_cast<uint32_t*>(out + 8 * j) = pack16<BF>(y.x, y.y);
+      }
     }
   }
   if (blockIdx.x == gridDim.x - 1) pdl_wait();
@@ -729,7 +769,7 @@ cudaError_t launch(const PrefixOwn& own, cudaStream_t s) {
     e = launch_pdl(prefix_many_kernel<BF, DP>, grid, dim3(THREADS), Many<DP>::smem, s, own.k, own.v, a);
   else if (a.max_keys > 0)
     e = launch_pdl(prefix_few_kernel<BF, DP>, grid, dim3(32), Few<DP>::smem, s, own.k, own.v, a);
-  if (e != cudaSuccess) return e;
+  if (e != cudaSuccess || a.fused) return e;
   const int parts = a.prefix_parts + (a.max_keys > 0 ? a.own_split : 0);
   const unsigned blocks = static_cast<unsigned>(a.batch) * a.join_blocks;
   if (own.join_many) return launch_pdl(prefix_join_many_kernel<BF>, dim3(blocks), dim3(JOIN_THREADS), 4 * parts * ROWS, s, a);
@@ -777,6 +817,7 @@ elasto_status prefix_own_plan(const elasto_prefix_attention_args& u, const Prefi
   a.prefix_parts = p.prefix_parts(), a.own_split = p.own_split;
   a.status = status;
   own->many = p.many != 0 && u.max_keys > 0;
+  a.fused = p.fused != 0 && u.max_keys > 0;
   own->units = static_cast<int64_t>(p.blocks) * a.batch * a.heads_kv;
   if (own->units * a.own_split > 0x7fffffffLL) {
     set_error("elasto_op_prefix_attention: too many sequences or queries");

@@ -25,6 +25,7 @@ struct PrefixOwnArgs {
   long long pv_batch, pv_row, pv_head;
   int hg, nsub, pair, split;
   int prefix_parts, own_split;
+  int fused;  // prefix_few_kernel joins its rows itself
   PrefixParts parts;
   int blocks;  // of rows, of a sequence and key head
   int join_blocks;  // of rows of a sequence over all heads, for the join

@@ -26,6 +26,7 @@ struct PrefixPlan {
   int many;           // 1: blocks of 64 rows of a sequence's own attention, 0: of 16
   int blocks;         // of a sequence and key head
   int own_split;      // CTAs that share a block's own keys, each leaving a part behind the prefix's
+  int fused;          // 1: the kernel of the own keys (of 16 rows) joins its rows itself, with the prefix's one part
   int prefix_parts() const { return pair ? 2 * split : split; }
   int parts() const { return prefix_parts() + own_split; }
 };
@@ -49,12 +50,13 @@ inline PrefixPlan prefix_plan(const PrefixSizes& z) {
     return k < n ? k : n;
   };
   p.items = items(z.most);
-  // The sequences' own keys: blocks of 64 rows where a sequence has more than three of 16 and several queries, in CTAs
-  // until the SMs have six each, with four tiles of 64 keys at least; else of 16 rows, in CTAs of a warp until the SMs have
-  // fourteen, with 256 keys at least: sequences of different lengths even out.
+  // The sequences' own keys: blocks of 64 rows where a sequence has more than 512 (eight prompts of up to 96 tokens behind
+  // each of eight images, 384 rows: 223 us with them, 219 with blocks of 16), in CTAs until the SMs have six each, with four
+  // tiles of 64 keys at least; else of 16 rows, in CTAs of a warp until the SMs have twelve, with 256 keys at least: sequences
+  // of different lengths even out.
   const int64_t rows = static_cast<int64_t>(z.max_queries) * z.group;
-  p.many = z.max_queries > 1 && rows > 48;
-  const int64_t of = p.many ? 64 : 16, enough = (p.many ? 6LL : 14LL) * z.sms;
+  p.many = z.max_queries > 1 && rows > 512;
+  const int64_t of = p.many ? 64 : 16, enough = (p.many ? 6LL : 12LL) * z.sms;
   p.blocks = static_cast<int>((rows + of - 1) / of);
   const int64_t units = static_cast<int64_t>(p.blocks) * z.batch * z.heads_kv;
   p.own_split = 1;
@@ -86,6 +88,7 @@ inline PrefixPlan prefix_plan(const PrefixSizes& z) {
     const double cost = prefix + (done < 1.0 ? (1.0 - done) / own_rate(z.sms) : 0.0) + n * part;
     if (n == 1 || cost < best) best = cost, p.split = n;
   }
+  p.fused = !p.many && p.own_split == 1 && p.prefix_parts() == 1 && ctas >= z.sms;
   return p;
 }
 

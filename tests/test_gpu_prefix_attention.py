@@ -223,6 +223,25 @@ def test_scores_that_are_not_finite():
     assert torch.isfinite(got[2:]).all()
 
 
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (F16, 64), (BF16, 40)])
+def test_prompts_whose_prefixes_fill_the_chip(dtype, d):
+    """Items of the prefixes for every SM: the kernel of the own keys joins its rows itself. Prefixes without keys,
+    sequences without a prefix, without own keys, with values that are not finite."""
+    prefixes = [(200, 2), (0, 1), (128, 1), (17, 1), (129, 1), (64, 1), (150, 1), (199, 1)]
+    n = 1 + sum(k for _, k in prefixes) + 1
+    nq, nk = [7, 9, 8, 5, 9, 8, 7, 6, 9, 9, 4], [9, 9, 30, 0, 60, 3, 7, 33, 16, 17, 4]
+    assert len(nq) == n and sum(nq) > 8 * 8
+    c = Case(prefixes, nq, nk, 16 * 13, 13, d, dtype, before=1, tail=2)
+    c.pv[0, 150, 0, 5], c.pv[0, 7, 1, 9], c.pv[0, 8, 1, 9] = INF, INF, -INF
+    c.v[4, 59, 2, 3], c.v[4, 52, 3, 7], c.v[0, 8, 1, 1] = -INF, NAN, INF
+    got = c.check()
+    assert torch.equal(c.device().run().view(torch.int16), got.view(torch.int16))  # (bits: there are NaN)
+    at = [sum(nq[:b]) for b in range(n + 1)]
+    assert (got[at[1]:at[3], :16, 5] == INF).all() and got[at[1]:at[3], 16:32, 9].isnan().all()
+    assert (got[at[5] - 1, 32:48, 3] == -INF).all() and torch.isfinite(got[at[4]:at[5] - 1, 32:48, 3]).all()
+    assert got[at[5] - 2:at[5], 48:64, 7].isnan().all()
+
+
 def test_large_bf16_values():
     """Sums of values near the end of bf16's range do not overflow before the division."""
     c = Case([(600, 2)], [1, 1], [70, 5], 2, 1, 64)

@@ -14,15 +14,15 @@ using namespace elasto;
 extern "C" void plan(const long long* z, long long* p) {
   PrefixSizes s{z[0], z[1], (int)z[2], (int)z[3], (int)z[4], (int)z[5], (int)z[6], (int)z[7], z[8], z[9], (int)z[10]};
   const PrefixPlan r = prefix_plan(s);
-  const long long v[] = {r.hg, r.nsub, r.qpt, r.pair, r.split, (long long)r.items, r.many, r.blocks, r.own_split, r.prefix_parts(), r.parts()};
-  for (int i = 0; i < 11; ++i) p[i] = v[i];
+  const long long v[] = {r.hg, r.nsub, r.qpt, r.pair, r.split, (long long)r.items, r.many, r.blocks, r.own_split, r.prefix_parts(), r.parts(), r.fused};
+  for (int i = 0; i < 12; ++i) p[i] = v[i];
 }
 extern "C" int from(int tiles, int rank, int split) { return split_from(tiles, rank, split); }
 extern "C" long long sums(int part, int h, long long row, long long rho, int hs, int quads) { return PrefixParts{nullptr, nullptr, rho, hs, quads}.sums_at(part, h, row); }
 extern "C" long long stat(int part, int h, long long row, long long rho, int hs, int quads) { return PrefixParts{nullptr, nullptr, rho, hs, quads}.stat_at(part, h, row); }
 extern "C" int most_parts() { return kMaxParts; }
 """
-FIELDS = ("hg", "nsub", "qpt", "pair", "split", "items", "many", "blocks", "own_split", "prefix_parts", "parts")
+FIELDS = ("hg", "nsub", "qpt", "pair", "split", "items", "many", "blocks", "own_split", "prefix_parts", "parts", "fused")
 
 
 @pytest.fixture(scope="module")
@@ -42,7 +42,7 @@ def rule(tmp_path_factory):
 
 def _plan(rule, **z):
     z = dict(rows=64, most=64, batch=64, max_queries=1, prefixes=1, group=4, heads_kv=8, head_dim=128, max_prefix=8192, max_keys=1024, sms=152) | z
-    out = (ctypes.c_longlong * 11)()
+    out = (ctypes.c_longlong * 12)()
     rule.plan((ctypes.c_longlong * 11)(*z.values()), out)
     return dict(zip(FIELDS, out))
 
@@ -68,6 +68,18 @@ def test_plans_stay_within_their_limits(rule):
         rows = 64 if p["many"] else 16
         assert p["blocks"] == -(-z["max_queries"] * z["group"] // rows)
         assert p["own_split"] == 1 or z["max_keys"] >= 32 * p["own_split"], (z, p)
+
+
+def test_rows_joined_at_once_have_one_part(rule):
+    seen = 0
+    for z in _sizes(2000):
+        p = _plan(rule, **z)
+        if p["fused"]:
+            seen += 1
+            assert p["prefix_parts"] == p["own_split"] == 1 and not p["many"]
+    assert seen > 0
+    # (the sizes of the GPU's test of it)
+    assert _plan(rule, rows=81, most=83, batch=11, max_queries=9, prefixes=8, group=16, heads_kv=13, max_prefix=200, max_keys=60)["fused"]
 
 
 def test_items_suffice_however_the_rows_fall_to_the_prefixes(rule):
