@@ -5,7 +5,7 @@
 // softmax in one pass. The own keys of a block are shared out over own_split CTAs, each of which leaves a part as
 // prefix_attention.cu's CTAs do.
 //   prefix_few_kernel    16 rows, single tokens and few: a CTA is one warp, which streams 16 keys at a time by TMA through
-//     a ring of its own. Nothing is shared between warps, and while one of an SM's nine CTAs starts or ends the others load.
+//     a ring of its own. Nothing is shared between warps, and while one of an SM's twelve CTAs starts or ends the others load.
 //   prefix_many_kernel   64 rows, longer runs of tokens: four warps with 16 rows each, a fifth loads tiles of 64 keys.
 // Neither waits for the prefixes' kernel: that one is bound by its products, these by reading the keys and values
 // once, and both run at the same time. Only the last CTA waits before it ends, so that what waits for this kernel waits
@@ -31,7 +31,7 @@ constexpr int JOIN_THREADS = 256;
 template <int DP>
 struct Few {
   static constexpr int halves = DP / 64, half = 16 * 128, tile = halves * half, stage = 2 * tile;  // 16 keys of 64 channels
-  static constexpr int stages = 24 * 1024 / stage;
+  static constexpr int stages = 16 * 1024 / stage;  // twelve CTAs an SM (eight with 24 KB each took 3 to 9 % longer, six with 32 KB 10 to 19)
   static constexpr int smem = 1024 + stages * stage + 64;
 };
 

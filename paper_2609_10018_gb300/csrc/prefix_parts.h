@@ -66,7 +66,8 @@ inline PrefixPlan prefix_plan(const PrefixSizes& z) {
   // on what is left. In microseconds: of a prefix's CTA its start and end and its key tiles (which wait longer for their
   // keys, where it alone reads them, while the other kernel reads at the memory's rate: 64 sequences behind 8192 keys took
   // 48 us with five CTAs a key head, 35 with ten); of a part of all rows, written and read; of the own keys (about 0.6 of
-  // the longest each) the memory's time, and an SM's for all their CTAs.
+  // the longest each) the memory's time, and an SM's for all their CTAs (three at a time, or as if nine of one warp: with
+  // twelve, as there are, drafts of 32 sequences got an SM too few and took 38 us in place of 30).
   const int64_t tiles = (z.max_prefix + kPrefixTile - 1) / kPrefixTile, each = items(z.rows), ctas = each * z.heads_kv * p.nsub;
   const double start = 5.0, tile = (p.pair ? 0.7 : 1.4) * (z.head_dim > 64 ? 1.0 : 0.7);
   const double part = (static_cast<double>(z.rows) * z.group * z.heads_kv * (8.0 * z.head_dim + 16) / 8e6 + 0.15) * (p.pair ? 2 : 1);
