@@ -11,8 +11,8 @@
 // once, and both run at the same time. Only the last CTA waits before it ends, so that what waits for this kernel waits
 // for both.
 //
-// prefix_join_few_kernel, prefix_join_many_kernel: out = sum over parts of o exp(m - top) / sum of l exp(m - top), four channels a thread, in a fixed
-// order. Where the prefixes' CTAs fill the chip by themselves and leave one part, prefix_few_kernel waits for them and joins its
+// prefix_join_few_kernel, prefix_join_many_kernel: out = sum over parts of o exp(m - top) / sum of l exp(m - top), four
+// channels a thread, in a fixed order. Where the prefixes' CTAs fill the chip by themselves and leave one part, prefix_few_kernel waits for them and joins its
 // rows itself.
 #include <algorithm>
 #include <type_traits>
@@ -593,6 +593,7 @@ __global__ void __launch_bounds__(JOIN_THREADS)
   find_prefix(a, b, parts, found);
   const int prefix = found.prefix, len = found.len;
   const int row = 32 * blk + (threadIdx.x >> 3), quads = a.head_dim / 4;
+  if (blockIdx.x == gridDim.x - 1 && blockIdx.y == gridDim.y - 1) pdl_wait();  // (where all sequences are empty nothing else does)
   if (row >= nq * a.heads_kv * a.group) return;
   const JoinRow r = join_row(a, q0, nq, row);
   const float* const st0 = a.parts.stat + a.parts.stat_at(0, r.h, r.rho);
@@ -665,7 +666,10 @@ __global__ void __launch_bounds__(JOIN_THREADS, 4)
   find_prefix(a, b, parts, found);
   const int prefix = found.prefix, len = found.len;
   const int row0 = blk * ROWS, nrows = min(nq * a.heads_kv * a.group - row0, ROWS);
-  if (nrows <= 0) return;
+  if (nrows <= 0) {
+    if (blockIdx.x == gridDim.x - 1) pdl_wait();
+    return;
+  }
   const float sc = a.scale_log2;
   auto factor = [&](float m, float top) { return m == -INFINITY ? 1.0f : ex2_approx((m - top) * sc); };
   {

@@ -310,6 +310,49 @@ def test_same_bits_again_captured_and_on_another_stream(queries):
         c.check(c.out.cpu())
 
 
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (F16, 128), (BF16, 64), (F16, 40)])
+@pytest.mark.parametrize("most", [600, 3400])
+@pytest.mark.parametrize("packed", [True, False])
+def test_room_for_many_queries(dtype, d, most, packed):
+    """Blocks of 64 rows, and from 40000 rows on their join: sequences that are short, empty, longer than a block, with own
+    keys of several tiles and of several CTAs, behind prefixes with and without keys and behind none."""
+    for longest in (130, 1100):  # (one CTA for a block's keys; two and more)
+        c = Case([(200, 2), (0, 1), (300, 1)], [70, 1, 0, 33, 9, 65], [longest, 30, 5, 33, 0, 64], 4, 2, d, dtype, packed=packed, before=1,
+                 tail=most - 178)
+        c.pv[0, 150, 0, 5], c.pv[0, 7, 1, 9], c.pv[0, 8, 1, 9] = INF, INF, -INF
+        flat = c.v[sum(c.nk[:3]):] if packed else c.v[3]
+        flat[32, 0, 3], flat[5, 1, 4] = -INF, NAN  # (the last of 33 queries sees both, the sixth and later the second)
+        got = c.check(c.device().run(max_queries=most))
+        assert (got[70, :2, 5] == INF).all() and got[70, 2:, 9].isnan().all()
+        assert (got[103, :2, 3] == -INF).all() and torch.isfinite(got[71:103, :2]).all()
+        assert torch.isfinite(got[71:76, 2:]).all() and got[76:104, 2:, 4].isnan().all()
+        assert torch.equal(c.device().run(max_queries=most).view(torch.int16), got.view(torch.int16))
+
+
+@pytest.mark.parametrize("d", [128, 72, 8])
+def test_join_of_many_rows_and_parts(d):
+    """Room for 128 queries in each of 320 sequences, 150 rows: parts of many CTAs, joined 64 rows at a time."""
+    nq = [(3 * i) % 4 % 3 for i in range(320)]
+    while sum(nq) > 128:
+        nq[nq.index(max(nq))] -= 1
+    c = Case([(20000, 150), (1900, 170)], nq, [11 * i % 70 for i in range(320)], 1, 1, d, tail=150 - sum(nq))
+    c.check(c.device().run(max_queries=128))
+    c.check(c.device().run(max_queries=150, q_rows=150))
+
+
+@pytest.mark.parametrize("most", [3, 600, 7000])
+def test_without_own_keys_and_room(most):
+    c = Case([(300, 3)], [1, 3, 2], [0, 0, 0], tail=most)
+    c.check(c.device().run(max_queries=most, max_keys=0, k=None, v=None, kv_rows=0, kv_len=None))
+
+
+@pytest.mark.parametrize("most", [1, 100, 7000])
+def test_all_sequences_empty(most):
+    Case([(300, 2)], [0, 0], [5, 9], tail=most).check()
+    c = Case([(300, 2)], [0, 0], [5, 9], tail=most)
+    c.check(c.device().run(max_queries=most))
+
+
 def test_more_rows_than_the_sequences_have():
     """q_rows is what the buffers hold, far more than max_queries allows for."""
     c = Case([(300, 2)], [1, 1], [9, 30], 4, 1, 64, tail=700)

@@ -112,3 +112,15 @@ def test_parts_do_not_overlap(rule):
     assert seen == set(range(parts * hs * rho * quads * 4))
     seen = {rule.stat(p, h, row, rho, hs, quads) for p in range(parts) for h in range(hs) for row in range(rho)}
     assert seen == set(range(0, 2 * parts * hs * rho, 2))
+
+
+def test_every_form_has_a_case(rule):
+    """What the tests on the GPU rely on to reach each form: blocks of 64 rows, in one and several CTAs; parts of one, a few and
+    more than eight."""
+    room = dict(batch=6, prefixes=3, group=2, heads_kv=2, max_prefix=300)
+    few, more = (_plan(rule, rows=600, most=600, max_queries=600, max_keys=k, **room) for k in (130, 1100))
+    assert few["many"] and few["own_split"] == 1 and more["many"] and more["own_split"] > 1
+    many = _plan(rule, rows=3400, most=3400, max_queries=3400, max_keys=130, **room)
+    assert many["many"] and many["parts"] == 2 and 3400 * 4 * 6 > 40000
+    parts = _plan(rule, rows=150, most=150, batch=320, max_queries=128, prefixes=2, group=1, heads_kv=1, max_prefix=20000, max_keys=69)
+    assert not parts["many"] and not parts["fused"] and parts["parts"] > 8 and 128 * 320 > 40000
