@@ -259,7 +259,8 @@ enum { ELASTO_NORM_NONE = 0, ELASTO_NORM_RMS = 1, ELASTO_NORM_LAYER = 2 };
  * y_scale: a factor for each column. gate, shift and scale (each may be NULL; mod_type ELASTO_F32, _BF16 or _F16) are tables
  * [groups, cols] with row stride mod_row: row r takes row group[r] of them (group NULL: row 0). groups 0: no tables. A row
  * with a group outside [0, groups) is left out, and *status_device is set to ELASTO_ERR_INVALID_ARG.
- * Squares are summed in fp32: from about 1e19 on they overflow, and the norm gives 0, or NaN for an infinity.
+ * Squares are summed in fp32: from about 1e19 on they overflow, and the norm gives 0, or NaN for an infinity. A row
+ * of zeros with eps 0: NaN.
  * cols: 1 to 16384. Row strides are at least cols. Data needs its types' alignment; rows whose starts are multiples of
  * eight values in memory are read and written wide. Outputs may not overlap the inputs (but x_out, x) or one another. */
 typedef struct {
@@ -359,7 +360,7 @@ elasto_status elasto_op_qk_norm_rope_axes(void* stream, const elasto_qk_norm_rop
  *   for v. At most max_prefix of them, max_prefix <= prefix_rows. Sequences in no prefix's range have their own keys only.
  * Own keys: packed, the rows kv_start[b] to kv_start[b + 1] of k and v, which have kv_rows rows; or (kv_start NULL) in
  *   a cache of kv_rows rows per sequence, k_batch and v_batch apart, the first kv_len[b] of them (kv_len NULL: max_keys). At
- *   most max_keys each; max_keys <= kv_rows. max_keys 0: none, and k, v, kv_rows and their strides are not used.
+ *   most max_keys each; in a cache max_keys <= kv_rows. max_keys 0: none, and k, v, kv_rows and their strides are not used.
  * q_start and seq_start ascend. Lengths on the device past these limits are cut to them; nothing is read or
  * written outside them. Rows of out that belong to no sequence are left as they were.
  * workspace: elasto_op_prefix_attention_workspace's bytes on the device, 16-byte aligned, for the results of the
@@ -401,7 +402,7 @@ typedef struct {
 } elasto_prefix_attention_args;
 elasto_status elasto_op_prefix_attention(void* stream, const elasto_prefix_attention_args* args, int* status_device);
 /* The bytes of workspace that a call with these sizes needs on the current device (of args the sizes alone are
- * read, no pointer but whether seq_start is NULL). Nothing is launched. */
+ * read, and whether q_start, seq_start and kv_start are NULL; give them as the call does). Nothing is launched. */
 elasto_status elasto_op_prefix_attention_workspace(const elasto_prefix_attention_args* args, size_t* bytes);
 
 /* Self-test of the bounded device-side wait that every kernel above (and the

@@ -63,8 +63,16 @@ elasto_status check_prefix_sizes(const elasto_prefix_attention_args& a, const ch
   if (a.prefixes <= 0 || (a.prefixes > 1 && !a.seq_start)) return no(": prefixes, or several without seq_start");
   if (a.q_rows <= 0 || a.q_rows > 1 << 30 || a.prefix_rows <= 0 || a.prefix_rows > 1 << 30 || a.max_prefix > a.prefix_rows)
     return no(": q_rows or prefix_rows");
-  if (a.max_keys > 0 && (a.kv_rows <= 0 || a.kv_rows > 1 << 30 || a.max_keys > a.kv_rows)) return no(": kv_rows");
+  if (a.max_keys > 0 && (a.kv_rows <= 0 || a.kv_rows > 1 << 30 || (!a.kv_start && a.max_keys > a.kv_rows))) return no(": kv_rows");
   return ELASTO_OK;
+}
+
+// The same call with no more keys of a sequence than rows there are: max_keys is a limit, and packed sequences may have fewer
+// rows altogether.
+elasto_prefix_attention_args with_keys_there_are(const elasto_prefix_attention_args& a) {
+  elasto_prefix_attention_args u = a;
+  if (u.max_keys > u.kv_rows && u.max_keys > 0) u.max_keys = static_cast<int>(u.kv_rows);
+  return u;
 }
 
 // The bounded wait every kernel uses (mbar_wait: a time limit, then false),
@@ -384,7 +392,7 @@ elasto_status elasto_op_prefix_attention_workspace(const elasto_prefix_attention
   if (st != ELASTO_OK) return st;
   st = check_device();
   if (st != ELASTO_OK) return st;
-  return prefix_attention_workspace(*args, bytes);
+  return prefix_attention_workspace(with_keys_there_are(*args), bytes);
 }
 
 elasto_status elasto_op_prefix_attention(void* stream, const elasto_prefix_attention_args* args, int* status_device) {
@@ -416,7 +424,7 @@ elasto_status elasto_op_prefix_attention(void* stream, const elasto_prefix_atten
   if (!a.workspace || !aligned(a.workspace, 16)) return refuse("elasto_op_prefix_attention: workspace (null or alignment)");
   st = check_device();
   if (st != ELASTO_OK) return st;
-  return prefix_attention_launch(a, status_device, static_cast<cudaStream_t>(stream));
+  return prefix_attention_launch(with_keys_there_are(a), status_device, static_cast<cudaStream_t>(stream));
 }
 
 elasto_status elasto_op_softmax(void* stream, const float* x, float* y, int rows, int cols) {

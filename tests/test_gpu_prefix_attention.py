@@ -382,3 +382,26 @@ def test_a_workspace_that_is_too_small():
     with pytest.raises(binding.ElastoError) as e:
         binding.elasto_op_prefix_attention(stream_handle(), args)
     assert e.value.status == binding.ERR_INVALID_ARG and "workspace" in str(e.value)
+
+
+@pytest.mark.parametrize("d,most", [(64, 70), (128, 600), (40, 2000), (128, 2 ** 31 - 1)])
+@pytest.mark.parametrize("nq,nk", [([1], [1]), ([7, 3], [7, 3]), ([40, 1, 20], [30, 0, 20])])
+def test_packed_keys_fewer_than_the_limit(d, most, nq, nk):
+    """max_keys is a limit: packed sequences may have fewer rows altogether."""
+    c = Case([(200, len(nq))], nq, nk, 4, 2, d, packed=True, room=0)
+    assert c.k.shape[0] < most
+    c.check(c.device().run(max_keys=most))
+    with pytest.raises(binding.ElastoError) as e:  # of a cache there are as many
+        c.device().run(max_keys=most, kv_start=None, kv_len=c.t["kv_len"].data_ptr())
+    assert e.value.status == binding.ERR_INVALID_ARG
+
+
+def test_sizes_past_any_workspace():
+    """Sizes whose workspace no memory holds (and 64 bits of bytes neither) are refused, not reckoned modulo 2^64."""
+    c = Case([(300, 1)], [1], [9]).device()
+    args = c.args()
+    args.q_rows, args.heads, args.heads_kv, args.head_dim = 1 << 30, 1 << 20, 1, 128
+    for call in (lambda: binding.elasto_op_prefix_attention_workspace(args), lambda: binding.elasto_op_prefix_attention(stream_handle(), args)):
+        with pytest.raises(binding.ElastoError) as e:
+            call()
+        assert e.value.status == binding.ERR_UNSUPPORTED
