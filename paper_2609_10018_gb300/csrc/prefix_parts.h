@@ -65,7 +65,7 @@ inline PrefixPlan prefix_plan(const PrefixSizes& z) {
   // How many CTAs share a prefix's keys. Both kernels run at the same time, the prefixes' with an SM a CTA, the other
   // on what is left. In microseconds: of a prefix's CTA its start and end and its key tiles (which wait longer for their
   // keys, where it alone reads them, while the other kernel reads at the memory's rate: 64 sequences behind 8192 keys took
-  // 48 us with five CTAs a key head, 35 with ten); of a part of all rows, written and read; of the own keys (about 0.6 of
+  // 48 us with five CTAs a key head, 45 with eight); of a part of all rows, written and read; of the own keys (about 0.6 of
   // the longest each) the memory's time, and an SM's for all their CTAs (three at a time, or as if nine of one warp: with
   // twelve, as there are, drafts of 32 sequences got an SM too few and took 38 us in place of 30).
   const int64_t tiles = (z.max_prefix + kPrefixTile - 1) / kPrefixTile, each = items(z.rows), ctas = each * z.heads_kv * p.nsub;
