@@ -488,27 +488,26 @@ __global__ void __launch_bounds__(THREADS, 3)
     }
     const float sc = a.scale_log2;
     const int krow = (lane & 7) + (lane >> 4) * 8, vrow = lane & 15;
-    bool ok = true;
-    int i = 0;
-    for (int t = t0; t < t1 && ok; ++t, ++i) {
-      const int s = i % S, key0 = t * KT;
-      ok = mbar_wait_warp(&full[s], (i / S) & 1);
-      if (!ok) break;
-      uint8_t* const kb = smem + s * T::stage;
-      const int whole = least - key0, left = most - key0;
-      if (whole < KT) {
-        if (clear_values<BF, DP>(kb + T::tile, HALF, KT, max(whole, 0), left, threadIdx.x, 32 * WARPS)) *bad = 1;
-        named_bar_sync(1, 32 * WARPS);
-      }
+    const bool ok = walk_tiles(
+        t0, t1, KT, least, [&](int i) { return mbar_wait_warp(&full[i % S], (i / S) & 1); },
+        [&](int i, int t, bool come) {
+          uint8_t* const v = smem + i % S * T::stage + T::tile;
+          const int key0 = t * KT;
+          if (come && clear_values<BF, DP>(v, HALF, KT, max(least - key0, 0), most - key0, threadIdx.x, 32 * WARPS)) *bad = 1;
+          named_bar_sync(1, 32 * WARPS);
+        },
+        [&](int i, int t) {
+          const int s = i % S, key0 = t * KT, whole = least - key0, left = most - key0;
+          uint8_t* const kb = smem + s * T::stage;
 #pragma unroll 1
-      for (int n = 0; n < KT && n < left; n += 32) {  // (32 keys at a time: with 64 the registers do for two CTAs an SM)
-        const int seen[2] = {vis[0] - key0 - n, vis[1] - key0 - n};
-        x.template step<2>(q, smem_addr(kb) + (n + krow) * 128, smem_addr(kb + T::tile) + (n + vrow) * 128, HALF, left - n, whole < n + 32, seen, sc,
-                           a.down, lane);
-      }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&empty[s]);
-    }
+          for (int n = 0; n < KT && n < left; n += 32) {  // (32 keys at a time: with 64 the registers do for two CTAs an SM)
+            const int seen[2] = {vis[0] - key0 - n, vis[1] - key0 - n};
+            x.template step<2>(q, smem_addr(kb) + (n + krow) * 128, smem_addr(kb + T::tile) + (n + vrow) * 128, HALF, left - n, whole < n + 32, seen, sc,
+                               a.down, lane);
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&empty[s]);
+        });
     if (!ok && lane == 0) record_status(a.status, ELASTO_ERR_TIMEOUT);
   }
   __syncthreads();  // all tiles are consumed: the ring's memory takes the results, [channels / 4][row] of four channels

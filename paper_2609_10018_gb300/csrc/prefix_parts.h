@@ -5,8 +5,10 @@
 
 #ifdef __CUDACC__
 #define ELASTO_HD __host__ __device__
+#define ELASTO_D __device__ __forceinline__
 #else
 #define ELASTO_HD
+#define ELASTO_D inline
 #endif
 
 namespace elasto {
@@ -112,6 +114,22 @@ constexpr int kQuadStep = 128;
 // The first key tile of a CTA.
 ELASTO_HD inline int split_from(int tiles, int rank, int split) {
   return static_cast<int>(static_cast<int64_t>(tiles) * rank / split);
+}
+
+// A warp's way over the tiles [t0, t1) of `keys` keys each that it shares with other warps, of which all rows see the first
+// `least` keys. came(i): whether tile number i has come; each warp waits for itself, and one may give up where another has
+// just seen the tile. meet(i, t, ok): a tile that some rows see in part, behind which all warps wait for one another; work(i, t).
+// A warp that has given up does nothing more, but meets the others at every such tile all the same: without it
+// they would wait for ever. Whether all tiles came.
+template <typename CAME, typename MEET, typename WORK>
+ELASTO_D bool walk_tiles(int t0, int t1, int keys, int least, CAME came, MEET meet, WORK work) {
+  bool ok = true;
+  for (int t = t0, i = 0; t < t1; ++t, ++i) {
+    ok = ok && came(i);
+    if (least - t * keys < keys) meet(i, t, ok);
+    if (ok) work(i, t);
+  }
+  return ok;
 }
 
 }  // namespace elasto

@@ -21,6 +21,12 @@ extern "C" int from(int tiles, int rank, int split) { return split_from(tiles, r
 extern "C" long long sums(int part, int h, long long row, long long rho, int hs, int quads) { return PrefixParts{nullptr, nullptr, rho, hs, quads}.sums_at(part, h, row); }
 extern "C" long long stat(int part, int h, long long row, long long rho, int hs, int quads) { return PrefixParts{nullptr, nullptr, rho, hs, quads}.stat_at(part, h, row); }
 extern "C" int most_parts() { return kMaxParts; }
+// A walk whose tile `missing` does not come: the tiles met, those worked on as bits; whether all came.
+extern "C" int walk(int t0, int t1, int keys, int least, int missing, int* meets, long long* worked) {
+  *meets = 0, *worked = 0;
+  return walk_tiles(t0, t1, keys, least, [&](int i) { return t0 + i != missing; }, [&](int, int, bool) { ++*meets; },
+                    [&](int i, int t) { *worked |= i == t - t0 ? 1LL << t : 1LL << 63; });
+}
 """
 FIELDS = ("hg", "nsub", "qpt", "pair", "split", "items", "many", "blocks", "own_split", "prefix_parts", "parts", "fused")
 
@@ -124,3 +130,16 @@ def test_every_form_has_a_case(rule):
     assert many["many"] and many["parts"] == 2 and 3400 * 4 * 6 > 40000
     parts = _plan(rule, rows=150, most=150, batch=320, max_queries=128, prefixes=2, group=1, heads_kv=1, max_prefix=20000, max_keys=69)
     assert not parts["many"] and not parts["fused"] and parts["parts"] > 8 and 128 * 320 > 40000
+
+
+@pytest.mark.parametrize("least", [0, 1, 63, 64, 100, 128, 500, 640])
+def test_a_warp_that_gives_up_meets_the_others(rule, least):
+    """Warps wait for each tile by themselves, and for one another at tiles that rows see in part. However far a warp comes
+    before it gives up, it has to meet the others as often as they do."""
+    for t0, t1 in ((0, 1), (0, 10), (3, 9), (4, 4)):
+        meets, worked = ctypes.c_int(), ctypes.c_longlong()
+        all_meets = [t for t in range(t0, t1) if least < 64 * (t + 1)]
+        for missing in range(t0, t1 + 1):
+            ok = rule.walk(t0, t1, 64, least, missing, ctypes.byref(meets), ctypes.byref(worked))
+            assert ok == (missing == t1) and meets.value == len(all_meets), (t0, t1, missing)
+            assert worked.value == sum(1 << t for t in range(t0, missing))  # (nothing from the tile on that did not come)
