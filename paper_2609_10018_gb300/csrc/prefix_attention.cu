@@ -409,7 +409,8 @@ __global__ void __launch_bounds__(THREADS, 1)
       const bool mine = place(query, head);
       const int part = pair ? 2 * rank + g : rank;
       const long long rho = static_cast<long long>(query) * a.hg + head;
-      if (mine) *reinterpret_cast<float2*>(a.parts.stat + a.parts.stat_at(part, h, rho)) = make_float2(m, sum);
+      // (-0 where all scores of the part are -infinity: an infinite value among its keys shows in no weighted sum then)
+      if (mine) *reinterpret_cast<float2*>(a.parts.stat + a.parts.stat_at(part, h, rho)) = make_float2(m, m == -INFINITY ? -sum : sum);
       float* const sums = a.parts.sums + a.parts.sums_at(part, h, rho);
 #pragma unroll 1
       for (int c = 0; c < DP; c += 32) {

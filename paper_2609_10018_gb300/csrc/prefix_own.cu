@@ -105,24 +105,26 @@ __device__ __noinline__ float bad_values(const uint16_t* v, long long row, int n
   return sum;
 }
 
+// Values that the weighted sums may not show: some own ones have been set to 0 because other rows do not see them, or all scores
+// of a part (of the own keys, of the prefix) are -infinity, whose weighted sums the joins pass over.
+enum { LOOK_OWN = 1, LOOK_PREFIX = 2 };
+
 // The result y of channel ch of a row that sees `seen` own keys and `len` of its prefix: the sum of the values that are not
-// finite, if it sees such. (An infinite value whose probability has rounded to 0 gave NaN; left_out: some have been set to 0
-// because other rows do not see them.)
+// finite, if it sees such. (An infinite value whose probability has rounded to 0 gave NaN.)
 template <bool BF>
-__device__ __noinline__ float put_bad_value(const PrefixOwnArgs& a, float y, int b, int kvh, int k0, int seen, int prefix, int len, int ch) {
+__device__ __noinline__ float put_bad_value(const PrefixOwnArgs& a, float y, int b, int kvh, int k0, int seen, int prefix, int len, int ch, int look) {
   float s = 0.0f;
   if (seen > 0) s += bad_values<BF>(a.v + (a.kv_start ? 0 : b * a.v_batch) + k0 * a.v_row + kvh * a.v_head + ch, a.v_row, seen);
-  if (!(fabsf(y) < INFINITY) && len > 0) s += bad_values<BF>(a.pv + prefix * a.pv_batch + kvh * a.pv_head + ch, a.pv_row, len);
+  if ((!(fabsf(y) < INFINITY) || (look & LOOK_PREFIX)) && len > 0) s += bad_values<BF>(a.pv + prefix * a.pv_batch + kvh * a.pv_head + ch, a.pv_row, len);
   return s != 0.0f ? s : y;  // (NaN too)
 }
 // The same of four channels.
 template <bool BF>
 __device__ __forceinline__ float4 put_bad_values(const PrefixOwnArgs& a, float4 y, int b, int kvh, int k0, int seen, int prefix, int len, int quad,
-                                                 bool left_out) {
+                                                 int look) {
   const float odd = fmaf(y.x, 0.0f, fmaf(y.y, 0.0f, fmaf(y.z, 0.0f, y.w * 0.0f)));
-  if (odd != 0.0f || left_out)
-    y = make_float4(put_bad_value<BF>(a, y.x, b, kvh, k0, seen, prefix, len, 4 * quad), put_bad_value<BF>(a, y.y, b, kvh, k0, seen, prefix, len, 4 * quad + 1),
-                    put_bad_value<BF>(a, y.z, b, kvh, k0, seen, prefix, len, 4 * quad + 2), put_bad_value<BF>(a, y.w, b, kvh, k0, seen, prefix, len, 4 * quad + 3));
+  auto one = [&](float x, int c) { return put_bad_value<BF>(a, x, b, kvh, k0, seen, prefix, len, 4 * quad + c, look); };
+  if (odd != 0.0f || look) y = make_float4(one(y.x, 0), one(y.y, 1), one(y.z, 2), one(y.w, 3));
   return y;
 }
 
@@ -369,8 +371,9 @@ __global__ void __launch_bounds__(32)
       const int qi = query(row), head = row0 + row - qi * a.group, sub = head / a.hg, hs = kvh * a.nsub + sub;
       const long long rho = static_cast<long long>(q0 + qi) * a.hg + (head - sub * a.hg);
       if (!a.fused) {
+        const bool look = left_out || (x.m[h] == -INFINITY && n > 0 && vis[h] > 16 * t0);  // (it sees keys of this part)
         if ((lane & 3) == 0)
-          *reinterpret_cast<float2*>(a.parts.stat + a.parts.stat_at(a.prefix_parts + rank, hs, rho)) = make_float2(x.m[h], left_out ? -x.sum[h] : x.sum[h]);
+          *reinterpret_cast<float2*>(a.parts.stat + a.parts.stat_at(a.prefix_parts + rank, hs, rho)) = make_float2(x.m[h], look ? -x.sum[h] : x.sum[h]);
         if (x.m[h] == -INFINITY) continue;
         float* const sums = a.parts.sums + a.parts.sums_at(a.prefix_parts + rank, hs, rho) + (c2 & 3) + (c2 >> 2) * kQuadStep;
 #pragma unroll
@@ -387,7 +390,7 @@ __global__ void __launch_bounds__(32)
       const float top = fmaxf(x.m[h], st.x);
       // (a part without a finite score has sums of zeros, or NaN that must stay)
       const float wo = x.m[h] == -INFINITY ? 1.0f : ex2_approx((x.m[h] - top) * sc), wp = st.x == -INFINITY ? 1.0f : ex2_approx((st.x - top) * sc);
-      const float total = x.sum[h] * wo + st.y * wp;
+      const float total = x.sum[h] * wo + fabsf(st.y) * wp;
       const int seen_own = visible(row);
       const float inv = len > 0 || seen_own > 0 ? 1.0f / total : 0.0f;
       uint16_t* const out = a.out + static_cast<long long>(q0 + qi) * a.out_row + static_cast<long long>(kvh * a.group + head) * a.out_head + c2;
@@ -397,8 +400,8 @@ __global__ void __launch_bounds__(32)
         float2 y = make_float2((x.o[j][2 * h] * wo + p[j].x * wp) * inv, (x.o[j][2 * h + 1] * wo + p[j].y * wp) * inv);
         if (total > 0.0f) {
           if (fmaf(y.x, 0.0f, y.y * 0.0f) != 0.0f || left_out)
-            y = make_float2(put_bad_value<BF>(a, y.x, b, kvh, k0, seen_own, prefix, len, 8 * j + c2),
-                            put_bad_value<BF>(a, y.y, b, kvh, k0, seen_own, prefix, len, 8 * j + c2 + 1));
+            y = make_float2(put_bad_value<BF>(a, y.x, b, kvh, k0, seen_own, prefix, len, 8 * j + c2, 0),
+                            put_bad_value<BF>(a, y.y, b, kvh, k0, seen_own, prefix, len, 8 * j + c2 + 1, 0));
         } else if (inv != 0.0f) {  // (a sum of 0 or NaN over visible keys)
           y.x = y.y = __int_as_float(0x7fc00000);
         }
@@ -534,7 +537,8 @@ __global__ void __launch_bounds__(THREADS, 3)
     const long long rho = static_cast<long long>(q0 + qi) * a.hg + (head - sub * a.hg);
     const float2 st = *reinterpret_cast<const float2*>(stat + 2 * row);
     float* const to = a.parts.sums + a.parts.sums_at(a.prefix_parts + rank, hs, rho);
-    if (threadIdx.x < ROWS) *reinterpret_cast<float2*>(a.parts.stat + a.parts.stat_at(a.prefix_parts + rank, hs, rho)) = make_float2(st.x, left_out ? -st.y : st.y);
+    const bool look = left_out || (st.x == -INFINITY && t0 < t1 && visible(row) > KT * t0);  // (it sees keys of this part)
+    if (threadIdx.x < ROWS) *reinterpret_cast<float2*>(a.parts.stat + a.parts.stat_at(a.prefix_parts + rank, hs, rho)) = make_float2(st.x, look ? -st.y : st.y);
     if (st.x != -INFINITY)
       for (int quad = threadIdx.x / ROWS; quad < quads; quad += 2)
         *reinterpret_cast<float4*>(to + quad * kQuadStep) = *reinterpret_cast<const float4*>(sums + quad * QUAD + 4 * row);
@@ -608,7 +612,7 @@ __global__ void __launch_bounds__(JOIN_THREADS)
   if (quad >= quads) return;
   float top = -INFINITY, total = 0.0f;
   float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  bool left_out = false;
+  int look = 0;
   pdl_wait();
   for (int p0 = 0; p0 < parts; p0 += N) {
     const uint32_t bits = found.written[p0 >> 5] >> (p0 & 31);
@@ -630,7 +634,7 @@ __global__ void __launch_bounds__(JOIN_THREADS)
     top = up;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      left_out |= __float_as_int(st[k].y) < 0;
+      if (__float_as_int(st[k].y) < 0) look |= p0 + k < a.prefix_parts ? LOOK_PREFIX : LOOK_OWN;
       // (a part without a finite score has a sum of 0, or NaN that must stay, and no weighted sums)
       const bool none = st[k].x == -INFINITY;
       const float w = none ? 1.0f : ex2_approx((st[k].x - top) * sc);
@@ -642,7 +646,7 @@ __global__ void __launch_bounds__(JOIN_THREADS)
   const float inv = len > 0 || seen > 0 ? 1.0f / total : 0.0f;
   y = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
   if (total > 0.0f)
-    y = put_bad_values<BF>(a, y, b, r.kvh, k0, seen, prefix, len, quad, left_out);
+    y = put_bad_values<BF>(a, y, b, r.kvh, k0, seen, prefix, len, quad, look);
   else if (inv != 0.0f)  // (a sum of 0 or NaN over visible keys)
     y.x = y.y = y.z = y.w = __int_as_float(0x7fc00000);
   *reinterpret_cast<uint2*>(out + 4 * quad) = make_uint2(pack16<BF>(y.x, y.y), pack16<BF>(y.z, y.w));
@@ -656,9 +660,10 @@ __global__ void __launch_bounds__(JOIN_THREADS, 4)
     prefix_join_many_kernel(const __grid_constant__ PrefixOwnArgs a) {
   constexpr int GROUPS = JOIN_THREADS / ROWS;  // threads that share a row's parts
   extern __shared__ float weight[];            // [part][ROWS]: times 1 / the joint sum; -1: not to be read
-  __shared__ float2 partial[GROUPS][ROWS];     // maximum and sum of a thread's parts (the sign: values left out)
+  __shared__ float2 partial[GROUPS][ROWS];     // maximum and sum of a thread's parts
+  __shared__ uint8_t looks[GROUPS][ROWS];      // and what they do not show
   __shared__ float base[ROWS];                 // 0, or NaN in rows without a sum above 0
-  __shared__ int look[ROWS];                   // 1: values that the row may see have been left out
+  __shared__ int look[ROWS];                   // LOOK_OWN, LOOK_PREFIX
   __shared__ Found found;
   const int b = static_cast<int>(a.by_join.quotient(blockIdx.x)), blk = static_cast<int>(blockIdx.x) - b * a.join_blocks;
   pdl_trigger();
@@ -681,27 +686,27 @@ __global__ void __launch_bounds__(JOIN_THREADS, 4)
     const float* const st = a.parts.stat + a.parts.stat_at(0, r.h, r.rho);
     const long long step = a.parts.stat_at(1, 0, 0);
     float top = -INFINITY, total = 0.0f;
-    bool left_out = false;
+    int bits = 0;
     pdl_wait();
 #pragma unroll 4
     for (int p = g; p < parts; p += GROUPS) {
       const float2 v = found.written[p >> 5] >> (p & 31) & 1 ? *reinterpret_cast<const float2*>(st + p * step) : make_float2(-INFINITY, 0.0f);
-      left_out |= __float_as_int(v.y) < 0;
+      if (__float_as_int(v.y) < 0) bits |= p < a.prefix_parts ? LOOK_PREFIX : LOOK_OWN;
       const float up = fmaxf(top, v.x);
       total = total * factor(top, up) + fabsf(v.y) * factor(v.x, up);
       top = up;
       weight[p * ROWS + row] = v.x;
     }
-    partial[g][row] = make_float2(top, left_out ? -total : total);
+    partial[g][row] = make_float2(top, total), looks[g][row] = static_cast<uint8_t>(bits);
     __syncthreads();
-    top = -INFINITY, total = 0.0f, left_out = false;
+    top = -INFINITY, total = 0.0f, bits = 0;
 #pragma unroll
     for (int k = 0; k < GROUPS; ++k) top = fmaxf(top, partial[k][row].x);
 #pragma unroll
     for (int k = 0; k < GROUPS; ++k) {
       const float2 v = partial[k][row];
-      left_out |= __float_as_int(v.y) < 0;
-      total += fabsf(v.y) * factor(v.x, top);
+      bits |= looks[k][row];
+      total += v.y * factor(v.x, top);
     }
     const float inv = 1.0f / total;
     for (int p = g; p < parts; p += GROUPS) {
@@ -711,7 +716,7 @@ __global__ void __launch_bounds__(JOIN_THREADS, 4)
     if (g == 0) {
       const bool sees = len > 0 || min(nk - nq + r.query + 1, nk) > 0;
       base[row] = sees && !(total > 0.0f) ? __int_as_float(0x7fc00000) : 0.0f;
-      look[row] = left_out;
+      look[row] = bits;
     }
     __syncthreads();
   }

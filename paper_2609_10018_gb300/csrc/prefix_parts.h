@@ -96,7 +96,8 @@ inline PrefixPlan prefix_plan(const PrefixSizes& z) {
 }
 
 // Parts of the results, those of the prefix and then those of the own keys: stat [part][key head x nsub][rho] (maximum and
-// sum of each row; of an own part the sum with its sign turned where values that some row sees were left out) and
+// sum of each row; the sum's sign is turned where the weighted sums do not show what the row sees: in an own part values that
+// some row sees were left out, or all scores of the part are -infinity) and
 // sums [part][key head x nsub][rho / 32][channels / 4][rho % 32] of four channels (not written where the maximum is
 // -infinity): what a warp writes or reads of 32 rows lies together, all channels of them in one piece of 16 KB at most.
 struct PrefixParts {

@@ -223,6 +223,34 @@ def test_scores_that_are_not_finite():
     assert torch.isfinite(got[2:]).all()
 
 
+@pytest.mark.parametrize("dtype,d", [(BF16, 64), (F16, 128), (BF16, 40)])
+@pytest.mark.parametrize("form,queries,heads,heads_kv,room", [("few", 1, 4, 2, 0), ("few", 4, 4, 2, 0), ("few", 5, 28, 4, 0), ("many", 1, 4, 2, 7000),
+                                                              ("many", 4, 4, 2, 7000), ("inside", 4, 32 * 52, 52, 0)])
+def test_infinite_values_behind_scores_of_minus_infinity(form, queries, heads, heads_kv, room, dtype, d):
+    """A part of the keys without a finite score has no weight, but an infinite or NaN value in it is one that the query sees. In the
+    joins of few and of many rows, and where the kernel of the own keys joins (tests/test_prefix_plan.py has the sizes)."""
+    c = Case([(140, 2), (60, 1)], [queries] * 3, [queries, queries + 2, 20], heads, heads_kv, d, dtype, tail=room)
+    c.q[:, :, 0] = c.q[:, :, 0].abs() + 1
+    c.k[0, :queries, 0, 0] = -INF  # all own keys of the first sequence, for the first key head,
+    c.pk[0, 128:140, 0, 0] = -INF  # those of a whole tile,
+    c.pk[1, :60, 0, 0] = -INF      # and of a whole prefix
+    finite = c.check(c.device().run(max_queries=max(queries, room)))
+    c.v[0, 0, 0, 5], c.v[0, queries - 1, 0, 6] = INF, -INF
+    c.pv[0, 130, 0, 7], c.pv[0, 139, 0, 4] = INF, NAN
+    c.pv[1, 59, 0, 3] = -INF
+    got = c.device().run(max_queries=max(queries, room))
+    n, first = queries, slice(0, heads // heads_kv)
+    assert (got[:n, first, 5] == INF).all() and (got[n - 1, first, 6] == -INF).all()
+    assert torch.isfinite(got[:n - 1, first, 6]).all()  # (hidden)
+    assert (got[:2 * n, first, 7] == INF).all() and got[:2 * n, first, 4].isnan().all()
+    assert (got[2 * n:3 * n, first, 3] == -INF).all()
+    # all others as with finite values there
+    got[:n, first, 5], got[n - 1, first, 6] = finite[:n, first, 5], finite[n - 1, first, 6]
+    got[:2 * n, first, 7], got[:2 * n, first, 4] = finite[:2 * n, first, 7], finite[:2 * n, first, 4]
+    got[2 * n:3 * n, first, 3] = finite[2 * n:3 * n, first, 3]
+    assert torch.equal(got, finite)
+
+
 @pytest.mark.parametrize("dtype,d", [(BF16, 128), (F16, 64), (BF16, 40)])
 def test_prompts_whose_prefixes_fill_the_chip(dtype, d):
     """Items of the prefixes for every SM: the kernel of the own keys joins its rows itself. Prefixes without keys,

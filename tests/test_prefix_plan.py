@@ -143,3 +143,17 @@ def test_a_warp_that_gives_up_meets_the_others(rule, least):
             ok = rule.walk(t0, t1, 64, least, missing, ctypes.byref(meets), ctypes.byref(worked))
             assert ok == (missing == t1) and meets.value == len(all_meets), (t0, t1, missing)
             assert worked.value == sum(1 << t for t in range(t0, missing))  # (nothing from the tile on that did not come)
+
+
+def test_forms_of_the_test_of_infinite_values(rule):
+    """Sizes of test_infinite_values_behind_scores_of_minus_infinity: several parts and few rows, many rows, a join inside."""
+    room = dict(batch=3, prefixes=2, max_prefix=140, max_keys=20)
+    for queries, group, heads_kv in ((1, 2, 2), (4, 2, 2), (5, 7, 4)):
+        p = _plan(rule, rows=3 * queries, most=3 * queries, max_queries=queries, group=group, heads_kv=heads_kv, **room)
+        assert not p["fused"] and not p["many"] and p["parts"] > 2, p
+    for queries in (1, 4):
+        most = 3 * queries + 7000
+        p = _plan(rule, rows=most, most=most, max_queries=7000, group=2, heads_kv=2, **room)
+        assert p["many"] and 7000 * 4 * 3 > 40000 and not p["fused"], p
+    p = _plan(rule, rows=12, most=12, max_queries=4, group=32, heads_kv=52, **room)
+    assert p["fused"], p
