@@ -9,7 +9,9 @@
 //   prefix_many_kernel   64 rows, longer runs of tokens: four warps with 16 rows each, a fifth loads tiles of 64 keys.
 // Neither waits for the prefixes' kernel: that one is bound by its products, these by reading the keys and values
 // once, and both run at the same time. Only the last CTA waits before it ends, so that what waits for this kernel waits
-// for both.
+// for both. The inputs are there all the same: no CTA of these kernels starts before every CTA of the prefixes' has waited for
+// the work before the call, whose results then are in the L2. What is read without a wait of the kernel's own is therefore read
+// from there, by TMA and by loads that pass over the L1 (where lines of a call before might be left).
 //
 // prefix_join_few_kernel, prefix_join_many_kernel: out = sum over parts of o exp(m - top) / sum of l exp(m - top), four
 // channels a thread, in a fixed order. Where the prefixes' CTAs fill the chip by themselves and leave one part, prefix_few_kernel waits for them and joins its
@@ -98,7 +100,7 @@ __device__ __noinline__ float bad_values(const uint16_t* v, long long row, int n
   float sum = 0.0f;
 #pragma unroll 8
   for (int j = 0; j < n; ++j) {
-    const uint16_t w = v[j * row];
+    const uint16_t w = __ldcg(v + j * row);
     const float x = BF ? __uint_as_float(static_cast<uint32_t>(w) << 16) : __half2float(__ushort_as_half(w));
     if (!(fabsf(x) < INFINITY)) sum += x;
   }
@@ -128,18 +130,25 @@ __device__ __forceinline__ float4 put_bad_values(const PrefixOwnArgs& a, float4 
   return y;
 }
 
+// The keys of prefix g, and whether sequence b is behind it.
+__device__ __forceinline__ int prefix_keys(const PrefixOwnArgs& a, int g) {
+  return a.prefix_len ? min(max(__ldcg(a.prefix_len + g), 0), a.max_prefix) : a.max_prefix;
+}
+__device__ __forceinline__ bool behind(const PrefixOwnArgs& a, int b, int g) {
+  return !a.seq_start || (__ldcg(a.seq_start + g) <= b && b < __ldcg(a.seq_start + g + 1));
+}
 // Rows of q and own keys of sequence b, cut to what the host allows.
 __device__ __forceinline__ void sequence(const PrefixOwnArgs& a, int b, int& q0, int& nq, int& k0, int& nk) {
   q0 = b * a.max_queries, nq = a.max_queries, k0 = 0, nk = a.max_keys;
   if (a.q_start) {
-    q0 = min(max(a.q_start[b], 0), a.q_rows);
-    nq = min(max(min(a.q_start[b + 1], a.q_rows) - q0, 0), a.max_queries);
+    q0 = min(max(__ldcg(a.q_start + b), 0), a.q_rows);
+    nq = min(max(min(__ldcg(a.q_start + b + 1), a.q_rows) - q0, 0), a.max_queries);
   }
   if (a.kv_start) {
-    k0 = min(max(a.kv_start[b], 0), a.kv_rows);
-    nk = min(max(min(a.kv_start[b + 1], a.kv_rows) - k0, 0), a.max_keys);
+    k0 = min(max(__ldcg(a.kv_start + b), 0), a.kv_rows);
+    nk = min(max(min(__ldcg(a.kv_start + b + 1), a.kv_rows) - k0, 0), a.max_keys);
   } else if (a.kv_len) {
-    nk = min(max(a.kv_len[b], 0), a.max_keys);
+    nk = min(max(__ldcg(a.kv_len + b), 0), a.max_keys);
   }
 }
 
@@ -241,6 +250,29 @@ struct Softmax {
   }
 };
 
+// The words of a row at p (`channels` of it) that a lane of the row's four has of the products' A operand, into q[..][h] and
+// q[..][h + 2]. A lane loads whole 16-byte pieces from the L2, every fourth of the row's, and the four exchange
+// words. (With loads of the single words eight images took 206 us in place of 199.)
+template <int DP>
+__device__ __forceinline__ void load_query(const uint16_t* p, int channels, int lane, int h, uint32_t (&q)[DP / 16][4]) {
+  const int c = lane & 3;
+  const bool odd = c & 1, up = c & 2;
+#pragma unroll
+  for (int m = 0; m < DP / 32; ++m) {
+    const int ch = 32 * m + 8 * c;
+    uint4 w = make_uint4(0u, 0u, 0u, 0u);
+    if (ch < channels) w = __ldcg(reinterpret_cast<const uint4*>(p + ch));
+    // (the transpose of 4 x 4 words: pairs of lanes, then pairs of pairs)
+    auto swap = [&](uint32_t& lo, uint32_t& hi, bool second, int with) {
+      const uint32_t other = __shfl_xor_sync(0xffffffffu, second ? lo : hi, with);
+      (second ? lo : hi) = other;
+    };
+    swap(w.x, w.y, odd, 1), swap(w.z, w.w, odd, 1);
+    swap(w.x, w.z, up, 2), swap(w.y, w.w, up, 2);
+    q[2 * m][h] = w.x, q[2 * m][h + 2] = w.y, q[2 * m + 1][h] = w.z, q[2 * m + 1][h + 2] = w.w;
+  }
+}
+
 // Values of the V tile at v (64 channels of `half` bytes, `keys` keys, 128 bytes each) that no row sees, from key `left` on,
 // become 0, and from key `from` on, where some rows do not see them, those that are not finite: 0 * NaN
 // would reach these rows. (The rows that see them get them at the end.) Whether there were any; thread `t` of `threads`.
@@ -290,7 +322,7 @@ __global__ void __launch_bounds__(32)
   }
   __syncwarp();
   pdl_trigger();
-  // The kernel before writes nothing but its parts, and waited for what came before it: the inputs may be read at once.
+  // (the inputs may be read at once, from the L2)
   int q0, nq, k0, nk;
   sequence(a, b, q0, nq, k0, nk);
   const int row0 = blk * 16, nrows = min(nq * a.group - row0, 16);
@@ -314,8 +346,8 @@ __global__ void __launch_bounds__(32)
     int prefix = -1, len = 0;
     if (a.fused)
       for (int g0 = 0; g0 < a.prefixes && prefix < 0; g0 += 32) {
-        const int g = g0 + lane, keys = g < a.prefixes && a.prefix_len ? min(max(a.prefix_len[g], 0), a.max_prefix) : a.max_prefix;
-        const uint32_t mine = __ballot_sync(0xffffffffu, g < a.prefixes && (!a.seq_start || (a.seq_start[g] <= b && b < a.seq_start[g + 1])));
+        const int g = g0 + lane, keys = g < a.prefixes ? prefix_keys(a, g) : 0;
+        const uint32_t mine = __ballot_sync(0xffffffffu, g < a.prefixes && behind(a, b, g));
         if (mine) prefix = g0 + __ffs(mine) - 1, len = __shfl_sync(0xffffffffu, keys, __ffs(mine) - 1);
       }
     const int r = lane >> 2, c2 = 2 * (lane & 3);
@@ -326,13 +358,7 @@ __global__ void __launch_bounds__(32)
       const int row = r + 8 * h, qi = query(row), head = row0 + row - qi * a.group;
       vis[h] = visible(row);
       const uint16_t* const p = a.q + static_cast<long long>(q0 + qi) * a.q_row + static_cast<long long>(kvh * a.group + head) * a.q_head;
-#pragma unroll
-      for (int k = 0; k < DP / 16; ++k)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int ch = 16 * k + c2 + 8 * j;
-          q[k][h + 2 * j] = row < nrows && ch < a.head_dim ? *reinterpret_cast<const uint32_t*>(p + ch) : 0u;
-        }
+      load_query<DP>(p, row < nrows ? a.head_dim : 0, lane, h, q);
     }
     const float sc = a.scale_log2;
     const int krow = (lane & 7) + (lane >> 4) * 8, vrow = lane & 15;  // this lane's in the ldmatrix loads of K and of V
@@ -438,7 +464,7 @@ __global__ void __launch_bounds__(THREADS, 3)
   }
   __syncthreads();
   pdl_trigger();
-  // (the inputs may be read at once, as by prefix_few_kernel)
+  // (the inputs may be read at once, from the L2)
   int q0, nq, k0, nk;
   sequence(a, b, q0, nq, k0, nk);
   const int row0 = blk * ROWS, nrows = min(nq * a.group - row0, ROWS);
@@ -481,13 +507,7 @@ __global__ void __launch_bounds__(THREADS, 3)
       const int row = base + r + 8 * h, qi = query(row), head = row0 + row - qi * a.group;
       vis[h] = visible(row);
       const uint16_t* const p = a.q + static_cast<long long>(q0 + qi) * a.q_row + static_cast<long long>(kvh * a.group + head) * a.q_head;
-#pragma unroll
-      for (int k = 0; k < DP / 16; ++k)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int ch = 16 * k + c2 + 8 * j;
-          q[k][h + 2 * j] = row < nrows && ch < a.head_dim ? *reinterpret_cast<const uint32_t*>(p + ch) : 0u;
-        }
+      load_query<DP>(p, row < nrows ? a.head_dim : 0, lane, h, q);
     }
     const float sc = a.scale_log2;
     const int krow = (lane & 7) + (lane >> 4) * 8, vrow = lane & 15;
@@ -572,8 +592,8 @@ __device__ __forceinline__ void find_prefix(const PrefixOwnArgs& a, int b, int p
   if (threadIdx.x == 0) found.prefix = a.seq_start ? -1 : 0, found.len = a.seq_start ? 0 : a.max_prefix;
   __syncthreads();
   for (int g = threadIdx.x; g < a.prefixes; g += JOIN_THREADS) {
-    const int n = a.prefix_len ? min(max(a.prefix_len[g], 0), a.max_prefix) : a.max_prefix;
-    if (!a.seq_start || (a.seq_start[g] <= b && b < a.seq_start[g + 1])) found.prefix = g, found.len = n;
+    const int n = prefix_keys(a, g);
+    if (behind(a, b, g)) found.prefix = g, found.len = n;
   }
   __syncthreads();
   if (threadIdx.x < (parts + 31) / 32 * 32) {
@@ -592,7 +612,7 @@ __global__ void __launch_bounds__(JOIN_THREADS)
   __shared__ Found found;
   const int b = static_cast<int>(a.by_join.quotient(blockIdx.x)), blk = static_cast<int>(blockIdx.x) - b * a.join_blocks;
   pdl_trigger();
-  // (the inputs may be read before the wait, as by prefix_few_kernel)
+  // (the inputs may be read before the wait, from the L2)
   int q0, nq, k0, nk;
   sequence(a, b, q0, nq, k0, nk);
   const int parts = a.prefix_parts + (a.max_keys > 0 ? a.own_split : 0);

@@ -213,3 +213,52 @@ def test_keys_and_lengths_from_the_calls_before(queries):
             for x in t.values():
                 x.fill_(float("nan"))
             assert torch.equal(after, want)
+
+
+@pytest.mark.parametrize("queries,batch", [(1, 48), (9, 16), (150, 3)])
+def test_queries_and_lengths_that_change_from_call_to_call(queries, batch):
+    """Calls right behind one another on the same buffers: before each a product writes other queries, and copies write other lengths and
+    other starts. The kernels that read these without a wait of their own may not find what a call before them read."""
+    g = torch.Generator(device="cuda").manual_seed(queries)
+    keys, lens, depth, rounds, row = 320, (70, 256), 512, 12, HEADS_KV * D
+    rand = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    pk, pv = (rand(2, lens[1], HEADS_KV, D).to(BF16) for _ in "kv")
+    k, v = (rand(batch, keys, HEADS_KV, D).to(BF16) for _ in "kv")
+    w = rand(D, depth).to(BF16)
+    a = [(rand(batch * queries * HEADS, depth) / depth ** 0.5).to(BF16) for _ in range(rounds)]
+    q = torch.empty((batch * queries, HEADS, D), dtype=BF16, device="cuda")
+    out = torch.empty_like(q)
+    rng = torch.Generator().manual_seed(queries)
+    draw = lambda lo, hi, n: torch.randint(lo, hi + 1, (n,), generator=rng)  # noqa: E731
+    now = {"q_start": _i32([0] * (batch + 1)), "kv_len": _i32([0] * batch), "seq_start": _i32([0] * 3), "prefix_len": _i32([0] * 2)}
+    each = []
+    for _ in range(rounds):
+        starts = torch.cat([torch.zeros(1, dtype=torch.long), draw(1, queries, batch).cumsum(0)])
+        cut = int(draw(0, batch, 1))
+        each.append({n: t.to(torch.int32).cuda() for n, t in (("q_start", starts), ("kv_len", draw(0, keys, batch)),
+                                                              ("seq_start", torch.tensor([0, cut, batch])), ("prefix_len", draw(*lens, 2)))})
+    args = binding.PrefixAttention(
+        dtype=binding.BF16, batch=batch, heads=HEADS, heads_kv=HEADS_KV, head_dim=D, scale=0.125, max_queries=queries, q_rows=q.shape[0],
+        q_start=now["q_start"].data_ptr(), q=q.data_ptr(), q_row=HEADS * D, q_head=D, out=out.data_ptr(), out_row=HEADS * D, out_head=D,
+        prefixes=2, seq_start=now["seq_start"].data_ptr(), max_prefix=lens[1], prefix_rows=lens[1], prefix_len=now["prefix_len"].data_ptr(),
+        prefix_k=pk.data_ptr(), prefix_k_batch=lens[1] * row, prefix_k_row=row, prefix_k_head=D, prefix_v=pv.data_ptr(),
+        prefix_v_batch=lens[1] * row, prefix_v_row=row, prefix_v_head=D, max_keys=keys, kv_rows=keys, kv_len=now["kv_len"].data_ptr(),
+        k=k.data_ptr(), k_batch=keys * row, k_row=row, k_head=D, v=v.data_ptr(), v_batch=keys * row, v_row=row, v_head=D)
+    work = torch.empty(binding.elasto_op_prefix_attention_workspace(args), dtype=torch.uint8, device="cuda")
+    args.workspace, args.workspace_bytes = work.data_ptr(), work.numel()
+
+    def call(i, wait):
+        out.zero_()
+        for n, t in now.items():
+            t.copy_(each[i][n])
+        binding.elasto_op_gemm(stream_handle(), a[i].data_ptr(), w.data_ptr(), None, q.data_ptr(), None, a[i].shape[0], D, depth, binding.EPI_BIAS_BF16)
+        if wait:
+            torch.cuda.synchronize()
+        binding.elasto_op_prefix_attention(stream_handle(), args)
+        return out.clone()
+
+    want = [call(i, True) for i in range(rounds)]
+    assert len({t.cpu().view(torch.int16).numpy().tobytes() for t in want}) == rounds
+    for _ in range(4):
+        got = [call(i, False) for i in range(rounds)]
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
