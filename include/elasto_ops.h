@@ -259,8 +259,8 @@ enum { ELASTO_NORM_NONE = 0, ELASTO_NORM_RMS = 1, ELASTO_NORM_LAYER = 2 };
  * y_scale: a factor for each column. gate, shift and scale (each may be NULL; mod_type ELASTO_F32, _BF16 or _F16) are tables
  * [groups, cols] with row stride mod_row: row r takes row group[r] of them (group NULL: row 0). groups 0: no tables. A row
  * with a group outside [0, groups) is left out, and *status_device is set to ELASTO_ERR_INVALID_ARG.
- * Squares are summed in fp32: from about 1e19 on they overflow, and the norm gives 0, or NaN for an infinity. A row
- * of zeros with eps 0: NaN.
+ * Squares are summed in fp32: from about 1e19 on they overflow, and the norm gives 0, or NaN for an infinity. Small rows
+ * (eps 0, or as small) are normed like others as long as their values are normal numbers of fp32. A row of zeros with eps 0: NaN.
  * cols: 1 to 16384. Row strides are at least cols. Data needs its types' alignment; rows whose starts are multiples of
  * eight values in memory are read and written wide. Outputs may not overlap the inputs (but x_out, x) or one another. */
 typedef struct {

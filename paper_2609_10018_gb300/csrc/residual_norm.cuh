@@ -13,7 +13,7 @@
 // column, so that a warp's accesses are neighbours.
 //
 // 50432 x 768, fp32 stream, 82 us, 5.7 TB/s (68.5 at a copy's rate; without norms 77); 32760 x 1536 bf16, gated and
-// modulated, 71 us, 5.6 TB/s, issue slots at 57 %; 8191 x 5000 to e4m3 63 us, issue slots at 59 %. (With rows loaded by the
+// modulated, 71 us, 5.6 TB/s, issue slots at 57 %; 8191 x 5000 to e4m3 64 us, issue slots at 59 %. (With rows loaded by the
 // threads that compute them, without a ring: 82.6, 124 and 151.)
 #pragma once
 #include <algorithm>
@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(LOG == 9 ? 512 : CTA_THREADS, 1)
   const elasto_residual_norm_args& a = args.u;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint64_t full[MAX_TEAMS][MAX_STAGES];
-  __shared__ __align__(16) float partial[4][MAX_TEAMS];
+  __shared__ __align__(16) float partial[5][MAX_TEAMS];
   __shared__ uint4 zeros[2];  // what lanes past the row's last column read
   const int teams = blockDim.x / TEAM, team = warp_uniform(threadIdx.x / TEAM), t = threadIdx.x & (T - 1), lane = threadIdx.x & 31;
   const int sub = rows_log > 0 ? lane >> LOG : 0;
@@ -288,7 +288,7 @@ __global__ void __launch_bounds__(LOG == 9 ? 512 : CTA_THREADS, 1)
       }
     }
   };
-  // v is centred (LAYER); returns 1 / sqrt(mean v^2 + eps)
+  // v is centred (LAYER), and scaled where it is small; returns 1 / sqrt(mean v^2 + eps)
   auto root = [&](float2 (&v)[PIECES][4], int kind, int slot) {
     float2 sum = make_float2(0.0f, 0.0f);
     if (kind == ELASTO_NORM_LAYER) {
@@ -304,12 +304,29 @@ __global__ void __launch_bounds__(LOG == 9 ? 512 : CTA_THREADS, 1)
           v[i][j] = add2(v[i][j], make_float2(inside(i, 2 * j) ? mean : 0.0f, inside(i, 2 * j + 1) ? mean : 0.0f));
       });
     }
-    pieces([&](int i) {
+    // Where the mean square is near the smallest normal number the squares have lost bits, or all of themselves: v times 2^100
+    // then, whose squares are exact enough and far from overflow (v < 2^-55 there). A second time around, since ordinary
+    // rows pay for more code (8191 x 5000 to e4m3 62.9 us without, 64.2 so, 68.7 with the second sum written out behind the first).
+    float m = 0.0f, eps = a.eps;
+#pragma unroll 1
+    for (int at = slot + 1;; at = 4) {
+      pieces([&](int i) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) sum = fma2(v[i][j], v[i][j], sum);
-    });
+        for (int j = 0; j < 4; ++j) sum = fma2(v[i][j], v[i][j], sum);
+      });
+      m = fmaf(row_sum(sum, at), inv_n, eps);
+      const bool small = m < 0x1p-124f;
+      if (at == 4 || !(T >= 32 ? small : __any_sync(0xffffffffu, small))) break;  // (the same in all threads of a row)
+      const float up = small ? 0x1p100f : 1.0f;
+      eps = eps * up * up;
+      sum = make_float2(0.0f, 0.0f);
+      pieces([&](int i) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[i][j] = mul2(v[i][j], make_float2(up, up));
+      });
+    }
     // (rsqrtf is off by up to two units in the last place; one step of Newton's method leaves half of one)
-    const float m = fmaf(row_sum(sum, slot + 1), inv_n, a.eps), rs = rsqrtf(m), e = fmaf(-m * rs, rs, 1.0f);
+    const float rs = rsqrtf(m), e = fmaf(-m * rs, rs, 1.0f);
     return fabsf(e) < 1.0f ? fmaf(0.5f * rs, e, rs) : rs;
   };
 

@@ -236,6 +236,21 @@ def test_e4m3_rows_are_those_of_the_quantiser():
         assert (d["z"]._base.view(-1)[:60 * (cols + 5)].view(60, cols + 5)[:, cols:] == 77).all()
 
 
+@pytest.mark.parametrize("cols,pad", [(8, 0), (100, 1), (200, 0), (384, 0), (1031, 3), (1536, 0), (6200, 0), (6201, 0)])
+@pytest.mark.parametrize("eps", [0.0, 1e-38])
+@pytest.mark.parametrize("post,pre,z", [(NONE, RMS, F32), (NONE, LAYER, F32), (RMS, LAYER, BF16), (LAYER, NONE, F32), (NONE, RMS, torch.float8_e4m3fn)])
+def test_small_rows(post, pre, z, eps, cols, pad):
+    """Rows whose squares are subnormal or 0 in fp32, beside rows of ordinary size: normed like these where eps leaves them."""
+    c = Case(23, cols, F32, F32, z, post, pre, pad=pad, offset=pad, eps=eps)
+    size = torch.tensor([1.0, 1e-17, 1e-18, 3e-19, 1e-19, 3e-20, 1e-20, 1e-21, 1e-22, 1e-23, 1e-24, 1e-27, 1e-30, 1e-34, 1.0, 1e3, 1e-26, 1e-10])
+    size = torch.cat([size, 1e-25 * torch.ones(c.rows - len(size))])[:, None]
+    c.x *= size
+    c.y *= size
+    d = c.device()
+    assert _run(c.args(d)) == 0
+    c.check(d)
+
+
 def test_same_bits_captured_and_on_another_stream():
     c = Case(300, 1536, BF16, BF16, BF16, LAYER, LAYER, mod=BF16, groups=7)
     d = c.device()
