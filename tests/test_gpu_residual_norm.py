@@ -281,3 +281,19 @@ def test_offsets_past_32_bits():
     d["x"] = d["x_out"] = view
     assert _run(c.args(d)) == 0
     c.check(d)
+
+
+@pytest.mark.parametrize("x,y,z,mod", [(F32, BF16, BF16, BF16), (BF16, F32, torch.float8_e4m3fn, F32), (BF16, BF16, F32, None)])
+@pytest.mark.parametrize("rows,cols,pad", [(60000, 104, 0), (60000, 100, 0), (30000, 256, 0), (30000, 257, 1), (9000, 1536, 0), (9000, 1535, 0),
+                                           (9000, 1536, 3), (3000, 5000, 0), (3000, 4999, 2), (700, 8192, 0), (700, 8191, 0)])
+def test_many_rows_through_the_ring(rows, cols, pad, x, y, z, mod):
+    """Several times as many rows as the rings of all SMs hold (152 CTAs of up to 24 teams with up to four stages each): a stage
+    is copied into again and again, with another alignment and another group's tables each time. In place, and the same
+    bits beside."""
+    c = Case(rows, cols, x, y, z, RMS, LAYER, affine=mod is not None, y_scale=True, mod=mod, groups=7 if mod else 0, pad=pad, offset=pad)
+    d = c.device(in_place=True)
+    assert _run(c.args(d)) == 0
+    c.check(d)
+    e = c.device()
+    assert _run(c.args(e)) == 0
+    assert torch.equal(d["x"], e["x_out"]) and torch.equal(d["z"], e["z"]) and torch.equal(d["z_scale"], e["z_scale"])
