@@ -615,7 +615,7 @@ __global__ void __launch_bounds__(JOIN_THREADS)
   // (the inputs may be read before the wait, from the L2)
   int q0, nq, k0, nk;
   sequence(a, b, q0, nq, k0, nk);
-  const int parts = a.prefix_parts + (a.max_keys > 0 ? a.own_split : 0);
+  const int parts = a.prefix_parts + a.own_parts;
   find_prefix(a, b, parts, found);
   const int prefix = found.prefix, len = found.len;
   const int row = 32 * blk + (threadIdx.x >> 3), quads = a.head_dim / 4;
@@ -689,7 +689,7 @@ __global__ void __launch_bounds__(JOIN_THREADS, 4)
   pdl_trigger();
   int q0, nq, k0, nk;
   sequence(a, b, q0, nq, k0, nk);
-  const int parts = a.prefix_parts + (a.max_keys > 0 ? a.own_split : 0);
+  const int parts = a.prefix_parts + a.own_parts;
   find_prefix(a, b, parts, found);
   const int prefix = found.prefix, len = found.len;
   const int row0 = blk * ROWS, nrows = min(nq * a.heads_kv * a.group - row0, ROWS);
@@ -801,7 +801,7 @@ cudaError_t launch(const PrefixOwn& own, cudaStream_t s) {
   else if (a.max_keys > 0)
     e = launch_pdl(prefix_few_kernel<BF, DP>, grid, dim3(32), Few<DP>::smem, s, own.k, own.v, a);
   if (e != cudaSuccess || a.fused) return e;
-  const int parts = a.prefix_parts + (a.max_keys > 0 ? a.own_split : 0);
+  const int parts = a.prefix_parts + a.own_parts;
   const unsigned blocks = static_cast<unsigned>(a.batch) * a.join_blocks;
   if (own.join_many) return launch_pdl(prefix_join_many_kernel<BF>, dim3(blocks), dim3(JOIN_THREADS), 4 * parts * ROWS, s, a);
   const dim3 grid2(blocks, (a.head_dim + 31) / 32);
@@ -845,10 +845,10 @@ elasto_status prefix_own_plan(const elasto_prefix_attention_args& u, const Prefi
   a.prefixes = u.prefixes, a.max_prefix = u.max_prefix, a.seq_start = u.seq_start, a.prefix_len = u.prefix_len;
   a.pv = static_cast<const uint16_t*>(u.prefix_v), a.pv_batch = u.prefix_v_batch, a.pv_row = u.prefix_v_row, a.pv_head = u.prefix_v_head;
   a.hg = p.hg, a.nsub = p.nsub, a.pair = p.pair, a.split = p.split, a.parts = parts;
-  a.prefix_parts = p.prefix_parts(), a.own_split = p.own_split;
+  a.prefix_parts = p.prefix_parts(), a.own_split = p.own_split, a.own_parts = p.own_parts;
   a.status = status;
   own->many = p.many != 0 && u.max_keys > 0;
-  a.fused = p.fused != 0 && u.max_keys > 0;
+  a.fused = p.fused;
   own->units = static_cast<int64_t>(p.blocks) * a.batch * a.heads_kv;
   if (own->units * a.own_split > 0x7fffffffLL) {
     set_error("elasto_op_prefix_attention: too many sequences or queries");

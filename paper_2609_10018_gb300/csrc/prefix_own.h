@@ -24,7 +24,7 @@ struct PrefixOwnArgs {
   const uint16_t* pv;
   long long pv_batch, pv_row, pv_head;
   int hg, nsub, pair, split;
-  int prefix_parts, own_split;
+  int prefix_parts, own_split, own_parts;
   int fused;  // prefix_few_kernel joins its rows itself
   PrefixParts parts;
   int blocks;  // of rows, of a sequence and key head

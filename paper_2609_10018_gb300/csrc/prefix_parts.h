@@ -27,10 +27,11 @@ struct PrefixPlan {
   int64_t items;      // for each key head and part of its heads, at most (those that there are not end at once)
   int many;           // 1: blocks of 64 rows of a sequence's own attention, 0: of 16
   int blocks;         // of a sequence and key head
-  int own_split;      // CTAs that share a block's own keys, each leaving a part behind the prefix's
+  int own_split;      // CTAs that share a block's own keys
+  int own_parts;      // what they leave behind the prefix's parts: one each, none where they join, or where there are no own keys
   int fused;          // 1: the kernel of the own keys (of 16 rows) joins its rows itself, with the prefix's one part
   int prefix_parts() const { return pair ? 2 * split : split; }
-  int parts() const { return prefix_parts() + own_split; }
+  int parts() const { return prefix_parts() + own_parts; }
 };
 
 struct PrefixSizes {
@@ -91,7 +92,8 @@ inline PrefixPlan prefix_plan(const PrefixSizes& z) {
     const double cost = prefix + (done < 1.0 ? (1.0 - done) / own_rate(z.sms) : 0.0) + n * part;
     if (n == 1 || cost < best) best = cost, p.split = n;
   }
-  p.fused = !p.many && p.own_split == 1 && p.prefix_parts() == 1 && ctas >= z.sms;
+  p.fused = z.max_keys > 0 && !p.many && p.own_split == 1 && p.prefix_parts() == 1 && ctas >= z.sms;
+  p.own_parts = p.fused || z.max_keys == 0 ? 0 : p.own_split;
   return p;
 }
 

@@ -157,3 +157,14 @@ def test_forms_of_the_test_of_infinite_values(rule):
         assert p["many"] and 7000 * 4 * 3 > 40000 and not p["fused"], p
     p = _plan(rule, rows=12, most=12, max_queries=4, group=32, heads_kv=52, **room)
     assert p["fused"], p
+
+
+def test_a_workspace_has_only_the_parts_that_are_written(rule):
+    """Where the kernel of the own keys joins its rows, and where there are no own keys, the prefix's parts are all."""
+    seen = set()
+    for z in _sizes(2000):
+        p = _plan(rule, **z)
+        own = 0 if p["fused"] or z["max_keys"] == 0 else p["own_split"]
+        assert p["parts"] == p["prefix_parts"] + own, (z, p)
+        seen.add((bool(p["fused"]), z["max_keys"] == 0))
+    assert seen == {(False, False), (True, False), (False, True)}
