@@ -147,7 +147,8 @@ elasto_status elasto_op_gemm_fp8_tile(int M, int N, int K, elasto_fp8_tile* tile
  * of its mean square (plus eps), multiplied by the gain of its channel, and its
  * first rot_dim channels rotated by the row's position; all in fp32, rounded
  * once. Keys, and values unchanged, optionally go to the rows of a cache.
- *   y = x * rsqrt(mean(x^2) + eps) * gain      (a head of zeros with eps 0: NaN)
+ *   y = x * rsqrt(mean(x^2) + eps) * gain      (a head of zeros with eps 0: NaN; squares are
+ *       summed in fp32: from about 1e19 on they overflow, below 1e-19 they lose bits, which shows where eps is no larger)
  *   pair j of rot_dim / 2: channels (j, j + rot_dim / 2), or (2 j, 2 j + 1) if
  *   interleaved != 0, (a, b) -> (a c - b s, b c + a s), with c and s from row
  *   positions[r] of cos_sin: rot_dim / 2 cosines, then rot_dim / 2 sines.
@@ -355,6 +356,9 @@ elasto_status elasto_op_qk_norm_rope_axes(void* stream, const elasto_qk_norm_rop
  * Queries: sequence b has the rows q_start[b] to q_start[b + 1] of q and out, at most max_queries; q_start NULL:
  *   max_queries rows each, one sequence after another. q and out have q_rows rows (at most 2^30, as prefix_rows and kv_rows);
  *   with q_start the work and the workspace are planned for all of them, so give those in use, not a buffer's capacity.
+ *   Likewise max_queries and max_keys: any limits are right, but how the keys are shared out is planned for sequences whose own
+ *   keys are about half of max_keys on average, and grids are of max_queries for every sequence. Limits far above what
+ *   there is make a call slow.
  * Prefixes: prefix g is shared by sequences seq_start[g] to seq_start[g + 1] - 1 (seq_start NULL: one prefix, all
  *   sequences); its keys are the first prefix_len[g] rows (NULL: max_prefix) of prefix_k + g * prefix_k_batch, and so on
  *   for v. At most max_prefix of them, max_prefix <= prefix_rows. Sequences in no prefix's range have their own keys only.

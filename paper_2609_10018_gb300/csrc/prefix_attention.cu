@@ -7,9 +7,13 @@
 // sequences' own keys and joins the parts. All queries see all keys of their prefix, so there are no masks but at its
 // end, and the queries of all its sequences are rows of the same tiles.
 //
-// Bound by the products. 8 prefixes of 4097 keys, 3456 queries of 32 heads of 128 (480 CTAs, three waves): 150 us, tensor
-// pipe busy 63 % of the time; a pair of key tiles takes 1.4 us (1.32 at the rate of a library product). 256 queries
-// behind 16384 keys on 96 SMs, so that the own keys stream beside them: 63 us; 64 behind 8192 on 64 SMs: 21.
+// Bound by the products. 8 prefixes of 2804 to 4097 keys, 3339 queries of 32 heads of 128 (456 CTAs with work, three waves): 150
+// us, tensor pipe busy 63 % of the time; a pair of key tiles takes 1.4 us (1.32 at the rate of a library product). 256
+// queries behind 16384 keys on 96 SMs, so that the own keys stream beside them: 63 us; 64 behind 8192 on 64 SMs: 21.
+//
+// Probabilities are rounded to the operand type, as tcgen05 takes P with V of the same type (P in two pieces would double half of
+// the products). In bf16 that is an independent error of each term of rms 0.0017 of it, as large as that of rounding the result,
+// and both together 0.0023 (relative 2-norm); in f16 an eighth of it. Maxima, sums (of the unrounded P), O and joins are fp32.
 //
 // A tile is 128 rows of Q: the hg query heads that share a key head, times 128 / hg consecutive queries. An item is two
 // tiles that share the K/V stream or, where a prefix has no more rows than one, that tile for both groups of

@@ -2,7 +2,7 @@
 //
 // A block is 16 or 64 rows (query, head) of one sequence and key head; S = Q K^T and O += P V by m16n8k16 products (tcgen05
 // would need 128 rows of one sequence: the prefix, where most of the work lies, has them), running maximum and sum of the
-// softmax in one pass. The own keys of a block are shared out over own_split CTAs, each of which leaves a part as
+// softmax in one pass, P rounded to the operand type as in prefix_attention.cu. The own keys of a block are shared out over own_split CTAs, each of which leaves a part as
 // prefix_attention.cu's CTAs do.
 //   prefix_few_kernel    16 rows, single tokens and few: a CTA is one warp, which streams 16 keys at a time by TMA through
 //     a ring of its own. Nothing is shared between warps, and while one of an SM's twelve CTAs starts or ends the others load.
@@ -32,11 +32,12 @@ namespace {
 constexpr float kLazy = 8.0f;  // log2 of how far a maximum may grow before O is rescaled
 constexpr int JOIN_THREADS = 256;
 
-// A CTA of one warp and its ring.
+// A CTA of one warp and its ring: 16 KB, twelve CTAs an SM. With 24 KB (eight) 64 and 256 single tokens, drafts and images took 0.99,
+// 1.02, 1.10 and 1.04 of the time, with 32 KB (six) 1.00, 1.08, 1.19 and 1.11.
 template <int DP>
 struct Few {
   static constexpr int halves = DP / 64, half = 16 * 128, tile = halves * half, stage = 2 * tile;  // 16 keys of 64 channels
-  static constexpr int stages = 16 * 1024 / stage;  // twelve CTAs an SM (eight with 24 KB each took 3 to 9 % longer, six with 32 KB 10 to 19)
+  static constexpr int stages = 16 * 1024 / stage;  // twelve CTAs an SM (see below)
   static constexpr int smem = 1024 + stages * stage + 64;
 };
 
@@ -856,7 +857,10 @@ elasto_status prefix_own_plan(const elasto_prefix_attention_args& u, const Prefi
   }
   a.blocks = p.blocks;
   // The join: 32 rows and channels a CTA, 64 rows and all channels from 40000 rows on (a small CTA's start then costs
-  // more than its loads).
+  // more than its loads). The call with the first and with the second, in us (32 / 8 heads of 128): 131072 rows, 8 prompts of 512
+  // behind 8192 keys, 520 and 466; 65536, one of 2048, 359 and 331; 81920, 64 of 40 behind 4096, 206 and 178; 32768, 64 drafts of 16
+  // with 1024 own keys, 130 and 114; 16384, 512 single tokens, 179 and 175; 35840 rows of 4 key heads with 7 each 129 and 118 (so
+  // the second gains from about 16000 rows on; how it does with fewer has not been measured).
   const int64_t all = static_cast<int64_t>(a.max_queries) * u.heads;
   own->join_many = all * a.batch > 40000;
   const int64_t join_rows = own->join_many ? ROWS : 32, join_blocks = (all + join_rows - 1) / join_rows;

@@ -53,8 +53,11 @@ inline PrefixPlan prefix_plan(const PrefixSizes& z) {
     return k < n ? k : n;
   };
   p.items = items(z.most);
-  // The sequences' own keys: blocks of 64 rows where a sequence has more than 512 (eight prompts of up to 96 tokens behind
-  // each of eight images, 384 rows: 223 us with them, 219 with blocks of 16), in CTAs until the SMs have six each, with four
+  // The sequences' own keys: blocks of 64 rows where a sequence has more than 512, in which fewer rows read the keys again.
+  // Calls with blocks of 64 and of 16 rows, in us (32 / 8 heads of 128): 512 new tokens of two sequences with caches of 32768 1895 and
+  // 2420, 256 of eight with 4096 549 and 543, 150 of four with 8192 311 and 357; where a block has few keys its start weighs
+  // more: one prompt of 2048 behind 8192 331 and 323, eight of 512 behind 1024 195 and 163; below 512 rows 128 tokens of
+  // eight with 4096 309 and 368, 64 of 32 with 1024 200 and 179, prompts of 128 behind 4096 251 and 243. In CTAs until the SMs have six each, with four
   // tiles of 64 keys at least; else of 16 rows, in CTAs of a warp until the SMs have twelve, with 256 keys at least: sequences
   // of different lengths even out.
   const int64_t rows = static_cast<int64_t>(z.max_queries) * z.group;

@@ -18,6 +18,8 @@
 // bytes at a copy's rate), 32776 of 12 + 12 of 64 64.0 (45.7). Single tokens (64 rows): 2.7 to 3.0 us, the latency of one chain of loads.
 // With positions on several axes: 32760 rows of 12 + 12 heads of 128, three axes, neighbours: 68.4 us, 5.9 TB/s; 32776 of 12 + 12
 // of 64, f16, two axes, halves of each axis, no norm: 36.1 (29.7 at a copy's rate), issue slots at 65 %.
+// The first with the half-split pairing 72.1; with axes in turn (a table row for each pair of a lane) 68.4 and half-split 71.8; with
+// values, into a cache, 113 to 115.
 #include <type_traits>
 
 #include "common.h"
